@@ -375,10 +375,15 @@ def work(case):
 
 # ---- the definitions in 64 bits ----------------------------------------------------------------------------------------
 
+def _power(n):
+    """2^n in float64 for whole n, exactly (pow() may be off in the last place, which would decide ties)."""
+    return (n.to(torch.int64) + 1023 << 52).view(torch.float64)
+
+
 def _nearest(x):
     """The 4-bit values nearest to x [..., 32] (float64): halves, wholes and twos by magnitude, ties to the even multiple."""
     top = x.abs().amax(-1, keepdim=True)
-    unit = torch.ldexp(torch.ones_like(top), torch.where(top > 0, torch.frexp(top)[1] - 3, torch.zeros_like(top, dtype=torch.int32)).clamp(min=-127))
+    unit = _power(torch.where(top > 0, torch.frexp(top)[1] - 3, -127).clamp(min=-127))
     y = x / unit
     step = torch.where(y.abs() < 2, 0.5, torch.where(y.abs() < 4, 1.0, 2.0)).double()
     return (torch.round(y / step) * step).clamp(-6, 6) * unit
@@ -397,10 +402,10 @@ def _stored(codes, scales):
     for half in (0, 1):
         n = (codes >> (4 * half)) & 15
         exponent, mantissa = ((n >> 1) & 3).double(), (n & 1).double()
-        size = torch.where(exponent == 0, mantissa / 2, (1 + mantissa / 2) * 2 ** (exponent - 1))
+        size = torch.where(exponent == 0, mantissa / 2, (1 + mantissa / 2) * _power(exponent - 1))
         c[..., half] = torch.where(n > 7, -size, size)
     at = torch.stack([(scales >> (8 * b)) & 255 for b in range(4)], -1)          # [W, R, 4]
-    return c.view(rows, words, 4, 32) * 2.0 ** (at.permute(1, 0, 2).double() - 127)[..., None]
+    return c.view(rows, words, 4, 32) * _power(at.permute(1, 0, 2) - 127)[..., None]
 
 
 def exact(case, seed):
