@@ -96,6 +96,7 @@ typedef struct kimad_config {
  * table remains that of TopK (the rounding of kept values, below 2^-22 of their energy, is not charged). */
 #define KIMAD_VALUES_F32 0u
 #define KIMAD_VALUES_F16 1u
+#define KIMAD_VALUES_BF16 2u            /* the operators below only; payloads are F32 or F16 */
 
 #define KIMAD_CFG_CLASSIC_PROFILE 1ull  /* profile with two full passes over g, h instead of the sampled
                                            single pass (same results; for comparison and testing) */
@@ -363,6 +364,102 @@ int kimad_selftest_allocate_withheld(kimad_plan_t* plan, const double* err_table
  * or not finite. */
 uint64_t kimad_budget_bytes(double bandwidth_bits_per_s, double t_seconds, double t_comp_seconds, double alpha,
                             uint64_t cap_bytes);
+
+/* ---- Operators beside a round: 4-bit floats, their product and their update, and distillation ------------------------------
+ *
+ * Microscaled 4-bit floats ("MX4").  32 neighbouring elements of a row are a block.  With a the block's largest magnitude, its
+ * scale is s = 2^(floor(log2 a) - 2), at least 2^-127, stored as the byte log2(s) + 127; an element v is stored as the 4-bit
+ * float nearest to v / s (bits: sign, two of exponent, one of mantissa; magnitudes 0, 0.5, 1, 1.5, 2, 3, 4, 6), ties to the even
+ * one, beyond 6 as 6.  A block of zeros has scale byte 0.  A block that holds an Inf or a NaN has scale byte 255 and
+ * stands for NaN as a whole.  Four blocks are a word: 64 bytes of codes (two a byte, the first one in the low half) and one
+ * 32-bit word of four scale bytes (the first block's lowest).
+ *   A matrix of R rows and C columns has W = ceil(C / 128) words a row:
+ *     codes   DEVICE uint8[R * 64 W], row by row, 16-byte aligned
+ *     scales  DEVICE uint32[W * R]: word w of row r at w * R + r, 4-byte aligned
+ *   Elements beyond column C are stored as zeros, which the product relies on.
+ * None of these calls allocates, waits or needs a plan; all may be recorded into a HIP graph.  type: KIMAD_VALUES_F32, _F16
+ * or _BF16.  Arrays that are read must not overlap arrays that are written, but where stated.  Sizes of 0 are
+ * allowed where an empty result makes sense (0 rows; K = 0 gives a product of zeros). */
+
+/* Quantises x, [rows, cols] of `type` with consecutive rows ld >= cols elements apart: along rows into codes, scales (both may
+ * be NULL), along columns into codes_t, scales_t (both may be NULL), which is the form of the transpose, a matrix of cols rows
+ * and rows columns: a training step needs both, and one call reads x once. */
+int kimad_mx4_quantise(const void* x, uint32_t type, uint64_t rows, uint64_t cols, uint64_t ld, void* codes, uint32_t* scales,
+                       void* codes_t, uint32_t* scales_t, void* stream);
+
+/* The values that a quantised matrix stands for, into out, [rows, cols] of `type` with rows ld >= cols elements apart.  Exact in F32
+ * and BF16; in F16 rounded, and Inf beyond its range. */
+int kimad_mx4_dequantise(const void* codes, const uint32_t* scales, uint64_t rows, uint64_t cols, void* out, uint32_t type,
+                         uint64_t ld, void* stream);
+
+/* Product C = A B^T of quantised matrices, A of M rows and K columns, B of N rows and K columns: out [M, N] of `type` with rows
+ * ld >= N elements apart.  Products are exact, sums are fp32, and the sum is rounded once to `type` (F16: Inf beyond its range).  The
+ * forward product of a layer takes activations and weights quantised along their columns' axis; its gradients take the
+ * transposed forms (kimad_mx4_quantise).
+ *   workspace  DEVICE, 16-byte aligned, kimad_mx4_matmul_workspace_bytes(M, N, K) bytes, or NULL: products with few rows and a long sum are
+ *              then not shared out along the sum, and slower.  Its contents need not be kept between calls; calls that may
+ *              run at the same time need one each. */
+uint64_t kimad_mx4_matmul_workspace_bytes(uint64_t M, uint64_t N, uint64_t K);
+int kimad_mx4_matmul(const void* a_codes, const uint32_t* a_scales, uint64_t M, const void* b_codes, const uint32_t* b_scales,
+                     uint64_t N, uint64_t K, void* out, uint32_t type, uint64_t ld, void* workspace, uint64_t workspace_bytes,
+                     void* stream);
+
+/* A worker's update in MX4 (Eq. EF21-2 with the quantiser in the place of TopK; Section 2.2 names quantisation beside
+ * sparsification): for every layer, blocks of 32 from its first entry on,
+ *     q = MX4(fl32(g - h)),   h <- fl32(h + q).
+ * 4.25 bits an entry are sent, whatever the budget; what the rounding lost stays in g - h for the next round.
+ *   g, h         DEVICE float[d], the layers back to back (4-byte alignment suffices); h is updated in place
+ *   layer_start  DEVICE uint64[L+1], element offsets of the layers, layer_start[L] = d; layers may be empty
+ *   codes        DEVICE uint8[64 * words], 16-byte aligned; scales DEVICE uint32[words]; words = kimad_mx4_update_words(L, d).
+ *                Layer i begins at word floor(layer_start[i] / 128) + i; words between layers hold zeros.
+ *   status_out   DEVICE int32[1] or NULL: KIMAD_OK, or KIMAD_ERR_BAD_OFFSETS if layer_start does not run from 0 to d without a
+ *                step back (then nothing else is written)
+ * A block of x with an Inf or a NaN turns the 32 entries of h to NaN, as a NaN among the kept entries of a sparse payload does to its own. */
+uint64_t kimad_mx4_update_words(uint32_t L, uint64_t d);
+int kimad_mx4_compress_ef(const float* g, float* h, const uint64_t* layer_start, uint32_t L, uint64_t d, void* codes,
+                          uint32_t* scales, int32_t* status_out, void* stream);
+
+/* kimad_server_apply for such updates, in one pass: u_hat_m <- fl32(u_hat_m + q_m), the workers' own addition, so that the copies
+ * stay equal bit for bit, and, if x is not NULL, x <- fl32(x - gamma * sum_m weights[m] u_hat_m) with the sum in fp64 in
+ * worker order.  updates: HOST array[M] of {codes, scales} as kimad_mx4_compress_ef writes them; the other arguments as in
+ * kimad_server_apply.  The M buffers and x must not overlap.
+ *   status_out   DEVICE int32[1] or NULL: KIMAD_OK, or KIMAD_ERR_BAD_OFFSETS (then nothing else is written) */
+typedef struct kimad_mx4_update {
+    const void* codes;        /* DEVICE, 16-byte aligned */
+    const uint32_t* scales;   /* DEVICE */
+} kimad_mx4_update_t;
+int kimad_mx4_server_apply(const kimad_mx4_update_t* updates, float* const* u_hat, const double* weights, uint32_t M,
+                           const uint64_t* layer_start, uint32_t L, uint64_t d, float* x, double gamma, int32_t* status_out,
+                           void* stream);
+
+/* Distillation from a teacher's top logits, loss and gradient.  For row r of the student's logits z with T = temperature,
+ * q = softmax(z / T) over the vocabulary and p = softmax(t / T) over the row's entries:
+ *     loss[r]    = w_r T^2 sum_j p_j (ln p_j - ln q_{idx_j})
+ *     grad[r, v] = w_r T (q_v - p_v)          (p_v = 0 where v is no entry)
+ *   logits      DEVICE [rows, vocab] of `type`, rows ld >= vocab elements apart; 1 <= vocab < 2^31
+ *   t_idx       DEVICE uint32[rows * k], t_val DEVICE float[rows * k]: the teacher's entries in any order, 0 <= k <= 1024.  An index of
+ *               vocab or more (0xFFFFFFFF) is no entry: rows may have fewer than k.  Entries of one index are one entry
+ *               with the sum of their probabilities.
+ *   temperature 2^-20 .. 2^20
+ *   row_weight  DEVICE float[rows] or NULL (1)
+ *   loss        DEVICE float[rows] or NULL
+ *   stats       DEVICE float[2 * rows] or NULL: the largest logit, and the sum of exp((z - largest) / T)
+ *   grad        DEVICE [rows, vocab] of `type`, rows ld_grad >= vocab elements apart, or NULL; may be logits itself with ld_grad = ld
+ *   workspace   DEVICE, 4-byte aligned, kimad_distill_workspace_bytes(rows, vocab, k) bytes (0 for most sizes: NULL will do).  As for
+ *               kimad_mx4_matmul, but a smaller one is refused (KIMAD_ERR_WORKSPACE_TOO_SMALL).
+ * At least one of loss, stats and grad is wanted.  Logits of -Inf are masked: q is 0 there, and so is the gradient; an entry with p > 0
+ * there makes the loss +Inf.  A row that leaves nothing (weight 0, no entry above -Inf, or no logit above -Inf) has loss,
+ * statistics and gradient 0.  A NaN or +Inf among a row's logits makes its loss and its gradient NaN. */
+uint64_t kimad_distill_workspace_bytes(uint64_t rows, uint64_t vocab, uint32_t k);
+int kimad_distill(const void* logits, uint32_t type, uint64_t rows, uint64_t vocab, uint64_t ld, const uint32_t* t_idx,
+                  const float* t_val, uint32_t k, float temperature, const float* row_weight, float* loss, float* stats,
+                  void* grad, uint64_t ld_grad, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* The gradient alone, from the statistics that an earlier kimad_distill on the same logits and temperature left (a row whose
+ * second number is 0 gets zeros); row_weight may have been multiplied by what came back from above. */
+int kimad_distill_grad(const void* logits, uint32_t type, uint64_t rows, uint64_t vocab, uint64_t ld, const uint32_t* t_idx,
+                       const float* t_val, uint32_t k, float temperature, const float* row_weight, const float* stats, void* grad,
+                       uint64_t ld_grad, void* stream);
 
 const char* kimad_strerror(int status);
 const char* kimad_version(void);

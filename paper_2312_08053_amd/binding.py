@@ -17,6 +17,7 @@ KIMAD_CFG_DENSE_FALLBACK = 8
 KIMAD_CFG_SAMPLE_ALWAYS = 16
 KIMAD_VALUES_F32 = 0
 KIMAD_VALUES_F16 = 1
+KIMAD_VALUES_BF16 = 2
 KIMAD_MAX_J = 64
 
 EXPORTED_SYMBOLS = [
@@ -27,6 +28,9 @@ EXPORTED_SYMBOLS = [
     "kimad_plan_set_timing", "kimad_plan_get_timings",
     "kimad_server_apply", "kimad_selftest_wave_primitives", "kimad_selftest_allocate_withheld",
     "kimad_budget_bytes", "kimad_strerror", "kimad_version",
+    "kimad_mx4_quantise", "kimad_mx4_dequantise", "kimad_mx4_matmul", "kimad_mx4_matmul_workspace_bytes",
+    "kimad_mx4_update_words", "kimad_mx4_compress_ef", "kimad_mx4_server_apply",
+    "kimad_distill", "kimad_distill_grad", "kimad_distill_workspace_bytes",
 ]
 
 
@@ -43,6 +47,10 @@ class _Layer(C.Structure):
 class _Payload(C.Structure):
     _fields_ = [("idx", C.c_void_p), ("val", C.c_void_p), ("offsets", C.c_void_p), ("capacity_pairs", C.c_uint64),
                 ("value_format", C.c_uint32), ("pad", C.c_uint32)]
+
+
+class _Mx4Update(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p)]
 
 
 class _Config(C.Structure):
@@ -87,6 +95,18 @@ def lib() -> C.CDLL:
                                      vp, C.c_double, vp, vp]
     L.kimad_selftest_wave_primitives.argtypes = [vp, vp, vp, vp, vp]
     L.kimad_selftest_allocate_withheld.argtypes = [vp, vp, u64, vp, vp, vp, i32p, u32, vp, vp]
+    f32 = C.c_float
+    L.kimad_mx4_quantise.argtypes = [vp, u32, u64, u64, u64, vp, vp, vp, vp, vp]
+    L.kimad_mx4_dequantise.argtypes = [vp, vp, u64, u64, vp, u32, u64, vp]
+    L.kimad_mx4_matmul_workspace_bytes.argtypes = [u64, u64, u64]
+    L.kimad_mx4_matmul.argtypes = [vp, vp, u64, vp, vp, u64, u64, vp, u32, u64, vp, u64, vp]
+    L.kimad_mx4_update_words.argtypes = [u32, u64]
+    L.kimad_mx4_compress_ef.argtypes = [vp, vp, vp, u32, u64, vp, vp, vp, vp]
+    L.kimad_mx4_server_apply.argtypes = [C.POINTER(_Mx4Update), C.POINTER(C.c_void_p), C.POINTER(C.c_double), u32, vp, u32, u64,
+                                         vp, C.c_double, vp, vp]
+    L.kimad_distill_workspace_bytes.argtypes = [u64, u64, u32]
+    L.kimad_distill.argtypes = [vp, u32, u64, u64, u64, vp, vp, u32, f32, vp, vp, vp, vp, u64, vp, u64, vp]
+    L.kimad_distill_grad.argtypes = [vp, u32, u64, u64, u64, vp, vp, u32, f32, vp, vp, vp, u64, vp]
     L.kimad_strerror.argtypes = [C.c_int]
     L.kimad_strerror.restype = C.c_char_p
     L.kimad_version.restype = C.c_char_p
@@ -94,7 +114,8 @@ def lib() -> C.CDLL:
         if name not in ("kimad_strerror", "kimad_version", "kimad_budget_bytes"):
             getattr(L, name).restype = C.c_int
     L.kimad_budget_bytes.argtypes = [C.c_double, C.c_double, C.c_double, C.c_double, C.c_uint64]
-    L.kimad_budget_bytes.restype = C.c_uint64
+    for name in ("kimad_budget_bytes", "kimad_mx4_matmul_workspace_bytes", "kimad_mx4_update_words", "kimad_distill_workspace_bytes"):
+        getattr(L, name).restype = C.c_uint64
     _lib = L
     return L
 
@@ -253,6 +274,170 @@ def kimad_selftest_allocate_withheld(plan: int, err_table, budget_bytes: int, j_
                                                   C.c_void_p(_ptr(j_out)), C.c_void_p(_ptr(K_out)), C.c_void_p(_ptr(offsets_out)),
                                                   C.c_void_p(_ptr(status_out)), int(polls), C.c_void_p(_ptr(given_up_out)),
                                                   C.c_void_p(_stream(stream))), "kimad_selftest_allocate_withheld")
+
+
+def _type(t) -> int:
+    """KIMAD_VALUES_* of a tensor's type."""
+    import torch
+    try:
+        return {torch.float32: KIMAD_VALUES_F32, torch.float16: KIMAD_VALUES_F16, torch.bfloat16: KIMAD_VALUES_BF16}[t.dtype]
+    except KeyError:
+        raise TypeError(f"float32, float16 or bfloat16 is wanted, got {t.dtype}") from None
+
+
+def _rows(t, what: str):
+    """(rows, columns, elements from row to row) of a matrix whose rows are contiguous."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+        raise ValueError(f"{what}: a matrix with contiguous rows is wanted, got shape {tuple(t.shape)}, strides {t.stride()}")
+    return t.shape[0], t.shape[1], (t.stride(0) if t.shape[0] > 1 else t.shape[1])
+
+
+def _holds(t, count: int, size: int, what: str) -> None:
+    """A contiguous tensor of at least `count` elements of `size` bytes."""
+    if t.element_size() != size or t.numel() < count or not t.is_contiguous():
+        raise ValueError(f"{what}: {count} contiguous elements of {size} bytes are wanted, got {t.numel()} of {t.dtype}, strides {t.stride()}")
+
+
+def _holds_mx4(codes, scales, rows: int, cols: int, what: str) -> None:
+    words = -(-cols // 128)
+    _holds(codes, rows * words * 64, 1, f"{what} codes")
+    _holds(scales, rows * words, 4, f"{what} scales")
+
+
+def mx4_empty(rows: int, cols: int, device="cuda"):
+    """(codes uint8 [rows, 64 W], scales int32 [W, rows]) for a matrix in 4 bits, W = ceil(cols / 128); not filled."""
+    import torch
+    words = -(-int(cols) // 128)
+    return (torch.empty(int(rows), 64 * words, dtype=torch.uint8, device=device),
+            torch.empty(words, int(rows), dtype=torch.int32, device=device))
+
+
+def kimad_mx4_quantise(x, codes=None, scales=None, codes_t=None, scales_t=None, stream=None) -> None:
+    """x [rows, cols] along rows into codes, scales, along columns into codes_t, scales_t (each pair from mx4_empty, or None)."""
+    rows, cols, ld = _rows(x, "x")
+    if codes is not None:
+        _holds_mx4(codes, scales, rows, cols, "row")
+    if codes_t is not None:
+        _holds_mx4(codes_t, scales_t, cols, rows, "column")
+    _check(lib().kimad_mx4_quantise(_ptr(x), _type(x), rows, cols, ld, _ptr(codes), _ptr(scales), _ptr(codes_t), _ptr(scales_t),
+                                    _stream(stream)), "kimad_mx4_quantise")
+
+
+def kimad_mx4_dequantise(codes, scales, out, stream=None) -> None:
+    """The values of a quantised matrix into out [rows, cols]."""
+    rows, cols, ld = _rows(out, "out")
+    _holds_mx4(codes, scales, rows, cols, "row")
+    _check(lib().kimad_mx4_dequantise(_ptr(codes), _ptr(scales), rows, cols, _ptr(out), _type(out), ld, _stream(stream)),
+           "kimad_mx4_dequantise")
+
+
+def kimad_mx4_matmul_workspace_bytes(M: int, N: int, K: int) -> int:
+    return int(lib().kimad_mx4_matmul_workspace_bytes(int(M), int(N), int(K)))
+
+
+def kimad_mx4_matmul(a_codes, a_scales, b_codes, b_scales, K: int, out, workspace=None, stream=None) -> None:
+    """out [M, N] = A B^T of quantised matrices A [M, K] and B [N, K].  workspace: a device tensor (allocated here if None and
+    one is of use)."""
+    M, N, ld = _rows(out, "out")
+    _holds_mx4(a_codes, a_scales, M, K, "A's")
+    _holds_mx4(b_codes, b_scales, N, K, "B's")
+    L = lib()
+    need = L.kimad_mx4_matmul_workspace_bytes(M, N, K)
+    if workspace is None and need:
+        import torch
+        workspace = torch.empty(need, dtype=torch.uint8, device=out.device)
+    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(L.kimad_mx4_matmul(_ptr(a_codes), _ptr(a_scales), M, _ptr(b_codes), _ptr(b_scales), N, int(K), _ptr(out), _type(out), ld,
+                              _ptr(workspace), nbytes, _stream(stream)), "kimad_mx4_matmul")
+
+
+def kimad_mx4_update_words(L: int, d: int) -> int:
+    return int(lib().kimad_mx4_update_words(int(L), int(d)))
+
+
+def kimad_mx4_compress_ef(g, h, layer_start, codes, scales, status_out=None, stream=None) -> None:
+    """One worker's update in 4 bits: g, h flat fp32 tensors (h is updated in place), layer_start device int64[L+1], codes uint8
+    [words, 64] and scales int32 [words] with words = kimad_mx4_update_words(L, d); status_out: device int32[1] or None."""
+    d, L = g.numel(), layer_start.numel() - 1
+    words = d // 128 + L
+    _holds(g, d, 4, "g")
+    _holds(h, d, 4, "h")
+    _holds(layer_start, 1, 8, "layer_start")
+    _holds(codes, words * 64, 1, "codes")
+    _holds(scales, words, 4, "scales")
+    _check(lib().kimad_mx4_compress_ef(_ptr(g), _ptr(h), _ptr(layer_start), L, d, _ptr(codes), _ptr(scales), _ptr(status_out),
+                                       _stream(stream)), "kimad_mx4_compress_ef")
+
+
+def kimad_mx4_server_apply(updates, u_hats, weights, layer_start, d: int, x=None, gamma: float = 0.0, status_out=None,
+                           stream=None) -> None:
+    """updates: list of (codes, scales) as kimad_mx4_compress_ef writes them, one per worker; u_hats: list of flat fp32 tensors
+    (updated in place); x: flat fp32 model or None; status_out: device int32[1] or None."""
+    M, L, d = len(u_hats), layer_start.numel() - 1, int(d)
+    words = d // 128 + L
+    _holds(layer_start, 1, 8, "layer_start")
+    if len(updates) != M or len(weights) != M:
+        raise ValueError(f"{M} estimators, {len(updates)} updates and {len(weights)} weights")
+    for (c, s), u in zip(updates, u_hats):
+        _holds(c, words * 64, 1, "codes")
+        _holds(s, words, 4, "scales")
+        _holds(u, d, 4, "u_hats")
+    if x is not None:
+        _holds(x, d, 4, "x")
+    up = (_Mx4Update * M)(*[_Mx4Update(_ptr(c), _ptr(s)) for (c, s) in updates])
+    uh = (C.c_void_p * M)(*[_ptr(u) for u in u_hats])
+    w = (C.c_double * M)(*[float(t) for t in weights])
+    _check(lib().kimad_mx4_server_apply(up, uh, w, M, _ptr(layer_start), L, d, _ptr(x), float(gamma), _ptr(status_out),
+                                        _stream(stream)), "kimad_mx4_server_apply")
+
+
+def kimad_distill_workspace_bytes(rows: int, vocab: int, k: int) -> int:
+    return int(lib().kimad_distill_workspace_bytes(int(rows), int(vocab), int(k)))
+
+
+def _distill_inputs(logits, t_idx, t_val, row_weight, grad):
+    rows, vocab, ld = _rows(logits, "logits")
+    k = t_idx.shape[1] if t_idx.dim() == 2 else -1
+    if tuple(t_idx.shape) != (rows, k) or t_val.shape != t_idx.shape:
+        raise ValueError(f"entries: [rows, k] is wanted twice, got {tuple(t_idx.shape)} and {tuple(t_val.shape)} for {rows} rows")
+    _holds(t_idx, rows * k, 4, "t_idx")
+    _holds(t_val, rows * k, 4, "t_val")
+    if row_weight is not None:
+        _holds(row_weight, rows, 4, "row_weight")
+    ld_grad = 0
+    if grad is not None:
+        g_rows, g_vocab, ld_grad = _rows(grad, "grad")
+        if (g_rows, g_vocab) != (rows, vocab) or grad.dtype != logits.dtype:
+            raise ValueError(f"grad: the logits' shape and type are wanted, got {tuple(grad.shape)} of {grad.dtype}")
+    return rows, vocab, ld, k, ld_grad
+
+
+def kimad_distill(logits, t_idx, t_val, temperature: float, loss=None, stats=None, grad=None, row_weight=None, workspace=None,
+                  stream=None) -> None:
+    """Distillation loss (float32 [rows]), statistics (float32 [rows, 2]) and gradient (like logits) of logits [rows, vocab]
+    against a teacher's top entries t_idx int32, t_val float32 [rows, k]; an output that is None is left out."""
+    rows, vocab, ld, k, ld_grad = _distill_inputs(logits, t_idx, t_val, row_weight, grad)
+    if loss is not None:
+        _holds(loss, rows, 4, "loss")
+    if stats is not None:
+        _holds(stats, 2 * rows, 4, "stats")
+    L = lib()
+    need = L.kimad_distill_workspace_bytes(rows, vocab, k)
+    if workspace is None and need:
+        import torch
+        workspace = torch.empty(need, dtype=torch.uint8, device=logits.device)
+    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(L.kimad_distill(_ptr(logits), _type(logits), rows, vocab, ld, _ptr(t_idx), _ptr(t_val), k, float(temperature),
+                           _ptr(row_weight), _ptr(loss), _ptr(stats), _ptr(grad), ld_grad, _ptr(workspace), nbytes,
+                           _stream(stream)), "kimad_distill")
+
+
+def kimad_distill_grad(logits, t_idx, t_val, temperature: float, stats, grad, row_weight=None, stream=None) -> None:
+    """The gradient alone, from the statistics of an earlier kimad_distill."""
+    rows, vocab, ld, k, ld_grad = _distill_inputs(logits, t_idx, t_val, row_weight, grad)
+    _holds(stats, 2 * rows, 4, "stats")
+    _check(lib().kimad_distill_grad(_ptr(logits), _type(logits), rows, vocab, ld, _ptr(t_idx), _ptr(t_val), k, float(temperature),
+                                    _ptr(row_weight), _ptr(stats), _ptr(grad), ld_grad, _stream(stream)), "kimad_distill_grad")
 
 
 class Plan:

@@ -9,6 +9,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libkimad.so")
 
+SOURCES = ["kimad_api.hip", "operators_api.hip"]
+
 # -packed-fp32-ops is switched off: hipcc must not form packed fp32 instructions from the
 # scalar float code.  Contraction is off so that x = g - h and h + x stay single IEEE operations.
 HIPCC_FLAGS = [
@@ -21,7 +23,7 @@ HIPCC_FLAGS = [
 def build(verbose: bool = True) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     cmd = [hipcc] + HIPCC_FLAGS + ["-I", os.path.join(HERE, "..", "include"),
-                                   "-o", LIB, os.path.join(CSRC, "kimad_api.hip")]
+                                   "-o", LIB] + [os.path.join(CSRC, f) for f in SOURCES]
     if verbose:
         print(" ".join(cmd), flush=True)
     res = subprocess.run(cmd, capture_output=True, text=True)

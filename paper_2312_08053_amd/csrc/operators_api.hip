@@ -1,0 +1,230 @@
+// C ABI of the operators beside a round: argument checks and kernel launches.  Declarations and contracts are in include/kimad.h.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <type_traits>
+
+#include "../../include/kimad.h"
+#include "k_mx4_quantise.h"
+#include "k_mx4_matmul.h"
+#include "k_mx4_update.h"
+#include "k_distill.h"
+
+namespace {
+
+using namespace kimad;
+
+static_assert(TYPE_F32 == KIMAD_VALUES_F32 && TYPE_F16 == KIMAD_VALUES_F16 && TYPE_BF16 == KIMAD_VALUES_BF16, "header and kernel constants");
+
+static_assert(UPDATE_MAX_WORKERS == KIMAD_MAX_WORKERS, "header and kernel constants");
+
+constexpr uint64_t MOST = 1ull << 40;                    // elements along an axis that the checks below let through
+constexpr uint64_t GRID_MOST = 0x7FFFFFFFull, GRID_Y_MOST = 65535;
+
+inline bool aligned(const void* p, uintptr_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
+inline uint64_t words_of(uint64_t cols) { return (cols + MX4_WORD - 1) / MX4_WORD; }
+inline int launched() { return hipGetLastError() == hipSuccess ? KIMAD_OK : KIMAD_ERR_HIP; }
+// codes and scales are both given or both missing
+inline bool pair_ok(const void* codes, const uint32_t* scales) {
+    return !codes == !scales && (!codes || (aligned(codes, 16) && aligned(scales, 4)));
+}
+inline uint64_t type_bytes(uint32_t type) { return type == KIMAD_VALUES_F32 ? 4 : 2; }
+
+// Calls f with the type as a compile-time constant.
+template <class F>
+inline int with_type(uint32_t type, F f) {
+    if (type == KIMAD_VALUES_F32) return f(std::integral_constant<uint32_t, TYPE_F32>{});
+    if (type == KIMAD_VALUES_F16) return f(std::integral_constant<uint32_t, TYPE_F16>{});
+    return f(std::integral_constant<uint32_t, TYPE_BF16>{});
+}
+
+// Workgroups and the run of words that each of them takes: runs of at least 16, and at most eight workgroups a compute unit.
+inline uint32_t update_grid(uint64_t words, uint64_t& share) {
+    const uint64_t wgs = std::min<uint64_t>((words + 15) / 16, 2048);
+    share = ((words + wgs - 1) / wgs + 15) / 16 * 16;
+    return (uint32_t)((words + share - 1) / share);
+}
+
+}  // namespace
+
+namespace {
+
+// Few long rows are shared out over the compute units.
+inline bool distill_split(uint64_t rows, uint64_t vocab) { return vocab > DISTILL_CHUNK && rows < 128; }
+inline uint32_t distill_chunks(uint64_t vocab) { return (uint32_t)((vocab + DISTILL_CHUNK - 1) / DISTILL_CHUNK); }
+
+int distill_args(DistillArgs& a, const void* logits, uint32_t type, uint64_t rows, uint64_t vocab, uint64_t ld, const uint32_t* t_idx,
+                 const float* t_val, uint32_t k, float temperature, const float* row_weight, const void* grad, uint64_t ld_grad) {
+    if (type > KIMAD_VALUES_BF16 || vocab == 0 || vocab >= (1ull << 31) || rows > GRID_MOST || ld < vocab || k > DISTILL_MAX_K) return KIMAD_ERR_INVALID_ARG;
+    if (!(temperature >= 0x1p-20f && temperature <= 0x1p20f)) return KIMAD_ERR_INVALID_ARG;
+    if (rows && (!logits || !aligned(logits, type_bytes(type)) || (k && (!t_idx || !t_val)))) return KIMAD_ERR_INVALID_ARG;
+    if (grad && (ld_grad < vocab || !aligned(grad, type_bytes(type)))) return KIMAD_ERR_INVALID_ARG;
+    if (rows * distill_chunks(vocab) > GRID_MOST) return KIMAD_ERR_INVALID_ARG;
+    a.z = logits; a.idx = t_idx; a.val = t_val; a.weight = row_weight; a.grad = const_cast<void*>(grad);
+    a.rows = rows; a.vocab = vocab; a.ld = ld; a.ld_grad = ld_grad; a.k = k; a.bloom = distill_bloom(k);
+    a.T = temperature; a.c = (float)(1.4426950408889634 / (double)temperature);
+    a.chunk = DISTILL_CHUNK; a.chunks = distill_chunks(vocab);
+    return KIMAD_OK;
+}
+
+template <uint32_t TYPE, uint32_t NT, uint32_t NV>
+int launch_row(const DistillArgs& a, hipStream_t s) {
+    if (a.grad) hipLaunchKernelGGL((k_distill_row<TYPE, NT, NV, true>), dim3((uint32_t)a.rows), dim3(NT), distill_lds(a.k), s, a);
+    else hipLaunchKernelGGL((k_distill_row<TYPE, NT, NV, false>), dim3((uint32_t)a.rows), dim3(NT), distill_lds(a.k), s, a);
+    return launched();
+}
+
+}  // namespace
+
+extern "C" {
+
+int kimad_mx4_quantise(const void* x, uint32_t type, uint64_t rows, uint64_t cols, uint64_t ld, void* codes, uint32_t* scales,
+                       void* codes_t, uint32_t* scales_t, void* stream) {
+    if (type > KIMAD_VALUES_BF16 || rows > MOST || cols > MOST || ld < cols || !pair_ok(codes, scales) || !pair_ok(codes_t, scales_t))
+        return KIMAD_ERR_INVALID_ARG;
+    if (rows == 0 || cols == 0) return KIMAD_OK;
+    if ((!codes && !codes_t) || !x || !aligned(x, type_bytes(type))) return KIMAD_ERR_INVALID_ARG;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const uint64_t W = words_of(cols), WT = words_of(rows);
+    if (codes_t) {
+        if (W > GRID_MOST || WT > GRID_Y_MOST) return KIMAD_ERR_INVALID_ARG;
+        return with_type(type, [&](auto t) {
+            hipLaunchKernelGGL(k_mx4_quantise_both<decltype(t)::value>, dim3((uint32_t)W, (uint32_t)WT), dim3(256), 0, s, x, rows, cols, ld, W, WT,
+                               static_cast<uint32_t*>(codes), scales, static_cast<uint32_t*>(codes_t), scales_t);
+            return launched();
+        });
+    }
+    const uint64_t gx = (rows + QROWS - 1) / QROWS, gy = (W + QWORDS - 1) / QWORDS;
+    if (gx > GRID_MOST || gy > GRID_Y_MOST) return KIMAD_ERR_INVALID_ARG;
+    return with_type(type, [&](auto t) {
+        hipLaunchKernelGGL(k_mx4_quantise_rows<decltype(t)::value>, dim3((uint32_t)gx, (uint32_t)gy), dim3(256), 0, s, x, rows, cols, ld, W,
+                           static_cast<uint32_t*>(codes), scales);
+        return launched();
+    });
+}
+
+int kimad_mx4_dequantise(const void* codes, const uint32_t* scales, uint64_t rows, uint64_t cols, void* out, uint32_t type,
+                         uint64_t ld, void* stream) {
+    if (type > KIMAD_VALUES_BF16 || rows > MOST || cols > MOST || ld < cols) return KIMAD_ERR_INVALID_ARG;
+    if (rows == 0 || cols == 0) return KIMAD_OK;
+    if (!codes || !pair_ok(codes, scales) || !out || !aligned(out, type_bytes(type))) return KIMAD_ERR_INVALID_ARG;
+    const uint64_t W = words_of(cols), gx = (rows + QROWS - 1) / QROWS, gy = (W + QWORDS - 1) / QWORDS;
+    if (gx > GRID_MOST || gy > GRID_Y_MOST) return KIMAD_ERR_INVALID_ARG;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return with_type(type, [&](auto t) {
+        hipLaunchKernelGGL(k_mx4_dequantise<decltype(t)::value>, dim3((uint32_t)gx, (uint32_t)gy), dim3(256), 0, s,
+                           static_cast<const uint32_t*>(codes), scales, rows, cols, W, out, ld);
+        return launched();
+    });
+}
+
+uint64_t kimad_mx4_matmul_workspace_bytes(uint64_t, uint64_t, uint64_t) { return 0; }
+
+int kimad_mx4_matmul(const void* a_codes, const uint32_t* a_scales, uint64_t M, const void* b_codes, const uint32_t* b_scales,
+                     uint64_t N, uint64_t K, void* out, uint32_t type, uint64_t ld, void* workspace, uint64_t workspace_bytes,
+                     void* stream) {
+    if (type > KIMAD_VALUES_BF16 || M > MOST || N > MOST || K > MOST || ld < N) return KIMAD_ERR_INVALID_ARG;
+    if (M == 0 || N == 0) return KIMAD_OK;
+    if (!out || !aligned(out, type_bytes(type))) return KIMAD_ERR_INVALID_ARG;
+    if (K && (!a_codes || !b_codes || !pair_ok(a_codes, a_scales) || !pair_ok(b_codes, b_scales))) return KIMAD_ERR_INVALID_ARG;
+    if (workspace && !aligned(workspace, 16)) return KIMAD_ERR_INVALID_ARG;
+    (void)workspace_bytes;
+    const uint64_t W = words_of(K), gx = (N + 63) / 64, gy = (M + 15) / 16;
+    if (gx > GRID_MOST || gy > GRID_Y_MOST) return KIMAD_ERR_INVALID_ARG;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return with_type(type, [&](auto t) {
+        hipLaunchKernelGGL(k_mx4_matmul<decltype(t)::value>, dim3((uint32_t)gx, (uint32_t)gy), dim3(256), 0, s,
+                           static_cast<const u32x4*>(a_codes), a_scales, M, static_cast<const u32x4*>(b_codes), b_scales, N, W, out, ld);
+        return launched();
+    });
+}
+
+uint64_t kimad_mx4_update_words(uint32_t L, uint64_t d) { return d / MX4_WORD + L; }
+
+int kimad_mx4_compress_ef(const float* g, float* h, const uint64_t* layer_start, uint32_t L, uint64_t d, void* codes,
+                          uint32_t* scales, int32_t* status_out, void* stream) {
+    if (!g || !h || !layer_start || L == 0 || d == 0 || d > MOST || !codes || !pair_ok(codes, scales) || !aligned(g, 4) || !aligned(h, 4))
+        return KIMAD_ERR_INVALID_ARG;
+    const uint64_t words = kimad_mx4_update_words(L, d);
+    uint64_t share;
+    const uint32_t wgs = update_grid(words, share);
+    hipLaunchKernelGGL(k_mx4_compress, dim3(wgs), dim3(256), 0, static_cast<hipStream_t>(stream), g, h, layer_start, L, d, words, share,
+                       static_cast<uint32_t*>(codes), scales, status_out, (int32_t)KIMAD_ERR_BAD_OFFSETS);
+    return launched();
+}
+
+int kimad_mx4_server_apply(const kimad_mx4_update_t* updates, float* const* u_hat, const double* weights, uint32_t M,
+                           const uint64_t* layer_start, uint32_t L, uint64_t d, float* x, double gamma, int32_t* status_out,
+                           void* stream) {
+    if (!updates || !u_hat || !weights || !layer_start || M == 0 || M > KIMAD_MAX_WORKERS || L == 0 || d == 0 || d > MOST || !aligned(x, 4))
+        return KIMAD_ERR_INVALID_ARG;
+    Mx4ServerArgs a{};
+    for (uint32_t m = 0; m < M; ++m) {
+        if (!updates[m].codes || !pair_ok(updates[m].codes, updates[m].scales) || !u_hat[m] || !aligned(u_hat[m], 4)) return KIMAD_ERR_INVALID_ARG;
+        a.codes[m] = static_cast<const uint32_t*>(updates[m].codes);
+        a.scales[m] = updates[m].scales;
+        a.u_hat[m] = u_hat[m];
+        a.w[m] = weights[m];
+    }
+    a.M = M; a.L = L; a.d = d; a.layer_start = layer_start; a.x = x; a.gamma = gamma;
+    a.words = kimad_mx4_update_words(L, d);
+    const uint32_t wgs = update_grid(a.words, a.share);
+    hipLaunchKernelGGL(k_mx4_server, dim3(wgs), dim3(256), 0, static_cast<hipStream_t>(stream), a, status_out, (int32_t)KIMAD_ERR_BAD_OFFSETS);
+    return launched();
+}
+
+uint64_t kimad_distill_workspace_bytes(uint64_t rows, uint64_t vocab, uint32_t k) {
+    return distill_split(rows, vocab) || vocab > 65536 ? 4 * rows * (2ull * distill_chunks(vocab) + k) : 0;
+}
+
+int kimad_distill(const void* logits, uint32_t type, uint64_t rows, uint64_t vocab, uint64_t ld, const uint32_t* t_idx,
+                  const float* t_val, uint32_t k, float temperature, const float* row_weight, float* loss, float* stats,
+                  void* grad, uint64_t ld_grad, void* workspace, uint64_t workspace_bytes, void* stream) {
+    DistillArgs a{};
+    if (!loss && !stats && !grad) return KIMAD_ERR_INVALID_ARG;
+    const int rc = distill_args(a, logits, type, rows, vocab, ld, t_idx, t_val, k, temperature, row_weight, grad, ld_grad);
+    if (rc || rows == 0) return rc;
+    a.loss = loss; a.stats = stats;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const uint64_t need = kimad_distill_workspace_bytes(rows, vocab, k);
+    if (need && (!workspace || workspace_bytes < need || !aligned(workspace, 4))) return KIMAD_ERR_WORKSPACE_TOO_SMALL;
+    if (need) {
+        a.parts = static_cast<float*>(workspace);
+        a.zj = a.parts + 2 * rows * a.chunks;
+        return with_type(type, [&](auto t) {
+            constexpr uint32_t TYPE = decltype(t)::value;
+            hipLaunchKernelGGL(k_distill_part<TYPE>, dim3((uint32_t)(rows * a.chunks)), dim3(CHUNK_NT), 0, s, a);
+            if (hipGetLastError() != hipSuccess) return (int)KIMAD_ERR_HIP;
+            if (a.grad) hipLaunchKernelGGL((k_distill_rest<TYPE, true, true>), dim3((uint32_t)(rows * a.chunks)), dim3(CHUNK_NT), distill_lds(k), s, a, a.chunks);
+            else hipLaunchKernelGGL((k_distill_rest<TYPE, true, false>), dim3((uint32_t)rows), dim3(CHUNK_NT), distill_lds(k), s, a, 1u);
+            return launched();
+        });
+    }
+    return with_type(type, [&](auto t) {
+        constexpr uint32_t TYPE = decltype(t)::value;
+        if (vocab <= 512) return launch_row<TYPE, 64, 1>(a, s);
+        if (vocab <= 2048) return launch_row<TYPE, 256, 1>(a, s);
+        if (vocab <= 8192) return launch_row<TYPE, 256, 4>(a, s);
+        if (vocab <= 16384) return launch_row<TYPE, 1024, 2>(a, s);
+        if (vocab <= 32768) return launch_row<TYPE, 1024, 4>(a, s);
+        return launch_row<TYPE, 1024, 8>(a, s);
+    });
+}
+
+int kimad_distill_grad(const void* logits, uint32_t type, uint64_t rows, uint64_t vocab, uint64_t ld, const uint32_t* t_idx,
+                       const float* t_val, uint32_t k, float temperature, const float* row_weight, const float* stats, void* grad,
+                       uint64_t ld_grad, void* stream) {
+    DistillArgs a{};
+    const int rc = distill_args(a, logits, type, rows, vocab, ld, t_idx, t_val, k, temperature, row_weight, grad, ld_grad);
+    if (rc || rows == 0) return rc;
+    if (!stats || !grad) return KIMAD_ERR_INVALID_ARG;
+    a.stats = const_cast<float*>(stats);
+    return with_type(type, [&](auto t) {
+        hipLaunchKernelGGL((k_distill_rest<decltype(t)::value, false, true>), dim3((uint32_t)(rows * a.chunks)), dim3(CHUNK_NT), distill_lds(k),
+                           static_cast<hipStream_t>(stream), a, a.chunks);
+        return launched();
+    });
+}
+
+}  // extern "C"

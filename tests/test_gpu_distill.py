@@ -1,0 +1,261 @@
+"""Distillation loss and gradient against the definition in 64 bits."""
+import numpy as np
+import pytest
+
+from tests import operators_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+HALF = {"float32": 2.0 ** -24, "float16": 2.0 ** -11, "bfloat16": 2.0 ** -8}
+TINY = {"float32": 0.0, "float16": 2.0 ** -25, "bfloat16": 0.0}
+
+
+def _kimad():
+    import paper_2312_08053_amd as kimad
+    return kimad
+
+
+def _inputs(rows, vocab, k, kind, seed, pad=0, offset=0):
+    """Logits inside a larger buffer, entries (some rows with fewer, some with none), weights (some 0)."""
+    import torch
+    rng = np.random.default_rng(seed)
+    z = torch.from_numpy(rng.normal(0, 4, (rows, vocab))).to(getattr(torch, kind))
+    buf = torch.full((offset + rows * (vocab + pad) + 64,), float("nan"), dtype=z.dtype, device="cuda")
+    zd = torch.as_strided(buf, (rows, vocab), (vocab + pad, 1), offset)
+    zd.copy_(z)
+    idx = np.stack([rng.choice(vocab, size=k, replace=False) for _ in range(rows)]).astype(np.int64) if k else np.zeros((rows, 0), np.int64)
+    count = np.where(rng.uniform(size=rows) < 0.25, rng.integers(0, k + 1, rows), k)
+    idx[np.arange(k)[None, :] >= count[:, None]] = -1
+    t = rng.normal(0, 4, (rows, k)).astype(np.float32)
+    w = np.where(rng.uniform(size=rows) < 0.15, 0.0, rng.uniform(0.1, 2, rows)).astype(np.float32)
+    return zd, idx, t, w
+
+
+def _run(zd, idx, t, T, w, stats=True, grad=True, loss=True):
+    import torch
+    kimad = _kimad()
+    rows, vocab = zd.shape
+    dev = lambda a: torch.from_numpy(a).cuda()                                        # noqa: E731
+    out = dict(loss=torch.full((rows,), 7.0, device="cuda") if loss else None, stats=torch.full((rows, 2), 7.0, device="cuda") if stats else None,
+               grad=torch.full((rows, vocab), 7.0, dtype=zd.dtype, device="cuda") if grad else None)
+    kimad.kimad_distill(zd, dev(idx.astype(np.int32)), dev(t), T, row_weight=None if w is None else dev(w), **out)
+    return out
+
+
+def _host(t):
+    return t.cpu().double().numpy()
+
+
+def _check(zd, idx, t, T, w, out, kind):
+    """Exponents carry the rounding of (z - m) and of its product with log2(e)/T (four parts in 2^24 of the exponent), the sums at
+    most 2^-24 an addition (fewer than 200 of them in a row), exponential, division and product a few parts more.  The loss adds
+    up to k terms; its logarithms' arguments carry the same errors."""
+    w = np.ones(zd.shape[0]) if w is None else w.astype(np.float64)
+    z = _host(zd)
+    loss, stats, grad = ref.distill(z, idx, t, T, w)
+    u = 2.0 ** -24
+    with np.errstate(all="ignore"):
+        far = np.where(np.isfinite(z), np.abs(z - stats[:, :1]) / T, 0.0)
+        q = grad / np.maximum(w[:, None] * T, 1e-300)
+        p = np.zeros_like(z)
+    t_far = 0.0
+    for r in range(z.shape[0]):
+        there = (idx[r] >= 0) & (idx[r] < z.shape[1])
+        if there.any() and stats[r, 1] != 0:
+            tv = t[r][there].astype(np.float64)
+            on = np.isfinite(tv)
+            if not on.any():
+                continue
+            e = np.where(on, np.exp((tv - tv[on].max()) / T), 0.0)
+            np.add.at(p[r], idx[r][there], e / e.sum())
+            t_far = max(t_far, float((tv[on].max() - tv[on].min()) / T))
+    q = np.abs(q + p) * (stats[:, 1:] != 0)
+    rel_q, rel_p = u * (8 * far + 240), u * (8 * t_far + 240)
+    if out.get("grad") is not None:
+        got = _host(out["grad"])
+        scale = (w * T)[:, None]
+        bound = scale * (q * rel_q + p * rel_p) + HALF[kind] * np.abs(grad) * 1.001 + TINY[kind] + 2.0 ** -125
+        assert np.array_equal(np.isnan(got), np.isnan(grad))
+        bad = np.abs(got - grad) > bound
+        assert not bad.any(), (np.argwhere(bad)[:3], got[bad][:3], grad[bad][:3], bound[bad][:3])
+    if out.get("loss") is not None:
+        got = _host(out["loss"])
+        fin = np.isfinite(loss)
+        assert np.array_equal(np.isnan(got), np.isnan(loss)) and np.array_equal(got[~fin & ~np.isnan(loss)], loss[~fin & ~np.isnan(loss)])
+        with np.errstate(all="ignore"):
+            size = np.where(p > 0, p * (np.abs(np.log(np.where(p > 0, p, 1))) + far + np.abs(np.log(np.maximum(stats[:, 1:], 1e-300))) + 1), 0).sum(1)
+        bound = w * T * T * size * u * (8 * t_far + 500) + 1e-37
+        bad = fin & (np.abs(got - loss) > bound)
+        assert not bad.any(), (np.argwhere(bad)[:3], got[bad][:3], loss[bad][:3], bound[bad][:3])
+    if out.get("stats") is not None:
+        got = _host(out["stats"])
+        live = stats[:, 1] != 0
+        assert np.array_equal(got[:, 0][~np.isnan(stats[:, 1])], stats[:, 0][~np.isnan(stats[:, 1])])
+        assert (got[~live] == 0).all()
+        assert np.allclose(got[live, 1], stats[live, 1], rtol=u * 1000, atol=0, equal_nan=True)
+
+
+SHAPES = [(1, 1, 1), (3, 2, 2), (5, 100, 7), (4, 511, 16), (9, 512, 1), (6, 513, 64), (3, 2048, 300), (4, 2049, 33), (2, 8192, 1024), (3, 8193, 50),
+          (130, 8200, 5), (3, 16385, 100), (2, 32000, 16), (129, 32769, 64), (2, 50257, 64), (1, 65536, 20), (2, 65537, 40), (1, 131073, 100), (130, 66000, 9),
+          (40, 300, 0), (64, 1000, 256)]
+
+
+@pytest.mark.parametrize("rows,vocab,k", SHAPES)
+@pytest.mark.parametrize("kind", ["float32", "float16", "bfloat16"])
+def test_loss_statistics_and_gradient(rows, vocab, k, kind):
+    T = (1.0, 0.7, 3.0)[(rows + vocab + k) % 3]
+    zd, idx, t, w = _inputs(rows, vocab, k, kind, rows * 7 + vocab)
+    out = _run(zd, idx, t, T, w)
+    _check(zd, idx, t, T, w, out, kind)
+
+
+@pytest.mark.parametrize("rows,vocab,k", [(3, 100, 5), (2, 5000, 20), (3, 40001, 30), (130, 40001, 30)])
+@pytest.mark.parametrize("kind", ["float32", "float16", "bfloat16"])
+@pytest.mark.parametrize("pad,offset", [(1, 1), (8, 0), (3, 5)])
+def test_rows_of_a_larger_buffer_and_each_output_alone(rows, vocab, k, kind, pad, offset):
+    import torch
+    zd, idx, t, w = _inputs(rows, vocab, k, kind, 5, pad, offset)
+    both = _run(zd, idx, t, 1.5, w)
+    _check(zd, idx, t, 1.5, w, both, kind)
+    loss = _run(zd, idx, t, 1.5, w, stats=False, grad=False)
+    assert torch.equal(loss["loss"], both["loss"])
+    stats = _run(zd, idx, t, 1.5, w, loss=False, grad=False)
+    assert torch.equal(stats["stats"], both["stats"])
+    grad = _run(zd, idx, t, 1.5, w, loss=False, stats=False)
+    assert torch.equal(grad["grad"], both["grad"])
+
+
+@pytest.mark.parametrize("rows,vocab,k", [(1, 1, 1), (5, 100, 7), (3, 8192, 64), (3, 8193, 64), (7, 32001, 100), (2, 70001, 1024), (200, 1000, 3)])
+@pytest.mark.parametrize("kind", ["float32", "float16", "bfloat16"])
+def test_gradient_behind_a_forward_pass(rows, vocab, k, kind):
+    import torch
+    kimad = _kimad()
+    T = 2.5
+    zd, idx, t, w = _inputs(rows, vocab, k, kind, 9, pad=3)
+    forward = _run(zd, idx, t, T, w, grad=False)
+    grad = torch.as_strided(torch.full((rows * (vocab + 5),), 7.0, dtype=zd.dtype, device="cuda"), (rows, vocab), (vocab + 5, 1))
+    idx_d, t_d, w_d = torch.from_numpy(idx.astype(np.int32)).cuda(), torch.from_numpy(t).cuda(), torch.from_numpy(w).cuda()
+    kimad.kimad_distill_grad(zd, idx_d, t_d, T, forward["stats"], grad, row_weight=w_d)
+    _check(zd, idx, t, T, w, dict(grad=grad), kind)
+    if rows > 1:
+        assert (grad.as_strided((rows - 1, 5), (vocab + 5, 1), vocab) == 7.0).all()
+
+
+@pytest.mark.parametrize("rows,vocab", [(4, 300), (4, 20000), (2, 70000), (140, 20000)])
+@pytest.mark.parametrize("kind", ["float32", "bfloat16"])
+def test_gradient_in_the_place_of_the_logits(rows, vocab, kind):
+    import torch
+    kimad = _kimad()
+    zd, idx, t, w = _inputs(rows, vocab, 50, kind, 2, pad=2)
+    both = _run(zd, idx, t, 1.0, w)
+    forward = _run(zd, idx, t, 1.0, w, grad=False)
+    idx_d, t_d, w_d = torch.from_numpy(idx.astype(np.int32)).cuda(), torch.from_numpy(t).cuda(), torch.from_numpy(w).cuda()
+    z2 = torch.empty(rows, vocab + 2, dtype=zd.dtype, device="cuda")[:, :vocab].copy_(zd)
+    loss, stats = torch.empty(rows, device="cuda"), torch.empty(rows, 2, device="cuda")
+    kimad.kimad_distill(z2, idx_d, t_d, 1.0, loss=loss, stats=stats, grad=z2, row_weight=w_d)
+    assert torch.equal(z2, both["grad"]) and torch.equal(loss, both["loss"]) and torch.equal(stats, both["stats"])
+    z3 = torch.empty(rows, vocab + 2, dtype=zd.dtype, device="cuda")[:, :vocab].copy_(zd)
+    kimad.kimad_distill_grad(z3, idx_d, t_d, 1.0, forward["stats"], z3, row_weight=w_d)
+    _check(zd, idx, t, 1.0, w, dict(grad=z3), kind)
+
+
+@pytest.mark.parametrize("vocab", [200, 9000, 40000, 70000])
+@pytest.mark.parametrize("kind", ["float32", "float16", "bfloat16"])
+def test_masks_and_what_is_not_finite(vocab, kind):
+    import torch
+    dt = getattr(torch, kind)
+    low = torch.finfo(dt).min
+    rows, k = 12, 6
+    rng = np.random.default_rng(3)
+    z = torch.from_numpy(rng.normal(0, 3, (rows, vocab))).to(dt)
+    idx = np.tile(np.array([3, 50, 7, 199, 150, 11]), (rows, 1))
+    t = rng.normal(0, 3, (rows, k)).astype(np.float32)
+    inf = float("inf")
+    z[0, 60:] = -inf                       # masked by -Inf, entries 199 and 150 among them: loss +Inf
+    z[1, 60:] = low                        # masked by the lowest value
+    z[2, :] = -inf                         # nothing left
+    z[3, :] = low                          # the lowest value everywhere: a uniform row
+    idx[4] = -1                            # no entry
+    t[5] = -inf                            # entries that the teacher rules out
+    t[6, 2:] = -inf
+    z[6, 150] = -inf                       # ruled out by both: adds nothing
+    z[7, 20] = inf
+    z[8, 20] = float("nan")
+    idx[9] = vocab + np.arange(k)          # beyond the vocabulary
+    z[10, :150], z[10, 151:] = -inf, -inf  # one logit alone, one entry alone
+    idx[10] = [150, -1, -1, -1, -1, -1]
+    idx[11] = [3, 7, 3, 3, 7, 11]          # indices given several times
+    for T in (0.5, 1.0, 4.0):
+        zd = z.cuda()
+        out = _run(zd, idx, t, T, None)
+        loss, stats, grad = (_host(out[n]) for n in ("loss", "stats", "grad"))
+        wl, ws, wg = ref.distill(_host(zd), idx, t, T, np.ones(rows))
+        for r in (2, 4, 5, 9):
+            assert loss[r] == 0 and not grad[r].any() and not stats[r].any(), r
+        assert loss[0] == inf and np.isfinite(grad[0]).all() and (grad[0, 60:][~np.isin(np.arange(60, vocab), (150, 199))] == 0).all()
+        assert np.isnan(loss[7]) and np.isnan(grad[7]).all() and np.isnan(loss[8]) and np.isnan(grad[8]).all()
+        with np.errstate(over="ignore"):   # (an entry masked by the lowest value may cost more than a float32 holds)
+            assert np.array_equal(np.isfinite(loss[[1, 3, 6, 10, 11]]), np.isfinite(wl[[1, 3, 6, 10, 11]].astype(np.float32)))
+        keep = [0, 6, 10, 11]
+        _check(zd[keep], idx[keep], t[keep], T, None, {n: out[n][keep] for n in ("loss", "stats", "grad")}, kind)
+        assert np.allclose(grad[3], wg[3], rtol=2 * HALF[kind] + 1e-4, atol=1e-9 + (2.0 ** -24 if kind == "float16" else 0))
+        assert np.allclose(grad[1, :60], wg[1, :60], rtol=2 * HALF[kind] + 1e-4, atol=1e-9 + (2.0 ** -24 if kind == "float16" else 0))
+        assert abs(loss[10]) < 1e-6 and abs(grad[10]).max() < 1e-6
+
+
+def test_gradient_against_differences_of_the_loss():
+    """Central differences of the library's own loss: steps of 1/16 keep the fp32 loss's rounding (2^-20 or so of a loss of some
+    units) below 1e-4 of the slope, and the cubic term, at most step^2/6 of a third derivative of at most 1/T, below 1e-3."""
+    import torch
+    kimad = _kimad()
+    vocab, k, T = 40, 5, 2.0
+    rng = np.random.default_rng(8)
+    z = rng.normal(0, 1, vocab).astype(np.float32)
+    idx, t = rng.choice(vocab, k, replace=False).astype(np.int32), rng.normal(0, 2, k).astype(np.float32)
+    step = 1.0 / 16
+    batch = np.tile(z, (2 * vocab, 1))
+    for v in range(vocab):
+        batch[2 * v, v] += step
+        batch[2 * v + 1, v] -= step
+    dev = lambda a: torch.from_numpy(np.ascontiguousarray(a)).cuda()                  # noqa: E731
+    loss = torch.empty(2 * vocab, device="cuda")
+    kimad.kimad_distill(dev(batch), dev(np.tile(idx, (2 * vocab, 1))), dev(np.tile(t, (2 * vocab, 1))), T, loss=loss)
+    loss = loss.cpu().double().numpy()
+    slope = (loss[0::2] - loss[1::2]) / (2 * step)
+    grad = torch.empty(1, vocab, device="cuda")
+    kimad.kimad_distill(dev(z[None]), dev(idx[None]), dev(t[None]), T, grad=grad)
+    assert np.abs(slope - grad.cpu().double().numpy()[0]).max() < 1e-3
+
+
+def test_again_and_on_another_stream_and_in_a_graph():
+    import torch
+    kimad = _kimad()
+    for rows, vocab in ((3, 50000), (300, 3000)):
+        zd, idx, t, w = _inputs(rows, vocab, 20, "float32", 4)
+        idx_d, t_d = torch.from_numpy(idx.astype(np.int32)).cuda(), torch.from_numpy(t).cuda()
+        loss, grad = torch.zeros(rows, device="cuda"), torch.zeros(rows, vocab, device="cuda")
+        ws = torch.empty(max(16, kimad.kimad_distill_workspace_bytes(rows, vocab, 20)), dtype=torch.uint8, device="cuda")
+
+        def work():
+            kimad.kimad_distill(zd, idx_d, t_d, 1.0, loss=loss, grad=grad, workspace=ws)
+
+        work()
+        torch.cuda.synchronize()
+        want = loss.clone(), grad.clone()
+        side = torch.cuda.Stream()
+        loss.zero_(), grad.zero_()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            work()
+        torch.cuda.current_stream().wait_stream(side)
+        assert torch.equal(loss, want[0]) and torch.equal(grad, want[1])
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            work()
+        for _ in range(3):
+            zd.mul_(0.5)
+            graph.replay()
+            got = loss.clone(), grad.clone()
+            work()
+            torch.cuda.synchronize()
+            assert torch.equal(loss, got[0]) and torch.equal(grad, got[1])

@@ -1,0 +1,115 @@
+"""What the operators beside a round refuse, before anything reaches a device (no GPU needed)."""
+import ctypes as C
+
+import pytest
+
+import paper_2312_08053_amd as kimad
+
+BAD, SMALL = -1, -2
+P = 0x10000                                                        # an address of the right alignment; nothing reads it
+
+
+def test_quantise_refuses():
+    f = kimad.lib().kimad_mx4_quantise
+    assert f(P, 3, 4, 4, 4, P, P, 0, 0, 0) == BAD                  # unknown type
+    assert f(P, 0, 4, 8, 7, P, P, 0, 0, 0) == BAD                  # rows overlap
+    assert f(P, 0, 4, 4, 4, 0, 0, 0, 0, 0) == BAD                  # nothing wanted
+    assert f(P, 0, 4, 4, 4, P, 0, 0, 0, 0) == BAD                  # codes without scales
+    assert f(P, 0, 4, 4, 4, P + 8, P, 0, 0, 0) == BAD              # alignment
+    assert f(P, 0, 4, 4, 4, P, P + 2, 0, 0, 0) == BAD
+    assert f(P + 2, 0, 4, 4, 4, P, P, 0, 0, 0) == BAD
+    assert f(P + 1, 2, 4, 4, 4, P, P, 0, 0, 0) == BAD
+    assert f(0, 0, 4, 4, 4, P, P, 0, 0, 0) == BAD
+    assert f(P, 0, 1 << 41, 4, 4, P, P, 0, 0, 0) == BAD
+    assert f(0, 0, 0, 4, 4, P, P, 0, 0, 0) == 0                    # no rows: nothing to do
+
+
+def test_dequantise_refuses():
+    f = kimad.lib().kimad_mx4_dequantise
+    assert f(P, P, 4, 4, P, 5, 4, 0) == BAD
+    assert f(P, P, 4, 4, P, 0, 3, 0) == BAD
+    assert f(0, P, 4, 4, P, 0, 4, 0) == BAD
+    assert f(P, P, 4, 4, 0, 0, 4, 0) == BAD
+    assert f(P + 4, P, 4, 4, P, 0, 4, 0) == BAD
+    assert f(P, P, 4, 4, P + 1, 1, 4, 0) == BAD
+    assert f(P, P, 4, 0, P, 0, 0, 0) == 0
+
+
+def test_matmul_refuses():
+    f = kimad.lib().kimad_mx4_matmul
+    assert f(P, P, 4, P, P, 4, 4, P, 3, 4, 0, 0, 0) == BAD
+    assert f(P, P, 4, P, P, 4, 4, P, 0, 3, 0, 0, 0) == BAD
+    assert f(0, P, 4, P, P, 4, 4, P, 0, 4, 0, 0, 0) == BAD
+    assert f(P, P, 4, P, 0, 4, 4, P, 0, 4, 0, 0, 0) == BAD
+    assert f(P, P, 4, P, P, 4, 4, 0, 0, 4, 0, 0, 0) == BAD
+    assert f(P, P, 4, P + 4, P, 4, 4, P, 0, 4, 0, 0, 0) == BAD
+    assert f(P, P, 4, P, P, 4, 4, P, 0, 4, P + 4, 64, 0) == BAD    # workspace alignment
+    assert f(P, P, 0, P, P, 4, 4, P, 0, 4, 0, 0, 0) == 0
+
+
+def test_update_and_server_refuse():
+    f = kimad.lib().kimad_mx4_compress_ef
+    assert f(0, P, P, 1, 4, P, P, 0, 0) == BAD
+    assert f(P, 0, P, 1, 4, P, P, 0, 0) == BAD
+    assert f(P, P, 0, 1, 4, P, P, 0, 0) == BAD
+    assert f(P, P, P, 0, 4, P, P, 0, 0) == BAD
+    assert f(P, P, P, 1, 0, P, P, 0, 0) == BAD
+    assert f(P, P, P, 1, 4, 0, 0, 0, 0) == BAD
+    assert f(P, P, P, 1, 4, P, 0, 0, 0) == BAD
+    assert f(P + 2, P, P, 1, 4, P, P, 0, 0) == BAD
+    assert kimad.kimad_mx4_update_words(3, 1000) == 10
+    from paper_2312_08053_amd.binding import _Mx4Update
+    s = kimad.lib().kimad_mx4_server_apply
+    up, bad, hat, w = (_Mx4Update * 1)(_Mx4Update(P, P)), (_Mx4Update * 1)(_Mx4Update(P, 0)), (C.c_void_p * 1)(P), (C.c_double * 1)(1.0)
+    none = (C.c_void_p * 1)(0)
+    assert s(up, hat, w, 0, P, 1, 4, 0, 0.0, 0, 0) == BAD
+    assert s(up, hat, w, 17, P, 1, 4, 0, 0.0, 0, 0) == BAD
+    assert s(bad, hat, w, 1, P, 1, 4, 0, 0.0, 0, 0) == BAD
+    assert s(up, none, w, 1, P, 1, 4, 0, 0.0, 0, 0) == BAD
+    assert s(up, hat, w, 1, 0, 1, 4, 0, 0.0, 0, 0) == BAD
+    assert s(up, hat, w, 1, P, 1, 4, P + 2, 0.0, 0, 0) == BAD
+
+
+def test_distillation_refuses():
+    f = kimad.lib().kimad_distill
+
+    def call(logits=P, kind=0, rows=4, vocab=100, ld=100, idx=P, val=P, k=8, T=1.0, weight=0, loss=P, stats=0, grad=0, ld_grad=0, ws=0, nbytes=0):
+        return f(logits, kind, rows, vocab, ld, idx, val, k, T, weight, loss, stats, grad, ld_grad, ws, nbytes, 0)
+
+    for bad in (dict(kind=3), dict(vocab=0), dict(vocab=1 << 31, ld=1 << 31), dict(ld=99), dict(k=1025), dict(T=0.0), dict(T=-1.0), dict(T=float("nan")),
+                dict(T=float("inf")), dict(T=1e-9), dict(logits=0), dict(idx=0), dict(val=0), dict(loss=0), dict(grad=P, ld_grad=99), dict(logits=P + 2),
+                dict(grad=P + 2, ld_grad=100)):
+        assert call(**bad) == BAD, bad
+    assert call(rows=0, logits=0) == 0
+    need = kimad.kimad_distill_workspace_bytes(1, 200000, 8)
+    assert need > 0
+    assert call(rows=1, vocab=200000, ld=200000) == SMALL
+    assert call(rows=1, vocab=200000, ld=200000, ws=P, nbytes=need - 1) == SMALL
+    g = kimad.lib().kimad_distill_grad
+    assert g(P, 0, 4, 100, 100, P, P, 8, 1.0, 0, 0, P, 100, 0) == BAD
+    assert g(P, 0, 4, 100, 100, P, P, 8, 1.0, 0, P, 0, 100, 0) == BAD
+
+
+def test_the_binding_refuses_tensors_that_do_not_fit():
+    import torch
+    x = torch.zeros(4, 100)
+    codes, scales = kimad.mx4_empty(4, 100, "cpu")
+    with pytest.raises(ValueError):
+        kimad.kimad_mx4_quantise(x.t(), codes, scales, stream=0)
+    with pytest.raises(ValueError):
+        kimad.kimad_mx4_quantise(torch.zeros(4, 200), codes, scales, stream=0)
+    with pytest.raises(ValueError):
+        kimad.kimad_mx4_quantise(torch.zeros(100), codes, scales, stream=0)
+    with pytest.raises(TypeError):
+        kimad.kimad_mx4_quantise(x.double(), codes, scales, stream=0)
+    with pytest.raises(ValueError):
+        kimad.kimad_mx4_matmul(codes, scales, codes, scales, 200, torch.zeros(4, 4), stream=0)
+    idx, val = torch.zeros(4, 3, dtype=torch.int32), torch.zeros(4, 3)
+    with pytest.raises(ValueError):
+        kimad.kimad_distill(x, idx[:3], val, 1.0, loss=torch.zeros(4), stream=0)
+    with pytest.raises(ValueError):
+        kimad.kimad_distill(x, idx, val, 1.0, loss=torch.zeros(3), stream=0)
+    with pytest.raises(ValueError):
+        kimad.kimad_distill(x, idx.long(), val, 1.0, loss=torch.zeros(4), stream=0)
+    with pytest.raises(ValueError):
+        kimad.kimad_distill(x, idx, val, 1.0, grad=torch.zeros(4, 99), stream=0)
