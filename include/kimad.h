@@ -393,7 +393,7 @@ int kimad_mx4_dequantise(const void* codes, const uint32_t* scales, uint64_t row
                          uint64_t ld, void* stream);
 
 /* Product C = A B^T of quantised matrices, A of M rows and K columns, B of N rows and K columns: out [M, N] of `type` with rows
- * ld >= N elements apart.  Products are exact, sums are fp32, and the sum is rounded once to `type` (F16: Inf beyond its range).  The
+ * ld >= N elements apart.  Products are exact, sums are fp32, and the sum is rounded once to `type` (F16: Inf beyond its range).  K is at most 2^25.  The
  * forward product of a layer takes activations and weights quantised along their columns' axis; its gradients take the
  * transposed forms (kimad_mx4_quantise).
  *   workspace  DEVICE, 16-byte aligned, kimad_mx4_matmul_workspace_bytes(M, N, K) bytes, or NULL: products with few rows and a long sum are

@@ -20,6 +20,7 @@ static_assert(TYPE_F32 == KIMAD_VALUES_F32 && TYPE_F16 == KIMAD_VALUES_F16 && TY
 static_assert(UPDATE_MAX_WORKERS == KIMAD_MAX_WORKERS, "header and kernel constants");
 
 constexpr uint64_t MOST = 1ull << 40;                    // elements along an axis that the checks below let through
+constexpr uint64_t MATMUL_MOST_K = 1ull << 25;           // a tile's 256 rows of codes are reached by 32-bit offsets
 constexpr uint64_t GRID_MOST = 0x7FFFFFFFull, GRID_Y_MOST = 65535;
 
 inline bool aligned(const void* p, uintptr_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
@@ -75,6 +76,15 @@ int launch_row(const DistillArgs& a, hipStream_t s) {
     return launched();
 }
 
+template <uint32_t TYPE, uint32_t BM, uint32_t BN, uint32_t WM, uint32_t WN>
+int launch_tile(MatmulArgs g, hipStream_t s) {
+    const uint64_t tm = (g.M + BM - 1) / BM, tn = (g.N + BN - 1) / BN;
+    if (tm * tn > GRID_MOST) return KIMAD_ERR_INVALID_ARG;
+    g.tiles_m = (uint32_t)tm; g.tiles_n = (uint32_t)tn;
+    hipLaunchKernelGGL((k_mx4_matmul_tile<TYPE, BM, BN, WM, WN>), dim3((uint32_t)(tm * tn)), dim3(64 * WM * WN), 0, s, g);
+    return launched();
+}
+
 }  // namespace
 
 extern "C" {
@@ -124,19 +134,21 @@ uint64_t kimad_mx4_matmul_workspace_bytes(uint64_t, uint64_t, uint64_t) { return
 int kimad_mx4_matmul(const void* a_codes, const uint32_t* a_scales, uint64_t M, const void* b_codes, const uint32_t* b_scales,
                      uint64_t N, uint64_t K, void* out, uint32_t type, uint64_t ld, void* workspace, uint64_t workspace_bytes,
                      void* stream) {
-    if (type > KIMAD_VALUES_BF16 || M > MOST || N > MOST || K > MOST || ld < N) return KIMAD_ERR_INVALID_ARG;
+    if (type > KIMAD_VALUES_BF16 || M > MOST || N > MOST || K > MATMUL_MOST_K || ld < N) return KIMAD_ERR_INVALID_ARG;
     if (M == 0 || N == 0) return KIMAD_OK;
     if (!out || !aligned(out, type_bytes(type))) return KIMAD_ERR_INVALID_ARG;
     if (K && (!a_codes || !b_codes || !pair_ok(a_codes, a_scales) || !pair_ok(b_codes, b_scales))) return KIMAD_ERR_INVALID_ARG;
     if (workspace && !aligned(workspace, 16)) return KIMAD_ERR_INVALID_ARG;
     (void)workspace_bytes;
-    const uint64_t W = words_of(K), gx = (N + 63) / 64, gy = (M + 15) / 16;
-    if (gx > GRID_MOST || gy > GRID_Y_MOST) return KIMAD_ERR_INVALID_ARG;
+    MatmulArgs g{};
+    g.a = static_cast<const uint8_t*>(a_codes); g.b = static_cast<const uint8_t*>(b_codes);
+    g.sa = a_scales; g.sb = b_scales; g.out = out; g.M = M; g.N = N; g.W = words_of(K); g.ld = ld;
     hipStream_t s = static_cast<hipStream_t>(stream);
     return with_type(type, [&](auto t) {
-        hipLaunchKernelGGL(k_mx4_matmul<decltype(t)::value>, dim3((uint32_t)gx, (uint32_t)gy), dim3(256), 0, s,
-                           static_cast<const u32x4*>(a_codes), a_scales, M, static_cast<const u32x4*>(b_codes), b_scales, N, W, out, ld);
-        return launched();
+        constexpr uint32_t TYPE = decltype(t)::value;
+        if (M * N >= 256ull * 256 * 128) return launch_tile<TYPE, 256, 256, 2, 4>(g, s);
+        if (M * N >= 128ull * 128 * 128) return launch_tile<TYPE, 128, 128, 2, 2>(g, s);
+        return launch_tile<TYPE, 64, 64, 2, 2>(g, s);
     });
 }
 
