@@ -10,6 +10,7 @@
 namespace kimad {
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 struct MatmulArgs {
@@ -18,6 +19,7 @@ struct MatmulArgs {
     void* out;
     uint64_t M, N, W, ld;        // W words a row
     uint32_t tiles_m, tiles_n;
+    uint32_t splits, share;      // parts of the sum, `share` stages each (the last one fewer); more than one: part p goes to out + p M ld
 };
 
 __device__ __forceinline__ i32x8 mx4_operand(u32x4 v) { return i32x8{(int)v.x, (int)v.y, (int)v.z, (int)v.w, 0, 0, 0, 0}; }
@@ -29,19 +31,49 @@ __device__ __forceinline__ void load_lds16(__amdgpu_buffer_rsrc_t from, uint32_t
     __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_u32*)(uintptr_t)lds, 16, (int)offset, (int)scalar_offset, 0, 0);
 }
 // 4 bytes of every lane, at `lds` + 4 * lane.
-__device__ __forceinline__ void load_lds4(const void* base, uint32_t offset, uint32_t lds) {
-    __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) uint32_t*)((uintptr_t)base + offset), (lds_u32*)(uintptr_t)lds, 4, 0, 0);
+__device__ __forceinline__ void load_lds4(__amdgpu_buffer_rsrc_t from, uint32_t offset, uint32_t lds) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_u32*)(uintptr_t)lds, 4, (int)offset, 0, 0, 0);
 }
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void* base, uint32_t bytes) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, (int)bytes, 0x00020000);
 }
-// Until at most N of the wave's loads are under way; then the workgroup's barrier.
-template <uint32_t N>
-__device__ __forceinline__ void vm_wait_barrier() {
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+// Until the wave's loads and stores are done but for the last N of them, or the last N + MORE where `more` is not 0; then the workgroup's barrier.  (One
+// piece of assembly, so that the loop around it stays one loop.)
+template <uint32_t N, uint32_t MORE>
+__device__ __forceinline__ void vm_wait_barrier(uint32_t more) {
+    static_assert(N + MORE < 64, "what the counter holds");
+    asm volatile("s_cmp_lg_u32 %2, 0\n\ts_cbranch_scc1 .Lmore%=\n\ts_waitcnt vmcnt(%0)\n.Lmore%=:\n\ts_waitcnt vmcnt(%1) lgkmcnt(0)\n\ts_barrier" ::"n"(N), "n"(N + MORE),
+                 "s"(__builtin_amdgcn_readfirstlane(more)) : "memory", "scc");
 }
 __device__ __forceinline__ uint32_t lds_address(const void* p) {
     return (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const void*)p);
+}
+
+// Four rows of one column in every lane of four neighbours -> four columns of one row: lane q of the four gets row q.  Two exchanges, of neighbours and of pairs.
+__device__ __forceinline__ void turn_quad(float v0, float v1, float v2, float v3, bool odd, bool high, float out[4]) {
+    auto swap1 = [](float x) { return __uint_as_float(dpp_u32<DPP_XOR1>(__float_as_uint(x))); };
+    auto swap2 = [](float x) { return __uint_as_float(dpp_u32<DPP_XOR2>(__float_as_uint(x))); };
+    const float r0 = swap1(odd ? v0 : v1), r1 = swap1(odd ? v2 : v3);
+    const float a0 = odd ? r0 : v0, a1 = odd ? v1 : r0, b0 = odd ? r1 : v2, b1 = odd ? v3 : r1;
+    const float s0 = swap2(high ? a0 : b0), s1 = swap2(high ? a1 : b1);
+    out[0] = high ? s0 : a0; out[1] = high ? s1 : a1; out[2] = high ? b0 : s0; out[3] = high ? b1 : s1;
+}
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+// Two values rounded to nearest even, the first one low.
+template <uint32_t TYPE>
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+    const f32x2 v = {a, b};
+    if (TYPE == TYPE_BF16) return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2));
+}
+// The same on pairs of 16-bit values: v01 holds rows 0 and 1, v23 rows 2 and 3.
+__device__ __forceinline__ void turn_quad16(uint32_t v01, uint32_t v23, bool odd, bool high, uint32_t out[2]) {
+    const uint32_t pick = odd ? 0x03020706u : 0x05040100u;                    // even: own low, other's low; odd: other's high, own high
+    const uint32_t a = __builtin_amdgcn_perm(dpp_u32<DPP_XOR1>(v01), v01, pick), b = __builtin_amdgcn_perm(dpp_u32<DPP_XOR1>(v23), v23, pick);
+    const uint32_t s = dpp_u32<DPP_XOR2>(high ? a : b);
+    out[0] = high ? s : a;
+    out[1] = high ? b : s;
 }
 
 // Tile number -> tile.  Workgroups go to the eight XCDs in turn; an XCD takes a run of tiles, in bands of eight rows of tiles, so that what its
@@ -54,170 +86,283 @@ __device__ __forceinline__ void tile_of(uint32_t id, uint32_t tm, uint32_t tn, u
     n = r / high;
 }
 
-// A tile of BM by BN, WM by WN waves.  Two words of K at a time, a stage, of which LDS holds two: codes (128 bytes a row, whole cache lines) and scale
-// words.  The blocks of a row are stored in an order that turns with the row (block b of row r at b ^ (r / 2 % 8)), so that sixteen lanes that
-// read one block of sixteen rows meet sixteen different groups of banks.
-template <uint32_t BM, uint32_t BN, uint32_t WM, uint32_t WN>
+// A tile of BM by BN, WM by WN waves.  Two words of K are a stage, of which LDS holds two: codes (128 bytes a row, whole cache lines: a word at a time, four
+// stages, took 8 % longer) and scale words.  The blocks of a row are stored in an order that turns with the row (block b of row r at b ^ (r / 2 % 8)), so
+// that sixteen lanes that read one block of sixteen rows meet sixteen different groups of banks.
+template <uint32_t BM_, uint32_t BN_, uint32_t WM_, uint32_t WN_>
 struct MatmulTile {
+    static constexpr uint32_t BM = BM_, BN = BN_, WM = WM_, WN = WN_;
     static constexpr uint32_t WAVES = WM * WN, TI = BM / WM / 32, TJ = BN / WN / 32;
-    static constexpr uint32_t LOADS = (BM + BN) / 8 / WAVES, GROUPS = (BM + BN) / 64 * 2, SLOADS = (GROUPS + WAVES - 1) / WAVES;
-    static constexpr uint32_t CODES = (BM + BN) * 128, STAGE = CODES + (BM + BN) * 8;
-    static constexpr uint32_t PITCH = 32 * TJ + 8;                            // of a row in the epilogue: 4 rows further, 32 banks further
-    static constexpr uint32_t LDS = 2 * STAGE > WAVES * 32 * PITCH * 4 ? 2 * STAGE : WAVES * 32 * PITCH * 4;
+    static constexpr uint32_t LOADS = (BM + BN) / 8 / WAVES, GROUPS = (BM + BN) / 32, SLOADS = (GROUPS + WAVES - 1) / WAVES;
+    static constexpr uint32_t CODES = (BM + BN) * 128, STAGE = CODES + (BM + BN) * 8, LDS = 2 * STAGE;
 };
 
-template <uint32_t TYPE, uint32_t BM, uint32_t BN, uint32_t WM, uint32_t WN>
-__global__ __launch_bounds__(64 * WM * WN) void k_mx4_matmul_tile(MatmulArgs g) {
-    using T = MatmulTile<BM, BN, WM, WN>;
+template <uint32_t TYPE, class T>
+__global__ __launch_bounds__(64 * T::WAVES, 2) void k_mx4_matmul_tile(MatmulArgs g) {
+    constexpr uint32_t BM = T::BM, BN = T::BN, WM = T::WM, WN = T::WN;
     __shared__ __attribute__((aligned(1024))) uint8_t s_mem[T::LDS];
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    uint32_t tm, tn;
-    tile_of(blockIdx.x, g.tiles_m, g.tiles_n, tm, tn);
-    const uint64_t m0 = (uint64_t)tm * BM, n0 = (uint64_t)tn * BN, row_bytes = g.W * 64;
+    const uint64_t row_bytes = g.W * 64, stages = (g.W + 1) / 2;
+    const uint32_t lds0 = lds_address(s_mem), tiles = g.tiles_m * g.tiles_n, items = tiles * g.splits;
 
-    // what the lane brings: of 8 rows a load, block (lane % 8) ^ (row / 2 % 8) of row lane / 8; zeros beyond the matrix.  Of a last stage of one
-    // word the lanes that would bring the second one bring the first.
+    // what the lane brings: of 8 rows a load, block (lane % 8) ^ (row / 2 % 8) of row lane / 8; zeros beyond the matrix
     static_assert(T::WAVES % 2 == 0, "a wave's groups of 8 rows have the same order of blocks");
     const uint32_t block = (lane & 7u) ^ ((4u * wave + (lane >> 4)) & 7u), offset = (lane >> 3) * (uint32_t)row_bytes + 16u * block;
     __amdgpu_buffer_rsrc_t from[T::LOADS];
-#pragma unroll
-    for (uint32_t i = 0; i < T::LOADS; ++i) {
-        const uint32_t group = i * T::WAVES + wave;                           // of 8 rows: A's first, then B's
-        const bool of_a = group < BM / 8;
-        const uint64_t first = (of_a ? m0 : n0) + 8 * (of_a ? group : group - BM / 8), rows = of_a ? g.M : g.N;
-        from[i] = buffer_of((of_a ? g.a : g.b) + first * row_bytes, first < rows ? (uint32_t)(rows - first < 8 ? rows - first : 8) * (uint32_t)row_bytes : 0u);
-    }
-    uint32_t soffset[T::SLOADS], sto[T::SLOADS], sword[T::SLOADS];
     const uint32_t* sbase[T::SLOADS];
-    uint64_t srows[T::SLOADS];
+    uint32_t sbytes[T::SLOADS];
+    uint64_t stage_in, stage_end;
+    auto aim = [&](uint32_t item) {
+        uint32_t tm = 0, tn = 0;
+        const bool none = item >= items;                                      // (behind the last one the loads go on, of nothing)
+        if (!none) tile_of(item % tiles, g.tiles_m, g.tiles_n, tm, tn);
+        stage_in = none ? 0 : (uint64_t)(item / tiles) * g.share;
+        stage_end = stage_in + g.share < stages ? stage_in + g.share : stages;
+        const uint64_t m0 = (uint64_t)tm * BM, n0 = (uint64_t)tn * BN;
 #pragma unroll
-    for (uint32_t i = 0; i < T::SLOADS; ++i) {
-        const uint32_t group = (i * T::WAVES + wave) % T::GROUPS;             // of 64 rows' scale words: A's, B's, then those of the second word
-        const uint32_t half = group % (T::GROUPS / 2);
-        const bool of_a = half < BM / 64;
-        const uint64_t first = of_a ? m0 : n0;
-        srows[i] = of_a ? g.M : g.N;
-        const uint32_t r = (of_a ? half : half - BM / 64) * 64 + lane, most = (uint32_t)(srows[i] - first < 256 ? srows[i] - first : 256) - 1;
-        sbase[i] = (of_a ? g.sa : g.sb) + first;
-        soffset[i] = 4u * (r < most ? r : most);
-        sword[i] = group / (T::GROUPS / 2);
-        sto[i] = T::CODES + group * 256u;
-    }
-    const uint32_t lds0 = lds_address(s_mem);
-    const uint64_t stages = (g.W + 1) / 2;
-
-    auto bring = [&](uint64_t s) {
-        const uint32_t stage = lds0 + (uint32_t)(s & 1) * T::STAGE;
-        const bool one = 2 * s + 1 == g.W;
+        for (uint32_t i = 0; i < T::LOADS; ++i) {
+            const uint32_t group = i * T::WAVES + wave;                       // of 8 rows: A's first, then B's
+            const bool of_a = group < BM / 8;
+            const uint64_t first = (of_a ? m0 : n0) + 8 * (of_a ? group : group - BM / 8), rows = none ? 0 : of_a ? g.M : g.N;
+            from[i] = buffer_of((of_a ? g.a : g.b) + first * row_bytes, first < rows ? (uint32_t)(rows - first < 8 ? rows - first : 8) * (uint32_t)row_bytes : 0u);
+        }
 #pragma unroll
-        for (uint32_t i = 0; i < T::LOADS; ++i) load_lds16(from[i], one && block >= 4 ? offset - 64u : offset, (uint32_t)s * 128u, stage + (i * T::WAVES + wave) * 1024u);
+        for (uint32_t i = 0; i < T::SLOADS; ++i) {
+            const uint32_t half = (i * T::WAVES + wave) % T::GROUPS % (T::GROUPS / 2);   // of 64 rows' scale words: A's, B's, then those of a second word
+            const bool of_a = half < BM / 64;
+            const uint64_t first = (of_a ? m0 : n0) + 64 * (of_a ? half : half - BM / 64), rows = none ? 0 : of_a ? g.M : g.N;
+            sbase[i] = (of_a ? g.sa : g.sb) + first;
+            sbytes[i] = first < rows ? (uint32_t)(rows - first < 64 ? rows - first : 64) * 4u : 0u;
+        }
+    };
+    // The stages of all the workgroup's items, one after another, into the two buffers in turn.
+    uint32_t item_in = blockIdx.x, buffer_in = 0;
+    aim(item_in);
+    auto bring = [&]() {
+        const uint32_t stage = lds0 + buffer_in * T::STAGE;
+        const bool one = 2 * stage_in + 1 == g.W;                             // (then the second word's codes are zeros, with the first one's scales)
 #pragma unroll
-        for (uint32_t i = 0; i < T::SLOADS; ++i) load_lds4(sbase[i] + (2 * s + (one ? 0 : sword[i])) * srows[i], soffset[i], stage + sto[i]);
+        for (uint32_t i = 0; i < T::LOADS; ++i)
+            load_lds16(from[i], one && block >= 4 ? 0xFFFFFFF0u : offset, (uint32_t)stage_in * 128u, stage + (i * T::WAVES + wave) * 1024u);
+#pragma unroll
+        for (uint32_t i = 0; i < T::SLOADS; ++i) {
+            const uint32_t group = (i * T::WAVES + wave) % T::GROUPS, word = group / (T::GROUPS / 2);
+            const uint64_t rows = group % (T::GROUPS / 2) < BM / 64 ? g.M : g.N;
+            load_lds4(buffer_of(sbase[i] + (2 * stage_in + (one ? 0 : word)) * rows, sbytes[i]), 4 * lane, stage + T::CODES + group * 256u);
+        }
+        buffer_in ^= 1u;
+        if (++stage_in == stage_end) {
+            item_in += gridDim.x;
+            aim(item_in);
+        }
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
     };
 
     const uint32_t wm = wave / WN, wn = wave % WN, r32 = lane & 31u, kb = lane >> 5;
     const uint32_t a_row = wm * (BM / WM) + r32, b_row = BM + wn * (BN / WN) + r32;
     f32x16 acc[T::TI][T::TJ];
-#pragma unroll
-    for (uint32_t i = 0; i < T::TI; ++i)
-#pragma unroll
-        for (uint32_t j = 0; j < T::TJ; ++j) acc[i][j] = f32x16{};
-
     // The operands of half a word: its codes, and the scale words turned so that the lane's own bytes are the lowest and the third.
     struct Half {
         u32x4 a[T::TI], b[T::TJ];
     } half0, half1;
-    uint32_t sa[2][T::TI], sb[2][T::TJ];
-    const uint32_t turn = (r32 >> 1) & 7u;                                    // (rows 32 apart have the same order of blocks)
-    auto read = [&](uint64_t s, uint32_t word, uint32_t step, Half& h) {
-        const uint8_t* at = s_mem + (uint32_t)(s & 1) * T::STAGE + 16u * ((4 * word + 2 * step + kb) ^ turn);
+    uint32_t sa[T::TI], sb[T::TJ], sa_raw[T::TI], sb_raw[T::TJ];
+    const uint32_t turn = (r32 >> 1) & 7u;                      // (rows 32 apart have the same order of blocks)
+    auto read = [&](uint32_t buffer, uint32_t word, uint32_t step, Half& h) {
+        const uint8_t* at = s_mem + buffer * T::STAGE + 16u * ((4 * word + 2 * step + kb) ^ turn);
 #pragma unroll
         for (uint32_t i = 0; i < T::TI; ++i) h.a[i] = *reinterpret_cast<const u32x4*>(at + (a_row + 32 * i) * 128);
 #pragma unroll
         for (uint32_t j = 0; j < T::TJ; ++j) h.b[j] = *reinterpret_cast<const u32x4*>(at + (b_row + 32 * j) * 128);
     };
-    auto read_scales = [&](uint64_t s, uint32_t word) {
-        const uint32_t* words = reinterpret_cast<const uint32_t*>(s_mem + (uint32_t)(s & 1) * T::STAGE + T::CODES) + word * (BM + BN);
+    auto read_scales = [&](uint32_t buffer, uint32_t word) {
+        const uint32_t* words = reinterpret_cast<const uint32_t*>(s_mem + buffer * T::STAGE + T::CODES) + word * (BM + BN);
 #pragma unroll
-        for (uint32_t i = 0; i < T::TI; ++i) sa[word][i] = words[a_row + 32 * i];
+        for (uint32_t i = 0; i < T::TI; ++i) sa_raw[i] = words[a_row + 32 * i];
 #pragma unroll
-        for (uint32_t j = 0; j < T::TJ; ++j) sb[word][j] = words[b_row + 32 * j];
+        for (uint32_t j = 0; j < T::TJ; ++j) sb_raw[j] = words[b_row + 32 * j];
     };
-    auto turn_scales = [&](uint32_t word) {
+    auto turn_scales = [&]() {
 #pragma unroll
-        for (uint32_t i = 0; i < T::TI; ++i) sa[word][i] >>= 8 * kb;
+        for (uint32_t i = 0; i < T::TI; ++i) sa[i] = sa_raw[i] >> (8 * kb);
 #pragma unroll
-        for (uint32_t j = 0; j < T::TJ; ++j) sb[word][j] >>= 8 * kb;
+        for (uint32_t j = 0; j < T::TJ; ++j) sb[j] = sb_raw[j] >> (8 * kb);
     };
-    auto multiply = [&](const Half& h, uint32_t word, auto opsel) {
+    auto multiply = [&](const Half& h, auto opsel) {
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (uint32_t i = 0; i < T::TI; ++i)
 #pragma unroll
             for (uint32_t j = 0; j < T::TJ; ++j)
-                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(mx4_operand(h.a[i]), mx4_operand(h.b[j]), acc[i][j], 4, 4, decltype(opsel)::value, sa[word][i],
-                                                                             decltype(opsel)::value, sb[word][j]);
+                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(mx4_operand(h.a[i]), mx4_operand(h.b[j]), acc[i][j], 4, 4, decltype(opsel)::value, sa[i],
+                                                                             decltype(opsel)::value, sb[j]);
+        // (used here: the compiler would otherwise move the products behind the branches and waits that follow, where no reads are left to hide)
+#pragma unroll
+        for (uint32_t i = 0; i < T::TI; ++i)
+#pragma unroll
+            for (uint32_t j = 0; j < T::TJ; ++j) asm volatile("" : "+v"(acc[i][j]));
         __builtin_amdgcn_sched_barrier(0);
     };
     constexpr std::integral_constant<int, 0> first_half{};
     constexpr std::integral_constant<int, 2> second_half{};
-    // The reads of one half are under way while the other is multiplied, across stages too: the barrier in front of a stage's last half waits for the
-    // next stage, whose first half is then read, and behind it this stage is no longer read and its buffer takes the one after the next.
-    if (g.W) {
-        bring(0);
-        if (stages > 1) {
-            bring(1);
-            vm_wait_barrier<T::LOADS + T::SLOADS>();
-        } else {
-            vm_wait_barrier<0>();
+    // The reads of one half are under way while the other is multiplied, across stages and items too: the barrier in front of a stage's last half waits for
+    // the next stage, whose first half is then read, and behind it this stage is no longer read and its buffer takes the one after the next.  A
+    // tile is stored while the next item's first stage comes; the next barrier lets these stores be.
+    constexpr uint32_t STORES = 4 * T::TI * T::TJ;
+    bring();
+    bring();
+    vm_wait_barrier<T::LOADS + T::SLOADS, 0>(0);
+    uint32_t buffer = 0;
+    read_scales(0, 0);
+    read(0, 0, 0, half0);
+    uint32_t stores_behind = 0;                                               // 1: the wave's last STORES accesses are a tile's stores
+    for (uint32_t item = blockIdx.x; item < items; item += gridDim.x) {
+        const uint64_t first = (uint64_t)(item / tiles) * g.share, here = stages - first < g.share ? stages - first : g.share;
+#pragma unroll
+        for (uint32_t i = 0; i < T::TI; ++i)
+#pragma unroll
+            for (uint32_t j = 0; j < T::TJ; ++j) acc[i][j] = f32x16{};
+#pragma nounroll
+        for (uint64_t s = 0; s < here; ++s) {
+            turn_scales();
+            read(buffer, 0, 1, half1);
+            multiply(half0, first_half);
+            read_scales(buffer, 1);
+            read(buffer, 1, 0, half0);
+            multiply(half1, second_half);
+            turn_scales();
+            read(buffer, 1, 1, half1);
+            multiply(half0, first_half);
+            vm_wait_barrier<0, STORES>(stores_behind);
+            stores_behind = 0;
+            bring();
+            buffer ^= 1u;
+            read_scales(buffer, 0);                                           // (behind the last item: of a buffer, and for nothing)
+            read(buffer, 0, 0, half0);
+            multiply(half1, second_half);
         }
-        read_scales(0, 0);
-        read(0, 0, 0, half0);
-    }
-    for (uint64_t s = 0; s < g.W / 2; ++s) {
-        turn_scales(0);
-        read(s, 0, 1, half1);
-        multiply(half0, 0, first_half);
-        read_scales(s, 1);
-        read(s, 1, 0, half0);
-        multiply(half1, 0, second_half);
-        turn_scales(1);
-        read(s, 1, 1, half1);
-        multiply(half0, 1, first_half);
-        vm_wait_barrier<0>();
-        if (s + 2 < stages) bring(s + 2);
-        read_scales(s + 1, 0);                                                // (behind the last stage: of a buffer, and for nothing)
-        read(s + 1, 0, 0, half0);
-        multiply(half1, 1, second_half);
-    }
-    if (g.W & 1) {
-        turn_scales(0);
-        read(g.W / 2, 0, 1, half1);
-        multiply(half0, 0, first_half);
-        multiply(half1, 0, second_half);
-    }
 
-    // the wave's tile leaves 32 rows at a time through LDS, so that stores run along the rows
-    __syncthreads();
-    float* mine = reinterpret_cast<float*>(s_mem) + wave * 32 * T::PITCH;
-    constexpr uint32_t COLS = 32 * T::TJ, LANES = COLS / 8;
+        uint32_t tm, tn;
+        tile_of(item % tiles, g.tiles_m, g.tiles_n, tm, tn);
+        const uint64_t tile_m = (uint64_t)tm * BM, tile_n = (uint64_t)tn * BN;
+        // four columns of a row in every lane, eight rows a store
+        constexpr uint32_t BYTES = TYPE == TYPE_F32 ? 4 : 2, BEYOND = 0xFFFFFFF0u;
+        uint32_t l;                                                           // the lane, found anew: kept through the loop, it would cost a register
+        asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(l));
+        const uint32_t row = wm * (BM / WM) + 4 * (l >> 5) + (l & 3u), col = wn * (BN / WN) + (l & 28u), at = (row * (uint32_t)g.ld + col) * BYTES;
+        const uint32_t rows = g.M - tile_m < BM ? (uint32_t)(g.M - tile_m) : BM, cols = g.N - tile_n < BN ? (uint32_t)(g.N - tile_n) : BN;
+        const bool odd = l & 1u, high = l & 2u;
+        const bool whole = rows == BM && cols == BN;
+        stores_behind = whole ? 1u : 0u;
 #pragma unroll
-    for (uint32_t i = 0; i < T::TI; ++i) {
+        for (uint32_t i = 0; i < T::TI; ++i) {
+            const __amdgpu_buffer_rsrc_t to = buffer_of(static_cast<uint8_t*>(g.out) + (((item / tiles) * g.M + tile_m + 32 * i) * g.ld + tile_n) * BYTES, 0xFFFFFF00u);
 #pragma unroll
-        for (uint32_t j = 0; j < T::TJ; ++j)
+            for (uint32_t j = 0; j < T::TJ; ++j)
 #pragma unroll
-            for (uint32_t e = 0; e < 16; ++e) mine[(8 * (e / 4) + 4 * kb + e % 4) * T::PITCH + 32 * j + r32] = acc[i][j][e];
-        wave_sync_lds();
+                for (uint32_t e = 0; e < 4; ++e) {
+                    const f32x16 v = acc[i][j];
+                    const uint32_t o = at + 32 * j * BYTES, step = 8 * e * (uint32_t)g.ld * BYTES;
+                    if (TYPE == TYPE_F32) {
+                        float r[4];
+                        turn_quad(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3], odd, high, r);
+                        if (whole) {
+                            __builtin_amdgcn_raw_buffer_store_b128(u32x4{__float_as_uint(r[0]), __float_as_uint(r[1]), __float_as_uint(r[2]), __float_as_uint(r[3])}, to, o, step, 0);
+                        } else {
 #pragma unroll
-        for (uint32_t p = 0; p < 32 * LANES / 64; ++p) {
-            const uint32_t r = p * (64 / LANES) + lane / LANES, c = 8 * (lane % LANES);
-            const f32x4 lo = *reinterpret_cast<const f32x4*>(mine + r * T::PITCH + c), hi = *reinterpret_cast<const f32x4*>(mine + r * T::PITCH + c + 4);
-            const float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-            const uint64_t m = m0 + wm * (BM / WM) + 32 * i + r, n = n0 + wn * COLS + c;
-            if (m < g.M) store8_first<TYPE>(g.out, m * g.ld + n, (int64_t)g.N - (int64_t)n, v);
+                            for (uint32_t k = 0; k < 4; ++k)
+                                __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(r[k]), to, row + 32 * i + 8 * e < rows && col + 32 * j + k < cols ? o + 4 * k : BEYOND, step, 0);
+                        }
+                    } else {
+                        uint32_t r[2];
+                        turn_quad16(pack2<TYPE>(v[4 * e], v[4 * e + 1]), pack2<TYPE>(v[4 * e + 2], v[4 * e + 3]), odd, high, r);
+                        if (whole) {
+                            __builtin_amdgcn_raw_buffer_store_b64(u32x2{r[0], r[1]}, to, o, step, 0);
+                        } else {
+#pragma unroll
+                            for (uint32_t k = 0; k < 4; ++k)
+                                __builtin_amdgcn_raw_buffer_store_b16((uint16_t)(r[k / 2] >> (16 * (k % 2))), to, row + 32 * i + 8 * e < rows && col + 32 * j + k < cols ? o + 2 * k : BEYOND, step, 0);
+                        }
+                    }
+                }
         }
-        wave_sync_lds();
+        if (!whole) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");          // (so many more stores that the counter would not tell)
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                          // no load may reach LDS that is another workgroup's by then
+}
+
+// The parts of a sum, in their order.
+template <uint32_t TYPE>
+__global__ __launch_bounds__(256) void k_mx4_matmul_join(const float* __restrict__ parts, uint32_t splits, uint64_t M, uint64_t N, void* __restrict__ out, uint64_t ld) {
+    const uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= M * N) return;
+    float v = parts[i];
+    for (uint32_t p = 1; p < splits; ++p) v += parts[p * M * N + i];
+    store1<TYPE>(out, i / N * ld + i % N, v);
+}
+
+// Few rows of A: sixteen rows of B by a workgroup, whose four waves take every fourth pair of words.  Bound by the reads of B, which go straight to
+// registers, eight words of a wave under way at a time.  MT: sixteens of A's rows.
+template <uint32_t TYPE, uint32_t MT>
+__global__ __launch_bounds__(256) void k_mx4_matmul_few(MatmulArgs g) {
+    __shared__ f32x4 s_part[3][MT][64];
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, r = lane & 15u, blk = lane >> 4;
+    const uint64_t n0 = (uint64_t)blockIdx.x * 16, n = n0 + r < g.N ? n0 + r : g.N - 1;
+    const u32x4* b = reinterpret_cast<const u32x4*>(g.b) + n * g.W * 4 + blk;
+    const u32x4* a[MT];
+    uint64_t m[MT];
+    f32x4 acc[MT];
+#pragma unroll
+    for (uint32_t t = 0; t < MT; ++t) {
+        m[t] = 16 * t + r < g.M ? 16 * t + r : g.M - 1;
+        a[t] = reinterpret_cast<const u32x4*>(g.a) + m[t] * g.W * 4 + blk;
+        acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    constexpr uint32_t U = MT == 1 ? 8 : 4;
+    for (uint64_t w0 = 2 * wave; w0 < g.W; w0 += 4 * U) {
+        u32x4 vb[U], va[U][MT];
+        uint32_t sb[U], sa[U][MT];
+#pragma unroll
+        for (uint32_t u = 0; u < U; ++u) {
+            const uint64_t at = w0 + 8 * (u / 2) + u % 2, w = at < g.W ? at : g.W - 1;   // (a word beyond the last one is the last one, with codes of zero)
+            vb[u] = b[w * 4];
+            sb[u] = g.sb[w * g.N + n];
+#pragma unroll
+            for (uint32_t t = 0; t < MT; ++t) {
+                va[u][t] = a[t][w * 4];
+                sa[u][t] = g.sa[w * g.M + m[t]];
+            }
+        }
+#pragma unroll
+        for (uint32_t u = 0; u < U; ++u) {
+            const bool in = w0 + 8 * (u / 2) + u % 2 < g.W;
+            const u32x4 v = in ? vb[u] : u32x4{0, 0, 0, 0};
+#pragma unroll
+            for (uint32_t t = 0; t < MT; ++t)
+                acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(mx4_operand(va[u][t]), mx4_operand(v), acc[t], 4, 4, 0, sa[u][t] >> (8 * blk), 0, sb[u] >> (8 * blk));
+        }
+    }
+    if (wave)
+#pragma unroll
+        for (uint32_t t = 0; t < MT; ++t) s_part[wave - 1][t][lane] = acc[t];
+    __syncthreads();
+    if (wave) return;
+#pragma unroll
+    for (uint32_t t = 0; t < MT; ++t) {
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) {
+            const float v = acc[t][i] + s_part[0][t][lane][i] + s_part[1][t][lane][i] + s_part[2][t][lane][i];
+            const uint64_t row = 16 * t + 4 * blk + i;
+            if (row < g.M && n0 + r < g.N) store1<TYPE>(g.out, row * g.ld + n0 + r, v);
+        }
+    }
+}
+
+// A product over no words.
+template <uint32_t TYPE>
+__global__ __launch_bounds__(256) void k_mx4_matmul_none(void* out, uint64_t M, uint64_t N, uint64_t ld) {
+    const uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i < M * N) store1<TYPE>(out, i / N * ld + i % N, 0.f);
 }
 
 }  // namespace kimad

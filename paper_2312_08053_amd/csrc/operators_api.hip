@@ -20,7 +20,9 @@ static_assert(TYPE_F32 == KIMAD_VALUES_F32 && TYPE_F16 == KIMAD_VALUES_F16 && TY
 static_assert(UPDATE_MAX_WORKERS == KIMAD_MAX_WORKERS, "header and kernel constants");
 
 constexpr uint64_t MOST = 1ull << 40;                    // elements along an axis that the checks below let through
-constexpr uint64_t MATMUL_MOST_K = 1ull << 25;           // a tile's 256 rows of codes are reached by 32-bit offsets
+constexpr uint64_t FEW_ROWS = 32;                        // products of so many rows go by k_mx4_matmul_few
+constexpr uint64_t UNITS = 256;                         // compute units of the device
+constexpr uint64_t MATMUL_MOST_K = 1ull << 25, MATMUL_MOST_LD = 1ull << 24;     // eight rows of codes and a tile's rows of the result are reached by 32-bit offsets
 constexpr uint64_t GRID_MOST = 0x7FFFFFFFull, GRID_Y_MOST = 65535;
 
 inline bool aligned(const void* p, uintptr_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
@@ -76,12 +78,46 @@ int launch_row(const DistillArgs& a, hipStream_t s) {
     return launched();
 }
 
-template <uint32_t TYPE, uint32_t BM, uint32_t BN, uint32_t WM, uint32_t WN>
-int launch_tile(MatmulArgs g, hipStream_t s) {
-    const uint64_t tm = (g.M + BM - 1) / BM, tn = (g.N + BN - 1) / BN;
-    if (tm * tn > GRID_MOST) return KIMAD_ERR_INVALID_ARG;
-    g.tiles_m = (uint32_t)tm; g.tiles_n = (uint32_t)tn;
-    hipLaunchKernelGGL((k_mx4_matmul_tile<TYPE, BM, BN, WM, WN>), dim3((uint32_t)(tm * tn)), dim3(64 * WM * WN), 0, s, g);
+typedef MatmulTile<256, 256, 2, 4> Tile256;
+typedef MatmulTile<128, 128, 2, 2> Tile128;
+typedef MatmulTile<64, 64, 2, 2> Tile64;
+
+// How a product is shared out.
+struct MatmulPlan {
+    enum { FEW, T64, T128, T256 } kind;
+    uint64_t tiles_m, tiles_n;
+    uint32_t splits, share;
+};
+template <class T>
+uint64_t rounds_of(uint64_t M, uint64_t N) {
+    const uint64_t tiles = ((M + T::BM - 1) / T::BM) * ((N + T::BN - 1) / T::BN), slots = UNITS * ((160 * 1024) / T::LDS);
+    return (tiles + slots - 1) / slots;
+}
+MatmulPlan matmul_plan(uint64_t M, uint64_t N, uint64_t W) {
+    MatmulPlan p{};
+    p.splits = 1;
+    p.share = (uint32_t)((W + 1) / 2);
+    if (M <= FEW_ROWS) {
+        p.kind = MatmulPlan::FEW;
+        return p;
+    }
+    const uint64_t cost256 = 100 * rounds_of<Tile256>(M, N), cost128 = 59 * rounds_of<Tile128>(M, N), cost64 = 40 * rounds_of<Tile64>(M, N);
+    uint64_t edge = 64, slots = UNITS * ((160 * 1024) / Tile64::LDS);
+    p.kind = MatmulPlan::T64;
+    if (cost256 <= cost128 && cost256 <= cost64) { p.kind = MatmulPlan::T256; edge = 256; slots = UNITS; }
+    else if (cost128 <= cost64) { p.kind = MatmulPlan::T128; edge = 128; slots = UNITS * ((160 * 1024) / Tile128::LDS); }
+    p.tiles_m = (M + edge - 1) / edge;
+    p.tiles_n = (N + edge - 1) / edge;
+    return p;
+}
+
+template <uint32_t TYPE, class T>
+int launch_tile(MatmulArgs g, const MatmulPlan& p, hipStream_t s) {
+    const uint64_t items = p.tiles_m * p.tiles_n * p.splits;
+    if (items > GRID_MOST) return KIMAD_ERR_INVALID_ARG;
+    constexpr uint64_t slots = UNITS * ((160 * 1024) / T::LDS);
+    g.tiles_m = (uint32_t)p.tiles_m; g.tiles_n = (uint32_t)p.tiles_n; g.splits = p.splits; g.share = p.share;
+    hipLaunchKernelGGL((k_mx4_matmul_tile<TYPE, T>), dim3((uint32_t)std::min<uint64_t>(items, slots)), dim3(64 * T::WAVES), 0, s, g);
     return launched();
 }
 
@@ -134,7 +170,7 @@ uint64_t kimad_mx4_matmul_workspace_bytes(uint64_t, uint64_t, uint64_t) { return
 int kimad_mx4_matmul(const void* a_codes, const uint32_t* a_scales, uint64_t M, const void* b_codes, const uint32_t* b_scales,
                      uint64_t N, uint64_t K, void* out, uint32_t type, uint64_t ld, void* workspace, uint64_t workspace_bytes,
                      void* stream) {
-    if (type > KIMAD_VALUES_BF16 || M > MOST || N > MOST || K > MATMUL_MOST_K || ld < N) return KIMAD_ERR_INVALID_ARG;
+    if (type > KIMAD_VALUES_BF16 || M > MOST || N > MOST || K > MATMUL_MOST_K || ld < N || ld > MATMUL_MOST_LD) return KIMAD_ERR_INVALID_ARG;
     if (M == 0 || N == 0) return KIMAD_OK;
     if (!out || !aligned(out, type_bytes(type))) return KIMAD_ERR_INVALID_ARG;
     if (K && (!a_codes || !b_codes || !pair_ok(a_codes, a_scales) || !pair_ok(b_codes, b_scales))) return KIMAD_ERR_INVALID_ARG;
@@ -142,13 +178,26 @@ int kimad_mx4_matmul(const void* a_codes, const uint32_t* a_scales, uint64_t M, 
     (void)workspace_bytes;
     MatmulArgs g{};
     g.a = static_cast<const uint8_t*>(a_codes); g.b = static_cast<const uint8_t*>(b_codes);
+    const MatmulPlan p = matmul_plan(M, N, words_of(K));
     g.sa = a_scales; g.sb = b_scales; g.out = out; g.M = M; g.N = N; g.W = words_of(K); g.ld = ld;
     hipStream_t s = static_cast<hipStream_t>(stream);
     return with_type(type, [&](auto t) {
         constexpr uint32_t TYPE = decltype(t)::value;
-        if (M * N >= 256ull * 256 * 128) return launch_tile<TYPE, 256, 256, 2, 4>(g, s);
-        if (M * N >= 128ull * 128 * 128) return launch_tile<TYPE, 128, 128, 2, 2>(g, s);
-        return launch_tile<TYPE, 64, 64, 2, 2>(g, s);
+        if (K == 0) {
+            if ((M * N + 255) / 256 > GRID_MOST) return (int)KIMAD_ERR_INVALID_ARG;
+            hipLaunchKernelGGL(k_mx4_matmul_none<TYPE>, dim3((uint32_t)((M * N + 255) / 256)), dim3(256), 0, s, out, M, N, ld);
+            return launched();
+        }
+        if (p.kind == MatmulPlan::FEW) {
+            const uint64_t wgs = (N + 15) / 16;
+            if (wgs > GRID_MOST) return (int)KIMAD_ERR_INVALID_ARG;
+            if (M <= 16) hipLaunchKernelGGL((k_mx4_matmul_few<TYPE, 1>), dim3((uint32_t)wgs), dim3(256), 0, s, g);
+            else hipLaunchKernelGGL((k_mx4_matmul_few<TYPE, 2>), dim3((uint32_t)wgs), dim3(256), 0, s, g);
+            return launched();
+        }
+        if (p.kind == MatmulPlan::T256) return launch_tile<TYPE, Tile256>(g, p, s);
+        if (p.kind == MatmulPlan::T128) return launch_tile<TYPE, Tile128>(g, p, s);
+        return launch_tile<TYPE, Tile64>(g, p, s);
     });
 }
 
