@@ -131,25 +131,31 @@ __global__ __launch_bounds__(64 * T::WAVES, 2) void k_mx4_matmul_tile(MatmulArgs
             const uint32_t half = (i * T::WAVES + wave) % T::GROUPS % (T::GROUPS / 2);   // of 64 rows' scale words: A's, B's, then those of a second word
             const bool of_a = half < BM / 64;
             const uint64_t first = (of_a ? m0 : n0) + 64 * (of_a ? half : half - BM / 64), rows = none ? 0 : of_a ? g.M : g.N;
-            sbase[i] = (of_a ? g.sa : g.sb) + first;
+            sbase[i] = (of_a ? g.sa : g.sb) + first + (2 * stage_in + (i * T::WAVES + wave) % T::GROUPS / (T::GROUPS / 2)) * (of_a ? g.M : g.N);
             sbytes[i] = first < rows ? (uint32_t)(rows - first < 64 ? rows - first : 64) * 4u : 0u;
         }
     };
     // The stages of all the workgroup's items, one after another, into the two buffers in turn.
     uint32_t item_in = blockIdx.x, buffer_in = 0;
     aim(item_in);
-    auto bring = [&]() {
+    // part `k` of `n` of a stage's loads
+    auto bring = [&](uint32_t k, uint32_t n) {
         const uint32_t stage = lds0 + buffer_in * T::STAGE;
         const bool one = 2 * stage_in + 1 == g.W;                             // (then the second word's codes are zeros, with the first one's scales)
+        const uint32_t lane_offset = one && block >= 4 ? 0xFFFFFFF0u : offset;
 #pragma unroll
-        for (uint32_t i = 0; i < T::LOADS; ++i)
-            load_lds16(from[i], one && block >= 4 ? 0xFFFFFFF0u : offset, (uint32_t)stage_in * 128u, stage + (i * T::WAVES + wave) * 1024u);
+        for (uint32_t i = k * T::LOADS / n; i < (k + 1) * T::LOADS / n; ++i)
+            load_lds16(from[i], lane_offset, (uint32_t)stage_in * 128u, stage + (i * T::WAVES + wave) * 1024u);
+        if (k + 1 < n) return;
 #pragma unroll
         for (uint32_t i = 0; i < T::SLOADS; ++i) {
-            const uint32_t group = (i * T::WAVES + wave) % T::GROUPS, word = group / (T::GROUPS / 2);
+            const uint32_t group = (i * T::WAVES + wave) % T::GROUPS;
             const uint64_t rows = group % (T::GROUPS / 2) < BM / 64 ? g.M : g.N;
-            load_lds4(buffer_of(sbase[i] + (2 * stage_in + (one ? 0 : word)) * rows, sbytes[i]), 4 * lane, stage + T::CODES + group * 256u);
+            load_lds4(buffer_of(one && group >= T::GROUPS / 2 ? sbase[i] - rows : sbase[i], sbytes[i]), 4 * lane, stage + T::CODES + group * 256u);
+            sbase[i] += 2 * rows;
         }
+    };
+    auto brought = [&]() {
         buffer_in ^= 1u;
         if (++stage_in == stage_end) {
             item_in += gridDim.x;
@@ -188,29 +194,31 @@ __global__ __launch_bounds__(64 * T::WAVES, 2) void k_mx4_matmul_tile(MatmulArgs
 #pragma unroll
         for (uint32_t j = 0; j < T::TJ; ++j) sb[j] = sb_raw[j] >> (8 * kb);
     };
-    auto multiply = [&](const Half& h, auto opsel) {
+    auto multiply = [&](const Half& h, auto opsel, auto between) {
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (uint32_t i = 0; i < T::TI; ++i)
 #pragma unroll
-            for (uint32_t j = 0; j < T::TJ; ++j)
+            for (uint32_t j = 0; j < T::TJ; ++j) {
                 acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(mx4_operand(h.a[i]), mx4_operand(h.b[j]), acc[i][j], 4, 4, decltype(opsel)::value, sa[i],
                                                                              decltype(opsel)::value, sb[j]);
-        // (used here: the compiler would otherwise move the products behind the branches and waits that follow, where no reads are left to hide)
-#pragma unroll
-        for (uint32_t i = 0; i < T::TI; ++i)
-#pragma unroll
-            for (uint32_t j = 0; j < T::TJ; ++j) asm volatile("" : "+v"(acc[i][j]));
+                // (used here: the compiler would otherwise move the products behind the branches and waits that follow, where no reads are left to hide)
+                asm volatile("" : "+v"(acc[i][j]));
+                between(i * T::TJ + j);
+            }
         __builtin_amdgcn_sched_barrier(0);
     };
+    auto nothing = [](uint32_t) {};
     constexpr std::integral_constant<int, 0> first_half{};
     constexpr std::integral_constant<int, 2> second_half{};
     // The reads of one half are under way while the other is multiplied, across stages and items too: the barrier in front of a stage's last half waits for
     // the next stage, whose first half is then read, and behind it this stage is no longer read and its buffer takes the one after the next.  A
     // tile is stored while the next item's first stage comes; the next barrier lets these stores be.
     constexpr uint32_t STORES = 4 * T::TI * T::TJ;
-    bring();
-    bring();
+    bring(0, 1);
+    brought();
+    bring(0, 1);
+    brought();
     vm_wait_barrier<T::LOADS + T::SLOADS, 0>(0);
     uint32_t buffer = 0;
     read_scales(0, 0);
@@ -226,20 +234,20 @@ __global__ __launch_bounds__(64 * T::WAVES, 2) void k_mx4_matmul_tile(MatmulArgs
         for (uint64_t s = 0; s < here; ++s) {
             turn_scales();
             read(buffer, 0, 1, half1);
-            multiply(half0, first_half);
+            multiply(half0, first_half, nothing);
             read_scales(buffer, 1);
             read(buffer, 1, 0, half0);
-            multiply(half1, second_half);
+            multiply(half1, second_half, nothing);
             turn_scales();
             read(buffer, 1, 1, half1);
-            multiply(half0, first_half);
+            multiply(half0, first_half, nothing);
             vm_wait_barrier<0, STORES>(stores_behind);
             stores_behind = 0;
-            bring();
             buffer ^= 1u;
             read_scales(buffer, 0);                                           // (behind the last item: of a buffer, and for nothing)
             read(buffer, 0, 0, half0);
-            multiply(half1, second_half);
+            multiply(half1, second_half, [&](uint32_t k) { bring(k, T::TI * T::TJ); });   // the loads between the products: what sets them up costs no time
+            brought();
         }
 
         uint32_t tm, tn;
@@ -301,13 +309,17 @@ __global__ __launch_bounds__(256) void k_mx4_matmul_join(const float* __restrict
     store1<TYPE>(out, i / N * ld + i % N, v);
 }
 
-// Few rows of A: sixteen rows of B by a workgroup, whose four waves take every fourth pair of words.  Bound by the reads of B, which go straight to
-// registers, eight words of a wave under way at a time.  MT: sixteens of A's rows.
-template <uint32_t TYPE, uint32_t MT>
+// Few rows of A: sixteen rows of B by a wave, or by a workgroup's four (SPLIT: each takes a quarter of the words), which go straight to registers, U words under way
+// at a time.  Bound by the reads of B.  MT: sixteens of A's rows.
+template <uint32_t TYPE, uint32_t MT, bool SPLIT>
 __global__ __launch_bounds__(256) void k_mx4_matmul_few(MatmulArgs g) {
-    __shared__ f32x4 s_part[3][MT][64];
-    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, r = lane & 15u, blk = lane >> 4;
-    const uint64_t n0 = (uint64_t)blockIdx.x * 16, n = n0 + r < g.N ? n0 + r : g.N - 1;
+    __shared__ f32x4 s_part[SPLIT ? 3 : 1][MT][64];
+    constexpr uint32_t U = MT == 1 ? 8 : 4;
+    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15u, blk = lane >> 4;
+    const uint64_t n0 = ((uint64_t)blockIdx.x * (SPLIT ? 1 : 4) + (SPLIT ? 0 : wave)) * 16, n = n0 + r < g.N ? n0 + r : g.N - 1;
+    if (!SPLIT && n0 >= g.N) return;
+    // (a multiple of two words: whole cache lines)
+    const uint64_t quarter = (g.W + 7) / 8 * 2, begin = SPLIT ? wave * quarter : 0, end = !SPLIT || begin + quarter > g.W ? g.W : begin + quarter;
     const u32x4* b = reinterpret_cast<const u32x4*>(g.b) + n * g.W * 4 + blk;
     const u32x4* a[MT];
     uint64_t m[MT];
@@ -318,44 +330,45 @@ __global__ __launch_bounds__(256) void k_mx4_matmul_few(MatmulArgs g) {
         a[t] = reinterpret_cast<const u32x4*>(g.a) + m[t] * g.W * 4 + blk;
         acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    constexpr uint32_t U = MT == 1 ? 8 : 4;
-    for (uint64_t w0 = 2 * wave; w0 < g.W; w0 += 4 * U) {
-        u32x4 vb[U], va[U][MT];
-        uint32_t sb[U], sa[U][MT];
+    auto words = [&](uint64_t w, auto count) {
+        constexpr uint32_t C = decltype(count)::value;
+        u32x4 vb[C], va[C][MT];
+        uint32_t sb[C], sa[C][MT];
 #pragma unroll
-        for (uint32_t u = 0; u < U; ++u) {
-            const uint64_t at = w0 + 8 * (u / 2) + u % 2, w = at < g.W ? at : g.W - 1;   // (a word beyond the last one is the last one, with codes of zero)
-            vb[u] = b[w * 4];
-            sb[u] = g.sb[w * g.N + n];
+        for (uint32_t u = 0; u < C; ++u) {
+            vb[u] = b[(w + u) * 4];
+            sb[u] = g.sb[(w + u) * g.N + n];
 #pragma unroll
             for (uint32_t t = 0; t < MT; ++t) {
-                va[u][t] = a[t][w * 4];
-                sa[u][t] = g.sa[w * g.M + m[t]];
+                va[u][t] = a[t][(w + u) * 4];
+                sa[u][t] = g.sa[(w + u) * g.M + m[t]];
             }
         }
 #pragma unroll
-        for (uint32_t u = 0; u < U; ++u) {
-            const bool in = w0 + 8 * (u / 2) + u % 2 < g.W;
-            const u32x4 v = in ? vb[u] : u32x4{0, 0, 0, 0};
+        for (uint32_t u = 0; u < C; ++u)
 #pragma unroll
             for (uint32_t t = 0; t < MT; ++t)
-                acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(mx4_operand(va[u][t]), mx4_operand(v), acc[t], 4, 4, 0, sa[u][t] >> (8 * blk), 0, sb[u] >> (8 * blk));
-        }
+                acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(mx4_operand(va[u][t]), mx4_operand(vb[u]), acc[t], 4, 4, 0, sa[u][t] >> (8 * blk), 0, sb[u] >> (8 * blk));
+    };
+    uint64_t w = begin;
+    for (; w + U <= end; w += U) words(w, std::integral_constant<uint32_t, U>{});
+    for (; w < end; ++w) words(w, std::integral_constant<uint32_t, 1>{});
+    if (SPLIT) {
+        if (wave)
+#pragma unroll
+            for (uint32_t t = 0; t < MT; ++t) s_part[wave - 1][t][lane] = acc[t];
+        __syncthreads();
+        if (wave) return;
+#pragma unroll
+        for (uint32_t t = 0; t < MT; ++t) acc[t] = acc[t] + s_part[0][t][lane] + s_part[SPLIT ? 1 : 0][t][lane] + s_part[SPLIT ? 2 : 0][t][lane];
     }
-    if (wave)
 #pragma unroll
-        for (uint32_t t = 0; t < MT; ++t) s_part[wave - 1][t][lane] = acc[t];
-    __syncthreads();
-    if (wave) return;
-#pragma unroll
-    for (uint32_t t = 0; t < MT; ++t) {
+    for (uint32_t t = 0; t < MT; ++t)
 #pragma unroll
         for (uint32_t i = 0; i < 4; ++i) {
-            const float v = acc[t][i] + s_part[0][t][lane][i] + s_part[1][t][lane][i] + s_part[2][t][lane][i];
             const uint64_t row = 16 * t + 4 * blk + i;
-            if (row < g.M && n0 + r < g.N) store1<TYPE>(g.out, row * g.ld + n0 + r, v);
+            if (row < g.M && n0 + r < g.N) store1<TYPE>(g.out, row * g.ld + n0 + r, acc[t][i]);
         }
-    }
 }
 
 // A product over no words.

@@ -82,34 +82,51 @@ typedef MatmulTile<256, 256, 2, 4> Tile256;
 typedef MatmulTile<128, 128, 2, 2> Tile128;
 typedef MatmulTile<64, 64, 2, 2> Tile64;
 
-// How a product is shared out.
+// How a product is shared out: by the least of the times below, which are fits (us) to measurements of each tile alone on products of 256 to 50257 rows, 768 to
+// 32000 columns and 6 to 128 words, good to a fifth.  c: tiles for the busiest compute unit, of `stages` stages (pairs of words) each.
+//   M      N      K        256 fit, measured   128              64               (rest: what a tile's beginning and end cost)
+//   512    2048   2048     29  23              12  12           6   7
+//   1024   2048   2048     29  24              12  12           9   9
+//   1024   4096   4096     46  35              19  19           24  21
+//   4096   768    16384    152 99              57  52           62  48
+//   2048   5632   2048     29  29              29  26           35  30
+//   8192   5632   2048     76  78              94  83           131 112
+//   50257  768    8192     234 232             278 268          ..  353
+// With few tiles and long sums the stages are shared out as well, and the parts added by a second launch.
 struct MatmulPlan {
     enum { FEW, T64, T128, T256 } kind;
     uint64_t tiles_m, tiles_n;
     uint32_t splits, share;
 };
-template <class T>
-uint64_t rounds_of(uint64_t M, uint64_t N) {
-    const uint64_t tiles = ((M + T::BM - 1) / T::BM) * ((N + T::BN - 1) / T::BN), slots = UNITS * ((160 * 1024) / T::LDS);
-    return (tiles + slots - 1) / slots;
-}
-MatmulPlan matmul_plan(uint64_t M, uint64_t N, uint64_t W) {
-    MatmulPlan p{};
-    p.splits = 1;
-    p.share = (uint32_t)((W + 1) / 2);
+MatmulPlan matmul_plan(uint64_t M, uint64_t N, uint64_t W, bool may_split) {
+    MatmulPlan best{};
+    best.splits = 1;
+    const uint64_t stages = (W + 1) / 2;
+    best.share = (uint32_t)stages;
     if (M <= FEW_ROWS) {
-        p.kind = MatmulPlan::FEW;
-        return p;
+        best.kind = MatmulPlan::FEW;
+        return best;
     }
-    const uint64_t cost256 = 100 * rounds_of<Tile256>(M, N), cost128 = 59 * rounds_of<Tile128>(M, N), cost64 = 40 * rounds_of<Tile64>(M, N);
-    uint64_t edge = 64, slots = UNITS * ((160 * 1024) / Tile64::LDS);
-    p.kind = MatmulPlan::T64;
-    if (cost256 <= cost128 && cost256 <= cost64) { p.kind = MatmulPlan::T256; edge = 256; slots = UNITS; }
-    else if (cost128 <= cost64) { p.kind = MatmulPlan::T128; edge = 128; slots = UNITS * ((160 * 1024) / Tile128::LDS); }
-    p.tiles_m = (M + edge - 1) / edge;
-    p.tiles_n = (N + edge - 1) / edge;
-    return p;
+    struct { decltype(best.kind) kind; uint64_t edge; double stage, tile, launch; } const kinds[] = {
+        {MatmulPlan::T256, 256, 2.2, 6.0, 5.0}, {MatmulPlan::T128, 128, 0.8, 1.8, 4.0}, {MatmulPlan::T64, 64, 0.3, 0.5, 3.0}};
+    double least = 0;
+    for (const auto& k : kinds) {
+        const uint64_t tm = (M + k.edge - 1) / k.edge, tn = (N + k.edge - 1) / k.edge;
+        for (uint64_t splits = 1; splits == 1 || (may_split && splits <= 16 && 4 * splits <= stages && tm * tn * splits <= 4 * UNITS); splits *= 2) {
+            const uint64_t share = (stages + splits - 1) / splits, parts = (stages + share - 1) / share;
+            const double c = (double)((tm * tn * parts + UNITS - 1) / UNITS);
+            double us = c * ((double)share * k.stage + k.tile) + k.launch;
+            if (parts > 1) us += 4.0 + (double)(parts * M * N) * 8.0 / 4e6;     // 4 bytes written and read, at 4 TB/s
+            if (least == 0 || us < least) {
+                least = us;
+                best.kind = k.kind; best.tiles_m = tm; best.tiles_n = tn;
+                best.splits = (uint32_t)parts; best.share = (uint32_t)share;
+            }
+        }
+    }
+    return best;
 }
+inline uint64_t matmul_parts_bytes(const MatmulPlan& p, uint64_t M, uint64_t N) { return p.splits > 1 ? 4 * p.splits * M * N : 0; }
 
 template <uint32_t TYPE, class T>
 int launch_tile(MatmulArgs g, const MatmulPlan& p, hipStream_t s) {
@@ -118,6 +135,22 @@ int launch_tile(MatmulArgs g, const MatmulPlan& p, hipStream_t s) {
     constexpr uint64_t slots = UNITS * ((160 * 1024) / T::LDS);
     g.tiles_m = (uint32_t)p.tiles_m; g.tiles_n = (uint32_t)p.tiles_n; g.splits = p.splits; g.share = p.share;
     hipLaunchKernelGGL((k_mx4_matmul_tile<TYPE, T>), dim3((uint32_t)std::min<uint64_t>(items, slots)), dim3(64 * T::WAVES), 0, s, g);
+    return launched();
+}
+
+template <uint32_t TYPE>
+int launch_kind(const MatmulArgs& g, const MatmulPlan& p, hipStream_t s) {
+    if (p.kind == MatmulPlan::T256) return launch_tile<TYPE, Tile256>(g, p, s);
+    if (p.kind == MatmulPlan::T128) return launch_tile<TYPE, Tile128>(g, p, s);
+    return launch_tile<TYPE, Tile64>(g, p, s);
+}
+
+// Sixteen rows of B by a wave where that makes a wave a SIMD and the sum is short, else by four (32000 rows, 16 words: 8.3 and 9.6 us; 16384 rows,
+// 128 words: 33.7 and 27.5).
+template <uint32_t TYPE, uint32_t MT>
+int launch_few(const MatmulArgs& g, uint64_t groups, hipStream_t s) {
+    if (groups >= 4 * UNITS && g.W <= 32) hipLaunchKernelGGL((k_mx4_matmul_few<TYPE, MT, false>), dim3((uint32_t)((groups + 3) / 4)), dim3(256), 0, s, g);
+    else hipLaunchKernelGGL((k_mx4_matmul_few<TYPE, MT, true>), dim3((uint32_t)groups), dim3(256), 0, s, g);
     return launched();
 }
 
@@ -165,7 +198,10 @@ int kimad_mx4_dequantise(const void* codes, const uint32_t* scales, uint64_t row
     });
 }
 
-uint64_t kimad_mx4_matmul_workspace_bytes(uint64_t, uint64_t, uint64_t) { return 0; }
+uint64_t kimad_mx4_matmul_workspace_bytes(uint64_t M, uint64_t N, uint64_t K) {
+    if (M > MOST || N > MOST || K > MATMUL_MOST_K || M == 0 || N == 0) return 0;
+    return matmul_parts_bytes(matmul_plan(M, N, words_of(K), true), M, N);
+}
 
 int kimad_mx4_matmul(const void* a_codes, const uint32_t* a_scales, uint64_t M, const void* b_codes, const uint32_t* b_scales,
                      uint64_t N, uint64_t K, void* out, uint32_t type, uint64_t ld, void* workspace, uint64_t workspace_bytes,
@@ -175,10 +211,10 @@ int kimad_mx4_matmul(const void* a_codes, const uint32_t* a_scales, uint64_t M, 
     if (!out || !aligned(out, type_bytes(type))) return KIMAD_ERR_INVALID_ARG;
     if (K && (!a_codes || !b_codes || !pair_ok(a_codes, a_scales) || !pair_ok(b_codes, b_scales))) return KIMAD_ERR_INVALID_ARG;
     if (workspace && !aligned(workspace, 16)) return KIMAD_ERR_INVALID_ARG;
-    (void)workspace_bytes;
     MatmulArgs g{};
     g.a = static_cast<const uint8_t*>(a_codes); g.b = static_cast<const uint8_t*>(b_codes);
-    const MatmulPlan p = matmul_plan(M, N, words_of(K));
+    MatmulPlan p = matmul_plan(M, N, words_of(K), true);
+    if (matmul_parts_bytes(p, M, N) > (workspace ? workspace_bytes : 0)) p = matmul_plan(M, N, words_of(K), false);
     g.sa = a_scales; g.sb = b_scales; g.out = out; g.M = M; g.N = N; g.W = words_of(K); g.ld = ld;
     hipStream_t s = static_cast<hipStream_t>(stream);
     return with_type(type, [&](auto t) {
@@ -189,15 +225,19 @@ int kimad_mx4_matmul(const void* a_codes, const uint32_t* a_scales, uint64_t M, 
             return launched();
         }
         if (p.kind == MatmulPlan::FEW) {
-            const uint64_t wgs = (N + 15) / 16;
-            if (wgs > GRID_MOST) return (int)KIMAD_ERR_INVALID_ARG;
-            if (M <= 16) hipLaunchKernelGGL((k_mx4_matmul_few<TYPE, 1>), dim3((uint32_t)wgs), dim3(256), 0, s, g);
-            else hipLaunchKernelGGL((k_mx4_matmul_few<TYPE, 2>), dim3((uint32_t)wgs), dim3(256), 0, s, g);
-            return launched();
+            const uint64_t groups = (N + 15) / 16;
+            if (groups > GRID_MOST) return (int)KIMAD_ERR_INVALID_ARG;
+            if (M <= 16) return launch_few<TYPE, 1>(g, groups, s);
+            return launch_few<TYPE, 2>(g, groups, s);
         }
-        if (p.kind == MatmulPlan::T256) return launch_tile<TYPE, Tile256>(g, p, s);
-        if (p.kind == MatmulPlan::T128) return launch_tile<TYPE, Tile128>(g, p, s);
-        return launch_tile<TYPE, Tile64>(g, p, s);
+        if (p.splits == 1) return launch_kind<TYPE>(g, p, s);
+        g.out = workspace; g.ld = N;
+        const int rc = launch_kind<TYPE_F32>(g, p, s);
+        if (rc) return rc;
+        const uint64_t wgs = (M * N + 255) / 256;
+        if (wgs > GRID_MOST) return (int)KIMAD_ERR_INVALID_ARG;
+        hipLaunchKernelGGL(k_mx4_matmul_join<TYPE>, dim3((uint32_t)wgs), dim3(256), 0, s, static_cast<const float*>(workspace), p.splits, M, N, out, ld);
+        return launched();
     });
 }
 
