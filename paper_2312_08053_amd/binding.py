@@ -147,11 +147,19 @@ def _ptr(t) -> int:
     return 0 if t is None else int(t.data_ptr())
 
 
+_raw_stream = None
+
+
 def _stream(stream) -> int:
-    if stream is None:
+    global _raw_stream
+    if stream is not None:
+        return int(getattr(stream, "cuda_stream", stream))
+    if _raw_stream is None:
         import torch
-        return int(torch.cuda.current_stream().cuda_stream)
-    return int(getattr(stream, "cuda_stream", stream))
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # the same number without an object around it
+        _raw_stream = ((lambda: raw(torch.cuda.current_device())) if raw is not None
+                       else lambda: int(torch.cuda.current_stream().cuda_stream))
+    return _raw_stream()
 
 
 def kimad_workspace_bytes(sizes: Sequence[int], J: int, pair_bytes=8, D=0, max_budget_bytes=0,
@@ -276,32 +284,43 @@ def kimad_selftest_allocate_withheld(plan: int, err_table, budget_bytes: int, j_
                                                   C.c_void_p(_stream(stream))), "kimad_selftest_allocate_withheld")
 
 
+# Small calls take less time on the device than in here: what follows asks each tensor for little, and for most of it once.
+_TYPES = {}
+
+
 def _type(t) -> int:
     """KIMAD_VALUES_* of a tensor's type."""
-    import torch
-    try:
-        return {torch.float32: KIMAD_VALUES_F32, torch.float16: KIMAD_VALUES_F16, torch.bfloat16: KIMAD_VALUES_BF16}[t.dtype]
-    except KeyError:
-        raise TypeError(f"float32, float16 or bfloat16 is wanted, got {t.dtype}") from None
+    if not _TYPES:
+        import torch
+        _TYPES.update({torch.float32: KIMAD_VALUES_F32, torch.float16: KIMAD_VALUES_F16, torch.bfloat16: KIMAD_VALUES_BF16})
+    kind = _TYPES.get(t.dtype)
+    if kind is None:
+        raise TypeError(f"float32, float16 or bfloat16 is wanted, got {t.dtype}")
+    return kind
 
 
 def _rows(t, what: str):
     """(rows, columns, elements from row to row) of a matrix whose rows are contiguous."""
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
-        raise ValueError(f"{what}: a matrix with contiguous rows is wanted, got shape {tuple(t.shape)}, strides {t.stride()}")
-    return t.shape[0], t.shape[1], (t.stride(0) if t.shape[0] > 1 else t.shape[1])
+    shape, strides = t.shape, t.stride()
+    if len(shape) == 2:
+        rows, cols = shape
+        ld, one = strides
+        if (one == 1 or cols <= 1) and (ld >= cols or rows <= 1):
+            return rows, cols, ld if rows > 1 else cols
+    raise ValueError(f"{what}: a matrix with contiguous rows is wanted, got shape {tuple(shape)}, strides {strides}")
 
 
-def _holds(t, count: int, size: int, what: str) -> None:
-    """A contiguous tensor of at least `count` elements of `size` bytes."""
-    if t.element_size() != size or t.numel() < count or not t.is_contiguous():
+def _holds(t, count: int, size: int, what: str) -> int:
+    """The address of a contiguous tensor of at least `count` elements of `size` bytes."""
+    if t.numel() < count or t.element_size() != size or not t.is_contiguous():
         raise ValueError(f"{what}: {count} contiguous elements of {size} bytes are wanted, got {t.numel()} of {t.dtype}, strides {t.stride()}")
+    return t.data_ptr()
 
 
-def _holds_mx4(codes, scales, rows: int, cols: int, what: str) -> None:
-    words = -(-cols // 128)
-    _holds(codes, rows * words * 64, 1, f"{what} codes")
-    _holds(scales, rows * words, 4, f"{what} scales")
+def _holds_mx4(codes, scales, rows: int, cols: int, what: str):
+    """The addresses of a quantised matrix."""
+    words = (cols + 127) // 128
+    return _holds(codes, rows * words * 64, 1, what), _holds(scales, rows * words, 4, what)
 
 
 def mx4_empty(rows: int, cols: int, device="cuda"):
@@ -315,20 +334,16 @@ def mx4_empty(rows: int, cols: int, device="cuda"):
 def kimad_mx4_quantise(x, codes=None, scales=None, codes_t=None, scales_t=None, stream=None) -> None:
     """x [rows, cols] along rows into codes, scales, along columns into codes_t, scales_t (each pair from mx4_empty, or None)."""
     rows, cols, ld = _rows(x, "x")
-    if codes is not None:
-        _holds_mx4(codes, scales, rows, cols, "row")
-    if codes_t is not None:
-        _holds_mx4(codes_t, scales_t, cols, rows, "column")
-    _check(lib().kimad_mx4_quantise(_ptr(x), _type(x), rows, cols, ld, _ptr(codes), _ptr(scales), _ptr(codes_t), _ptr(scales_t),
-                                    _stream(stream)), "kimad_mx4_quantise")
+    c, s = (0, 0) if codes is None else _holds_mx4(codes, scales, rows, cols, "codes and scales")
+    ct, st = (0, 0) if codes_t is None else _holds_mx4(codes_t, scales_t, cols, rows, "codes_t and scales_t")
+    _check(lib().kimad_mx4_quantise(x.data_ptr(), _type(x), rows, cols, ld, c, s, ct, st, _stream(stream)), "kimad_mx4_quantise")
 
 
 def kimad_mx4_dequantise(codes, scales, out, stream=None) -> None:
     """The values of a quantised matrix into out [rows, cols]."""
     rows, cols, ld = _rows(out, "out")
-    _holds_mx4(codes, scales, rows, cols, "row")
-    _check(lib().kimad_mx4_dequantise(_ptr(codes), _ptr(scales), rows, cols, _ptr(out), _type(out), ld, _stream(stream)),
-           "kimad_mx4_dequantise")
+    c, s = _holds_mx4(codes, scales, rows, cols, "codes and scales")
+    _check(lib().kimad_mx4_dequantise(c, s, rows, cols, out.data_ptr(), _type(out), ld, _stream(stream)), "kimad_mx4_dequantise")
 
 
 def kimad_mx4_matmul_workspace_bytes(M: int, N: int, K: int) -> int:
@@ -339,16 +354,18 @@ def kimad_mx4_matmul(a_codes, a_scales, b_codes, b_scales, K: int, out, workspac
     """out [M, N] = A B^T of quantised matrices A [M, K] and B [N, K].  workspace: a device tensor (allocated here if None and
     one is of use)."""
     M, N, ld = _rows(out, "out")
-    _holds_mx4(a_codes, a_scales, M, K, "A's")
-    _holds_mx4(b_codes, b_scales, N, K, "B's")
+    a, sa = _holds_mx4(a_codes, a_scales, M, K, "A's codes and scales")
+    b, sb = _holds_mx4(b_codes, b_scales, N, K, "B's codes and scales")
     L = lib()
-    need = L.kimad_mx4_matmul_workspace_bytes(M, N, K)
-    if workspace is None and need:
-        import torch
-        workspace = torch.empty(need, dtype=torch.uint8, device=out.device)
-    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(L.kimad_mx4_matmul(_ptr(a_codes), _ptr(a_scales), M, _ptr(b_codes), _ptr(b_scales), N, int(K), _ptr(out), _type(out), ld,
-                              _ptr(workspace), nbytes, _stream(stream)), "kimad_mx4_matmul")
+    ws = nbytes = 0
+    if workspace is None:
+        nbytes = L.kimad_mx4_matmul_workspace_bytes(M, N, K)
+        if nbytes:
+            import torch
+            workspace = torch.empty(nbytes, dtype=torch.uint8, device=out.device)
+    if workspace is not None:
+        ws, nbytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    _check(L.kimad_mx4_matmul(a, sa, M, b, sb, N, K, out.data_ptr(), _type(out), ld, ws, nbytes, _stream(stream)), "kimad_mx4_matmul")
 
 
 def kimad_mx4_update_words(L: int, d: int) -> int:
@@ -360,12 +377,8 @@ def kimad_mx4_compress_ef(g, h, layer_start, codes, scales, status_out=None, str
     [words, 64] and scales int32 [words] with words = kimad_mx4_update_words(L, d); status_out: device int32[1] or None."""
     d, L = g.numel(), layer_start.numel() - 1
     words = d // 128 + L
-    _holds(g, d, 4, "g")
-    _holds(h, d, 4, "h")
-    _holds(layer_start, 1, 8, "layer_start")
-    _holds(codes, words * 64, 1, "codes")
-    _holds(scales, words, 4, "scales")
-    _check(lib().kimad_mx4_compress_ef(_ptr(g), _ptr(h), _ptr(layer_start), L, d, _ptr(codes), _ptr(scales), _ptr(status_out),
+    _check(lib().kimad_mx4_compress_ef(_holds(g, d, 4, "g"), _holds(h, d, 4, "h"), _holds(layer_start, 2, 8, "layer_start"), L, d,
+                                       _holds(codes, words * 64, 1, "codes"), _holds(scales, words, 4, "scales"), _ptr(status_out),
                                        _stream(stream)), "kimad_mx4_compress_ef")
 
 
@@ -375,20 +388,15 @@ def kimad_mx4_server_apply(updates, u_hats, weights, layer_start, d: int, x=None
     (updated in place); x: flat fp32 model or None; status_out: device int32[1] or None."""
     M, L, d = len(u_hats), layer_start.numel() - 1, int(d)
     words = d // 128 + L
-    _holds(layer_start, 1, 8, "layer_start")
     if len(updates) != M or len(weights) != M:
         raise ValueError(f"{M} estimators, {len(updates)} updates and {len(weights)} weights")
-    for (c, s), u in zip(updates, u_hats):
-        _holds(c, words * 64, 1, "codes")
-        _holds(s, words, 4, "scales")
-        _holds(u, d, 4, "u_hats")
-    if x is not None:
-        _holds(x, d, 4, "x")
-    up = (_Mx4Update * M)(*[_Mx4Update(_ptr(c), _ptr(s)) for (c, s) in updates])
-    uh = (C.c_void_p * M)(*[_ptr(u) for u in u_hats])
-    w = (C.c_double * M)(*[float(t) for t in weights])
-    _check(lib().kimad_mx4_server_apply(up, uh, w, M, _ptr(layer_start), L, d, _ptr(x), float(gamma), _ptr(status_out),
-                                        _stream(stream)), "kimad_mx4_server_apply")
+    up, uh, w = (_Mx4Update * M)(), (C.c_void_p * M)(), (C.c_double * M)(*weights)
+    for m, (codes, scales) in enumerate(updates):
+        up[m].codes, up[m].scales = _holds(codes, words * 64, 1, "codes"), _holds(scales, words, 4, "scales")
+        uh[m] = _holds(u_hats[m], d, 4, "u_hats")
+    _check(lib().kimad_mx4_server_apply(up, uh, w, M, _holds(layer_start, 2, 8, "layer_start"), L, d,
+                                        0 if x is None else _holds(x, d, 4, "x"), gamma, _ptr(status_out), _stream(stream)),
+           "kimad_mx4_server_apply")
 
 
 def kimad_distill_workspace_bytes(rows: int, vocab: int, k: int) -> int:
@@ -396,48 +404,47 @@ def kimad_distill_workspace_bytes(rows: int, vocab: int, k: int) -> int:
 
 
 def _distill_inputs(logits, t_idx, t_val, row_weight, grad):
+    """The leading arguments of both calls, and the trailing ones for row_weight and grad."""
     rows, vocab, ld = _rows(logits, "logits")
+    kind = _type(logits)
     k = t_idx.shape[1] if t_idx.dim() == 2 else -1
-    if tuple(t_idx.shape) != (rows, k) or t_val.shape != t_idx.shape:
+    if t_idx.shape != (rows, k) or t_val.shape != (rows, k):
         raise ValueError(f"entries: [rows, k] is wanted twice, got {tuple(t_idx.shape)} and {tuple(t_val.shape)} for {rows} rows")
-    _holds(t_idx, rows * k, 4, "t_idx")
-    _holds(t_val, rows * k, 4, "t_val")
-    if row_weight is not None:
-        _holds(row_weight, rows, 4, "row_weight")
-    ld_grad = 0
-    if grad is not None:
-        g_rows, g_vocab, ld_grad = _rows(grad, "grad")
-        if (g_rows, g_vocab) != (rows, vocab) or grad.dtype != logits.dtype:
-            raise ValueError(f"grad: the logits' shape and type are wanted, got {tuple(grad.shape)} of {grad.dtype}")
-    return rows, vocab, ld, k, ld_grad
+    lead = (logits.data_ptr(), kind, rows, vocab, ld, _holds(t_idx, rows * k, 4, "t_idx"), _holds(t_val, rows * k, 4, "t_val"), k)
+    weight = 0 if row_weight is None else _holds(row_weight, rows, 4, "row_weight")
+    if grad is None:
+        return lead, weight, 0, 0
+    g_rows, g_vocab, ld_grad = _rows(grad, "grad")
+    if (g_rows, g_vocab) != (rows, vocab) or _type(grad) != kind:
+        raise ValueError(f"grad: the logits' shape and type are wanted, got {tuple(grad.shape)} of {grad.dtype}")
+    return lead, weight, grad.data_ptr(), ld_grad
 
 
 def kimad_distill(logits, t_idx, t_val, temperature: float, loss=None, stats=None, grad=None, row_weight=None, workspace=None,
                   stream=None) -> None:
     """Distillation loss (float32 [rows]), statistics (float32 [rows, 2]) and gradient (like logits) of logits [rows, vocab]
     against a teacher's top entries t_idx int32, t_val float32 [rows, k]; an output that is None is left out."""
-    rows, vocab, ld, k, ld_grad = _distill_inputs(logits, t_idx, t_val, row_weight, grad)
-    if loss is not None:
-        _holds(loss, rows, 4, "loss")
-    if stats is not None:
-        _holds(stats, 2 * rows, 4, "stats")
+    lead, weight, g, ld_grad = _distill_inputs(logits, t_idx, t_val, row_weight, grad)
+    _, _, rows, vocab, _, _, _, k = lead
     L = lib()
-    need = L.kimad_distill_workspace_bytes(rows, vocab, k)
-    if workspace is None and need:
-        import torch
-        workspace = torch.empty(need, dtype=torch.uint8, device=logits.device)
-    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(L.kimad_distill(_ptr(logits), _type(logits), rows, vocab, ld, _ptr(t_idx), _ptr(t_val), k, float(temperature),
-                           _ptr(row_weight), _ptr(loss), _ptr(stats), _ptr(grad), ld_grad, _ptr(workspace), nbytes,
-                           _stream(stream)), "kimad_distill")
+    ws = nbytes = 0
+    if workspace is None:
+        nbytes = L.kimad_distill_workspace_bytes(rows, vocab, k)
+        if nbytes:
+            import torch
+            workspace = torch.empty(nbytes, dtype=torch.uint8, device=logits.device)
+    if workspace is not None:
+        ws, nbytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    _check(L.kimad_distill(*lead, temperature, weight, 0 if loss is None else _holds(loss, rows, 4, "loss"),
+                           0 if stats is None else _holds(stats, 2 * rows, 4, "stats"), g, ld_grad, ws, nbytes, _stream(stream)),
+           "kimad_distill")
 
 
 def kimad_distill_grad(logits, t_idx, t_val, temperature: float, stats, grad, row_weight=None, stream=None) -> None:
     """The gradient alone, from the statistics of an earlier kimad_distill."""
-    rows, vocab, ld, k, ld_grad = _distill_inputs(logits, t_idx, t_val, row_weight, grad)
-    _holds(stats, 2 * rows, 4, "stats")
-    _check(lib().kimad_distill_grad(_ptr(logits), _type(logits), rows, vocab, ld, _ptr(t_idx), _ptr(t_val), k, float(temperature),
-                                    _ptr(row_weight), _ptr(stats), _ptr(grad), ld_grad, _stream(stream)), "kimad_distill_grad")
+    lead, weight, g, ld_grad = _distill_inputs(logits, t_idx, t_val, row_weight, grad)
+    _check(lib().kimad_distill_grad(*lead, temperature, weight, _holds(stats, 2 * lead[2], 4, "stats"), g, ld_grad, _stream(stream)),
+           "kimad_distill_grad")
 
 
 class Plan:
