@@ -20,8 +20,8 @@ struct DistillArgs {
     void* grad;
     float* parts;                // split rows: [rows][chunks][2], the same two numbers of a chunk ...
     float* zj;                   // ... and [rows][k], the student's logits at the entries
-    uint64_t rows, vocab, ld, ld_grad, chunk;
-    uint32_t k, chunks, bloom;   // bloom: words of the table that finds indices given twice, a power of two
+    uint64_t rows, ld, ld_grad;
+    uint32_t vocab, k, chunks, bloom;   // bloom: words of the table that finds indices given twice, a power of two
     float T, c;                  // c = log2(e) / T
 };
 // LDS that a workgroup asks for: index, p and student's logit of every entry, and the table.
@@ -47,11 +47,17 @@ __device__ __forceinline__ Softmax join(Softmax a, Softmax b, float c) {
     const float sa = a.m == m ? a.s : a.s * exp2_fast((a.m - m) * c), sb = b.m == m ? b.s : b.s * exp2_fast((b.m - m) * c);
     return {m, sa + sb};
 }
-// Over a workgroup's threads, the result in all of them.  `room` is free again behind the next barrier.
-template <uint32_t NT>
-__device__ __forceinline__ Softmax join_block(Softmax v, float c, Softmax* room) {
+// Over a wave's lanes, the result in all of them.
+__device__ __forceinline__ Softmax join_wave(Softmax v, float c) {
 #pragma unroll
     for (uint32_t o = 1; o < 64; o <<= 1) v = join(v, Softmax{__shfl_xor(v.m, o), __shfl_xor(v.s, o)}, c);
+    return v;
+}
+// Over a workgroup's threads.
+template <uint32_t NT>
+__device__ __forceinline__ Softmax join_block(Softmax v, float c, Softmax* room) {
+    v = join_wave(v, c);
+    if (NT == 64) return v;
     if ((threadIdx.x & 63u) == 0) room[threadIdx.x >> 6] = v;
     __syncthreads();
     v = room[0];
@@ -59,39 +65,112 @@ __device__ __forceinline__ Softmax join_block(Softmax v, float c, Softmax* room)
     for (uint32_t i = 1; i < NT / 64; ++i) v = join(v, room[i], c);
     return v;
 }
-template <uint32_t NT>
-__device__ __forceinline__ float sum_block(float v, float* room) {
-#pragma unroll
-    for (uint32_t o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o);
-    if ((threadIdx.x & 63u) == 0) room[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = room[0];
-#pragma unroll
-    for (uint32_t i = 1; i < NT / 64; ++i) v += room[i];
-    return v;
-}
 
-template <uint32_t NT>
-struct DistillRoom {
-    Softmax teacher[NT / 64], row[NT / 64];
-    float sum[NT / 64];
-    uint32_t any, twice;
+// A row's elements in groups of eight that begin at 16-byte addresses: with mis elements in front of the row's first one back to such an address, group j
+// holds elements 8 j - mis and on.  Reads take whole 16 bytes, of which the first and the last may hold neighbours of the row (never another page);
+// what is not the row's is masked, and not written.
+template <uint32_t TYPE>
+constexpr uint32_t bytes_of() { return TYPE == TYPE_F32 ? 4 : 2; }
+template <uint32_t TYPE>
+__device__ __forceinline__ uint32_t misplaced(const void* p, uint64_t element) {
+    return (uint32_t)((reinterpret_cast<uintptr_t>(p) / bytes_of<TYPE>() + element) % (16 / bytes_of<TYPE>()));
+}
+// NV * NT groups from group j0 on (the same for the workgroup), of which thread t holds every NT-th one from j0 + t on.
+template <uint32_t TYPE, uint32_t NT, uint32_t NV>
+struct Groups {
+    Raw8<TYPE> raw[NV];
+    static constexpr uint32_t B = bytes_of<TYPE>(), GROUP = 8 * B;
+    static __device__ __forceinline__ bool whole(uint32_t i, uint32_t j0, uint32_t mis, uint32_t vocab) {
+        return (mis == 0 || j0 + i > 0) && 8ull * (j0 + (i + 1) * NT) <= (uint64_t)mis + vocab;
+    }
+    static __device__ __forceinline__ uint32_t element(uint32_t i, uint32_t j0, uint32_t mis) { return 8u * (j0 + i * NT + threadIdx.x) - mis; }   // (of group 0: below 0, a large number)
+
+    __device__ __forceinline__ void load(const void* p, uint64_t row, uint32_t j0, uint32_t mis, uint32_t vocab) {
+        const uint64_t end = ((uint64_t)mis + vocab) * B + 15 & ~15ull, begin = (uint64_t)j0 * GROUP, left = end > begin ? end - begin : 0;
+        const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(static_cast<uint8_t*>(const_cast<void*>(p)) + (row - mis) * B + begin, 0,
+                                                                               (int)(left < NV * NT * GROUP ? left : NV * NT * GROUP), 0x00020000);
+#pragma unroll
+        for (uint32_t i = 0; i < NV; ++i) {
+#pragma unroll
+            for (uint32_t h = 0; h < GROUP / 16; ++h) {
+                const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(from, threadIdx.x * GROUP + 16 * h, i * NT * GROUP, 0);
+#pragma unroll
+                for (uint32_t k = 0; k < 4; ++k) raw[i].r[(4 * h + k) % (GROUP / 4)] = v[k];
+            }
+        }
+    }
+    // What is not the row's becomes -Inf.
+    __device__ __forceinline__ void mask(uint32_t j0, uint32_t mis, uint32_t vocab) {
+#pragma unroll
+        for (uint32_t i = 0; i < NV; ++i)
+            if (!whole(i, j0, mis, vocab)) {
+                const uint32_t e = element(i, j0, mis);
+#pragma unroll
+                for (uint32_t x = 0; x < 8; ++x)
+                    if (e + x >= vocab) raw[i].set(x, minus_inf<TYPE>());
+            }
+    }
+    // Largest element and sum, a group at a time: an element is taken apart once, and only as it lies in memory does it stay in a register.
+    __device__ __forceinline__ Softmax softmax(float c) const {
+        Softmax q = {-INFINITY, 0.f};
+#pragma unroll
+        for (uint32_t i = 0; i < NV; ++i) {
+            float v[8], m = q.m;
+#pragma unroll
+            for (uint32_t x = 0; x < 8; ++x) {
+                v[x] = raw[i].at(x);
+                m = fmaxf(m, v[x]);
+            }
+            const float from = m == -INFINITY ? 0.f : m;
+            float sum = 0.f;
+#pragma unroll
+            for (uint32_t x = 0; x < 8; ++x) sum += exp2_fast((v[x] - from) * c);
+            q.s = (q.m == m ? q.s : q.s * exp2_fast((q.m - m) * c)) + sum;
+            q.m = m;
+        }
+        return q;
+    }
+    // The gradient but for the entries' part, f q; zeros where `live` is false.
+    __device__ __forceinline__ void store_gradient(void* p, uint64_t row, uint32_t j0, uint32_t mis, uint32_t vocab, Softmax q, float c, float f, bool live) {
+#pragma unroll
+        for (uint32_t i = 0; i < NV; ++i)
+#pragma unroll
+            for (uint32_t k = 0; k < GROUP / 4; ++k) asm volatile("" : "+v"(raw[i].r[k]));   // (what was taken apart before is not kept: twice the registers)
+        const float fs = f / q.s;
+        uint8_t* base = static_cast<uint8_t*>(p) + (row - mis) * B + (uint64_t)j0 * GROUP;
+#pragma unroll
+        for (uint32_t i = 0; i < NV; ++i) {
+            float v[8];
+#pragma unroll
+            for (uint32_t x = 0; x < 8; ++x) v[x] = live ? exp2_fast((raw[i].at(x) - q.m) * c) * fs : 0.f;
+            uint8_t* to = base + i * NT * GROUP;
+            if (whole(i, j0, mis, vocab)) {
+                store8<TYPE>(to + threadIdx.x * GROUP, 0, v);
+            } else {
+                const uint32_t e = element(i, j0, mis);
+                if (e < vocab && vocab - e >= 8) store8<TYPE>(to + threadIdx.x * GROUP, 0, v);
+                else
+#pragma unroll
+                    for (uint32_t x = 0; x < 8; ++x)
+                        if (e + x < vocab) store1<TYPE>(to + threadIdx.x * GROUP, x, v[x]);
+            }
+        }
+    }
 };
 
-// A row's entries: indices (those beyond the vocabulary are none and become 0xFFFFFFFF), probabilities, and the student's logits
-// unless they are given or those of other chunks' columns.  False where there is no entry.
-// Entries of one index are one entry with the sum of their probabilities; it goes to the first of them, the others
-// get 0xFFFFFFFF.  They are looked for only where two of the row's indices meet in the table.
-template <uint32_t TYPE, uint32_t NT>
-__device__ __forceinline__ bool read_teacher(const DistillArgs& a, uint64_t row, uint64_t from, uint64_t to, const float* zj, uint32_t* s_idx,
-                                             float* s_p, float* s_z, uint32_t* s_table, DistillRoom<NT>& room) {
-    const uint32_t k = a.k;
-    if (threadIdx.x == 0) { room.any = 0; room.twice = 0; }
-    for (uint32_t i = threadIdx.x; i < a.bloom; i += NT) s_table[i] = 0;
-    __syncthreads();
+// A row's entries, by one wave: indices (those beyond the vocabulary are none and become 0xFFFFFFFF), probabilities, and the student's logits unless
+// they are given or stand outside [from, to).  False where there is no entry.  Entries of one index are one entry with the sum
+// of their probabilities; it goes to the first of them, the others get 0xFFFFFFFF.  They are looked for only where two of the row's indices
+// meet in the table.
+template <uint32_t TYPE>
+__device__ __forceinline__ bool read_teacher(const DistillArgs& a, uint64_t row, uint32_t from, uint32_t to, const float* zj, uint32_t* s_idx,
+                                             float* s_p, float* s_z, uint32_t* s_table) {
+    const uint32_t k = a.k, lane = threadIdx.x & 63u;
+    for (uint32_t i = lane; i < a.bloom; i += 64) s_table[i] = 0;
+    wave_sync_lds();
     Softmax v = {-INFINITY, 0.f};
     bool any = false, meets = false;
-    for (uint32_t j = threadIdx.x; j < k; j += NT) {
+    for (uint32_t j = lane; j < k; j += 64) {
         const uint32_t i = a.idx[row * k + j];
         const bool in = i < a.vocab;
         const float t = in ? a.val[row * k + j] : -INFINITY;
@@ -103,106 +182,92 @@ __device__ __forceinline__ bool read_teacher(const DistillArgs& a, uint64_t row,
         if (t != t) v.s = t;
         if (in) meets = meets || (atomicOr(&s_table[(i >> 5) & (a.bloom - 1u)], 1u << (i & 31u)) >> (i & 31u) & 1u);
     }
-    if (any) room.any = 1;
-    if (__syncthreads_or(meets)) {
-        for (uint32_t j = threadIdx.x; j < k; j += NT)
-            for (uint32_t l = 0; l < j; ++l)
-                if (s_idx[l] == s_idx[j] && s_idx[j] != 0xFFFFFFFFu) room.twice = 1;
-    }
-    v = join_block<NT>(v, a.c, room.teacher);
-    if (!room.any) return false;
-    for (uint32_t j = threadIdx.x; j < k; j += NT) {
+    if (!ballot(any)) return false;
+    v = join_wave(v, a.c);
+    wave_sync_lds();
+    bool twice = false;
+    if (ballot(meets))
+        for (uint32_t j = lane; j < k; j += 64)
+            for (uint32_t l = 0; l < j; ++l) twice = twice || (s_idx[l] == s_idx[j] && s_idx[j] != 0xFFFFFFFFu);
+    for (uint32_t j = lane; j < k; j += 64) {
         const float t = s_p[j];
         s_p[j] = t == -INFINITY ? 0.f : exp2_fast((t - v.m) * a.c) / v.s;
     }
-    __syncthreads();
-    if (room.twice) {
-        for (uint32_t j0 = 0; j0 < k; j0 += NT) {            // the sums, from untouched probabilities: s_z keeps its place, the table is free
-            const uint32_t j = j0 + threadIdx.x;
-            if (j < k && s_idx[j] != 0xFFFFFFFFu) {
-                bool first = true;
-                float p = 0.f;
-                for (uint32_t l = 0; l < k; ++l)
-                    if (s_idx[l] == s_idx[j]) { first = first && l >= j; p += s_p[l]; }
-                s_table[j] = __float_as_uint(first ? p : -1.f);      // (no probability is negative)
-            }
+    wave_sync_lds();
+    if (ballot(twice)) {
+        for (uint32_t j = lane; j < k; j += 64) {
+            bool first = true;
+            float p = 0.f;
+            for (uint32_t l = 0; l < k; ++l)
+                if (s_idx[l] == s_idx[j]) { first = first && l >= j; p += s_p[l]; }
+            s_table[j] = __float_as_uint(first ? p : -1.f);      // (no probability is negative)
         }
-        __syncthreads();
-        for (uint32_t j = threadIdx.x; j < k; j += NT)
-            if (s_idx[j] != 0xFFFFFFFFu) {
-                if (__uint_as_float(s_table[j]) == -1.f) { s_idx[j] = 0xFFFFFFFFu; s_p[j] = 0.f; }
-                else s_p[j] = __uint_as_float(s_table[j]);
-            }
-        __syncthreads();
+        wave_sync_lds();
+        for (uint32_t j = lane; j < k; j += 64) {
+            const float p = __uint_as_float(s_table[j]);
+            if (p == -1.f) s_idx[j] = 0xFFFFFFFFu;
+            s_p[j] = p == -1.f || s_idx[j] == 0xFFFFFFFFu ? 0.f : p;
+        }
+        wave_sync_lds();
     }
     return true;
 }
 
-// T sum_j p_j (ln p_j - ln q_j) over the threads' entries; an entry with p = 0 adds nothing, whatever the student's logit.  (Times T, so
-// that a logit of the type's lowest value overflows only where the loss does.)
-template <uint32_t NT>
+// T sum_j p_j (ln p_j - ln q_j), by one wave; an entry with p = 0 adds nothing, whatever the student's logit.  (Times T, so that a logit of the type's
+// lowest value overflows only where the loss does.)
 __device__ __forceinline__ float cross_terms(const DistillArgs& a, const uint32_t* s_idx, const float* s_p, const float* s_z, Softmax q) {
     const float log_s = logf(q.s);
     float sum = 0.f;
-    for (uint32_t j = threadIdx.x; j < a.k; j += NT) {
+    for (uint32_t j = threadIdx.x & 63u; j < a.k; j += 64) {
         const float p = s_p[j];
         if (s_idx[j] != 0xFFFFFFFFu && p != 0.f) sum += p * (a.T * (logf(p) + log_s) - (s_z[j] - q.m));
     }
+#pragma unroll
+    for (uint32_t o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
     return sum;
 }
 
-// A row by one workgroup, held in registers between the softmax's sums and the gradient: read once, written once.
+// A row by one workgroup, held in registers between the softmax's sums and the gradient: read once, written once.  The first wave reads the entries while
+// the row comes.
 template <uint32_t TYPE, uint32_t NT, uint32_t NV, bool GRAD>
-__global__ __launch_bounds__(NT) void k_distill_row(DistillArgs a) {
+__global__ __launch_bounds__(NT, TYPE == TYPE_F32 && NV == 8 ? 4 : 8) void k_distill_row(DistillArgs a) {
     extern __shared__ uint32_t s_dyn[];
-    __shared__ DistillRoom<NT> room;
+    __shared__ Softmax s_wave[NT / 64];
+    __shared__ uint32_t s_any;
     uint32_t* s_idx = s_dyn;
     float *s_p = reinterpret_cast<float*>(s_dyn + a.k), *s_z = s_p + a.k;
     uint32_t* s_table = s_dyn + 3u * a.k;
     const uint64_t row = blockIdx.x;
     const float w = a.weight ? a.weight[row] : 1.f;
-    Raw8<TYPE> raw[NV];
+    const uint32_t mis = misplaced<TYPE>(a.z, row * a.ld);
+    const bool first_wave = threadIdx.x < 64u;
+    Groups<TYPE, NT, NV> z;
     bool live = w != 0.f;
     Softmax q = {-INFINITY, 0.f};
     if (live) {
-#pragma unroll
-        for (uint32_t i = 0; i < NV; ++i) {
-            const uint64_t e = 8ull * (i * NT + threadIdx.x);
-            raw[i] = load8_first<TYPE>(a.z, row * a.ld + e, (int64_t)a.vocab - (int64_t)e, minus_inf<TYPE>());
+        z.load(a.z, row * a.ld, 0, mis, a.vocab);
+        if (first_wave) {
+            const bool any = read_teacher<TYPE>(a, row, 0, a.vocab, nullptr, s_idx, s_p, s_z, s_table);
+            if (threadIdx.x == 0) s_any = any;
         }
-        live = read_teacher<TYPE, NT>(a, row, 0, a.vocab, nullptr, s_idx, s_p, s_z, s_table, room);
+        z.mask(0, mis, a.vocab);
+        q = join_block<NT>(z.softmax(a.c), a.c, s_wave);
+        if (NT == 64) wave_sync_lds();
+        live = s_any && q.s != 0.f;
     }
-    if (live) {
-#pragma unroll
-        for (uint32_t i = 0; i < NV; ++i)
-#pragma unroll
-            for (uint32_t e = 0; e < 8; ++e) q.m = fmaxf(q.m, raw[i].at(e));
-        const float m = q.m == -INFINITY ? 0.f : q.m;
-#pragma unroll
-        for (uint32_t i = 0; i < NV; ++i)
-#pragma unroll
-            for (uint32_t e = 0; e < 8; ++e) q.s += exp2_fast((raw[i].at(e) - m) * a.c);
-        q = join_block<NT>(q, a.c, room.row);
-        live = q.s != 0.f;
-    }
-    if (a.loss) {
-        const float sum = live ? sum_block<NT>(cross_terms<NT>(a, s_idx, s_p, s_z, q), room.sum) : 0.f;
-        if (threadIdx.x == 0) a.loss[row] = live ? w * a.T * sum : 0.f;
-    }
-    if (a.stats && threadIdx.x == 0) {
-        a.stats[2 * row] = live ? q.m : 0.f;
-        a.stats[2 * row + 1] = live ? q.s : 0.f;
+    if (first_wave) {
+        const float sum = live && a.loss ? cross_terms(a, s_idx, s_p, s_z, q) : 0.f;
+        if (threadIdx.x == 0) {
+            if (a.loss) a.loss[row] = live ? w * a.T * sum : 0.f;
+            if (a.stats) {
+                a.stats[2 * row] = live ? q.m : 0.f;
+                a.stats[2 * row + 1] = live ? q.s : 0.f;
+            }
+        }
     }
     if (GRAD) {
-        const float f = w * a.T, fs = f / q.s;
-#pragma unroll
-        for (uint32_t i = 0; i < NV; ++i) {
-            const uint64_t e = 8ull * (i * NT + threadIdx.x);
-            float v[8];
-#pragma unroll
-            for (uint32_t x = 0; x < 8; ++x) v[x] = live ? exp2_fast((raw[i].at(x) - q.m) * a.c) * fs : 0.f;
-            store8_first<TYPE>(a.grad, row * a.ld_grad + e, (int64_t)a.vocab - (int64_t)e, v);
-        }
+        const float f = w * a.T;
+        z.store_gradient(a.grad, row * a.ld_grad, 0, mis, a.vocab, q, a.c, f, live);
         if (live) {
             __syncthreads();                     // the entries' columns once more, behind the others' stores
             for (uint32_t j = threadIdx.x; j < a.k; j += NT)
@@ -211,7 +276,7 @@ __global__ __launch_bounds__(NT) void k_distill_row(DistillArgs a) {
     }
 }
 
-constexpr uint32_t CHUNK_NT = 256, CHUNK_NV = 4, DISTILL_CHUNK = 8 * CHUNK_NT * CHUNK_NV;
+constexpr uint32_t CHUNK_NT = 256, CHUNK_NV = 4, DISTILL_CHUNK = CHUNK_NT * CHUNK_NV;   // groups of a chunk
 
 // A chunk of a row: its part of the softmax's sums; the first chunk's workgroup also puts the student's logits at the entries aside.
 template <uint32_t TYPE>
@@ -220,31 +285,14 @@ __global__ __launch_bounds__(CHUNK_NT) void k_distill_part(DistillArgs a) {
     const uint64_t row = blockIdx.x / a.chunks;
     const uint32_t chunk = blockIdx.x % a.chunks;
     if (a.weight && a.weight[row] == 0.f) return;
-    const uint64_t from = chunk * a.chunk, to = from + a.chunk < a.vocab ? from + a.chunk : a.vocab;
-    Softmax q = {-INFINITY, 0.f};
-    for (uint64_t e0 = from; e0 < to; e0 += DISTILL_CHUNK) {
-        Raw8<TYPE> raw[CHUNK_NV];
-#pragma unroll
-        for (uint32_t i = 0; i < CHUNK_NV; ++i) {
-            const uint64_t e = e0 + 8ull * (i * CHUNK_NT + threadIdx.x);
-            raw[i] = load8_first<TYPE>(a.z, row * a.ld + e, (int64_t)to - (int64_t)e, minus_inf<TYPE>());
-        }
-        Softmax v = {-INFINITY, 0.f};
-#pragma unroll
-        for (uint32_t i = 0; i < CHUNK_NV; ++i)
-#pragma unroll
-            for (uint32_t e = 0; e < 8; ++e) v.m = fmaxf(v.m, raw[i].at(e));
-        const float m = v.m == -INFINITY ? 0.f : v.m;
-#pragma unroll
-        for (uint32_t i = 0; i < CHUNK_NV; ++i)
-#pragma unroll
-            for (uint32_t e = 0; e < 8; ++e) v.s += exp2_fast((raw[i].at(e) - m) * a.c);
-        q = join(q, v, a.c);
-    }
-    q = join_block<CHUNK_NT>(q, a.c, room);
+    const uint32_t mis = misplaced<TYPE>(a.z, row * a.ld), j0 = chunk * DISTILL_CHUNK;
+    Groups<TYPE, CHUNK_NT, CHUNK_NV> z;
+    z.load(a.z, row * a.ld, j0, mis, a.vocab);
+    z.mask(j0, mis, a.vocab);
+    const Softmax q = join_block<CHUNK_NT>(z.softmax(a.c), a.c, room);
     if (threadIdx.x == 0) {
-        a.parts[2 * ((uint64_t)row * a.chunks + chunk)] = q.m;
-        a.parts[2 * ((uint64_t)row * a.chunks + chunk) + 1] = q.s;
+        a.parts[2 * (row * a.chunks + chunk)] = q.m;
+        a.parts[2 * (row * a.chunks + chunk) + 1] = q.s;
     }
     if (chunk == 0)
         for (uint32_t j = threadIdx.x; j < a.k; j += CHUNK_NT) {
@@ -253,68 +301,64 @@ __global__ __launch_bounds__(CHUNK_NT) void k_distill_part(DistillArgs a) {
         }
 }
 
-// A chunk of a row behind its sums, which come from the chunks' parts (PARTS) or from an earlier call's statistics: the
-// gradient (GRAD), and in the first chunk the loss and the statistics.
+// A chunk of a row behind its sums, which come from the chunks' parts (PARTS) or from an earlier call's statistics: the gradient (GRAD), and in the
+// first chunk the loss and the statistics.
 template <uint32_t TYPE, bool PARTS, bool GRAD>
 __global__ __launch_bounds__(CHUNK_NT) void k_distill_rest(DistillArgs a, uint32_t grid_chunks) {
     constexpr uint32_t NT = CHUNK_NT;
     extern __shared__ uint32_t s_dyn[];
-    __shared__ DistillRoom<NT> room;
+    __shared__ uint32_t s_any;
     uint32_t* s_idx = s_dyn;
     float *s_p = reinterpret_cast<float*>(s_dyn + a.k), *s_z = s_p + a.k;
     uint32_t* s_table = s_dyn + 3u * a.k;
     const uint64_t row = blockIdx.x / grid_chunks;
     const uint32_t chunk = blockIdx.x % grid_chunks;
-    const uint64_t from = chunk * a.chunk, to = from + a.chunk < a.vocab ? from + a.chunk : a.vocab;
+    const uint32_t mis = misplaced<TYPE>(a.z, row * a.ld), j0 = chunk * DISTILL_CHUNK;
     const float w = a.weight ? a.weight[row] : 1.f;
+    const bool first_wave = threadIdx.x < 64u;
     Softmax q = {-INFINITY, 0.f};
+    Groups<TYPE, NT, CHUNK_NV> z;
     bool live = w != 0.f;
     if (live) {
+        if (GRAD) z.load(a.z, row * a.ld, j0, mis, a.vocab);
         if (PARTS) {
-            for (uint32_t i = threadIdx.x; i < a.chunks; i += NT) {
-                const float* p = a.parts + 2 * ((uint64_t)row * a.chunks + i);
+            for (uint32_t i = threadIdx.x & 63u; i < a.chunks; i += 64) {
+                const float* p = a.parts + 2 * (row * a.chunks + i);
                 q = join(q, Softmax{p[0], p[1]}, a.c);
             }
-            q = join_block<NT>(q, a.c, room.row);
+            q = join_wave(q, a.c);
         } else {
             q = Softmax{a.stats[2 * row], a.stats[2 * row + 1]};
         }
-        live = q.s != 0.f;
-    }
-    if (live) live = read_teacher<TYPE, NT>(a, row, from, to, PARTS ? a.zj : nullptr, s_idx, s_p, s_z, s_table, room);
-    if (PARTS && chunk == 0) {
-        if (a.loss) {
-            const float sum = live ? sum_block<NT>(cross_terms<NT>(a, s_idx, s_p, s_z, q), room.sum) : 0.f;
-            if (threadIdx.x == 0) a.loss[row] = live ? w * a.T * sum : 0.f;
+        if (first_wave) {
+            // (the columns of the chunk's groups: what an entry there was is read before it is written)
+            const uint32_t begin = chunk * DISTILL_CHUNK * 8, from = begin < mis ? 0 : begin - mis;
+            const bool any = read_teacher<TYPE>(a, row, from, from + DISTILL_CHUNK * 8, PARTS ? a.zj : nullptr, s_idx, s_p, s_z, s_table);
+            if (threadIdx.x == 0) s_any = any;
         }
-        if (a.stats && threadIdx.x == 0) {
-            a.stats[2 * row] = live ? q.m : 0.f;
-            a.stats[2 * row + 1] = live ? q.s : 0.f;
+        __syncthreads();
+        live = s_any && q.s != 0.f;
+    }
+    if (PARTS && chunk == 0 && first_wave) {
+        const float sum = live && a.loss ? cross_terms(a, s_idx, s_p, s_z, q) : 0.f;
+        if (threadIdx.x == 0) {
+            if (a.loss) a.loss[row] = live ? w * a.T * sum : 0.f;
+            if (a.stats) {
+                a.stats[2 * row] = live ? q.m : 0.f;
+                a.stats[2 * row + 1] = live ? q.s : 0.f;
+            }
         }
     }
     if (GRAD) {
-        const float f = w * a.T, fs = f / q.s;
-        for (uint64_t e0 = from; e0 < to; e0 += DISTILL_CHUNK) {
-            Raw8<TYPE> raw[CHUNK_NV];
-#pragma unroll
-            for (uint32_t i = 0; i < CHUNK_NV; ++i) {
-                const uint64_t e = e0 + 8ull * (i * NT + threadIdx.x);
-                if (live) raw[i] = load8_first<TYPE>(a.z, row * a.ld + e, (int64_t)to - (int64_t)e, minus_inf<TYPE>());
-            }
-#pragma unroll
-            for (uint32_t i = 0; i < CHUNK_NV; ++i) {
-                const uint64_t e = e0 + 8ull * (i * NT + threadIdx.x);
-                float v[8];
-#pragma unroll
-                for (uint32_t x = 0; x < 8; ++x) v[x] = live ? exp2_fast((raw[i].at(x) - q.m) * a.c) * fs : 0.f;
-                store8_first<TYPE>(a.grad, row * a.ld_grad + e, (int64_t)to - (int64_t)e, v);
-            }
-        }
+        const float f = w * a.T;
+        z.store_gradient(a.grad, row * a.ld_grad, j0, mis, a.vocab, q, a.c, f, live);
         if (live) {
             __syncthreads();
-            for (uint32_t j = threadIdx.x; j < a.k; j += NT)
-                if (s_idx[j] >= from && s_idx[j] < to)
-                    store1<TYPE>(a.grad, row * a.ld_grad + s_idx[j], f * (exp2_fast((s_z[j] - q.m) * a.c) / q.s - s_p[j]));
+            for (uint32_t j = threadIdx.x; j < a.k; j += NT) {
+                const uint32_t i = s_idx[j];
+                if (i != 0xFFFFFFFFu && (i + mis) / (8 * DISTILL_CHUNK) == chunk)
+                    store1<TYPE>(a.grad, row * a.ld_grad + i, f * (exp2_fast((s_z[j] - q.m) * a.c) / q.s - s_p[j]));
+            }
         }
     }
 }

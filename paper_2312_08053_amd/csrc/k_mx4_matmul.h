@@ -58,15 +58,6 @@ __device__ __forceinline__ void turn_quad(float v0, float v1, float v2, float v3
     const float s0 = swap2(high ? a0 : b0), s1 = swap2(high ? a1 : b1);
     out[0] = high ? s0 : a0; out[1] = high ? s1 : a1; out[2] = high ? b0 : s0; out[3] = high ? b1 : s1;
 }
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-// Two values rounded to nearest even, the first one low.
-template <uint32_t TYPE>
-__device__ __forceinline__ uint32_t pack2(float a, float b) {
-    const f32x2 v = {a, b};
-    if (TYPE == TYPE_BF16) return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
-    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2));
-}
 // The same on pairs of 16-bit values: v01 holds rows 0 and 1, v23 rows 2 and 3.
 __device__ __forceinline__ void turn_quad16(uint32_t v01, uint32_t v23, bool odd, bool high, uint32_t out[2]) {
     const uint32_t pick = odd ? 0x03020706u : 0x05040100u;                    // even: own low, other's low; odd: other's high, own high

@@ -17,12 +17,14 @@ typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 
 __device__ __forceinline__ float half_to_float(uint32_t bits) { return (float)__builtin_bit_cast(_Float16, (uint16_t)bits); }
-__device__ __forceinline__ uint32_t float_to_half(float v) { return __builtin_bit_cast(uint16_t, (_Float16)v); }
-// Rounds to nearest even; a NaN stays one.
-__device__ __forceinline__ uint32_t float_to_bfloat(float v) {
-    const uint32_t b = __float_as_uint(v);
-    const uint32_t r = b + 0x7FFFu + ((b >> 16) & 1u);
-    return (v != v ? (b | 0x400000u) : r) >> 16;
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+// Two values rounded to nearest even, the first one low; a NaN stays one.
+template <uint32_t TYPE>
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+    const f32x2 v = {a, b};
+    if (TYPE == TYPE_BF16) return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2));
 }
 
 // One element of a typed array, and eight that stand side by side.
@@ -35,7 +37,7 @@ __device__ __forceinline__ float load1(const void* p, uint64_t i) {
 template <uint32_t TYPE>
 __device__ __forceinline__ void store1(void* p, uint64_t i, float v) {
     if (TYPE == TYPE_F32) static_cast<float*>(p)[i] = v;
-    else static_cast<uint16_t*>(p)[i] = (uint16_t)(TYPE == TYPE_F16 ? float_to_half(v) : float_to_bfloat(v));
+    else static_cast<uint16_t*>(p)[i] = (uint16_t)pack2<TYPE>(v, v);
 }
 
 // Eight elements as they lie in memory (four or eight registers), loaded now and turned into floats later.
@@ -92,9 +94,7 @@ __device__ __forceinline__ void store8(void* p, uint64_t i, const float v[8]) {
     } else {
         u32x4 a;
 #pragma unroll
-        for (uint32_t k = 0; k < 4; ++k)
-            a[k] = TYPE == TYPE_F16 ? float_to_half(v[2 * k]) | float_to_half(v[2 * k + 1]) << 16
-                                    : float_to_bfloat(v[2 * k]) | float_to_bfloat(v[2 * k + 1]) << 16;
+        for (uint32_t k = 0; k < 4; ++k) a[k] = pack2<TYPE>(v[2 * k], v[2 * k + 1]);
         *reinterpret_cast<u32x4_any*>(static_cast<uint16_t*>(p) + i) = a;
     }
 }

@@ -53,9 +53,10 @@ inline uint32_t update_grid(uint64_t words, uint64_t& share) {
 
 namespace {
 
-// Few long rows are shared out over the compute units.
-inline bool distill_split(uint64_t rows, uint64_t vocab) { return vocab > DISTILL_CHUNK && rows < 128; }
-inline uint32_t distill_chunks(uint64_t vocab) { return (uint32_t)((vocab + DISTILL_CHUNK - 1) / DISTILL_CHUNK); }
+// Few long rows are shared out over the compute units, and rows that no workgroup's registers hold.
+constexpr uint64_t DISTILL_ROW_MOST = 65536 - 7;         // elements of a row that k_distill_row holds (a group more where it begins off a 16-byte address)
+inline uint32_t distill_chunks(uint64_t vocab) { return (uint32_t)((vocab + 7 + 8 * DISTILL_CHUNK - 1) / (8 * DISTILL_CHUNK)); }
+inline bool distill_split(uint64_t rows, uint64_t vocab) { return vocab > DISTILL_ROW_MOST || (vocab > 8192 && rows < 128); }
 
 int distill_args(DistillArgs& a, const void* logits, uint32_t type, uint64_t rows, uint64_t vocab, uint64_t ld, const uint32_t* t_idx,
                  const float* t_val, uint32_t k, float temperature, const float* row_weight, const void* grad, uint64_t ld_grad) {
@@ -65,9 +66,9 @@ int distill_args(DistillArgs& a, const void* logits, uint32_t type, uint64_t row
     if (grad && (ld_grad < vocab || !aligned(grad, type_bytes(type)))) return KIMAD_ERR_INVALID_ARG;
     if (rows * distill_chunks(vocab) > GRID_MOST) return KIMAD_ERR_INVALID_ARG;
     a.z = logits; a.idx = t_idx; a.val = t_val; a.weight = row_weight; a.grad = const_cast<void*>(grad);
-    a.rows = rows; a.vocab = vocab; a.ld = ld; a.ld_grad = ld_grad; a.k = k; a.bloom = distill_bloom(k);
+    a.rows = rows; a.vocab = (uint32_t)vocab; a.ld = ld; a.ld_grad = ld_grad; a.k = k; a.bloom = distill_bloom(k);
     a.T = temperature; a.c = (float)(1.4426950408889634 / (double)temperature);
-    a.chunk = DISTILL_CHUNK; a.chunks = distill_chunks(vocab);
+    a.chunks = distill_chunks(vocab);
     return KIMAD_OK;
 }
 
@@ -276,7 +277,7 @@ int kimad_mx4_server_apply(const kimad_mx4_update_t* updates, float* const* u_ha
 }
 
 uint64_t kimad_distill_workspace_bytes(uint64_t rows, uint64_t vocab, uint32_t k) {
-    return distill_split(rows, vocab) || vocab > 65536 ? 4 * rows * (2ull * distill_chunks(vocab) + k) : 0;
+    return distill_split(rows, vocab) ? 4 * rows * (2ull * distill_chunks(vocab) + k) : 0;
 }
 
 int kimad_distill(const void* logits, uint32_t type, uint64_t rows, uint64_t vocab, uint64_t ld, const uint32_t* t_idx,
@@ -304,11 +305,12 @@ int kimad_distill(const void* logits, uint32_t type, uint64_t rows, uint64_t voc
     }
     return with_type(type, [&](auto t) {
         constexpr uint32_t TYPE = decltype(t)::value;
-        if (vocab <= 512) return launch_row<TYPE, 64, 1>(a, s);
-        if (vocab <= 2048) return launch_row<TYPE, 256, 1>(a, s);
-        if (vocab <= 8192) return launch_row<TYPE, 256, 4>(a, s);
-        if (vocab <= 16384) return launch_row<TYPE, 1024, 2>(a, s);
-        if (vocab <= 32768) return launch_row<TYPE, 1024, 4>(a, s);
+        const uint64_t groups = (vocab + 7 + 7) / 8;
+        if (groups <= 64) return launch_row<TYPE, 64, 1>(a, s);
+        if (groups <= 256) return launch_row<TYPE, 256, 1>(a, s);
+        if (groups <= 1024) return launch_row<TYPE, 256, 4>(a, s);
+        if (groups <= 2048) return launch_row<TYPE, 1024, 2>(a, s);
+        if (groups <= 4096) return launch_row<TYPE, 1024, 4>(a, s);
         return launch_row<TYPE, 1024, 8>(a, s);
     });
 }
