@@ -111,7 +111,7 @@ template <int CTRL>
 __device__ __forceinline__ uint32_t dpp_u32(uint32_t v) {
     return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, CTRL, 0xF, 0xF, true);
 }
-constexpr int DPP_XOR1 = 0xB1, DPP_XOR2 = 0x4E, DPP_ROR4 = 0x124, DPP_ROR8 = 0x128;
+constexpr int DPP_XOR1 = 0xB1, DPP_XOR2 = 0x4E, DPP_ROR4 = 0x124, DPP_ROR8 = 0x128, DPP_HALF_MIRROR = 0x141;
 
 // The scale byte of a block whose largest magnitude has these bits: two below the exponent, so that the largest element lies in
 // [4, 8) and rounds to 4 or 6.  The smallest scale is 2^-127; a block with Inf or NaN gets 255 and stands for NaN as a whole.
@@ -140,6 +140,29 @@ __device__ __forceinline__ uint32_t mx4_encode8(const float v[8], uint32_t& byte
     c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[4], v[5], s, 2);
     c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[6], v[7], s, 3);
     return byte == 255u ? 0u : c;
+}
+// The same with four elements a lane, of a block that eight neighbours share: 16 bits of codes.
+__device__ __forceinline__ uint32_t mx4_encode4(const float v[4], uint32_t& byte) {
+    uint32_t a = 0;
+#pragma unroll
+    for (uint32_t k = 0; k < 4; ++k) { const uint32_t b = key_of(v[k]); a = a > b ? a : b; }
+    uint32_t o = dpp_u32<DPP_XOR1>(a);
+    a = a > o ? a : o;
+    o = dpp_u32<DPP_XOR2>(a);
+    a = a > o ? a : o;
+    o = dpp_u32<DPP_HALF_MIRROR>(a);
+    a = a > o ? a : o;
+    byte = mx4_scale_byte(a);
+    const float s = mx4_scale(byte);
+    uint32_t c = 0;
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[0], v[1], s, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[2], v[3], s, 1);
+    return byte == 255u ? 0u : c;
+}
+__device__ __forceinline__ void mx4_decode4(uint32_t codes, uint32_t byte, float v[4]) {
+    const float s = mx4_scale(byte);
+    const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, s, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, s, 1);
+    v[0] = a[0]; v[1] = a[1]; v[2] = b[0]; v[3] = b[1];
 }
 // What eight codes stand for.
 __device__ __forceinline__ void mx4_decode8(uint32_t codes, uint32_t byte, float v[8]) {

@@ -248,11 +248,13 @@ int kimad_mx4_compress_ef(const float* g, float* h, const uint64_t* layer_start,
                           uint32_t* scales, int32_t* status_out, void* stream) {
     if (!g || !h || !layer_start || L == 0 || d == 0 || d > MOST || !codes || !pair_ok(codes, scales) || !aligned(g, 4) || !aligned(h, 4))
         return KIMAD_ERR_INVALID_ARG;
-    const uint64_t words = kimad_mx4_update_words(L, d);
-    uint64_t share;
-    const uint32_t wgs = update_grid(words, share);
-    hipLaunchKernelGGL(k_mx4_compress, dim3(wgs), dim3(256), 0, static_cast<hipStream_t>(stream), g, h, layer_start, L, d, words, share,
-                       static_cast<uint32_t*>(codes), scales, status_out, (int32_t)KIMAD_ERR_BAD_OFFSETS);
+    Mx4CompressArgs a{};
+    a.g = g; a.h = h; a.layer_start = layer_start; a.L = L; a.d = d;
+    a.codes = static_cast<uint16_t*>(codes); a.scales = scales;
+    a.words = kimad_mx4_update_words(L, d);
+    a.streams = aligned(g, 128) && aligned(h, 128) && update_streams(8 * d);
+    const uint32_t wgs = update_grid(a.words, a.share);
+    hipLaunchKernelGGL(k_mx4_compress, dim3(wgs), dim3(256), 0, static_cast<hipStream_t>(stream), a, status_out, (int32_t)KIMAD_ERR_BAD_OFFSETS);
     return launched();
 }
 
@@ -262,14 +264,17 @@ int kimad_mx4_server_apply(const kimad_mx4_update_t* updates, float* const* u_ha
     if (!updates || !u_hat || !weights || !layer_start || M == 0 || M > KIMAD_MAX_WORKERS || L == 0 || d == 0 || d > MOST || !aligned(x, 4))
         return KIMAD_ERR_INVALID_ARG;
     Mx4ServerArgs a{};
+    bool lined = true;
     for (uint32_t m = 0; m < M; ++m) {
         if (!updates[m].codes || !pair_ok(updates[m].codes, updates[m].scales) || !u_hat[m] || !aligned(u_hat[m], 4)) return KIMAD_ERR_INVALID_ARG;
-        a.codes[m] = static_cast<const uint32_t*>(updates[m].codes);
+        a.codes[m] = static_cast<const uint16_t*>(updates[m].codes);
         a.scales[m] = updates[m].scales;
         a.u_hat[m] = u_hat[m];
         a.w[m] = weights[m];
+        lined = lined && aligned(u_hat[m], 128);
     }
     a.M = M; a.L = L; a.d = d; a.layer_start = layer_start; a.x = x; a.gamma = gamma;
+    a.streams = lined && aligned(x, 128) && update_streams(4 * (M + 1) * d);
     a.words = kimad_mx4_update_words(L, d);
     const uint32_t wgs = update_grid(a.words, a.share);
     hipLaunchKernelGGL(k_mx4_server, dim3(wgs), dim3(256), 0, static_cast<hipStream_t>(stream), a, status_out, (int32_t)KIMAD_ERR_BAD_OFFSETS);
