@@ -5,7 +5,8 @@
 
 namespace kimad {
 
-constexpr uint32_t QROWS = 16, QWORDS = 64;  // rows and words of a workgroup's share
+constexpr uint32_t QROWS = 16, QWORDS = 8;    // rows and words of a workgroup's share
+constexpr uint32_t QU = 4;                   // words of a lane under way together
 
 // Along rows: a workgroup takes 16 rows of up to 64 words.  Its sixteen groups of sixteen lanes walk row by row through the share, so
 // that reads and codes run on without gaps; the scale words, whose neighbours in memory are other rows' words, are collected in LDS
@@ -16,19 +17,28 @@ __global__ __launch_bounds__(256) void k_mx4_quantise_rows(const void* __restric
     __shared__ uint32_t s_scale[QWORDS * QROWS];
     const uint64_t row0 = (uint64_t)blockIdx.x * QROWS, word0 = (uint64_t)blockIdx.y * QWORDS;
     const uint32_t nr = (uint32_t)(rows - row0 < QROWS ? rows - row0 : QROWS), nw = (uint32_t)(W - word0 < QWORDS ? W - word0 : QWORDS);
-    const uint32_t lane16 = threadIdx.x & 15u;
-    for (uint32_t u = threadIdx.x >> 4; u < nr * nw; u += 16u) {
-        const uint32_t r = u / nw, w = u - r * nw;
-        const uint64_t row = row0 + r, col = (word0 + w) * MX4_WORD + 8u * lane16;
-        const Raw8<TYPE> raw = load8_first<TYPE>(x, row * ld + col, (int64_t)cols - (int64_t)col, 0u);
-        float v[8];
+    const uint32_t lane16 = threadIdx.x & 15u, units = nr * nw;
+    for (uint32_t u0 = threadIdx.x >> 4; u0 < units; u0 += 16u * QU) {
+        Raw8<TYPE> raw[QU];
 #pragma unroll
-        for (uint32_t k = 0; k < 8; ++k) v[k] = raw.at(k);
-        uint32_t byte;
-        const uint32_t c = mx4_encode8(v, byte);
-        codes[(row * W + word0 + w) * 16u + lane16] = c;
-        const uint32_t sw = mx4_scale_word(byte, lane16);
-        if (lane16 == 0) s_scale[w * QROWS + r] = sw;
+        for (uint32_t i = 0; i < QU; ++i) {
+            const uint32_t u = u0 + 16u * i, r = u / nw, w = u - r * nw;
+            const uint64_t col = (word0 + w) * MX4_WORD + 8u * lane16;
+            raw[i] = load8_first<TYPE>(x, (row0 + r) * ld + col, u < units ? (int64_t)cols - (int64_t)col : 0, 0u);
+        }
+#pragma unroll
+        for (uint32_t i = 0; i < QU; ++i) {
+            const uint32_t u = u0 + 16u * i, r = u / nw, w = u - r * nw;
+            if (u >= units) break;
+            float v[8];
+#pragma unroll
+            for (uint32_t k = 0; k < 8; ++k) v[k] = raw[i].at(k);
+            uint32_t byte;
+            const uint32_t c = mx4_encode8(v, byte);
+            codes[((row0 + r) * W + word0 + w) * 16u + lane16] = c;
+            const uint32_t sw = mx4_scale_word(byte, lane16);
+            if (lane16 == 0) s_scale[w * QROWS + r] = sw;
+        }
     }
     __syncthreads();
     for (uint32_t i = threadIdx.x; i < nw * QROWS; i += 256u) {
@@ -124,18 +134,32 @@ __global__ __launch_bounds__(256) void k_mx4_dequantise(const uint32_t* __restri
     __shared__ uint32_t s_scale[QWORDS * QROWS];
     const uint64_t row0 = (uint64_t)blockIdx.x * QROWS, word0 = (uint64_t)blockIdx.y * QWORDS;
     const uint32_t nr = (uint32_t)(rows - row0 < QROWS ? rows - row0 : QROWS), nw = (uint32_t)(W - word0 < QWORDS ? W - word0 : QWORDS);
+    const uint32_t lane16 = threadIdx.x & 15u, units = nr * nw;
     for (uint32_t i = threadIdx.x; i < nw * QROWS; i += 256u) {
         const uint32_t w = i / QROWS, r = i % QROWS;
         if (r < nr) s_scale[i] = scales[(word0 + w) * rows + row0 + r];
     }
+    uint32_t c[QU];
+    auto fetch = [&](uint32_t u0) {
+#pragma unroll
+        for (uint32_t i = 0; i < QU; ++i) {
+            const uint32_t u = u0 + 16u * i, r = u / nw, w = u - r * nw;
+            c[i] = u < units ? codes[((row0 + r) * W + word0 + w) * 16u + lane16] : 0u;
+        }
+    };
+    fetch(threadIdx.x >> 4);
     __syncthreads();
-    const uint32_t lane16 = threadIdx.x & 15u;
-    for (uint32_t u = threadIdx.x >> 4; u < nr * nw; u += 16u) {
-        const uint32_t r = u / nw, w = u - r * nw;
-        const uint64_t row = row0 + r, col = (word0 + w) * MX4_WORD + 8u * lane16;
-        float v[8];
-        mx4_decode8(codes[(row * W + word0 + w) * 16u + lane16], (s_scale[w * QROWS + r] >> (8u * (lane16 >> 2))) & 255u, v);
-        store8_first<TYPE>(out, row * ld + col, (int64_t)cols - (int64_t)col, v);
+    for (uint32_t u0 = threadIdx.x >> 4; u0 < units; u0 += 16u * QU) {
+        if (u0 >= 16u * QU) fetch(u0);
+#pragma unroll
+        for (uint32_t i = 0; i < QU; ++i) {
+            const uint32_t u = u0 + 16u * i, r = u / nw, w = u - r * nw;
+            if (u >= units) break;
+            const uint64_t col = (word0 + w) * MX4_WORD + 8u * lane16;
+            float v[8];
+            mx4_decode8(c[i], (s_scale[w * QROWS + r] >> (8u * (lane16 >> 2))) & 255u, v);
+            store8_first<TYPE>(out, (row0 + r) * ld + col, (int64_t)cols - (int64_t)col, v);
+        }
     }
 }
 
