@@ -261,26 +261,28 @@ __global__ __launch_bounds__(64 * T::WAVES, 2) void k_mx4_matmul_tile(MatmulArgs
 #pragma unroll
                 for (uint32_t e = 0; e < 4; ++e) {
                     const f32x16 v = acc[i][j];
-                    const uint32_t o = at + 32 * j * BYTES, step = 8 * e * (uint32_t)g.ld * BYTES;
+                    // (the whole offset in the lane's register: a 16-byte store with a scalar offset as well has stored values that the next instructions
+                    // wrote into its data registers, in rows with such an offset and in no others)
+                    const uint32_t o = at + (32 * j + 8 * e * (uint32_t)g.ld) * BYTES;
                     if (TYPE == TYPE_F32) {
                         float r[4];
                         turn_quad(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3], odd, high, r);
                         if (whole) {
-                            __builtin_amdgcn_raw_buffer_store_b128(u32x4{__float_as_uint(r[0]), __float_as_uint(r[1]), __float_as_uint(r[2]), __float_as_uint(r[3])}, to, o, step, 0);
+                            __builtin_amdgcn_raw_buffer_store_b128(u32x4{__float_as_uint(r[0]), __float_as_uint(r[1]), __float_as_uint(r[2]), __float_as_uint(r[3])}, to, o, 0, 0);
                         } else {
 #pragma unroll
                             for (uint32_t k = 0; k < 4; ++k)
-                                __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(r[k]), to, row + 32 * i + 8 * e < rows && col + 32 * j + k < cols ? o + 4 * k : BEYOND, step, 0);
+                                __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(r[k]), to, row + 32 * i + 8 * e < rows && col + 32 * j + k < cols ? o + 4 * k : BEYOND, 0, 0);
                         }
                     } else {
                         uint32_t r[2];
                         turn_quad16(pack2<TYPE>(v[4 * e], v[4 * e + 1]), pack2<TYPE>(v[4 * e + 2], v[4 * e + 3]), odd, high, r);
                         if (whole) {
-                            __builtin_amdgcn_raw_buffer_store_b64(u32x2{r[0], r[1]}, to, o, step, 0);
+                            __builtin_amdgcn_raw_buffer_store_b64(u32x2{r[0], r[1]}, to, o, 0, 0);
                         } else {
 #pragma unroll
                             for (uint32_t k = 0; k < 4; ++k)
-                                __builtin_amdgcn_raw_buffer_store_b16((uint16_t)(r[k / 2] >> (16 * (k % 2))), to, row + 32 * i + 8 * e < rows && col + 32 * j + k < cols ? o + 2 * k : BEYOND, step, 0);
+                                __builtin_amdgcn_raw_buffer_store_b16((uint16_t)(r[k / 2] >> (16 * (k % 2))), to, row + 32 * i + 8 * e < rows && col + 32 * j + k < cols ? o + 2 * k : BEYOND, 0, 0);
                         }
                     }
                 }

@@ -194,6 +194,42 @@ def test_product(M, N, K):
     _product_close(_host(out), av, bv, K, kind)
 
 
+def _large_operand(rows, K, seed):
+    """The same for sizes that only the device multiplies in 64 bits: random codes, scales that keep sums within a float16."""
+    import torch
+    gen = torch.Generator().manual_seed(seed)
+    words = -(-K // 128)
+    packed = torch.randint(0, 256, (rows, 64 * words), dtype=torch.uint8, generator=gen)
+    full = K // 2
+    packed[:, full + K % 2:] = 0
+    if K % 2:
+        packed[:, full] &= 15
+    byte = torch.randint(122, 128, (rows, 4 * words), dtype=torch.int64, generator=gen)
+    byte[:, -(-K // 32):] = 0
+    scale = (byte.view(rows, words, 4) << torch.tensor([0, 8, 16, 24])).sum(-1).to(torch.int32).t().contiguous()
+    packed, byte = packed.cuda(), byte.cuda()
+    magnitudes = torch.tensor(ref.MAGNITUDES, device="cuda")
+    codes = torch.stack([packed & 15, packed >> 4], -1).view(rows, -1).long()
+    sign = torch.where(codes >= 8, -1.0, 1.0).double()
+    return (packed, scale.cuda()), sign * magnitudes[codes & 7] * (2.0 ** (byte - 127).double()).repeat_interleave(32, 1)
+
+
+# sizes at which workgroups go through several tiles, of each tile's size, with rows and columns left over and without, words even and odd
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("M,N,K", [(8192, 5632, 768), (8200, 5641, 600), (4200, 4200, 260), (6000, 2050, 129), (3000, 2900, 100), (2049, 4100, 1300), (512, 768, 16384)])
+def test_product_over_several_tiles_a_workgroup(M, N, K, kind):
+    import torch
+    (a, sa), av = _large_operand(M, K, 1)
+    (b, sb), bv = _large_operand(N, K, 2)
+    out = torch.full((M, N), 99.0, dtype=getattr(torch, kind), device="cuda")
+    _kimad().kimad_mx4_matmul(a, sa, b, sb, K, out)
+    bt, bt_size = bv.t().contiguous(), bv.abs().t().contiguous()
+    want, size = av @ bt, av.abs() @ bt_size
+    half = {"float32": 2.0 ** -24, "float16": 2.0 ** -11, "bfloat16": 2.0 ** -8}[kind]
+    bad = (out.double() - want).abs() > (K + 128) * 2.0 ** -23 * size + half * want.abs() * 1.0001
+    assert not bad.any(), (int(bad.sum()), bad.nonzero()[:3].tolist())
+
+
 @pytest.mark.parametrize("kind", TYPES)
 @pytest.mark.parametrize("M,N,K", [(1, 70, 300), (20, 33, 260), (130, 140, 400), (257, 300, 1100)])
 @pytest.mark.parametrize("pad,offset", [(0, 0), (5, 1), (8, 0)])
