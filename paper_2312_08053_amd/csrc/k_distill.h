@@ -170,17 +170,37 @@ __device__ __forceinline__ bool read_teacher(const DistillArgs& a, uint64_t row,
     wave_sync_lds();
     Softmax v = {-INFINITY, 0.f};
     bool any = false, meets = false;
-    for (uint32_t j = lane; j < k; j += 64) {
-        const uint32_t i = a.idx[row * k + j];
-        const bool in = i < a.vocab;
-        const float t = in ? a.val[row * k + j] : -INFINITY;
-        s_idx[j] = in ? i : 0xFFFFFFFFu;
-        s_p[j] = t;
-        s_z[j] = zj ? zj[row * k + j] : in && i >= from && i < to ? load1<TYPE>(a.z, row * a.ld + i) : 0.f;
-        any = any || (in && t != -INFINITY);
-        v = join(v, Softmax{t, t == -INFINITY ? 0.f : 1.f}, a.c);
-        if (t != t) v.s = t;
-        if (in) meets = meets || (atomicOr(&s_table[(i >> 5) & (a.bloom - 1u)], 1u << (i & 31u)) >> (i & 31u) & 1u);
+    constexpr uint32_t U = 4;                            // entries of a lane under way together
+    for (uint32_t j0 = lane; j0 < k; j0 += 64 * U) {
+        uint32_t i[U];
+        float t[U], z[U];
+#pragma unroll
+        for (uint32_t u = 0; u < U; ++u) {
+            const uint32_t j = j0 + 64 * u;
+            i[u] = j < k ? a.idx[row * k + j] : 0xFFFFFFFFu;
+            t[u] = j < k ? a.val[row * k + j] : 0.f;
+        }
+#pragma unroll
+        for (uint32_t u = 0; u < U; ++u) {
+            const uint32_t j = j0 + 64 * u;
+            if (zj) z[u] = j < k ? zj[row * k + j] : 0.f;
+            else z[u] = i[u] < a.vocab && i[u] >= from && i[u] < to ? load1<TYPE>(a.z, row * a.ld + i[u]) : 0.f;
+        }
+#pragma unroll
+        for (uint32_t u = 0; u < U; ++u) {
+            const uint32_t j = j0 + 64 * u;
+            if (j >= k) break;
+            const bool in = i[u] < a.vocab;
+            if (!in) t[u] = -INFINITY;
+            s_idx[j] = in ? i[u] : 0xFFFFFFFFu;
+            s_p[j] = t[u];
+            s_z[j] = z[u];
+            any = any || (in && t[u] != -INFINITY);
+            const bool nan = t[u] != t[u];
+            v = join(v, Softmax{t[u], t[u] == -INFINITY ? 0.f : 1.f}, a.c);
+            if (nan) v.s = t[u];
+            if (in) meets = meets || (atomicOr(&s_table[(i[u] >> 5) & (a.bloom - 1u)], 1u << (i[u] & 31u)) >> (i[u] & 31u) & 1u);
+        }
     }
     if (!ballot(any)) return false;
     v = join_wave(v, a.c);

@@ -312,10 +312,12 @@ int kimad_distill(const void* logits, uint32_t type, uint64_t rows, uint64_t voc
         constexpr uint32_t TYPE = decltype(t)::value;
         const uint64_t groups = (vocab + 7 + 7) / 8;
         if (groups <= 64) return launch_row<TYPE, 64, 1>(a, s);
-        if (groups <= 256) return launch_row<TYPE, 256, 1>(a, s);
+        if (groups <= 128) return launch_row<TYPE, 64, 2>(a, s);
+        if (groups <= 256) return launch_row<TYPE, 64, 4>(a, s);
+        if (groups <= 512) return launch_row<TYPE, 128, 4>(a, s);
         if (groups <= 1024) return launch_row<TYPE, 256, 4>(a, s);
-        if (groups <= 2048) return launch_row<TYPE, 1024, 2>(a, s);
-        if (groups <= 4096) return launch_row<TYPE, 1024, 4>(a, s);
+        if (groups <= 2048) return launch_row<TYPE, 256, 8>(a, s);
+        if (groups <= 4096) return launch_row<TYPE, 512, 8>(a, s);
         return launch_row<TYPE, 1024, 8>(a, s);
     });
 }
