@@ -80,6 +80,8 @@ template <uint32_t TYPE, uint32_t NT, uint32_t NV>
 struct Groups {
     Raw8<TYPE> raw[NV];
     static constexpr uint32_t B = bytes_of<TYPE>(), GROUP = 8 * B;
+    // (a group of NT beyond the row is passed over by all threads)
+    static __device__ __forceinline__ bool beyond(uint32_t i, uint32_t j0, uint32_t mis, uint32_t vocab) { return 8ull * (j0 + i * NT) >= (uint64_t)mis + vocab; }
     static __device__ __forceinline__ bool whole(uint32_t i, uint32_t j0, uint32_t mis, uint32_t vocab) {
         return (mis == 0 || j0 + i > 0) && 8ull * (j0 + (i + 1) * NT) <= (uint64_t)mis + vocab;
     }
@@ -91,11 +93,13 @@ struct Groups {
                                                                                (int)(left < NV * NT * GROUP ? left : NV * NT * GROUP), 0x00020000);
 #pragma unroll
         for (uint32_t i = 0; i < NV; ++i) {
+            if (!beyond(i, j0, mis, vocab)) {
 #pragma unroll
-            for (uint32_t h = 0; h < GROUP / 16; ++h) {
-                const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(from, threadIdx.x * GROUP + 16 * h, i * NT * GROUP, 0);
+                for (uint32_t h = 0; h < GROUP / 16; ++h) {
+                    const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(from, threadIdx.x * GROUP + 16 * h, i * NT * GROUP, 0);
 #pragma unroll
-                for (uint32_t k = 0; k < 4; ++k) raw[i].r[(4 * h + k) % (GROUP / 4)] = v[k];
+                    for (uint32_t k = 0; k < 4; ++k) raw[i].r[(4 * h + k) % (GROUP / 4)] = v[k];
+                }
             }
         }
     }
@@ -103,7 +107,7 @@ struct Groups {
     __device__ __forceinline__ void mask(uint32_t j0, uint32_t mis, uint32_t vocab) {
 #pragma unroll
         for (uint32_t i = 0; i < NV; ++i)
-            if (!whole(i, j0, mis, vocab)) {
+            if (!whole(i, j0, mis, vocab) && !beyond(i, j0, mis, vocab)) {
                 const uint32_t e = element(i, j0, mis);
 #pragma unroll
                 for (uint32_t x = 0; x < 8; ++x)
@@ -111,22 +115,24 @@ struct Groups {
             }
     }
     // Largest element and sum, a group at a time: an element is taken apart once, and only as it lies in memory does it stay in a register.
-    __device__ __forceinline__ Softmax softmax(float c) const {
+    __device__ __forceinline__ Softmax softmax(uint32_t j0, uint32_t mis, uint32_t vocab, float c) const {
         Softmax q = {-INFINITY, 0.f};
 #pragma unroll
         for (uint32_t i = 0; i < NV; ++i) {
-            float v[8], m = q.m;
+            if (!beyond(i, j0, mis, vocab)) {
+                float v[8], m = q.m;
 #pragma unroll
-            for (uint32_t x = 0; x < 8; ++x) {
-                v[x] = raw[i].at(x);
-                m = fmaxf(m, v[x]);
+                for (uint32_t x = 0; x < 8; ++x) {
+                    v[x] = raw[i].at(x);
+                    m = fmaxf(m, v[x]);
+                }
+                const float from = m == -INFINITY ? 0.f : m;
+                float sum = 0.f;
+#pragma unroll
+                for (uint32_t x = 0; x < 8; ++x) sum += exp2_fast((v[x] - from) * c);
+                q.s = (q.m == m ? q.s : q.s * exp2_fast((q.m - m) * c)) + sum;
+                q.m = m;
             }
-            const float from = m == -INFINITY ? 0.f : m;
-            float sum = 0.f;
-#pragma unroll
-            for (uint32_t x = 0; x < 8; ++x) sum += exp2_fast((v[x] - from) * c);
-            q.s = (q.m == m ? q.s : q.s * exp2_fast((q.m - m) * c)) + sum;
-            q.m = m;
         }
         return q;
     }
@@ -140,19 +146,18 @@ struct Groups {
         uint8_t* base = static_cast<uint8_t*>(p) + (row - mis) * B + (uint64_t)j0 * GROUP;
 #pragma unroll
         for (uint32_t i = 0; i < NV; ++i) {
-            float v[8];
+            if (!beyond(i, j0, mis, vocab)) {
+                float v[8] = {};
+                if (live)
 #pragma unroll
-            for (uint32_t x = 0; x < 8; ++x) v[x] = live ? exp2_fast((raw[i].at(x) - q.m) * c) * fs : 0.f;
-            uint8_t* to = base + i * NT * GROUP;
-            if (whole(i, j0, mis, vocab)) {
-                store8<TYPE>(to + threadIdx.x * GROUP, 0, v);
-            } else {
+                    for (uint32_t x = 0; x < 8; ++x) v[x] = exp2_fast((raw[i].at(x) - q.m) * c) * fs;
+                uint8_t* to = base + i * NT * GROUP + threadIdx.x * GROUP;
                 const uint32_t e = element(i, j0, mis);
-                if (e < vocab && vocab - e >= 8) store8<TYPE>(to + threadIdx.x * GROUP, 0, v);
+                if (whole(i, j0, mis, vocab) || (e < vocab && vocab - e >= 8)) store8<TYPE>(to, 0, v);
                 else
 #pragma unroll
                     for (uint32_t x = 0; x < 8; ++x)
-                        if (e + x < vocab) store1<TYPE>(to + threadIdx.x * GROUP, x, v[x]);
+                        if (e + x < vocab) store1<TYPE>(to, x, v[x]);
             }
         }
     }
@@ -247,10 +252,16 @@ __device__ __forceinline__ float cross_terms(const DistillArgs& a, const uint32_
     return sum;
 }
 
+// Waves of a SIMD that the registers allow: the row's own and about 28 more.
+template <uint32_t TYPE>
+constexpr uint32_t distill_waves(uint32_t nv) {
+    const uint32_t waves = 512 / ((TYPE == TYPE_F32 ? 8 : 4) * nv + 28);
+    return waves > 8 ? 8 : waves;
+}
 // A row by one workgroup, held in registers between the softmax's sums and the gradient: read once, written once.  The first wave reads the entries while
 // the row comes.
 template <uint32_t TYPE, uint32_t NT, uint32_t NV, bool GRAD>
-__global__ __launch_bounds__(NT, TYPE == TYPE_F32 && NV == 8 ? 4 : 8) void k_distill_row(DistillArgs a) {
+__global__ __launch_bounds__(NT, distill_waves<TYPE>(NV)) void k_distill_row(DistillArgs a) {
     extern __shared__ uint32_t s_dyn[];
     __shared__ Softmax s_wave[NT / 64];
     __shared__ uint32_t s_any;
@@ -271,7 +282,7 @@ __global__ __launch_bounds__(NT, TYPE == TYPE_F32 && NV == 8 ? 4 : 8) void k_dis
             if (threadIdx.x == 0) s_any = any;
         }
         z.mask(0, mis, a.vocab);
-        q = join_block<NT>(z.softmax(a.c), a.c, s_wave);
+        q = join_block<NT>(z.softmax(0, mis, a.vocab, a.c), a.c, s_wave);
         if (NT == 64) wave_sync_lds();
         live = s_any && q.s != 0.f;
     }
@@ -309,7 +320,7 @@ __global__ __launch_bounds__(CHUNK_NT) void k_distill_part(DistillArgs a) {
     Groups<TYPE, CHUNK_NT, CHUNK_NV> z;
     z.load(a.z, row * a.ld, j0, mis, a.vocab);
     z.mask(j0, mis, a.vocab);
-    const Softmax q = join_block<CHUNK_NT>(z.softmax(a.c), a.c, room);
+    const Softmax q = join_block<CHUNK_NT>(z.softmax(j0, mis, a.vocab, a.c), a.c, room);
     if (threadIdx.x == 0) {
         a.parts[2 * (row * a.chunks + chunk)] = q.m;
         a.parts[2 * (row * a.chunks + chunk) + 1] = q.s;
