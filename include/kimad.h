@@ -445,7 +445,7 @@ int kimad_mx4_server_apply(const kimad_mx4_update_t* updates, float* const* u_ha
  *   loss        DEVICE float[rows] or NULL
  *   stats       DEVICE float[2 * rows] or NULL: the largest logit, and the sum of exp((z - largest) / T)
  *   grad        DEVICE [rows, vocab] of `type`, rows ld_grad >= vocab elements apart, or NULL; may be logits itself with ld_grad = ld
- *   workspace   DEVICE, 4-byte aligned, kimad_distill_workspace_bytes(rows, vocab, k) bytes (0 for most sizes: NULL will do).  As for
+ *   workspace   DEVICE, 4-byte aligned, kimad_distill_workspace_bytes(rows, vocab, k) bytes (0 up to 65529 columns: NULL will do).  As for
  *               kimad_mx4_matmul, but a smaller one is refused (KIMAD_ERR_WORKSPACE_TOO_SMALL).
  * At least one of loss, stats and grad is wanted.  Logits of -Inf are masked: q is 0 there, and so is the gradient; an entry with p > 0
  * there makes the loss +Inf.  A row that leaves nothing (weight 0, no entry above -Inf, or no logit above -Inf) has loss,

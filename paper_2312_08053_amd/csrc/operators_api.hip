@@ -53,10 +53,11 @@ inline uint32_t update_grid(uint64_t words, uint64_t& share) {
 
 namespace {
 
-// Few long rows are shared out over the compute units, and rows that no workgroup's registers hold.
-constexpr uint64_t DISTILL_ROW_MOST = 65536 - 7;         // elements of a row that k_distill_row holds (a group more where it begins off a 16-byte address)
+// Rows that no workgroup's registers hold go by chunks, in two launches.  (Shorter ones do not, however few they are: one row of 9000 elements 11 us by chunks
+// and 7 whole, of 32000 10 and 9.6, of 50257 10.4 and 11.9, the loss alone 9.1 and 6.6 to 8.2; 64 rows of 32000 12 and 10.5, of 50257 13.5 and 13.2.)
+constexpr uint64_t DISTILL_ROW_MOST = 65536 - 7;         // (a row that begins off a 16-byte address takes a group more)
 inline uint32_t distill_chunks(uint64_t vocab) { return (uint32_t)((vocab + 7 + 8 * DISTILL_CHUNK - 1) / (8 * DISTILL_CHUNK)); }
-inline bool distill_split(uint64_t rows, uint64_t vocab) { return vocab > DISTILL_ROW_MOST || (vocab > 8192 && rows < 128); }
+inline bool distill_by_chunks(uint64_t vocab) { return vocab > DISTILL_ROW_MOST; }
 
 int distill_args(DistillArgs& a, const void* logits, uint32_t type, uint64_t rows, uint64_t vocab, uint64_t ld, const uint32_t* t_idx,
                  const float* t_val, uint32_t k, float temperature, const float* row_weight, const void* grad, uint64_t ld_grad) {
@@ -282,7 +283,7 @@ int kimad_mx4_server_apply(const kimad_mx4_update_t* updates, float* const* u_ha
 }
 
 uint64_t kimad_distill_workspace_bytes(uint64_t rows, uint64_t vocab, uint32_t k) {
-    return distill_split(rows, vocab) ? 4 * rows * (2ull * distill_chunks(vocab) + k) : 0;
+    return distill_by_chunks(vocab) ? 4 * rows * (2ull * distill_chunks(vocab) + k) : 0;
 }
 
 int kimad_distill(const void* logits, uint32_t type, uint64_t rows, uint64_t vocab, uint64_t ld, const uint32_t* t_idx,
