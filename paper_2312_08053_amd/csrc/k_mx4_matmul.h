@@ -18,6 +18,7 @@ struct MatmulArgs {
     const uint32_t *sa, *sb;     // scale words
     void* out;
     uint64_t M, N, W, ld;        // W words a row
+    uint64_t scale_rows;         // rows of the matrix that A's M rows are of: from word to word of A's scales
     uint32_t tiles_m, tiles_n;
     uint32_t splits, share;      // parts of the sum, `share` stages each (the last one fewer); more than one: part p goes to out + p M ld
 };
@@ -122,7 +123,7 @@ __global__ __launch_bounds__(64 * T::WAVES, 2) void k_mx4_matmul_tile(MatmulArgs
             const uint32_t half = (i * T::WAVES + wave) % T::GROUPS % (T::GROUPS / 2);   // of 64 rows' scale words: A's, B's, then those of a second word
             const bool of_a = half < BM / 64;
             const uint64_t first = (of_a ? m0 : n0) + 64 * (of_a ? half : half - BM / 64), rows = none ? 0 : of_a ? g.M : g.N;
-            sbase[i] = (of_a ? g.sa : g.sb) + first + (2 * stage_in + (i * T::WAVES + wave) % T::GROUPS / (T::GROUPS / 2)) * (of_a ? g.M : g.N);
+            sbase[i] = (of_a ? g.sa : g.sb) + first + (2 * stage_in + (i * T::WAVES + wave) % T::GROUPS / (T::GROUPS / 2)) * (of_a ? g.scale_rows : g.N);
             sbytes[i] = first < rows ? (uint32_t)(rows - first < 64 ? rows - first : 64) * 4u : 0u;
         }
     };
@@ -141,7 +142,7 @@ __global__ __launch_bounds__(64 * T::WAVES, 2) void k_mx4_matmul_tile(MatmulArgs
 #pragma unroll
         for (uint32_t i = 0; i < T::SLOADS; ++i) {
             const uint32_t group = (i * T::WAVES + wave) % T::GROUPS;
-            const uint64_t rows = group % (T::GROUPS / 2) < BM / 64 ? g.M : g.N;
+            const uint64_t rows = group % (T::GROUPS / 2) < BM / 64 ? g.scale_rows : g.N;
             load_lds4(buffer_of(one && group >= T::GROUPS / 2 ? sbase[i] - rows : sbase[i], sbytes[i]), 4 * lane, stage + T::CODES + group * 256u);
             sbase[i] += 2 * rows;
         }
@@ -334,7 +335,7 @@ __global__ __launch_bounds__(256) void k_mx4_matmul_few(MatmulArgs g) {
 #pragma unroll
             for (uint32_t t = 0; t < MT; ++t) {
                 va[u][t] = a[t][(w + u) * 4];
-                sa[u][t] = g.sa[(w + u) * g.M + m[t]];
+                sa[u][t] = g.sa[(w + u) * g.scale_rows + m[t]];
             }
         }
 #pragma unroll

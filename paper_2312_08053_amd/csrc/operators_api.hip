@@ -99,6 +99,7 @@ struct MatmulPlan {
     enum { FEW, T64, T128, T256 } kind;
     uint64_t tiles_m, tiles_n;
     uint32_t splits, share;
+    double us;
 };
 MatmulPlan matmul_plan(uint64_t M, uint64_t N, uint64_t W, bool may_split) {
     MatmulPlan best{};
@@ -107,11 +108,11 @@ MatmulPlan matmul_plan(uint64_t M, uint64_t N, uint64_t W, bool may_split) {
     best.share = (uint32_t)stages;
     if (M <= FEW_ROWS) {
         best.kind = MatmulPlan::FEW;
+        best.us = 3.0 + (double)N * (double)W * 68.0 / 4e6;                   // B's codes and scales at 4 TB/s
         return best;
     }
     struct { decltype(best.kind) kind; uint64_t edge; double stage, tile, launch; } const kinds[] = {
         {MatmulPlan::T256, 256, 2.2, 6.0, 5.0}, {MatmulPlan::T128, 128, 0.8, 1.8, 4.0}, {MatmulPlan::T64, 64, 0.3, 0.5, 3.0}};
-    double least = 0;
     for (const auto& k : kinds) {
         const uint64_t tm = (M + k.edge - 1) / k.edge, tn = (N + k.edge - 1) / k.edge;
         for (uint64_t splits = 1; splits == 1 || (may_split && splits <= 16 && 4 * splits <= stages && tm * tn * splits <= 4 * UNITS); splits *= 2) {
@@ -119,14 +120,25 @@ MatmulPlan matmul_plan(uint64_t M, uint64_t N, uint64_t W, bool may_split) {
             const double c = (double)((tm * tn * parts + UNITS - 1) / UNITS);
             double us = c * ((double)share * k.stage + k.tile) + k.launch;
             if (parts > 1) us += 4.0 + (double)(parts * M * N) * 8.0 / 4e6;     // 4 bytes written and read, at 4 TB/s
-            if (least == 0 || us < least) {
-                least = us;
+            if (best.us == 0 || us < best.us) {
+                best.us = us;
                 best.kind = k.kind; best.tiles_m = tm; best.tiles_n = tn;
                 best.splits = (uint32_t)parts; best.share = (uint32_t)share;
             }
         }
     }
     return best;
+}
+// Tiles of 256 rows that leave most compute units without work in their last round: so many of A's rows make whole rounds, the rest goes by a second launch,
+// if both together are expected to take less (50257 x 768 x 8192, 591 tiles on 256 units: 222 and 193 us).  0: one launch.
+inline uint64_t matmul_first_rows(const MatmulPlan& p, uint64_t M, uint64_t N, uint64_t W, MatmulPlan& rest) {
+    const uint64_t tiles = p.tiles_m * p.tiles_n, rounds = tiles / UNITS;
+    if (p.kind != MatmulPlan::T256 || p.splits != 1 || rounds == 0) return 0;
+    const uint64_t rows = rounds * UNITS / p.tiles_n * 256;
+    if (rows == 0 || rows >= M) return 0;
+    rest = matmul_plan(M - rows, N, W, false);
+    const double each = (p.us - 5.0) / (double)((tiles + UNITS - 1) / UNITS);
+    return (double)rounds * each + 5.0 + rest.us < p.us ? rows : 0;
 }
 inline uint64_t matmul_parts_bytes(const MatmulPlan& p, uint64_t M, uint64_t N) { return p.splits > 1 ? 4 * p.splits * M * N : 0; }
 
@@ -140,13 +152,6 @@ int launch_tile(MatmulArgs g, const MatmulPlan& p, hipStream_t s) {
     return launched();
 }
 
-template <uint32_t TYPE>
-int launch_kind(const MatmulArgs& g, const MatmulPlan& p, hipStream_t s) {
-    if (p.kind == MatmulPlan::T256) return launch_tile<TYPE, Tile256>(g, p, s);
-    if (p.kind == MatmulPlan::T128) return launch_tile<TYPE, Tile128>(g, p, s);
-    return launch_tile<TYPE, Tile64>(g, p, s);
-}
-
 // Sixteen rows of B by a wave where that makes a wave a SIMD and the sum is short, else by four (32000 rows, 16 words: 8.3 and 9.6 us; 16384 rows,
 // 128 words: 33.7 and 27.5).
 template <uint32_t TYPE, uint32_t MT>
@@ -154,6 +159,18 @@ int launch_few(const MatmulArgs& g, uint64_t groups, hipStream_t s) {
     if (groups >= 4 * UNITS && g.W <= 32) hipLaunchKernelGGL((k_mx4_matmul_few<TYPE, MT, false>), dim3((uint32_t)((groups + 3) / 4)), dim3(256), 0, s, g);
     else hipLaunchKernelGGL((k_mx4_matmul_few<TYPE, MT, true>), dim3((uint32_t)groups), dim3(256), 0, s, g);
     return launched();
+}
+
+template <uint32_t TYPE>
+int launch_kind(const MatmulArgs& g, const MatmulPlan& p, hipStream_t s) {
+    if (p.kind == MatmulPlan::FEW) {
+        const uint64_t groups = (g.N + 15) / 16;
+        if (groups > GRID_MOST) return KIMAD_ERR_INVALID_ARG;
+        return g.M <= 16 ? launch_few<TYPE, 1>(g, groups, s) : launch_few<TYPE, 2>(g, groups, s);
+    }
+    if (p.kind == MatmulPlan::T256) return launch_tile<TYPE, Tile256>(g, p, s);
+    if (p.kind == MatmulPlan::T128) return launch_tile<TYPE, Tile128>(g, p, s);
+    return launch_tile<TYPE, Tile64>(g, p, s);
 }
 
 }  // namespace
@@ -217,7 +234,7 @@ int kimad_mx4_matmul(const void* a_codes, const uint32_t* a_scales, uint64_t M, 
     g.a = static_cast<const uint8_t*>(a_codes); g.b = static_cast<const uint8_t*>(b_codes);
     MatmulPlan p = matmul_plan(M, N, words_of(K), true);
     if (matmul_parts_bytes(p, M, N) > (workspace ? workspace_bytes : 0)) p = matmul_plan(M, N, words_of(K), false);
-    g.sa = a_scales; g.sb = b_scales; g.out = out; g.M = M; g.N = N; g.W = words_of(K); g.ld = ld;
+    g.sa = a_scales; g.sb = b_scales; g.out = out; g.M = M; g.N = N; g.W = words_of(K); g.ld = ld; g.scale_rows = M;
     hipStream_t s = static_cast<hipStream_t>(stream);
     return with_type(type, [&](auto t) {
         constexpr uint32_t TYPE = decltype(t)::value;
@@ -226,11 +243,17 @@ int kimad_mx4_matmul(const void* a_codes, const uint32_t* a_scales, uint64_t M, 
             hipLaunchKernelGGL(k_mx4_matmul_none<TYPE>, dim3((uint32_t)((M * N + 255) / 256)), dim3(256), 0, s, out, M, N, ld);
             return launched();
         }
-        if (p.kind == MatmulPlan::FEW) {
-            const uint64_t groups = (N + 15) / 16;
-            if (groups > GRID_MOST) return (int)KIMAD_ERR_INVALID_ARG;
-            if (M <= 16) return launch_few<TYPE, 1>(g, groups, s);
-            return launch_few<TYPE, 2>(g, groups, s);
+        MatmulPlan rest{};
+        if (const uint64_t rows = matmul_first_rows(p, M, N, g.W, rest)) {
+            MatmulArgs first = g;
+            first.M = rows;
+            MatmulPlan fp = p;
+            fp.tiles_m = rows / 256;
+            const int rc = launch_kind<TYPE>(first, fp, s);
+            if (rc) return rc;
+            g.a += rows * g.W * 64; g.sa += rows; g.M = M - rows;
+            g.out = static_cast<uint8_t*>(out) + rows * ld * type_bytes(type);
+            return launch_kind<TYPE>(g, rest, s);
         }
         if (p.splits == 1) return launch_kind<TYPE>(g, p, s);
         g.out = workspace; g.ld = N;
