@@ -10,7 +10,8 @@ constexpr uint32_t QU = 4;                   // words of a lane under way togeth
 
 // Along rows: a workgroup takes 16 rows of up to 64 words.  Its sixteen groups of sixteen lanes walk row by row through the share, so
 // that reads and codes run on without gaps; the scale words, whose neighbours in memory are other rows' words, are collected in LDS
-// and leave in runs of 16.  Bound by memory.
+// and leave in runs of 16.  Bound by memory: 50257 x 768
+// in fp32 40 us, 4.4 TB/s, 8192 x 2048 in bfloat16 9.7 us.  (Shares of 4, 8, 16 and 64 words, 256 x 2048: 3.0, 5.4, 6.8 and 6.8 us; 8192 x 2048: 11.2, 9.7, 10.0, 10.0.)
 template <uint32_t TYPE>
 __global__ __launch_bounds__(256) void k_mx4_quantise_rows(const void* __restrict__ x, uint64_t rows, uint64_t cols, uint64_t ld,
                                                            uint64_t W, uint32_t* __restrict__ codes, uint32_t* __restrict__ scales) {
@@ -49,7 +50,7 @@ __global__ __launch_bounds__(256) void k_mx4_quantise_rows(const void* __restric
 
 // Along columns, and along rows from the same read where `codes` is given: a workgroup holds a tile of 128 by 128 in LDS.  Behind every 32
 // rows sixteen words are left out: a wave then reads sixteen columns of four blocks of rows from 64 different banks, and
-// writes the 64 bytes of a column's word side by side.
+// writes the 64 bytes of a column's word side by side.  Bound by memory: 50257 x 768 in fp32, both ways, 48 us, 4.1 TB/s.
 constexpr uint32_t QT_PITCH = 128;
 template <uint32_t TYPE>
 __global__ __launch_bounds__(256) void k_mx4_quantise_both(const void* __restrict__ x, uint64_t rows, uint64_t cols, uint64_t ld, uint64_t W,
@@ -127,7 +128,7 @@ __global__ __launch_bounds__(256) void k_mx4_quantise_both(const void* __restric
     }
 }
 
-// Reading back: the same shares as along rows.
+// Reading back: the same shares as along rows.  Bound by memory: 50257 x 768 into bfloat16 16.7 us, 5.8 TB/s (30 us with one word of a lane under way).
 template <uint32_t TYPE>
 __global__ __launch_bounds__(256) void k_mx4_dequantise(const uint32_t* __restrict__ codes, const uint32_t* __restrict__ scales, uint64_t rows,
                                                         uint64_t cols, uint64_t W, void* __restrict__ out, uint64_t ld) {

@@ -220,7 +220,7 @@ __device__ __forceinline__ void server_words(const Mx4ServerArgs& a, LayerWalk a
 }
 
 // One pass over everything: the workers' words, their estimators read and written, and the model's step from the values at hand.  The sum in
-// fp64 in the workers' order, as in k_server_step.  Bound by memory.
+// fp64 in the workers' order, as in k_server_step.  Bound by memory: 124 M entries of one worker 422 us, of four 1094 (4.8 TB/s, off cache lines), on lines 987 for 120 M.
 __global__ __launch_bounds__(256) void k_mx4_server(Mx4ServerArgs a, int32_t* status_out, int32_t err) {
     __shared__ StartsRoom room;
     const bool fit = starts_fit(a.layer_start, a.L, a.d, room);
