@@ -383,18 +383,19 @@ uint64_t kimad_budget_bytes(double bandwidth_bits_per_s, double t_seconds, doubl
 
 /* Quantises x, [rows, cols] of `type` with consecutive rows ld >= cols elements apart: along rows into codes, scales (both may
  * be NULL), along columns into codes_t, scales_t (both may be NULL), which is the form of the transpose, a matrix of cols rows
- * and rows columns: a training step needs both, and one call reads x once. */
+ * and rows columns: a training step needs both, and one call reads x once.
+ * At most 67107840 columns, or 8388480 rows where columns are quantised (a grid's limits); more are refused. */
 int kimad_mx4_quantise(const void* x, uint32_t type, uint64_t rows, uint64_t cols, uint64_t ld, void* codes, uint32_t* scales,
                        void* codes_t, uint32_t* scales_t, void* stream);
 
 /* The values that a quantised matrix stands for, into out, [rows, cols] of `type` with rows ld >= cols elements apart.  Exact in F32
- * and BF16; in F16 rounded, and Inf beyond its range. */
+ * and BF16; in F16 rounded, and Inf beyond its range.  At most 67107840 columns. */
 int kimad_mx4_dequantise(const void* codes, const uint32_t* scales, uint64_t rows, uint64_t cols, void* out, uint32_t type,
                          uint64_t ld, void* stream);
 
 /* Product C = A B^T of quantised matrices, A of M rows and K columns, B of N rows and K columns: out [M, N] of `type` with rows
- * ld >= N elements apart.  Products are exact, sums are fp32, and the sum is rounded once to `type` (F16: Inf beyond its range).  K is at most 2^25.  The
- * forward product of a layer takes activations and weights quantised along their columns' axis; its gradients take the
+ * ld >= N elements apart.  Products are exact, sums are fp32, and the sum is rounded once to `type` (F16: Inf beyond its range).  K is at most 2^25 and
+ * ld at most 2^24: 32-bit offsets reach a few rows from where they begin.  The forward product of a layer takes activations and weights quantised along their columns' axis; its gradients take the
  * transposed forms (kimad_mx4_quantise).
  *   workspace  DEVICE, 16-byte aligned, kimad_mx4_matmul_workspace_bytes(M, N, K) bytes, or NULL: products with few rows and a long sum are
  *              then not shared out along the sum, and slower.  Its contents need not be kept between calls; calls that may

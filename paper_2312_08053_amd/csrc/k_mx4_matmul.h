@@ -252,14 +252,15 @@ __global__ __launch_bounds__(64 * T::WAVES, 2) void k_mx4_matmul_tile(MatmulArgs
         constexpr uint32_t BYTES = TYPE == TYPE_F32 ? 4 : 2, BEYOND = 0xFFFFFFF0u;
         uint32_t l;                                                           // the lane, found anew: kept through the loop, it would cost a register
         asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(l));
-        const uint32_t row = wm * (BM / WM) + 4 * (l >> 5) + (l & 3u), col = wn * (BN / WN) + (l & 28u), at = (row * (uint32_t)g.ld + col) * BYTES;
+        const uint32_t row = 4 * (l >> 5) + (l & 3u), col = wn * (BN / WN) + (l & 28u), at = (row * (uint32_t)g.ld + col) * BYTES;
         const uint32_t rows = g.M - tile_m < BM ? (uint32_t)(g.M - tile_m) : BM, cols = g.N - tile_n < BN ? (uint32_t)(g.N - tile_n) : BN;
         const bool odd = l & 1u, high = l & 2u;
         const bool whole = rows == BM && cols == BN;
         stores_behind = whole ? 1u : 0u;
 #pragma unroll
         for (uint32_t i = 0; i < T::TI; ++i) {
-            const __amdgpu_buffer_rsrc_t to = buffer_of(static_cast<uint8_t*>(g.out) + (((item / tiles) * g.M + tile_m + 32 * i) * g.ld + tile_n) * BYTES, 0xFFFFFF00u);
+            const uint32_t first = wm * (BM / WM) + 32 * i;                   // the store's rows begin here: the lanes' offsets are those of 32 rows, below 2^32
+            const __amdgpu_buffer_rsrc_t to = buffer_of(static_cast<uint8_t*>(g.out) + (((item / tiles) * g.M + tile_m + first) * g.ld + tile_n) * BYTES, 0xFFFFFF00u);
 #pragma unroll
             for (uint32_t j = 0; j < T::TJ; ++j)
 #pragma unroll
@@ -276,7 +277,7 @@ __global__ __launch_bounds__(64 * T::WAVES, 2) void k_mx4_matmul_tile(MatmulArgs
                         } else {
 #pragma unroll
                             for (uint32_t k = 0; k < 4; ++k)
-                                __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(r[k]), to, row + 32 * i + 8 * e < rows && col + 32 * j + k < cols ? o + 4 * k : BEYOND, 0, 0);
+                                __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(r[k]), to, first + row + 8 * e < rows && col + 32 * j + k < cols ? o + 4 * k : BEYOND, 0, 0);
                         }
                     } else {
                         uint32_t r[2];
@@ -286,7 +287,7 @@ __global__ __launch_bounds__(64 * T::WAVES, 2) void k_mx4_matmul_tile(MatmulArgs
                         } else {
 #pragma unroll
                             for (uint32_t k = 0; k < 4; ++k)
-                                __builtin_amdgcn_raw_buffer_store_b16((uint16_t)(r[k / 2] >> (16 * (k % 2))), to, row + 32 * i + 8 * e < rows && col + 32 * j + k < cols ? o + 2 * k : BEYOND, 0, 0);
+                                __builtin_amdgcn_raw_buffer_store_b16((uint16_t)(r[k / 2] >> (16 * (k % 2))), to, first + row + 8 * e < rows && col + 32 * j + k < cols ? o + 2 * k : BEYOND, 0, 0);
                         }
                     }
                 }

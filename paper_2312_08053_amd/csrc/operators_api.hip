@@ -22,7 +22,7 @@ static_assert(UPDATE_MAX_WORKERS == KIMAD_MAX_WORKERS, "header and kernel consta
 constexpr uint64_t MOST = 1ull << 40;                    // elements along an axis that the checks below let through
 constexpr uint64_t FEW_ROWS = 32;                        // products of so many rows go by k_mx4_matmul_few
 constexpr uint64_t UNITS = 256;                         // compute units of the device
-constexpr uint64_t MATMUL_MOST_K = 1ull << 25, MATMUL_MOST_LD = 1ull << 24;     // eight rows of codes and a tile's rows of the result are reached by 32-bit offsets
+constexpr uint64_t MATMUL_MOST_K = 1ull << 25, MATMUL_MOST_LD = 1ull << 24;     // eight rows of codes and 32 rows of the result are reached by 32-bit offsets
 constexpr uint64_t GRID_MOST = 0x7FFFFFFFull, GRID_Y_MOST = 65535;
 
 inline bool aligned(const void* p, uintptr_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }

@@ -87,6 +87,27 @@ def test_product_of_codes_beyond_four_gibibytes():
     assert torch.equal(few, out[-3:].t())
 
 
+@pytest.mark.parametrize("M, N, K", [(256, 65536, 256), (250, 65500, 256), (200, 20000, 128), (100, 1000, 1024)])
+def test_product_into_rows_far_apart(M, N, K):
+    import torch
+    kimad = _kimad()
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    a, sa = kimad.mx4_empty(M, K)
+    b, sb = kimad.mx4_empty(N, K)
+    kimad.kimad_mx4_quantise(torch.randn(M, K, generator=gen, device="cuda"), a, sa)
+    kimad.kimad_mx4_quantise(torch.randn(N, K, generator=gen, device="cuda"), b, sb)
+    for dtype in (torch.float32, torch.bfloat16):
+        near = torch.empty(M, N, dtype=dtype, device="cuda")
+        kimad.kimad_mx4_matmul(a, sa, b, sb, K, near)
+        ld = 1 << 24                                                # 256 rows: 17 GB in 32 bits
+        buf = torch.full((M * ld,), -77.0, dtype=dtype, device="cuda")
+        far = torch.as_strided(buf, (M, N), (ld, 1))
+        kimad.kimad_mx4_matmul(a, sa, b, sb, K, far)
+        assert torch.equal(far, near)                               # (the same sums in the same order)
+        assert bool((buf.view(M, ld)[:, N:] == -77.0).all())
+        del buf, far
+
+
 def test_update_of_more_than_two_to_the_thirty_entries():
     import torch
     kimad = _kimad()
