@@ -162,6 +162,17 @@ def _stream(stream) -> int:
     return _raw_stream()
 
 
+def _scratch(nbytes: int, device, stream):
+    """Device memory for one call on `stream`.  It comes from that stream's own pool: memory of another stream's would go
+    to that stream's next allocation as soon as the call returns, with the kernels still to run."""
+    import torch
+    handle = _stream(stream)
+    if handle == _stream(None):
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    with torch.cuda.stream(torch.cuda.ExternalStream(handle, device=device) if handle else torch.cuda.default_stream(device)):
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
 def kimad_workspace_bytes(sizes: Sequence[int], J: int, pair_bytes=8, D=0, max_budget_bytes=0,
                           cfg_flags=0, max_workgroups=0, value_format=0) -> int:
     n = (C.c_uint64 * len(sizes))(*[int(s) for s in sizes])
@@ -361,8 +372,7 @@ def kimad_mx4_matmul(a_codes, a_scales, b_codes, b_scales, K: int, out, workspac
     if workspace is None:
         nbytes = L.kimad_mx4_matmul_workspace_bytes(M, N, K)
         if nbytes:
-            import torch
-            workspace = torch.empty(nbytes, dtype=torch.uint8, device=out.device)
+            workspace = _scratch(nbytes, out.device, stream)
     if workspace is not None:
         ws, nbytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     _check(L.kimad_mx4_matmul(a, sa, M, b, sb, N, K, out.data_ptr(), _type(out), ld, ws, nbytes, _stream(stream)), "kimad_mx4_matmul")
@@ -431,8 +441,7 @@ def kimad_distill(logits, t_idx, t_val, temperature: float, loss=None, stats=Non
     if workspace is None:
         nbytes = L.kimad_distill_workspace_bytes(rows, vocab, k)
         if nbytes:
-            import torch
-            workspace = torch.empty(nbytes, dtype=torch.uint8, device=logits.device)
+            workspace = _scratch(nbytes, logits.device, stream)
     if workspace is not None:
         ws, nbytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     _check(L.kimad_distill(*lead, temperature, weight, 0 if loss is None else _holds(loss, rows, 4, "loss"),

@@ -259,3 +259,29 @@ def test_again_and_on_another_stream_and_in_a_graph():
             work()
             torch.cuda.synchronize()
             assert torch.equal(loss, got[0]) and torch.equal(grad, got[1])
+
+
+def test_workspace_that_the_call_makes_stays_its_own_on_a_given_stream():
+    import torch
+    kimad = _kimad()
+    rows, vocab = 2, 70001
+    zd, idx, t, w = _inputs(rows, vocab, 20, "float32", 9)
+    idx_d, t_d = torch.from_numpy(idx.astype(np.int32)).cuda(), torch.from_numpy(t).cuda()
+    nbytes = kimad.kimad_distill_workspace_bytes(rows, vocab, 20)
+    assert nbytes > 0
+    want, loss = torch.empty(rows, device="cuda"), torch.zeros(rows, device="cuda")
+    kimad.kimad_distill(zd, idx_d, t_d, 1.0, loss=want)
+    big = torch.randn(4096, 4096, device="cuda")
+    for handle in (False, True):
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            for _ in range(20):
+                busy = big @ big                                     # some milliseconds in front of the call
+        kimad.kimad_distill(zd, idx_d, t_d, 1.0, loss=loss, stream=side.cuda_stream if handle else side)
+        others = [torch.full((nbytes,), 255, dtype=torch.uint8, device="cuda") for _ in range(8)]
+        torch.cuda.synchronize()
+        assert torch.equal(loss, want)
+        loss.zero_()
+        torch.cuda.synchronize()
+        del others, busy

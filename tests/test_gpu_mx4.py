@@ -323,3 +323,30 @@ def test_product_on_another_stream_and_in_a_graph():
         x.mul_(2.0)
         graph.replay()
         assert np.array_equal(_host(out), want * 2.0 ** (turn + 1))
+
+
+def test_workspace_that_the_product_makes_stays_its_own_on_a_given_stream():
+    import torch
+    kimad = _kimad()
+    M, N, K = 100, 90, 16384
+    forms = [kimad.mx4_empty(M, K), kimad.mx4_empty(N, K)]
+    kimad.kimad_mx4_quantise(_matrix(M, K, "bfloat16", 1), *forms[0])
+    kimad.kimad_mx4_quantise(_matrix(N, K, "bfloat16", 2), *forms[1])
+    nbytes = kimad.kimad_mx4_matmul_workspace_bytes(M, N, K)
+    assert nbytes > 0
+    want, out = torch.empty(M, N, device="cuda"), torch.zeros(M, N, device="cuda")
+    kimad.kimad_mx4_matmul(*forms[0], *forms[1], K, want)
+    big = torch.randn(4096, 4096, device="cuda")
+    for handle in (False, True):
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            for _ in range(20):
+                busy = big @ big                                     # some milliseconds in front of the call
+        kimad.kimad_mx4_matmul(*forms[0], *forms[1], K, out, stream=side.cuda_stream if handle else side)
+        others = [torch.full((nbytes,), 255, dtype=torch.uint8, device="cuda") for _ in range(8)]
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+        out.zero_()
+        torch.cuda.synchronize()
+        del others, busy
