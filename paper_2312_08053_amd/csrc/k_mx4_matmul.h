@@ -50,24 +50,6 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) {
     return (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const void*)p);
 }
 
-// Four rows of one column in every lane of four neighbours -> four columns of one row: lane q of the four gets row q.  Two exchanges, of neighbours and of pairs.
-__device__ __forceinline__ void turn_quad(float v0, float v1, float v2, float v3, bool odd, bool high, float out[4]) {
-    auto swap1 = [](float x) { return __uint_as_float(dpp_u32<DPP_XOR1>(__float_as_uint(x))); };
-    auto swap2 = [](float x) { return __uint_as_float(dpp_u32<DPP_XOR2>(__float_as_uint(x))); };
-    const float r0 = swap1(odd ? v0 : v1), r1 = swap1(odd ? v2 : v3);
-    const float a0 = odd ? r0 : v0, a1 = odd ? v1 : r0, b0 = odd ? r1 : v2, b1 = odd ? v3 : r1;
-    const float s0 = swap2(high ? a0 : b0), s1 = swap2(high ? a1 : b1);
-    out[0] = high ? s0 : a0; out[1] = high ? s1 : a1; out[2] = high ? b0 : s0; out[3] = high ? b1 : s1;
-}
-// The same on pairs of 16-bit values: v01 holds rows 0 and 1, v23 rows 2 and 3.
-__device__ __forceinline__ void turn_quad16(uint32_t v01, uint32_t v23, bool odd, bool high, uint32_t out[2]) {
-    const uint32_t pick = odd ? 0x03020706u : 0x05040100u;                    // even: own low, other's low; odd: other's high, own high
-    const uint32_t a = __builtin_amdgcn_perm(dpp_u32<DPP_XOR1>(v01), v01, pick), b = __builtin_amdgcn_perm(dpp_u32<DPP_XOR1>(v23), v23, pick);
-    const uint32_t s = dpp_u32<DPP_XOR2>(high ? a : b);
-    out[0] = high ? s : a;
-    out[1] = high ? b : s;
-}
-
 // Tile number -> tile.  Workgroups go to the eight XCDs in turn; an XCD takes a run of tiles, in bands of eight rows of tiles, so that what its
 // compute units read at a time stays in its L2.
 __device__ __forceinline__ void tile_of(uint32_t id, uint32_t tm, uint32_t tn, uint32_t& m, uint32_t& n) {
@@ -89,7 +71,9 @@ struct MatmulTile {
     static constexpr uint32_t BM = BM_, BN = BN_, WM = WM_, WN = WN_;
     static constexpr uint32_t WAVES = WM * WN, TI = BM / WM / 32, TJ = BN / WN / 32;
     static constexpr uint32_t LOADS = (BM + BN) / 8 / WAVES, GROUPS = (BM + BN) / 32, SLOADS = (GROUPS + WAVES - 1) / WAVES;
-    static constexpr uint32_t CODES = (BM + BN) * 128, STAGE = CODES + (BM + BN) * 8, LDS = 2 * STAGE;
+    static constexpr uint32_t CODES = (BM + BN) * 128, STAGE = CODES + (BM + BN) * 8;
+    static constexpr uint32_t COLS = 32 * TJ, PITCH = COLS + 8;               // of a wave's rows on their way out: 4 rows further, 32 banks further
+    static constexpr uint32_t OUT = 8 * PITCH * 4, LDS = 2 * STAGE + WAVES * OUT;
 };
 
 template <uint32_t TYPE, class T>
@@ -209,7 +193,7 @@ __global__ __launch_bounds__(64 * T::WAVES, 2) void k_mx4_matmul_tile(MatmulArgs
     // The reads of one half are under way while the other is multiplied, across stages and items too: the barrier in front of a stage's last half waits for
     // the next stage, whose first half is then read, and behind it this stage is no longer read and its buffer takes the one after the next.  A
     // tile is stored while the next item's first stage comes; the next barrier lets these stores be.
-    constexpr uint32_t STORES = 4 * T::TI * T::TJ;
+    constexpr uint32_t STORES = 4 * T::TI * (TYPE == TYPE_F32 ? T::TJ : 1);
     bring(0, 1);
     brought();
     bring(0, 1);
@@ -248,51 +232,61 @@ __global__ __launch_bounds__(64 * T::WAVES, 2) void k_mx4_matmul_tile(MatmulArgs
         uint32_t tm, tn;
         tile_of(item % tiles, g.tiles_m, g.tiles_n, tm, tn);
         const uint64_t tile_m = (uint64_t)tm * BM, tile_n = (uint64_t)tn * BN;
-        // four columns of a row in every lane, eight rows a store
-        constexpr uint32_t BYTES = TYPE == TYPE_F32 ? 4 : 2, BEYOND = 0xFFFFFFF0u;
+        // Eight rows at a time through LDS, so that stores run along the rows: 16 bytes a lane, whole cache lines.  (Four columns a lane by lane exchanges, whose
+        // neighbours stored to four rows, took 75 us for 8192 x 5632 x 2048 in 16 bits, and this 61; 85 and 44 for 1000 x 50257 x 768.)
+        constexpr uint32_t BYTES = TYPE == TYPE_F32 ? 4 : 2, BEYOND = 0xFFFFFFF0u, EACH = 16 / BYTES, LANES = T::COLS / EACH;   // elements of a lane, lanes of a row
+        constexpr uint32_t PASSES = 8 * LANES > 64 ? 8 * LANES / 64 : 1, PASS_ROWS = 8 / PASSES;
         uint32_t l;                                                           // the lane, found anew: kept through the loop, it would cost a register
         asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(l));
-        const uint32_t row = 4 * (l >> 5) + (l & 3u), col = wn * (BN / WN) + (l & 28u), at = (row * (uint32_t)g.ld + col) * BYTES;
+        float* mine = reinterpret_cast<float*>(s_mem + 2 * T::STAGE + wave * T::OUT);
         const uint32_t rows = g.M - tile_m < BM ? (uint32_t)(g.M - tile_m) : BM, cols = g.N - tile_n < BN ? (uint32_t)(g.N - tile_n) : BN;
-        const bool odd = l & 1u, high = l & 2u;
-        const bool whole = rows == BM && cols == BN;
-        stores_behind = whole ? 1u : 0u;
+        const bool cut = cols % EACH != 0;                                    // some lanes have elements on both sides of the last column
+        const uint32_t row = l / LANES, col = EACH * (l % LANES), wcol = wn * T::COLS + col, at = (row * (uint32_t)g.ld + wcol) * BYTES;
 #pragma unroll
         for (uint32_t i = 0; i < T::TI; ++i) {
             const uint32_t first = wm * (BM / WM) + 32 * i;                   // the store's rows begin here: the lanes' offsets are those of 32 rows, below 2^32
             const __amdgpu_buffer_rsrc_t to = buffer_of(static_cast<uint8_t*>(g.out) + (((item / tiles) * g.M + tile_m + first) * g.ld + tile_n) * BYTES, 0xFFFFFF00u);
 #pragma unroll
-            for (uint32_t j = 0; j < T::TJ; ++j)
+            for (uint32_t e = 0; e < 4; ++e) {
 #pragma unroll
-                for (uint32_t e = 0; e < 4; ++e) {
+                for (uint32_t j = 0; j < T::TJ; ++j) {
                     const f32x16 v = acc[i][j];
+#pragma unroll
+                    for (uint32_t k = 0; k < 4; ++k) mine[(4 * (l >> 5) + k) * T::PITCH + 32 * j + (l & 31u)] = v[4 * e + k];
+                }
+                wave_sync_lds();
+                f32x4 v[PASSES][EACH / 4];
+#pragma unroll
+                for (uint32_t p = 0; p < PASSES; ++p)
+#pragma unroll
+                    for (uint32_t q = 0; q < EACH / 4; ++q) v[p][q] = *reinterpret_cast<const f32x4*>(mine + ((p * PASS_ROWS + row) & 7u) * T::PITCH + col + 4 * q);
+                wave_sync_lds();
+#pragma unroll
+                for (uint32_t p = 0; p < PASSES; ++p) {
                     // (the whole offset in the lane's register: a 16-byte store with a scalar offset as well has stored values that the next instructions
                     // wrote into its data registers, in rows with such an offset and in no others)
-                    const uint32_t o = at + (32 * j + 8 * e * (uint32_t)g.ld) * BYTES;
-                    if (TYPE == TYPE_F32) {
-                        float r[4];
-                        turn_quad(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3], odd, high, r);
-                        if (whole) {
-                            __builtin_amdgcn_raw_buffer_store_b128(u32x4{__float_as_uint(r[0]), __float_as_uint(r[1]), __float_as_uint(r[2]), __float_as_uint(r[3])}, to, o, 0, 0);
-                        } else {
+                    const uint32_t r = 8 * e + p * PASS_ROWS, o = at + r * (uint32_t)g.ld * BYTES;
+                    u32x4 out;
 #pragma unroll
-                            for (uint32_t k = 0; k < 4; ++k)
-                                __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(r[k]), to, first + row + 8 * e < rows && col + 32 * j + k < cols ? o + 4 * k : BEYOND, 0, 0);
-                        }
-                    } else {
-                        uint32_t r[2];
-                        turn_quad16(pack2<TYPE>(v[4 * e], v[4 * e + 1]), pack2<TYPE>(v[4 * e + 2], v[4 * e + 3]), odd, high, r);
-                        if (whole) {
-                            __builtin_amdgcn_raw_buffer_store_b64(u32x2{r[0], r[1]}, to, o, 0, 0);
-                        } else {
+                    for (uint32_t k = 0; k < 4; ++k) {
+                        if (TYPE == TYPE_F32) out[k] = __float_as_uint(v[p][0][k]);
+                        else out[k] = pack2<TYPE>(v[p][(k / 2) % (EACH / 4)][2 * k % 4], v[p][(k / 2) % (EACH / 4)][2 * k % 4 + 1]);
+                    }
+                    const bool in = (PASSES > 1 || row < 8) && first + r + row < rows;
+                    __builtin_amdgcn_raw_buffer_store_b128(out, to, in && wcol + EACH <= cols ? o : BEYOND, 0, 0);
+                    if (cut && in && wcol < cols && wcol + EACH > cols) {
 #pragma unroll
-                            for (uint32_t k = 0; k < 4; ++k)
-                                __builtin_amdgcn_raw_buffer_store_b16((uint16_t)(r[k / 2] >> (16 * (k % 2))), to, first + row + 8 * e < rows && col + 32 * j + k < cols ? o + 2 * k : BEYOND, 0, 0);
+                        for (uint32_t k = 0; k < EACH; ++k) {
+                            const uint32_t ok = wcol + k < cols ? o + k * BYTES : BEYOND;
+                            if (TYPE == TYPE_F32) __builtin_amdgcn_raw_buffer_store_b32(out[k % 4], to, ok, 0, 0);
+                            else __builtin_amdgcn_raw_buffer_store_b16((uint16_t)(out[k / 2] >> (16 * (k % 2))), to, ok, 0, 0);
                         }
                     }
                 }
+            }
         }
-        if (!whole) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");          // (so many more stores that the counter would not tell)
+        stores_behind = cut ? 0u : 1u;
+        if (cut) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");          // (so many more stores that the counter would not tell)
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                          // no load may reach LDS that is another workgroup's by then
 }
