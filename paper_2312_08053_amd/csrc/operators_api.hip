@@ -85,23 +85,24 @@ typedef MatmulTile<128, 128, 2, 2> Tile128;
 typedef MatmulTile<64, 64, 2, 2> Tile64;
 
 // How a product is shared out: by the least of the times below, which are fits (us) to measurements of each tile alone on products of 256 to 50257 rows, 768 to
-// 32000 columns and 6 to 128 words, good to a fifth.  c: tiles for the busiest compute unit, of `stages` stages (pairs of words) each.
-//   M      N      K        256 fit, measured   128              64               (rest: what a tile's beginning and end cost)
-//   512    2048   2048     29  23              12  12           6   7
-//   1024   2048   2048     29  24              12  12           9   9
-//   1024   4096   4096     46  35              19  19           24  21
-//   4096   768    16384    152 99              57  52           62  48
-//   2048   5632   2048     29  29              29  26           35  30
-//   8192   5632   2048     76  78              94  83           131 112
-//   50257  768    8192     234 232             278 268          ..  353
-// With few tiles and long sums the stages are shared out as well, and the parts added by a second launch.
+// 50257 columns and 6 to 128 words, most of them good to a tenth: rounds of as many tiles as compute units, of `stages` stages (pairs of words) each, and a last
+// one that costs less the fewer units it fills.  Measured, and in the end here, into 32 bits (into 16):
+//   M      N      K        256            128            64             here
+//   512    2048   2048     20  (19)       11  (11)       7.1 (7.1)      7.1 (7.0)
+//   1024   4096   4096     31  (30)       20  (18)       21  (20)       19  (17)
+//   4096   768    16384    91  (91)       51  (50)       48  (48)       49  (48)
+//   2048   5632   2048     24  (23)       32  (23)       28  (28)       25  (22)
+//   8192   5632   2048     73  (62)       75  (69)       102 (100)      72  (62)
+//   50257  768    8192     195 (182)      222 (205)      309 (296)      195 (182)
+//   1000   50257  768      55  (44)       51  (43)       65  (63)       48  (43)
+// With few tiles and long sums the stages are shared out as well, and the parts, which are of 32 bits, added by a second launch.  wide: a result of 32 bits.
 struct MatmulPlan {
     enum { FEW, T64, T128, T256 } kind;
     uint64_t tiles_m, tiles_n;
     uint32_t splits, share;
     double us;
 };
-MatmulPlan matmul_plan(uint64_t M, uint64_t N, uint64_t W, bool may_split) {
+MatmulPlan matmul_plan(uint64_t M, uint64_t N, uint64_t W, bool wide, bool may_split) {
     MatmulPlan best{};
     best.splits = 1;
     const uint64_t stages = (W + 1) / 2;
@@ -111,14 +112,17 @@ MatmulPlan matmul_plan(uint64_t M, uint64_t N, uint64_t W, bool may_split) {
         best.us = 3.0 + (double)N * (double)W * 68.0 / 4e6;                   // B's codes and scales at 4 TB/s
         return best;
     }
-    struct { decltype(best.kind) kind; uint64_t edge; double stage, tile, launch; } const kinds[] = {
-        {MatmulPlan::T256, 256, 2.2, 6.0, 5.0}, {MatmulPlan::T128, 128, 0.8, 1.8, 4.0}, {MatmulPlan::T64, 64, 0.3, 0.5, 3.0}};
+    // of one tile: a stage where few compute units have one and where all do, its end in 16 bits and in 32; the launch
+    struct { decltype(best.kind) kind; uint64_t edge; double lone, stage, end16, end32, launch; } const kinds[] = {
+        {MatmulPlan::T256, 256, 1.3, 1.95, 3.0, 6.0, 5.0}, {MatmulPlan::T128, 128, 0.64, 0.64, 1.0, 1.5, 5.0}, {MatmulPlan::T64, 64, 0.24, 0.24, 0.35, 0.35, 4.5}};
     for (const auto& k : kinds) {
         const uint64_t tm = (M + k.edge - 1) / k.edge, tn = (N + k.edge - 1) / k.edge;
         for (uint64_t splits = 1; splits == 1 || (may_split && splits <= 16 && 4 * splits <= stages && tm * tn * splits <= 4 * UNITS); splits *= 2) {
             const uint64_t share = (stages + splits - 1) / splits, parts = (stages + share - 1) / share;
-            const double c = (double)((tm * tn * parts + UNITS - 1) / UNITS);
-            double us = c * ((double)share * k.stage + k.tile) + k.launch;
+            const uint64_t items = tm * tn * parts, rounds = items / UNITS;
+            const double part = (double)(items % UNITS) / UNITS, end = wide || parts > 1 ? k.end32 : k.end16;
+            double us = (double)rounds * ((double)share * k.stage + end) + k.launch;
+            if (part > 0) us += (double)share * (k.lone + part * (k.stage - k.lone)) + end;
             if (parts > 1) us += 4.0 + (double)(parts * M * N) * 8.0 / 4e6;     // 4 bytes written and read, at 4 TB/s
             if (best.us == 0 || us < best.us) {
                 best.us = us;
@@ -129,16 +133,17 @@ MatmulPlan matmul_plan(uint64_t M, uint64_t N, uint64_t W, bool may_split) {
     }
     return best;
 }
-// Tiles of 256 rows that leave most compute units without work in their last round: so many of A's rows make whole rounds, the rest goes by a second launch,
-// if both together are expected to take less (50257 x 768 x 8192, 591 tiles on 256 units: 222 and 193 us).  0: one launch.
-inline uint64_t matmul_first_rows(const MatmulPlan& p, uint64_t M, uint64_t N, uint64_t W, MatmulPlan& rest) {
+// Tiles of 256 rows that leave at least three quarters of the compute units without work in their last round: so many of A's rows make whole rounds, the rest
+// goes by a second launch, if both together are expected to take less (8704 x 4096 x 8192, an eighth of the units in the last round: 180 and 160 us; 9216, a
+// quarter: 182 and 170; but 50257 x 768 x 8192, a third: 195 and 208).  0: one launch.
+inline uint64_t matmul_first_rows(const MatmulPlan& p, uint64_t M, uint64_t N, uint64_t W, bool wide, MatmulPlan& rest) {
     const uint64_t tiles = p.tiles_m * p.tiles_n, rounds = tiles / UNITS;
-    if (p.kind != MatmulPlan::T256 || p.splits != 1 || rounds == 0) return 0;
+    if (p.kind != MatmulPlan::T256 || p.splits != 1 || rounds == 0 || tiles % UNITS > UNITS / 4) return 0;
     const uint64_t rows = rounds * UNITS / p.tiles_n * 256;
     if (rows == 0 || rows >= M) return 0;
-    rest = matmul_plan(M - rows, N, W, false);
-    const double each = (p.us - 5.0) / (double)((tiles + UNITS - 1) / UNITS);
-    return (double)rounds * each + 5.0 + rest.us < p.us ? rows : 0;
+    rest = matmul_plan(M - rows, N, W, wide, false);
+    const MatmulPlan first = matmul_plan(rows, N, W, wide, false);
+    return first.kind == MatmulPlan::T256 && first.us + rest.us < p.us ? rows : 0;
 }
 inline uint64_t matmul_parts_bytes(const MatmulPlan& p, uint64_t M, uint64_t N) { return p.splits > 1 ? 4 * p.splits * M * N : 0; }
 
@@ -219,7 +224,7 @@ int kimad_mx4_dequantise(const void* codes, const uint32_t* scales, uint64_t row
 
 uint64_t kimad_mx4_matmul_workspace_bytes(uint64_t M, uint64_t N, uint64_t K) {
     if (M > MOST || N > MOST || K > MATMUL_MOST_K || M == 0 || N == 0) return 0;
-    return matmul_parts_bytes(matmul_plan(M, N, words_of(K), true), M, N);
+    return matmul_parts_bytes(matmul_plan(M, N, words_of(K), true, true), M, N);
 }
 
 int kimad_mx4_matmul(const void* a_codes, const uint32_t* a_scales, uint64_t M, const void* b_codes, const uint32_t* b_scales,
@@ -232,8 +237,8 @@ int kimad_mx4_matmul(const void* a_codes, const uint32_t* a_scales, uint64_t M, 
     if (workspace && !aligned(workspace, 16)) return KIMAD_ERR_INVALID_ARG;
     MatmulArgs g{};
     g.a = static_cast<const uint8_t*>(a_codes); g.b = static_cast<const uint8_t*>(b_codes);
-    MatmulPlan p = matmul_plan(M, N, words_of(K), true);
-    if (matmul_parts_bytes(p, M, N) > (workspace ? workspace_bytes : 0)) p = matmul_plan(M, N, words_of(K), false);
+    MatmulPlan p = matmul_plan(M, N, words_of(K), type == KIMAD_VALUES_F32, true);
+    if (matmul_parts_bytes(p, M, N) > (workspace ? workspace_bytes : 0)) p = matmul_plan(M, N, words_of(K), type == KIMAD_VALUES_F32, false);
     g.sa = a_scales; g.sb = b_scales; g.out = out; g.M = M; g.N = N; g.W = words_of(K); g.ld = ld; g.scale_rows = M;
     hipStream_t s = static_cast<hipStream_t>(stream);
     return with_type(type, [&](auto t) {
@@ -244,7 +249,7 @@ int kimad_mx4_matmul(const void* a_codes, const uint32_t* a_scales, uint64_t M, 
             return launched();
         }
         MatmulPlan rest{};
-        if (const uint64_t rows = matmul_first_rows(p, M, N, g.W, rest)) {
+        if (const uint64_t rows = matmul_first_rows(p, M, N, g.W, type == KIMAD_VALUES_F32, rest)) {
             MatmulArgs first = g;
             first.M = rows;
             MatmulPlan fp = p;

@@ -350,3 +350,10 @@ def test_workspace_that_the_product_makes_stays_its_own_on_a_given_stream():
         out.zero_()
         torch.cuda.synchronize()
         del others, busy
+
+
+# whole rounds of large tiles and some rows beyond: those go by a second launch, of small tiles or of few rows
+@pytest.mark.parametrize("kind", ["float32", "bfloat16"])
+@pytest.mark.parametrize("M,N,K", [(16404, 4096, 1024), (16385, 4096, 520), (16700, 4090, 1100), (33200, 2041, 900)])
+def test_product_with_rows_beyond_whole_rounds(M, N, K, kind):
+    test_product_over_several_tiles_a_workgroup(M, N, K, kind)
