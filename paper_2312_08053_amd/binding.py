@@ -328,6 +328,13 @@ def _holds(t, count: int, size: int, what: str) -> int:
     return t.data_ptr()
 
 
+def _on_device(*tensors) -> None:
+    """Host memory is refused: a kernel that reads it faults."""
+    for t in tensors:
+        if t is not None and not t.is_cuda:
+            raise ValueError(f"device tensors are wanted, got one of shape {tuple(t.shape)} on {t.device}")
+
+
 def _holds_mx4(codes, scales, rows: int, cols: int, what: str):
     """The addresses of a quantised matrix."""
     words = (cols + 127) // 128
@@ -347,14 +354,18 @@ def kimad_mx4_quantise(x, codes=None, scales=None, codes_t=None, scales_t=None, 
     rows, cols, ld = _rows(x, "x")
     c, s = (0, 0) if codes is None else _holds_mx4(codes, scales, rows, cols, "codes and scales")
     ct, st = (0, 0) if codes_t is None else _holds_mx4(codes_t, scales_t, cols, rows, "codes_t and scales_t")
-    _check(lib().kimad_mx4_quantise(x.data_ptr(), _type(x), rows, cols, ld, c, s, ct, st, _stream(stream)), "kimad_mx4_quantise")
+    kind = _type(x)
+    _on_device(x, codes, scales, codes_t, scales_t)
+    _check(lib().kimad_mx4_quantise(x.data_ptr(), kind, rows, cols, ld, c, s, ct, st, _stream(stream)), "kimad_mx4_quantise")
 
 
 def kimad_mx4_dequantise(codes, scales, out, stream=None) -> None:
     """The values of a quantised matrix into out [rows, cols]."""
     rows, cols, ld = _rows(out, "out")
     c, s = _holds_mx4(codes, scales, rows, cols, "codes and scales")
-    _check(lib().kimad_mx4_dequantise(c, s, rows, cols, out.data_ptr(), _type(out), ld, _stream(stream)), "kimad_mx4_dequantise")
+    kind = _type(out)
+    _on_device(codes, scales, out)
+    _check(lib().kimad_mx4_dequantise(c, s, rows, cols, out.data_ptr(), kind, ld, _stream(stream)), "kimad_mx4_dequantise")
 
 
 def kimad_mx4_matmul_workspace_bytes(M: int, N: int, K: int) -> int:
@@ -367,6 +378,8 @@ def kimad_mx4_matmul(a_codes, a_scales, b_codes, b_scales, K: int, out, workspac
     M, N, ld = _rows(out, "out")
     a, sa = _holds_mx4(a_codes, a_scales, M, K, "A's codes and scales")
     b, sb = _holds_mx4(b_codes, b_scales, N, K, "B's codes and scales")
+    kind = _type(out)
+    _on_device(a_codes, a_scales, b_codes, b_scales, out, workspace)
     L = lib()
     ws = nbytes = 0
     if workspace is None:
@@ -375,7 +388,7 @@ def kimad_mx4_matmul(a_codes, a_scales, b_codes, b_scales, K: int, out, workspac
             workspace = _scratch(nbytes, out.device, stream)
     if workspace is not None:
         ws, nbytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    _check(L.kimad_mx4_matmul(a, sa, M, b, sb, N, K, out.data_ptr(), _type(out), ld, ws, nbytes, _stream(stream)), "kimad_mx4_matmul")
+    _check(L.kimad_mx4_matmul(a, sa, M, b, sb, N, K, out.data_ptr(), kind, ld, ws, nbytes, _stream(stream)), "kimad_mx4_matmul")
 
 
 def kimad_mx4_update_words(L: int, d: int) -> int:
@@ -387,9 +400,10 @@ def kimad_mx4_compress_ef(g, h, layer_start, codes, scales, status_out=None, str
     [words, 64] and scales int32 [words] with words = kimad_mx4_update_words(L, d); status_out: device int32[1] or None."""
     d, L = g.numel(), layer_start.numel() - 1
     words = d // 128 + L
-    _check(lib().kimad_mx4_compress_ef(_holds(g, d, 4, "g"), _holds(h, d, 4, "h"), _holds(layer_start, 2, 8, "layer_start"), L, d,
-                                       _holds(codes, words * 64, 1, "codes"), _holds(scales, words, 4, "scales"), _ptr(status_out),
-                                       _stream(stream)), "kimad_mx4_compress_ef")
+    args = (_holds(g, d, 4, "g"), _holds(h, d, 4, "h"), _holds(layer_start, 2, 8, "layer_start"), L, d,
+            _holds(codes, words * 64, 1, "codes"), _holds(scales, words, 4, "scales"), _ptr(status_out))
+    _on_device(g, h, layer_start, codes, scales, status_out)
+    _check(lib().kimad_mx4_compress_ef(*args, _stream(stream)), "kimad_mx4_compress_ef")
 
 
 def kimad_mx4_server_apply(updates, u_hats, weights, layer_start, d: int, x=None, gamma: float = 0.0, status_out=None,
@@ -404,9 +418,10 @@ def kimad_mx4_server_apply(updates, u_hats, weights, layer_start, d: int, x=None
     for m, (codes, scales) in enumerate(updates):
         up[m].codes, up[m].scales = _holds(codes, words * 64, 1, "codes"), _holds(scales, words, 4, "scales")
         uh[m] = _holds(u_hats[m], d, 4, "u_hats")
-    _check(lib().kimad_mx4_server_apply(up, uh, w, M, _holds(layer_start, 2, 8, "layer_start"), L, d,
-                                        0 if x is None else _holds(x, d, 4, "x"), gamma, _ptr(status_out), _stream(stream)),
-           "kimad_mx4_server_apply")
+        _on_device(codes, scales, u_hats[m])
+    args = (up, uh, w, M, _holds(layer_start, 2, 8, "layer_start"), L, d, 0 if x is None else _holds(x, d, 4, "x"), gamma, _ptr(status_out))
+    _on_device(layer_start, x, status_out)
+    _check(lib().kimad_mx4_server_apply(*args, _stream(stream)), "kimad_mx4_server_apply")
 
 
 def kimad_distill_workspace_bytes(rows: int, vocab: int, k: int) -> int:
@@ -436,6 +451,10 @@ def kimad_distill(logits, t_idx, t_val, temperature: float, loss=None, stats=Non
     against a teacher's top entries t_idx int32, t_val float32 [rows, k]; an output that is None is left out."""
     lead, weight, g, ld_grad = _distill_inputs(logits, t_idx, t_val, row_weight, grad)
     _, _, rows, vocab, _, _, _, k = lead
+    for out, count, what in ((loss, rows, "loss"), (stats, 2 * rows, "stats")):
+        if out is not None:
+            _holds(out, count, 4, what)
+    _on_device(logits, t_idx, t_val, loss, stats, grad, row_weight, workspace)
     L = lib()
     ws = nbytes = 0
     if workspace is None:
@@ -444,16 +463,15 @@ def kimad_distill(logits, t_idx, t_val, temperature: float, loss=None, stats=Non
             workspace = _scratch(nbytes, logits.device, stream)
     if workspace is not None:
         ws, nbytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    _check(L.kimad_distill(*lead, temperature, weight, 0 if loss is None else _holds(loss, rows, 4, "loss"),
-                           0 if stats is None else _holds(stats, 2 * rows, 4, "stats"), g, ld_grad, ws, nbytes, _stream(stream)),
-           "kimad_distill")
+    _check(L.kimad_distill(*lead, temperature, weight, _ptr(loss), _ptr(stats), g, ld_grad, ws, nbytes, _stream(stream)), "kimad_distill")
 
 
 def kimad_distill_grad(logits, t_idx, t_val, temperature: float, stats, grad, row_weight=None, stream=None) -> None:
     """The gradient alone, from the statistics of an earlier kimad_distill."""
     lead, weight, g, ld_grad = _distill_inputs(logits, t_idx, t_val, row_weight, grad)
-    _check(lib().kimad_distill_grad(*lead, temperature, weight, _holds(stats, 2 * lead[2], 4, "stats"), g, ld_grad, _stream(stream)),
-           "kimad_distill_grad")
+    at = _holds(stats, 2 * lead[2], 4, "stats")
+    _on_device(logits, t_idx, t_val, stats, grad, row_weight)
+    _check(lib().kimad_distill_grad(*lead, temperature, weight, at, g, ld_grad, _stream(stream)), "kimad_distill_grad")
 
 
 class Plan:

@@ -113,3 +113,20 @@ def test_the_binding_refuses_tensors_that_do_not_fit():
         kimad.kimad_distill(x, idx.long(), val, 1.0, loss=torch.zeros(4), stream=0)
     with pytest.raises(ValueError):
         kimad.kimad_distill(x, idx, val, 1.0, grad=torch.zeros(4, 99), stream=0)
+
+
+def test_the_binding_refuses_host_memory():
+    import torch
+    x, idx, val = torch.zeros(4, 128), torch.zeros(4, 3, dtype=torch.int32), torch.zeros(4, 3)
+    codes, scales = kimad.mx4_empty(4, 128, "cpu")
+    starts, flat = torch.tensor([0, 512]), torch.zeros(512)
+    up = torch.zeros(5, 64, dtype=torch.uint8), torch.zeros(5, dtype=torch.int32)
+    for call in (lambda: kimad.kimad_mx4_quantise(x, codes, scales, stream=0),
+                 lambda: kimad.kimad_mx4_dequantise(codes, scales, x, stream=0),
+                 lambda: kimad.kimad_mx4_matmul(codes, scales, codes, scales, 128, torch.zeros(4, 4), stream=0),
+                 lambda: kimad.kimad_distill(x, idx, val, 1.0, loss=torch.zeros(4), stream=0),
+                 lambda: kimad.kimad_distill_grad(x, idx, val, 1.0, torch.zeros(4, 2), torch.zeros(4, 128), stream=0),
+                 lambda: kimad.kimad_mx4_compress_ef(flat, flat.clone(), starts, *up, stream=0),
+                 lambda: kimad.kimad_mx4_server_apply([up], [flat], [1.0], starts, 512, stream=0)):
+        with pytest.raises(ValueError, match="device tensors are wanted"):
+            call()
