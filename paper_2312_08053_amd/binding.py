@@ -451,9 +451,8 @@ def kimad_distill(logits, t_idx, t_val, temperature: float, loss=None, stats=Non
     against a teacher's top entries t_idx int32, t_val float32 [rows, k]; an output that is None is left out."""
     lead, weight, g, ld_grad = _distill_inputs(logits, t_idx, t_val, row_weight, grad)
     _, _, rows, vocab, _, _, _, k = lead
-    for out, count, what in ((loss, rows, "loss"), (stats, 2 * rows, "stats")):
-        if out is not None:
-            _holds(out, count, 4, what)
+    at_loss = 0 if loss is None else _holds(loss, rows, 4, "loss")
+    at_stats = 0 if stats is None else _holds(stats, 2 * rows, 4, "stats")
     _on_device(logits, t_idx, t_val, loss, stats, grad, row_weight, workspace)
     L = lib()
     ws = nbytes = 0
@@ -463,7 +462,7 @@ def kimad_distill(logits, t_idx, t_val, temperature: float, loss=None, stats=Non
             workspace = _scratch(nbytes, logits.device, stream)
     if workspace is not None:
         ws, nbytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    _check(L.kimad_distill(*lead, temperature, weight, _ptr(loss), _ptr(stats), g, ld_grad, ws, nbytes, _stream(stream)), "kimad_distill")
+    _check(L.kimad_distill(*lead, temperature, weight, at_loss, at_stats, g, ld_grad, ws, nbytes, _stream(stream)), "kimad_distill")
 
 
 def kimad_distill_grad(logits, t_idx, t_val, temperature: float, stats, grad, row_weight=None, stream=None) -> None:
