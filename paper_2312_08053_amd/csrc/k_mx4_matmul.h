@@ -65,7 +65,7 @@ __device__ __forceinline__ void tile_of(uint32_t id, uint32_t tm, uint32_t tn, u
 // that sixteen lanes that read one block of sixteen rows meet sixteen different groups of banks.
 // Bound by the loads of a compute unit, some 25 bytes a clock however they are made (K = 16384, a tile of 256 a unit, 64 stages: loads alone 78 us, products
 // alone 87, reads of LDS alone 43, all 117 where the codes are zeros), and by power where they are not (150 us).  8192 x 5632 x 2048 into bfloat16
-// 66 to 74 us by machine, 2.6 to 2.9 PFLOP/s; 50257 x 768 x 8192 into fp32 202 to 214 us, 3.0 to 3.1.
+// 60 to 63 us by machine, 3.0 to 3.1 PFLOP/s; 50257 x 768 x 8192 into fp32 192 to 205 us, 3.1 to 3.3.
 template <uint32_t BM_, uint32_t BN_, uint32_t WM_, uint32_t WN_>
 struct MatmulTile {
     static constexpr uint32_t BM = BM_, BN = BN_, WM = WM_, WN = WN_;
@@ -286,7 +286,7 @@ __global__ __launch_bounds__(64 * T::WAVES, 2) void k_mx4_matmul_tile(MatmulArgs
             }
         }
         stores_behind = cut ? 0u : 1u;
-        if (cut) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");          // (so many more stores that the counter would not tell)
+        if (cut) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");            // (so many more stores that the counter would not tell)
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                          // no load may reach LDS that is another workgroup's by then
 }
