@@ -107,6 +107,7 @@ MatmulPlan matmul_plan(uint64_t M, uint64_t N, uint64_t W, bool wide, bool may_s
     best.splits = 1;
     const uint64_t stages = (W + 1) / 2;
     best.share = (uint32_t)stages;
+    if (W == 0) return best;                                                  // (nothing to share out; such a product goes by none of these)
     if (M <= FEW_ROWS) {
         best.kind = MatmulPlan::FEW;
         best.us = 3.0 + (double)N * (double)W * 68.0 / 4e6;                   // B's codes and scales at 4 TB/s

@@ -357,3 +357,14 @@ def test_workspace_that_the_product_makes_stays_its_own_on_a_given_stream():
 @pytest.mark.parametrize("M,N,K", [(16404, 4096, 1024), (16385, 4096, 520), (16700, 4090, 1100), (33200, 2041, 900)])
 def test_product_with_rows_beyond_whole_rounds(M, N, K, kind):
     test_product_over_several_tiles_a_workgroup(M, N, K, kind)
+
+
+@pytest.mark.parametrize("M,N", [(1, 1), (33, 70), (300, 70), (1000, 5)])
+def test_a_product_over_no_columns_is_zeros_at_every_size(M, N):
+    import torch
+    kimad = _kimad()
+    a, sa = kimad.mx4_empty(M, 0)
+    b, sb = kimad.mx4_empty(N, 0)
+    out = torch.full((M, N), 3.0, device="cuda")
+    kimad.kimad_mx4_matmul(a, sa, b, sb, 0, out)
+    assert (_host(out) == 0).all()

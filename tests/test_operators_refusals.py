@@ -130,3 +130,11 @@ def test_the_binding_refuses_host_memory():
                  lambda: kimad.kimad_mx4_server_apply([up], [flat], [1.0], starts, 512, stream=0)):
         with pytest.raises(ValueError, match="device tensors are wanted"):
             call()
+
+
+def test_the_workspace_of_any_product_is_told():
+    for K in (0, 1, 128, 129, 5000, 1 << 25, (1 << 25) + 1):
+        for M in (0, 1, 32, 33, 64, 65, 1000, 100000, 1 << 40, (1 << 40) + 1):
+            for N in (0, 1, 70, 50257, 1 << 24):
+                need = kimad.kimad_mx4_matmul_workspace_bytes(M, N, K)
+                assert need % 4 == 0 and (need == 0 or (K > 0 and need >= 8 * M * N))
