@@ -20,7 +20,7 @@ static_assert(TYPE_F32 == KIMAD_VALUES_F32 && TYPE_F16 == KIMAD_VALUES_F16 && TY
 static_assert(UPDATE_MAX_WORKERS == KIMAD_MAX_WORKERS, "header and kernel constants");
 
 constexpr uint64_t MOST = 1ull << 40;                    // elements along an axis that the checks below let through
-constexpr uint64_t FEW_ROWS = 32;                        // products of so many rows go by k_mx4_matmul_few
+constexpr uint64_t FEW_ROWS = 32;                        // products of so many rows may go by k_mx4_matmul_few
 constexpr uint64_t UNITS = 256;                         // compute units of the device
 constexpr uint64_t MATMUL_MOST_K = 1ull << 25, MATMUL_MOST_LD = 1ull << 24;     // eight rows of codes and 32 rows of the result are reached by 32-bit offsets
 constexpr uint64_t GRID_MOST = 0x7FFFFFFFull, GRID_Y_MOST = 65535;
@@ -95,7 +95,14 @@ typedef MatmulTile<64, 64, 2, 2> Tile64;
 //   8192   5632   2048     73  (62)       75  (69)       102 (100)      72  (62)
 //   50257  768    8192     195 (182)      222 (205)      309 (296)      195 (182)
 //   1000   50257  768      55  (44)       51  (43)       65  (63)       48  (43)
-// With few tiles and long sums the stages are shared out as well, and the parts, which are of 32 bits, added by a second launch.  wide: a result of 32 bits.
+// Products of up to 32 rows (B's codes and scales not used just before, us; few: k_mx4_matmul_few, whose waves read all of A each):
+//   M      N      K        few   64    128       M      N      K        few   64    128
+//   8      32000  2048     10.0  11.6  14.1      8      50257  8192     49    52    52
+//   16     32000  2048     11.0  11.7  14.1      16     50257  8192     58    52    52
+//   32     32000  2048     14.8  11.9  14.3      32     50257  8192     83    55    53
+//   32     5632   2048     5.9   7.8   11.1      32     8192   8192     15.2  17.7  17.8
+// With few tiles and long sums the stages are shared out as well (64 x 8192 x 8192 19.6 and 15.1 us, 48 x 4096 x 16384 34 and 14.9),
+// and the parts, which are of 32 bits, added by a second launch.  wide: a result of 32 bits.
 struct MatmulPlan {
     enum { FEW, T64, T128, T256 } kind;
     uint64_t tiles_m, tiles_n;
@@ -108,14 +115,15 @@ MatmulPlan matmul_plan(uint64_t M, uint64_t N, uint64_t W, bool wide, bool may_s
     const uint64_t stages = (W + 1) / 2;
     best.share = (uint32_t)stages;
     if (W == 0) return best;                                                  // (nothing to share out; such a product goes by none of these)
+    const double read = 2.0 + (double)((M + N) * W) * 68.0 / 4.5e6;           // both operands from memory
     if (M <= FEW_ROWS) {
         best.kind = MatmulPlan::FEW;
-        best.us = 3.0 + (double)N * (double)W * 68.0 / 4e6;                   // B's codes and scales at 4 TB/s
-        return best;
+        best.us = std::max(read, 2.2 + (double)(N * W) * 68.0 / 7.2e6 * (1.0 + (double)M / 28.0) + (double)(N * M) * 1.2e-6);
     }
-    // of one tile: a stage where few compute units have one and where all do, its end in 16 bits and in 32; the launch
-    struct { decltype(best.kind) kind; uint64_t edge; double lone, stage, end16, end32, launch; } const kinds[] = {
-        {MatmulPlan::T256, 256, 1.3, 1.95, 3.0, 6.0, 5.0}, {MatmulPlan::T128, 128, 0.64, 0.64, 1.0, 1.5, 5.0}, {MatmulPlan::T64, 64, 0.24, 0.24, 0.35, 0.35, 4.5}};
+    // of one tile: a stage with nothing beside it on its compute unit, what comes from beyond the L2; among others, where few units have one and where all do;
+    // its end in 16 bits and in 32; the launch
+    struct { decltype(best.kind) kind; uint64_t edge; double alone, lone, stage, end16, end32, launch; } const kinds[] = {
+        {MatmulPlan::T256, 256, 1.3, 1.3, 1.95, 3.0, 6.0, 5.0}, {MatmulPlan::T128, 128, 0.69, 0.64, 0.64, 1.0, 1.5, 5.0}, {MatmulPlan::T64, 64, 0.45, 0.24, 0.24, 0.35, 0.35, 4.5}};
     for (const auto& k : kinds) {
         const uint64_t tm = (M + k.edge - 1) / k.edge, tn = (N + k.edge - 1) / k.edge;
         for (uint64_t splits = 1; splits == 1 || (may_split && splits <= 16 && 4 * splits <= stages && tm * tn * splits <= 4 * UNITS); splits *= 2) {
@@ -125,6 +133,7 @@ MatmulPlan matmul_plan(uint64_t M, uint64_t N, uint64_t W, bool wide, bool may_s
             double us = (double)rounds * ((double)share * k.stage + end) + k.launch;
             if (part > 0) us += (double)share * (k.lone + part * (k.stage - k.lone)) + end;
             if (parts > 1) us += 4.0 + (double)(parts * M * N) * 8.0 / 4e6;     // 4 bytes written and read, at 4 TB/s
+            us = std::max(std::max(us, k.launch + (double)share * k.alone + end), read);
             if (best.us == 0 || us < best.us) {
                 best.us = us;
                 best.kind = k.kind; best.tiles_m = tm; best.tiles_n = tn;

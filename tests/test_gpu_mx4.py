@@ -359,6 +359,13 @@ def test_product_with_rows_beyond_whole_rounds(M, N, K, kind):
     test_product_over_several_tiles_a_workgroup(M, N, K, kind)
 
 
+# about where products of few rows go by tiles instead, with sums shared out and not
+@pytest.mark.parametrize("kind", ["float32", "bfloat16"])
+@pytest.mark.parametrize("M,N,K", [(12, 32000, 2048), (16, 32000, 2048), (32, 32001, 2048), (18, 50257, 768), (32, 50257, 768), (24, 16390, 4096), (32, 8192, 8192), (33, 8191, 8192), (64, 2048, 5632)])
+def test_product_of_few_rows_by_many(M, N, K, kind):
+    test_product_over_several_tiles_a_workgroup(M, N, K, kind)
+
+
 @pytest.mark.parametrize("M,N", [(1, 1), (33, 70), (300, 70), (1000, 5)])
 def test_a_product_over_no_columns_is_zeros_at_every_size(M, N):
     import torch
