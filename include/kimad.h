@@ -384,12 +384,14 @@ uint64_t kimad_budget_bytes(double bandwidth_bits_per_s, double t_seconds, doubl
 /* Quantises x, [rows, cols] of `type` with consecutive rows ld >= cols elements apart: along rows into codes, scales (both may
  * be NULL), along columns into codes_t, scales_t (both may be NULL), which is the form of the transpose, a matrix of cols rows
  * and rows columns: a training step needs both, and one call reads x once.
- * At most 67107840 columns, or 8388480 rows where columns are quantised (a grid's limits); more are refused. */
+ * At most 67107840 columns, or 8388480 rows where columns are quantised, else 268435440 (a
+ * grid's limits); more are refused. */
 int kimad_mx4_quantise(const void* x, uint32_t type, uint64_t rows, uint64_t cols, uint64_t ld, void* codes, uint32_t* scales,
                        void* codes_t, uint32_t* scales_t, void* stream);
 
 /* The values that a quantised matrix stands for, into out, [rows, cols] of `type` with rows ld >= cols elements apart.  Exact in F32
- * and BF16; in F16 rounded, and Inf beyond its range.  At most 67107840 columns. */
+ * and BF16; in F16 rounded, and Inf beyond its range.  At most 67107840 columns and
+ * 268435440 rows. */
 int kimad_mx4_dequantise(const void* codes, const uint32_t* scales, uint64_t rows, uint64_t cols, void* out, uint32_t type,
                          uint64_t ld, void* stream);
 
@@ -437,7 +439,8 @@ int kimad_mx4_server_apply(const kimad_mx4_update_t* updates, float* const* u_ha
  * q = softmax(z / T) over the vocabulary and p = softmax(t / T) over the row's entries:
  *     loss[r]    = w_r T^2 sum_j p_j (ln p_j - ln q_{idx_j})
  *     grad[r, v] = w_r T (q_v - p_v)          (p_v = 0 where v is no entry)
- *   logits      DEVICE [rows, vocab] of `type`, rows ld >= vocab elements apart; 1 <= vocab < 2^31
+ *   logits      DEVICE [rows, vocab] of `type`, rows ld >= vocab elements apart; 1 <= vocab < 2^31.  A launch holds 2^32 threads: up to
+ *               4194303 rows fit (rows * ceil((vocab + 7) / 8192) up to 16777215 in kimad_distill_grad and beyond 65529 columns); more may be refused
  *   t_idx       DEVICE uint32[rows * k], t_val DEVICE float[rows * k]: the teacher's entries in any order, 0 <= k <= 1024.  An index of
  *               vocab or more (0xFFFFFFFF) is no entry: rows may have fewer than k.  Entries of one index are one entry
  *               with the sum of their probabilities.

@@ -24,6 +24,8 @@ constexpr uint64_t FEW_ROWS = 32;                        // products of so many 
 constexpr uint64_t UNITS = 256;                         // compute units of the device
 constexpr uint64_t MATMUL_MOST_K = 1ull << 25, MATMUL_MOST_LD = 1ull << 24;     // eight rows of codes and 32 rows of the result are reached by 32-bit offsets
 constexpr uint64_t GRID_MOST = 0x7FFFFFFFull, GRID_Y_MOST = 65535;
+// a launch's workgroups along x: their threads are counted in 32 bits
+inline bool grid_ok(uint64_t wgs, uint64_t threads) { return wgs <= GRID_MOST && wgs <= 0xFFFFFFFFull / threads; }
 
 inline bool aligned(const void* p, uintptr_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
 inline uint64_t words_of(uint64_t cols) { return (cols + MX4_WORD - 1) / MX4_WORD; }
@@ -65,7 +67,7 @@ int distill_args(DistillArgs& a, const void* logits, uint32_t type, uint64_t row
     if (!(temperature >= 0x1p-20f && temperature <= 0x1p20f)) return KIMAD_ERR_INVALID_ARG;
     if (rows && (!logits || !aligned(logits, type_bytes(type)) || (k && (!t_idx || !t_val)))) return KIMAD_ERR_INVALID_ARG;
     if (grad && (ld_grad < vocab || !aligned(grad, type_bytes(type)))) return KIMAD_ERR_INVALID_ARG;
-    if (rows * distill_chunks(vocab) > GRID_MOST) return KIMAD_ERR_INVALID_ARG;
+    if (distill_by_chunks(vocab) && !grid_ok(rows * distill_chunks(vocab), CHUNK_NT)) return KIMAD_ERR_INVALID_ARG;
     a.z = logits; a.idx = t_idx; a.val = t_val; a.weight = row_weight; a.grad = const_cast<void*>(grad);
     a.rows = rows; a.vocab = (uint32_t)vocab; a.ld = ld; a.ld_grad = ld_grad; a.k = k; a.bloom = distill_bloom(k);
     a.T = temperature; a.c = (float)(1.4426950408889634 / (double)temperature);
@@ -75,6 +77,7 @@ int distill_args(DistillArgs& a, const void* logits, uint32_t type, uint64_t row
 
 template <uint32_t TYPE, uint32_t NT, uint32_t NV>
 int launch_row(const DistillArgs& a, hipStream_t s) {
+    if (!grid_ok(a.rows, NT)) return KIMAD_ERR_INVALID_ARG;
     if (a.grad) hipLaunchKernelGGL((k_distill_row<TYPE, NT, NV, true>), dim3((uint32_t)a.rows), dim3(NT), distill_lds(a.k), s, a);
     else hipLaunchKernelGGL((k_distill_row<TYPE, NT, NV, false>), dim3((uint32_t)a.rows), dim3(NT), distill_lds(a.k), s, a);
     return launched();
@@ -180,7 +183,7 @@ template <uint32_t TYPE>
 int launch_kind(const MatmulArgs& g, const MatmulPlan& p, hipStream_t s) {
     if (p.kind == MatmulPlan::FEW) {
         const uint64_t groups = (g.N + 15) / 16;
-        if (groups > GRID_MOST) return KIMAD_ERR_INVALID_ARG;
+        if (!grid_ok(groups, 256)) return KIMAD_ERR_INVALID_ARG;
         return g.M <= 16 ? launch_few<TYPE, 1>(g, groups, s) : launch_few<TYPE, 2>(g, groups, s);
     }
     if (p.kind == MatmulPlan::T256) return launch_tile<TYPE, Tile256>(g, p, s);
@@ -201,7 +204,7 @@ int kimad_mx4_quantise(const void* x, uint32_t type, uint64_t rows, uint64_t col
     hipStream_t s = static_cast<hipStream_t>(stream);
     const uint64_t W = words_of(cols), WT = words_of(rows);
     if (codes_t) {
-        if (W > GRID_MOST || WT > GRID_Y_MOST) return KIMAD_ERR_INVALID_ARG;
+        if (!grid_ok(W, 256) || WT > GRID_Y_MOST) return KIMAD_ERR_INVALID_ARG;
         return with_type(type, [&](auto t) {
             hipLaunchKernelGGL(k_mx4_quantise_both<decltype(t)::value>, dim3((uint32_t)W, (uint32_t)WT), dim3(256), 0, s, x, rows, cols, ld, W, WT,
                                static_cast<uint32_t*>(codes), scales, static_cast<uint32_t*>(codes_t), scales_t);
@@ -209,7 +212,7 @@ int kimad_mx4_quantise(const void* x, uint32_t type, uint64_t rows, uint64_t col
         });
     }
     const uint64_t gx = (rows + QROWS - 1) / QROWS, gy = (W + QWORDS - 1) / QWORDS;
-    if (gx > GRID_MOST || gy > GRID_Y_MOST) return KIMAD_ERR_INVALID_ARG;
+    if (!grid_ok(gx, 256) || gy > GRID_Y_MOST) return KIMAD_ERR_INVALID_ARG;
     return with_type(type, [&](auto t) {
         hipLaunchKernelGGL(k_mx4_quantise_rows<decltype(t)::value>, dim3((uint32_t)gx, (uint32_t)gy), dim3(256), 0, s, x, rows, cols, ld, W,
                            static_cast<uint32_t*>(codes), scales);
@@ -223,7 +226,7 @@ int kimad_mx4_dequantise(const void* codes, const uint32_t* scales, uint64_t row
     if (rows == 0 || cols == 0) return KIMAD_OK;
     if (!codes || !pair_ok(codes, scales) || !out || !aligned(out, type_bytes(type))) return KIMAD_ERR_INVALID_ARG;
     const uint64_t W = words_of(cols), gx = (rows + QROWS - 1) / QROWS, gy = (W + QWORDS - 1) / QWORDS;
-    if (gx > GRID_MOST || gy > GRID_Y_MOST) return KIMAD_ERR_INVALID_ARG;
+    if (!grid_ok(gx, 256) || gy > GRID_Y_MOST) return KIMAD_ERR_INVALID_ARG;
     hipStream_t s = static_cast<hipStream_t>(stream);
     return with_type(type, [&](auto t) {
         hipLaunchKernelGGL(k_mx4_dequantise<decltype(t)::value>, dim3((uint32_t)gx, (uint32_t)gy), dim3(256), 0, s,
@@ -254,7 +257,7 @@ int kimad_mx4_matmul(const void* a_codes, const uint32_t* a_scales, uint64_t M, 
     return with_type(type, [&](auto t) {
         constexpr uint32_t TYPE = decltype(t)::value;
         if (K == 0) {
-            if ((M * N + 255) / 256 > GRID_MOST) return (int)KIMAD_ERR_INVALID_ARG;
+            if (M > MOST / N * 256 || !grid_ok((M * N + 255) / 256, 256)) return (int)KIMAD_ERR_INVALID_ARG;
             hipLaunchKernelGGL(k_mx4_matmul_none<TYPE>, dim3((uint32_t)((M * N + 255) / 256)), dim3(256), 0, s, out, M, N, ld);
             return launched();
         }
@@ -275,7 +278,7 @@ int kimad_mx4_matmul(const void* a_codes, const uint32_t* a_scales, uint64_t M, 
         const int rc = launch_kind<TYPE_F32>(g, p, s);
         if (rc) return rc;
         const uint64_t wgs = (M * N + 255) / 256;
-        if (wgs > GRID_MOST) return (int)KIMAD_ERR_INVALID_ARG;
+        if (!grid_ok(wgs, 256)) return (int)KIMAD_ERR_INVALID_ARG;
         hipLaunchKernelGGL(k_mx4_matmul_join<TYPE>, dim3((uint32_t)wgs), dim3(256), 0, s, static_cast<const float*>(workspace), p.splits, M, N, out, ld);
         return launched();
     });
@@ -373,7 +376,7 @@ int kimad_distill_grad(const void* logits, uint32_t type, uint64_t rows, uint64_
     DistillArgs a{};
     const int rc = distill_args(a, logits, type, rows, vocab, ld, t_idx, t_val, k, temperature, row_weight, grad, ld_grad);
     if (rc || rows == 0) return rc;
-    if (!stats || !grad) return KIMAD_ERR_INVALID_ARG;
+    if (!stats || !grad || !grid_ok(rows * a.chunks, CHUNK_NT)) return KIMAD_ERR_INVALID_ARG;
     a.stats = const_cast<float*>(stats);
     return with_type(type, [&](auto t) {
         hipLaunchKernelGGL((k_distill_rest<decltype(t)::value, false, true>), dim3((uint32_t)(rows * a.chunks)), dim3(CHUNK_NT), distill_lds(k),

@@ -138,3 +138,15 @@ def test_the_workspace_of_any_product_is_told():
             for N in (0, 1, 70, 50257, 1 << 24):
                 need = kimad.kimad_mx4_matmul_workspace_bytes(M, N, K)
                 assert need % 4 == 0 and (need == 0 or (K > 0 and need >= 8 * M * N))
+
+
+def test_more_threads_than_a_launch_holds_are_refused():
+    L = kimad.lib()
+    assert L.kimad_mx4_quantise(P, 0, 1 << 29, 4, 4, P, P, 0, 0, 0) == BAD
+    assert L.kimad_mx4_dequantise(P, P, 1 << 29, 4, P, 0, 4, 0) == BAD
+    assert L.kimad_mx4_matmul(P, P, 1 << 30, P, P, 1 << 20, 0, P, 0, 1 << 20, 0, 0, 0) == BAD
+    assert L.kimad_mx4_matmul(P, P, 1 << 40, P, P, 1 << 24, 0, P, 0, 1 << 24, 0, 0, 0) == BAD
+    for rows, vocab in ((1 << 30, 100), (1 << 23, 40000), (1 << 22, 65000)):
+        assert L.kimad_distill(P, 0, rows, vocab, vocab, P, P, 8, 1.0, 0, P, 0, 0, 0, 0, 0, 0) == BAD, (rows, vocab)
+    assert L.kimad_distill(P, 0, 1 << 20, 1 << 20, 1 << 20, P, P, 8, 1.0, 0, P, 0, 0, 0, P, 1 << 60, 0) == BAD
+    assert L.kimad_distill_grad(P, 0, 1 << 25, 100, 100, P, P, 8, 1.0, 0, P, P, 100, 0) == BAD
