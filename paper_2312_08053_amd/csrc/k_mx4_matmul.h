@@ -10,7 +10,6 @@
 namespace kimad {
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 struct MatmulArgs {
