@@ -412,7 +412,8 @@ int kimad_mx4_matmul(const void* a_codes, const uint32_t* a_scales, uint64_t M, 
  *     q = MX4(fl32(g - h)),   h <- fl32(h + q).
  * 4.25 bits an entry are sent, whatever the budget; what the rounding lost stays in g - h for the next round.
  *   g, h         DEVICE float[d], the layers back to back (4-byte alignment suffices); h is updated in place
- *   layer_start  DEVICE uint64[L+1], element offsets of the layers, layer_start[L] = d; layers may be empty
+ *   layer_start  DEVICE uint64[L+1], element offsets of the layers, layer_start[L] = d; layers may be empty, and there may be
+ *                2147483647 of them (more are refused)
  *   codes        DEVICE uint8[64 * words], 16-byte aligned; scales DEVICE uint32[words]; words = kimad_mx4_update_words(L, d).
  *                Layer i begins at word floor(layer_start[i] / 128) + i; words between layers hold zeros.
  *   status_out   DEVICE int32[1] or NULL: KIMAD_OK, or KIMAD_ERR_BAD_OFFSETS if layer_start does not run from 0 to d without a

@@ -24,6 +24,7 @@ constexpr uint64_t FEW_ROWS = 32;                        // products of so many 
 constexpr uint64_t UNITS = 256;                         // compute units of the device
 constexpr uint64_t MATMUL_MOST_K = 1ull << 25, MATMUL_MOST_LD = 1ull << 24;     // eight rows of codes and 32 rows of the result are reached by 32-bit offsets
 constexpr uint64_t GRID_MOST = 0x7FFFFFFFull, GRID_Y_MOST = 65535;
+constexpr uint32_t UPDATE_MOST_L = 0x7FFFFFFFu;          // layers of an update: the kernels count them, and search among them, in 32 bits
 // a launch's workgroups along x: their threads are counted in 32 bits
 inline bool grid_ok(uint64_t wgs, uint64_t threads) { return wgs <= GRID_MOST && wgs <= 0xFFFFFFFFull / threads; }
 
@@ -288,7 +289,7 @@ uint64_t kimad_mx4_update_words(uint32_t L, uint64_t d) { return d / MX4_WORD + 
 
 int kimad_mx4_compress_ef(const float* g, float* h, const uint64_t* layer_start, uint32_t L, uint64_t d, void* codes,
                           uint32_t* scales, int32_t* status_out, void* stream) {
-    if (!g || !h || !layer_start || L == 0 || d == 0 || d > MOST || !codes || !pair_ok(codes, scales) || !aligned(g, 4) || !aligned(h, 4))
+    if (!g || !h || !layer_start || L == 0 || L > UPDATE_MOST_L || d == 0 || d > MOST || !codes || !pair_ok(codes, scales) || !aligned(g, 4) || !aligned(h, 4))
         return KIMAD_ERR_INVALID_ARG;
     Mx4CompressArgs a{};
     a.g = g; a.h = h; a.layer_start = layer_start; a.L = L; a.d = d;
@@ -303,7 +304,8 @@ int kimad_mx4_compress_ef(const float* g, float* h, const uint64_t* layer_start,
 int kimad_mx4_server_apply(const kimad_mx4_update_t* updates, float* const* u_hat, const double* weights, uint32_t M,
                            const uint64_t* layer_start, uint32_t L, uint64_t d, float* x, double gamma, int32_t* status_out,
                            void* stream) {
-    if (!updates || !u_hat || !weights || !layer_start || M == 0 || M > KIMAD_MAX_WORKERS || L == 0 || d == 0 || d > MOST || !aligned(x, 4))
+    if (!updates || !u_hat || !weights || !layer_start || M == 0 || M > KIMAD_MAX_WORKERS || L == 0 || L > UPDATE_MOST_L || d == 0 || d > MOST ||
+        !aligned(x, 4))
         return KIMAD_ERR_INVALID_ARG;
     Mx4ServerArgs a{};
     bool lined = true;

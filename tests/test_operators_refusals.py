@@ -150,3 +150,12 @@ def test_more_threads_than_a_launch_holds_are_refused():
         assert L.kimad_distill(P, 0, rows, vocab, vocab, P, P, 8, 1.0, 0, P, 0, 0, 0, 0, 0, 0) == BAD, (rows, vocab)
     assert L.kimad_distill(P, 0, 1 << 20, 1 << 20, 1 << 20, P, P, 8, 1.0, 0, P, 0, 0, 0, P, 1 << 60, 0) == BAD
     assert L.kimad_distill_grad(P, 0, 1 << 25, 100, 100, P, P, 8, 1.0, 0, P, P, 100, 0) == BAD
+
+
+def test_more_layers_than_the_kernels_count_are_refused():
+    from paper_2312_08053_amd.binding import _Mx4Update
+    L = kimad.lib()
+    up, hat, w = (_Mx4Update * 1)(_Mx4Update(P, P)), (C.c_void_p * 1)(P), (C.c_double * 1)(1.0)
+    for layers in (1 << 31, (1 << 32) - 256, (1 << 32) - 1):
+        assert L.kimad_mx4_compress_ef(P, P, P, layers, 4, P, P, 0, 0) == BAD, layers
+        assert L.kimad_mx4_server_apply(up, hat, w, 1, P, layers, 4, 0, 0.0, 0, 0) == BAD, layers
