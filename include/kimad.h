@@ -452,7 +452,7 @@ int kimad_mx4_server_apply(const kimad_mx4_update_t* updates, float* const* u_ha
  *   grad        DEVICE [rows, vocab] of `type`, rows ld_grad >= vocab elements apart, or NULL; may be logits itself with ld_grad = ld
  *   workspace   DEVICE, 4-byte aligned, kimad_distill_workspace_bytes(rows, vocab, k) bytes (0 up to 65529 columns: NULL will do).  As for
  *               kimad_mx4_matmul, but a smaller one is refused (KIMAD_ERR_WORKSPACE_TOO_SMALL).
- * At least one of loss, stats and grad is wanted.  Logits of -Inf are masked: q is 0 there, and so is the gradient; an entry with p > 0
+ * At least one of loss, stats and grad is wanted, unless there are no rows (empty arrays may have no address).  Logits of -Inf are masked: q is 0 there, and so is the gradient; an entry with p > 0
  * there makes the loss +Inf.  A row that leaves nothing (weight 0, no entry above -Inf, or no logit above -Inf) has loss,
  * statistics and gradient 0.  A NaN or +Inf among a row's logits makes its loss and its gradient NaN. */
 uint64_t kimad_distill_workspace_bytes(uint64_t rows, uint64_t vocab, uint32_t k);

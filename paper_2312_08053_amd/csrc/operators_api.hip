@@ -333,9 +333,9 @@ int kimad_distill(const void* logits, uint32_t type, uint64_t rows, uint64_t voc
                   const float* t_val, uint32_t k, float temperature, const float* row_weight, float* loss, float* stats,
                   void* grad, uint64_t ld_grad, void* workspace, uint64_t workspace_bytes, void* stream) {
     DistillArgs a{};
-    if (!loss && !stats && !grad) return KIMAD_ERR_INVALID_ARG;
     const int rc = distill_args(a, logits, type, rows, vocab, ld, t_idx, t_val, k, temperature, row_weight, grad, ld_grad);
     if (rc || rows == 0) return rc;
+    if (!loss && !stats && !grad) return KIMAD_ERR_INVALID_ARG;
     a.loss = loss; a.stats = stats;
     hipStream_t s = static_cast<hipStream_t>(stream);
     const uint64_t need = kimad_distill_workspace_bytes(rows, vocab, k);

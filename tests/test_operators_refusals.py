@@ -159,3 +159,11 @@ def test_more_layers_than_the_kernels_count_are_refused():
     for layers in (1 << 31, (1 << 32) - 256, (1 << 32) - 1):
         assert L.kimad_mx4_compress_ef(P, P, P, layers, 4, P, P, 0, 0) == BAD, layers
         assert L.kimad_mx4_server_apply(up, hat, w, 1, P, layers, 4, 0, 0.0, 0, 0) == BAD, layers
+
+
+def test_a_distillation_of_no_rows_has_nothing_to_do():
+    L = kimad.lib()                                                # empty tensors have no address
+    assert L.kimad_distill(0, 0, 0, 100, 100, 0, 0, 8, 1.0, 0, 0, 0, 0, 0, 0, 0, 0) == 0
+    assert L.kimad_distill_grad(0, 0, 0, 100, 100, 0, 0, 8, 1.0, 0, 0, 0, 100, 0) == 0
+    assert L.kimad_distill(0, 3, 0, 100, 100, 0, 0, 8, 1.0, 0, 0, 0, 0, 0, 0, 0, 0) == BAD
+    assert L.kimad_distill(P, 0, 1, 100, 100, P, P, 8, 1.0, 0, 0, 0, 0, 0, 0, 0, 0) == BAD
