@@ -378,8 +378,9 @@ uint64_t kimad_budget_bytes(double bandwidth_bits_per_s, double t_seconds, doubl
  *     scales  DEVICE uint32[W * R]: word w of row r at w * R + r, 4-byte aligned
  *   Elements beyond column C are stored as zeros, which the product relies on.
  * None of these calls allocates, waits or needs a plan; all may be recorded into a HIP graph.  type: KIMAD_VALUES_F32, _F16
- * or _BF16.  Arrays that are read must not overlap arrays that are written, but where stated.  Sizes of 0 are
- * allowed where an empty result makes sense (0 rows; K = 0 gives a product of zeros). */
+ * or _BF16.  Every array is aligned like its elements, where no more is asked for.  Arrays that are read must not overlap
+ * arrays that are written, but where stated.  Sizes of 0 are allowed where an empty result makes sense (0 rows; K = 0 gives a
+ * product of zeros). */
 
 /* Quantises x, [rows, cols] of `type` with consecutive rows ld >= cols elements apart: along rows into codes, scales (both may
  * be NULL), along columns into codes_t, scales_t (both may be NULL), which is the form of the transpose, a matrix of cols rows

@@ -63,10 +63,12 @@ inline uint32_t distill_chunks(uint64_t vocab) { return (uint32_t)((vocab + 7 + 
 inline bool distill_by_chunks(uint64_t vocab) { return vocab > DISTILL_ROW_MOST; }
 
 int distill_args(DistillArgs& a, const void* logits, uint32_t type, uint64_t rows, uint64_t vocab, uint64_t ld, const uint32_t* t_idx,
-                 const float* t_val, uint32_t k, float temperature, const float* row_weight, const void* grad, uint64_t ld_grad) {
+                 const float* t_val, uint32_t k, float temperature, const float* row_weight, const float* loss, const float* stats, const void* grad,
+                 uint64_t ld_grad) {
     if (type > KIMAD_VALUES_BF16 || vocab == 0 || vocab >= (1ull << 31) || rows > GRID_MOST || ld < vocab || k > DISTILL_MAX_K) return KIMAD_ERR_INVALID_ARG;
     if (!(temperature >= 0x1p-20f && temperature <= 0x1p20f)) return KIMAD_ERR_INVALID_ARG;
     if (rows && (!logits || !aligned(logits, type_bytes(type)) || (k && (!t_idx || !t_val)))) return KIMAD_ERR_INVALID_ARG;
+    if (!aligned(t_idx, 4) || !aligned(t_val, 4) || !aligned(row_weight, 4) || !aligned(loss, 4) || !aligned(stats, 4)) return KIMAD_ERR_INVALID_ARG;
     if (grad && (ld_grad < vocab || !aligned(grad, type_bytes(type)))) return KIMAD_ERR_INVALID_ARG;
     if (distill_by_chunks(vocab) && !grid_ok(rows * distill_chunks(vocab), CHUNK_NT)) return KIMAD_ERR_INVALID_ARG;
     a.z = logits; a.idx = t_idx; a.val = t_val; a.weight = row_weight; a.grad = const_cast<void*>(grad);
@@ -289,7 +291,8 @@ uint64_t kimad_mx4_update_words(uint32_t L, uint64_t d) { return d / MX4_WORD + 
 
 int kimad_mx4_compress_ef(const float* g, float* h, const uint64_t* layer_start, uint32_t L, uint64_t d, void* codes,
                           uint32_t* scales, int32_t* status_out, void* stream) {
-    if (!g || !h || !layer_start || L == 0 || L > UPDATE_MOST_L || d == 0 || d > MOST || !codes || !pair_ok(codes, scales) || !aligned(g, 4) || !aligned(h, 4))
+    if (!g || !h || !layer_start || L == 0 || L > UPDATE_MOST_L || d == 0 || d > MOST || !codes || !pair_ok(codes, scales) || !aligned(g, 4) || !aligned(h, 4) ||
+        !aligned(layer_start, 8) || !aligned(status_out, 4))
         return KIMAD_ERR_INVALID_ARG;
     Mx4CompressArgs a{};
     a.g = g; a.h = h; a.layer_start = layer_start; a.L = L; a.d = d;
@@ -305,7 +308,7 @@ int kimad_mx4_server_apply(const kimad_mx4_update_t* updates, float* const* u_ha
                            const uint64_t* layer_start, uint32_t L, uint64_t d, float* x, double gamma, int32_t* status_out,
                            void* stream) {
     if (!updates || !u_hat || !weights || !layer_start || M == 0 || M > KIMAD_MAX_WORKERS || L == 0 || L > UPDATE_MOST_L || d == 0 || d > MOST ||
-        !aligned(x, 4))
+        !aligned(x, 4) || !aligned(layer_start, 8) || !aligned(status_out, 4))
         return KIMAD_ERR_INVALID_ARG;
     Mx4ServerArgs a{};
     bool lined = true;
@@ -333,7 +336,7 @@ int kimad_distill(const void* logits, uint32_t type, uint64_t rows, uint64_t voc
                   const float* t_val, uint32_t k, float temperature, const float* row_weight, float* loss, float* stats,
                   void* grad, uint64_t ld_grad, void* workspace, uint64_t workspace_bytes, void* stream) {
     DistillArgs a{};
-    const int rc = distill_args(a, logits, type, rows, vocab, ld, t_idx, t_val, k, temperature, row_weight, grad, ld_grad);
+    const int rc = distill_args(a, logits, type, rows, vocab, ld, t_idx, t_val, k, temperature, row_weight, loss, stats, grad, ld_grad);
     if (rc || rows == 0) return rc;
     if (!loss && !stats && !grad) return KIMAD_ERR_INVALID_ARG;
     a.loss = loss; a.stats = stats;
@@ -376,7 +379,7 @@ int kimad_distill_grad(const void* logits, uint32_t type, uint64_t rows, uint64_
                        const float* t_val, uint32_t k, float temperature, const float* row_weight, const float* stats, void* grad,
                        uint64_t ld_grad, void* stream) {
     DistillArgs a{};
-    const int rc = distill_args(a, logits, type, rows, vocab, ld, t_idx, t_val, k, temperature, row_weight, grad, ld_grad);
+    const int rc = distill_args(a, logits, type, rows, vocab, ld, t_idx, t_val, k, temperature, row_weight, nullptr, stats, grad, ld_grad);
     if (rc || rows == 0) return rc;
     if (!stats || !grad || !grid_ok(rows * a.chunks, CHUNK_NT)) return KIMAD_ERR_INVALID_ARG;
     a.stats = const_cast<float*>(stats);

@@ -167,3 +167,19 @@ def test_a_distillation_of_no_rows_has_nothing_to_do():
     assert L.kimad_distill_grad(0, 0, 0, 100, 100, 0, 0, 8, 1.0, 0, 0, 0, 100, 0) == 0
     assert L.kimad_distill(0, 3, 0, 100, 100, 0, 0, 8, 1.0, 0, 0, 0, 0, 0, 0, 0, 0) == BAD
     assert L.kimad_distill(P, 0, 1, 100, 100, P, P, 8, 1.0, 0, 0, 0, 0, 0, 0, 0, 0) == BAD
+
+
+def test_arrays_that_are_not_aligned_like_their_elements_are_refused():
+    from paper_2312_08053_amd.binding import _Mx4Update
+    L = kimad.lib()
+    names = ("idx", "val", "weight", "loss", "stats")
+    for off in names:
+        at = {n: P + 2 * (n == off) for n in names}
+        assert L.kimad_distill(P, 0, 4, 100, 100, at["idx"], at["val"], 8, 1.0, at["weight"], at["loss"], at["stats"], 0, 0, 0, 0, 0) == BAD, off
+        if off != "loss":
+            assert L.kimad_distill_grad(P, 0, 4, 100, 100, at["idx"], at["val"], 8, 1.0, at["weight"], at["stats"], P, 100, 0) == BAD, off
+    assert L.kimad_mx4_compress_ef(P, P, P + 4, 1, 4, P, P, 0, 0) == BAD
+    assert L.kimad_mx4_compress_ef(P, P, P, 1, 4, P, P, P + 1, 0) == BAD
+    up, hat, w = (_Mx4Update * 1)(_Mx4Update(P, P)), (C.c_void_p * 1)(P), (C.c_double * 1)(1.0)
+    assert L.kimad_mx4_server_apply(up, hat, w, 1, P + 4, 1, 4, 0, 0.0, 0, 0) == BAD
+    assert L.kimad_mx4_server_apply(up, hat, w, 1, P, 1, 4, 0, 0.0, P + 2, 0) == BAD
