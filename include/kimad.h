@@ -380,12 +380,12 @@ uint64_t kimad_budget_bytes(double bandwidth_bits_per_s, double t_seconds, doubl
  * None of these calls allocates, waits or needs a plan; all may be recorded into a HIP graph.  type: KIMAD_VALUES_F32, _F16
  * or _BF16.  Every array is aligned like its elements, where no more is asked for.  Arrays that are read must not overlap
  * arrays that are written, but where stated.  Sizes of 0 are allowed where an empty result makes sense (0 rows; K = 0 gives a
- * product of zeros). */
+ * product of zeros); an update has at least one layer and one entry (L = 0 and d = 0 are refused). */
 
 /* Quantises x, [rows, cols] of `type` with consecutive rows ld >= cols elements apart: along rows into codes, scales (both may
  * be NULL), along columns into codes_t, scales_t (both may be NULL), which is the form of the transpose, a matrix of cols rows
  * and rows columns: a training step needs both, and one call reads x once.
- * At most 67107840 columns, or 8388480 rows where columns are quantised, else 268435440 (a
+ * At most 2147483520 columns and 8388480 rows where columns are quantised, else 67107840 columns and 268435440 rows (a
  * grid's limits); more are refused. */
 int kimad_mx4_quantise(const void* x, uint32_t type, uint64_t rows, uint64_t cols, uint64_t ld, void* codes, uint32_t* scales,
                        void* codes_t, uint32_t* scales_t, void* stream);

@@ -183,3 +183,12 @@ def test_arrays_that_are_not_aligned_like_their_elements_are_refused():
     up, hat, w = (_Mx4Update * 1)(_Mx4Update(P, P)), (C.c_void_p * 1)(P), (C.c_double * 1)(1.0)
     assert L.kimad_mx4_server_apply(up, hat, w, 1, P + 4, 1, 4, 0, 0.0, 0, 0) == BAD
     assert L.kimad_mx4_server_apply(up, hat, w, 1, P, 1, 4, 0, 0.0, P + 2, 0) == BAD
+
+
+def test_a_quantisation_beyond_the_header_s_limits_is_refused():
+    L = kimad.lib()
+    for cols, rows, pairs in ((2147483520, 8388480, (P, P, P, P)), (2147483520, 8388480, (0, 0, P, P)), (67107840, 268435440, (P, P, 0, 0))):
+        assert L.kimad_mx4_quantise(P, 0, 1, cols + 1, cols + 1, *pairs, 0) == BAD
+        assert L.kimad_mx4_quantise(P, 0, rows + 1, 1, 1, *pairs, 0) == BAD
+    assert L.kimad_mx4_dequantise(P, P, 1, 67107841, P, 0, 67107841, 0) == BAD
+    assert L.kimad_mx4_dequantise(P, P, 268435441, 1, P, 0, 1, 0) == BAD
