@@ -336,8 +336,11 @@ def _on_device(*tensors) -> None:
 
 
 def _holds_mx4(codes, scales, rows: int, cols: int, what: str):
-    """The addresses of a quantised matrix."""
+    """The addresses of a quantised matrix.  Its codes and scales have its own shape: both are laid out by it, so that a part of a
+    larger matrix's is no smaller matrix.  One-dimensional ones are buffers with room for it, as through the C call."""
     words = (cols + 127) // 128
+    if (codes.shape != (rows, 64 * words) and codes.dim() != 1) or (scales.shape != (words, rows) and scales.dim() != 1):
+        raise ValueError(f"{what}: shapes {(rows, 64 * words)} and {(words, rows)} are wanted, got {tuple(codes.shape)} and {tuple(scales.shape)}")
     return _holds(codes, rows * words * 64, 1, what), _holds(scales, rows * words, 4, what)
 
 
@@ -352,6 +355,8 @@ def mx4_empty(rows: int, cols: int, device="cuda"):
 def kimad_mx4_quantise(x, codes=None, scales=None, codes_t=None, scales_t=None, stream=None) -> None:
     """x [rows, cols] along rows into codes, scales, along columns into codes_t, scales_t (each pair from mx4_empty, or None)."""
     rows, cols, ld = _rows(x, "x")
+    if (codes is None) != (scales is None) or (codes_t is None) != (scales_t is None):
+        raise ValueError("codes and scales are wanted together")
     c, s = (0, 0) if codes is None else _holds_mx4(codes, scales, rows, cols, "codes and scales")
     ct, st = (0, 0) if codes_t is None else _holds_mx4(codes_t, scales_t, cols, rows, "codes_t and scales_t")
     kind = _type(x)

@@ -192,3 +192,31 @@ def test_a_quantisation_beyond_the_header_s_limits_is_refused():
         assert L.kimad_mx4_quantise(P, 0, rows + 1, 1, 1, *pairs, 0) == BAD
     assert L.kimad_mx4_dequantise(P, P, 1, 67107841, P, 0, 67107841, 0) == BAD
     assert L.kimad_mx4_dequantise(P, P, 268435441, 1, P, 0, 1, 0) == BAD
+
+
+def test_the_binding_refuses_parts_of_a_quantised_matrix_that_are_none():
+    import torch
+    codes, scales = kimad.mx4_empty(100, 512, "cpu")
+    other, other_scales = kimad.mx4_empty(70, 512, "cpu")
+    out, product = torch.zeros(100, 512), torch.zeros(100, 70)
+    for call in (lambda: kimad.kimad_mx4_dequantise(codes[:50], scales, out[:50], stream=0),               # scales of 100 rows
+                 lambda: kimad.kimad_mx4_dequantise(codes, scales, out[:50], stream=0),
+                 lambda: kimad.kimad_mx4_dequantise(codes, scales, out[:, :128], stream=0),                # fewer words a row
+                 lambda: kimad.kimad_mx4_dequantise(codes.view(50, 512), scales.view(8, 50), out[:50], stream=0),
+                 lambda: kimad.kimad_mx4_quantise(out[:50], codes, scales, stream=0),
+                 lambda: kimad.kimad_mx4_quantise(out[:, :300], codes, scales, stream=0),
+                 lambda: kimad.kimad_mx4_quantise(out, None, None, codes, scales, stream=0),                # the transpose's shape is another
+                 lambda: kimad.kimad_mx4_matmul(codes, scales, other, other_scales, 128, product, stream=0),   # K of another quantisation
+                 lambda: kimad.kimad_mx4_matmul(codes[:50], scales, other, other_scales, 512, product[:50], stream=0),
+                 lambda: kimad.kimad_mx4_matmul(codes, scales, other, other_scales, 512, product[:, :60], stream=0)):
+        with pytest.raises(ValueError, match="shapes"):
+            call()
+    for pairs in ((codes, None), (None, scales), (codes, scales, codes, None), (None, None, None, scales)):
+        with pytest.raises(ValueError, match="together"):
+            kimad.kimad_mx4_quantise(out, *pairs, stream=0)
+    # as much as is wanted: what is refused then is that it is host memory
+    for call in (lambda: kimad.kimad_mx4_dequantise(codes, scales, out[:, :390], stream=0),
+                 lambda: kimad.kimad_mx4_dequantise(torch.zeros(90000, dtype=torch.uint8), torch.zeros(1000, dtype=torch.int32), out, stream=0),
+                 lambda: kimad.kimad_mx4_matmul(codes, scales, other, other_scales, 400, product, stream=0)):
+        with pytest.raises(ValueError, match="device tensors are wanted"):
+            call()
