@@ -321,10 +321,18 @@ def _rows(t, what: str):
     raise ValueError(f"{what}: a matrix with contiguous rows is wanted, got shape {tuple(shape)}, strides {strides}")
 
 
-def _holds(t, count: int, size: int, what: str) -> int:
-    """The address of a contiguous tensor of at least `count` elements of `size` bytes."""
-    if t.numel() < count or t.element_size() != size or not t.is_contiguous():
-        raise ValueError(f"{what}: {count} contiguous elements of {size} bytes are wanted, got {t.numel()} of {t.dtype}, strides {t.stride()}")
+_KINDS = {}
+
+
+def _holds(t, count: int, kind: str, what: str) -> int:
+    """The address of a contiguous tensor of at least `count` elements of a kind: "float32", or "int32", "int64", "uint8", the whole numbers
+    of so many bits (of the two larger ones, unsigned ones too)."""
+    if not _KINDS:
+        import torch
+        _KINDS.update({torch.float32: "float32", torch.int32: "int32", torch.uint32: "int32", torch.int64: "int64", torch.uint64: "int64",
+                       torch.uint8: "uint8"})
+    if _KINDS.get(t.dtype) != kind or t.numel() < count or not t.is_contiguous():
+        raise ValueError(f"{what}: {count} contiguous elements of {kind} are wanted, got {t.numel()} of {t.dtype}, strides {t.stride()}")
     return t.data_ptr()
 
 
@@ -341,7 +349,7 @@ def _holds_mx4(codes, scales, rows: int, cols: int, what: str):
     words = (cols + 127) // 128
     if (codes.shape != (rows, 64 * words) and codes.dim() != 1) or (scales.shape != (words, rows) and scales.dim() != 1):
         raise ValueError(f"{what}: shapes {(rows, 64 * words)} and {(words, rows)} are wanted, got {tuple(codes.shape)} and {tuple(scales.shape)}")
-    return _holds(codes, rows * words * 64, 1, what), _holds(scales, rows * words, 4, what)
+    return _holds(codes, rows * words * 64, "uint8", what), _holds(scales, rows * words, "int32", what)
 
 
 def mx4_empty(rows: int, cols: int, device="cuda"):
@@ -405,8 +413,8 @@ def kimad_mx4_compress_ef(g, h, layer_start, codes, scales, status_out=None, str
     [words, 64] and scales int32 [words] with words = kimad_mx4_update_words(L, d); status_out: device int32[1] or None."""
     d, L = g.numel(), layer_start.numel() - 1
     words = d // 128 + L
-    args = (_holds(g, d, 4, "g"), _holds(h, d, 4, "h"), _holds(layer_start, 2, 8, "layer_start"), L, d,
-            _holds(codes, words * 64, 1, "codes"), _holds(scales, words, 4, "scales"), _ptr(status_out))
+    args = (_holds(g, d, "float32", "g"), _holds(h, d, "float32", "h"), _holds(layer_start, 2, "int64", "layer_start"), L, d,
+            _holds(codes, words * 64, "uint8", "codes"), _holds(scales, words, "int32", "scales"), _ptr(status_out))
     _on_device(g, h, layer_start, codes, scales, status_out)
     _check(lib().kimad_mx4_compress_ef(*args, _stream(stream)), "kimad_mx4_compress_ef")
 
@@ -421,11 +429,10 @@ def kimad_mx4_server_apply(updates, u_hats, weights, layer_start, d: int, x=None
         raise ValueError(f"{M} estimators, {len(updates)} updates and {len(weights)} weights")
     up, uh, w = (_Mx4Update * M)(), (C.c_void_p * M)(), (C.c_double * M)(*weights)
     for m, (codes, scales) in enumerate(updates):
-        up[m].codes, up[m].scales = _holds(codes, words * 64, 1, "codes"), _holds(scales, words, 4, "scales")
-        uh[m] = _holds(u_hats[m], d, 4, "u_hats")
-        _on_device(codes, scales, u_hats[m])
-    args = (up, uh, w, M, _holds(layer_start, 2, 8, "layer_start"), L, d, 0 if x is None else _holds(x, d, 4, "x"), gamma, _ptr(status_out))
-    _on_device(layer_start, x, status_out)
+        up[m].codes, up[m].scales = _holds(codes, words * 64, "uint8", "codes"), _holds(scales, words, "int32", "scales")
+        uh[m] = _holds(u_hats[m], d, "float32", "u_hats")
+    args = (up, uh, w, M, _holds(layer_start, 2, "int64", "layer_start"), L, d, 0 if x is None else _holds(x, d, "float32", "x"), gamma, _ptr(status_out))
+    _on_device(layer_start, x, status_out, *u_hats, *(t for pair in updates for t in pair))
     _check(lib().kimad_mx4_server_apply(*args, _stream(stream)), "kimad_mx4_server_apply")
 
 
@@ -440,8 +447,8 @@ def _distill_inputs(logits, t_idx, t_val, row_weight, grad):
     k = t_idx.shape[1] if t_idx.dim() == 2 else -1
     if t_idx.shape != (rows, k) or t_val.shape != (rows, k):
         raise ValueError(f"entries: [rows, k] is wanted twice, got {tuple(t_idx.shape)} and {tuple(t_val.shape)} for {rows} rows")
-    lead = (logits.data_ptr(), kind, rows, vocab, ld, _holds(t_idx, rows * k, 4, "t_idx"), _holds(t_val, rows * k, 4, "t_val"), k)
-    weight = 0 if row_weight is None else _holds(row_weight, rows, 4, "row_weight")
+    lead = (logits.data_ptr(), kind, rows, vocab, ld, _holds(t_idx, rows * k, "int32", "t_idx"), _holds(t_val, rows * k, "float32", "t_val"), k)
+    weight = 0 if row_weight is None else _holds(row_weight, rows, "float32", "row_weight")
     if grad is None:
         return lead, weight, 0, 0
     g_rows, g_vocab, ld_grad = _rows(grad, "grad")
@@ -456,8 +463,8 @@ def kimad_distill(logits, t_idx, t_val, temperature: float, loss=None, stats=Non
     against a teacher's top entries t_idx int32, t_val float32 [rows, k]; an output that is None is left out."""
     lead, weight, g, ld_grad = _distill_inputs(logits, t_idx, t_val, row_weight, grad)
     _, _, rows, vocab, _, _, _, k = lead
-    at_loss = 0 if loss is None else _holds(loss, rows, 4, "loss")
-    at_stats = 0 if stats is None else _holds(stats, 2 * rows, 4, "stats")
+    at_loss = 0 if loss is None else _holds(loss, rows, "float32", "loss")
+    at_stats = 0 if stats is None else _holds(stats, 2 * rows, "float32", "stats")
     _on_device(logits, t_idx, t_val, loss, stats, grad, row_weight, workspace)
     L = lib()
     ws = nbytes = 0
@@ -473,7 +480,7 @@ def kimad_distill(logits, t_idx, t_val, temperature: float, loss=None, stats=Non
 def kimad_distill_grad(logits, t_idx, t_val, temperature: float, stats, grad, row_weight=None, stream=None) -> None:
     """The gradient alone, from the statistics of an earlier kimad_distill."""
     lead, weight, g, ld_grad = _distill_inputs(logits, t_idx, t_val, row_weight, grad)
-    at = _holds(stats, 2 * lead[2], 4, "stats")
+    at = _holds(stats, 2 * lead[2], "float32", "stats")
     _on_device(logits, t_idx, t_val, stats, grad, row_weight)
     _check(lib().kimad_distill_grad(*lead, temperature, weight, at, g, ld_grad, _stream(stream)), "kimad_distill_grad")
 

@@ -220,3 +220,35 @@ def test_the_binding_refuses_parts_of_a_quantised_matrix_that_are_none():
                  lambda: kimad.kimad_mx4_matmul(codes, scales, other, other_scales, 400, product, stream=0)):
         with pytest.raises(ValueError, match="device tensors are wanted"):
             call()
+
+
+def test_the_binding_refuses_other_types_of_the_same_size():
+    import torch
+    x, idx, val = torch.zeros(4, 128), torch.zeros(4, 3, dtype=torch.int32), torch.zeros(4, 3)
+    codes, scales = kimad.mx4_empty(4, 128, "cpu")
+    starts, flat = torch.tensor([0, 512]), torch.zeros(512)
+    up = torch.zeros(5, 64, dtype=torch.uint8), torch.zeros(5, dtype=torch.int32)
+    whole, row, stats = torch.zeros(4, dtype=torch.int32), torch.zeros(4), torch.zeros(4, 2)
+    for call in (lambda: kimad.kimad_distill(x, val, val, 1.0, loss=row, stream=0),                        # entries' numbers as floats
+                 lambda: kimad.kimad_distill(x, idx, idx, 1.0, loss=row, stream=0),
+                 lambda: kimad.kimad_distill(x, idx, val, 1.0, loss=whole, stream=0),
+                 lambda: kimad.kimad_distill(x, idx, val, 1.0, stats=stats.int(), stream=0),
+                 lambda: kimad.kimad_distill(x, idx, val, 1.0, loss=row, row_weight=whole, stream=0),
+                 lambda: kimad.kimad_distill_grad(x, idx, val, 1.0, stats.int(), x.clone(), stream=0),
+                 lambda: kimad.kimad_mx4_quantise(x, codes.bool(), scales, stream=0),
+                 lambda: kimad.kimad_mx4_quantise(x, codes, scales.float(), stream=0),
+                 lambda: kimad.kimad_mx4_dequantise(codes, scales.float(), x, stream=0),
+                 lambda: kimad.kimad_mx4_matmul(codes, scales, codes.bool(), scales, 128, torch.zeros(4, 4), stream=0),
+                 lambda: kimad.kimad_mx4_compress_ef(flat.int(), flat, starts, *up, stream=0),
+                 lambda: kimad.kimad_mx4_compress_ef(flat, flat.int(), starts, *up, stream=0),
+                 lambda: kimad.kimad_mx4_compress_ef(flat, flat, starts.double(), *up, stream=0),
+                 lambda: kimad.kimad_mx4_compress_ef(flat, flat, starts, up[0].bool(), up[1], stream=0),
+                 lambda: kimad.kimad_mx4_compress_ef(flat, flat, starts, up[0], up[1].float(), stream=0),
+                 lambda: kimad.kimad_mx4_server_apply([up], [flat.int()], [1.0], starts, 512, stream=0),
+                 lambda: kimad.kimad_mx4_server_apply([up], [flat], [1.0], starts.double(), 512, stream=0),
+                 lambda: kimad.kimad_mx4_server_apply([up], [flat], [1.0], starts, 512, flat.int(), stream=0)):
+        with pytest.raises(ValueError, match="contiguous elements of"):
+            call()
+    # whole numbers without a sign are the same numbers
+    with pytest.raises(ValueError, match="device tensors are wanted"):
+        kimad.kimad_mx4_compress_ef(flat, flat.clone(), starts.to(torch.uint64), up[0], up[1].view(torch.uint32), stream=0)
