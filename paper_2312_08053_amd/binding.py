@@ -414,7 +414,7 @@ def kimad_mx4_compress_ef(g, h, layer_start, codes, scales, status_out=None, str
     d, L = g.numel(), layer_start.numel() - 1
     words = d // 128 + L
     args = (_holds(g, d, "float32", "g"), _holds(h, d, "float32", "h"), _holds(layer_start, 2, "int64", "layer_start"), L, d,
-            _holds(codes, words * 64, "uint8", "codes"), _holds(scales, words, "int32", "scales"), _ptr(status_out))
+            _holds(codes, words * 64, "uint8", "codes"), _holds(scales, words, "int32", "scales"), 0 if status_out is None else _holds(status_out, 1, "int32", "status_out"))
     _on_device(g, h, layer_start, codes, scales, status_out)
     _check(lib().kimad_mx4_compress_ef(*args, _stream(stream)), "kimad_mx4_compress_ef")
 
@@ -431,7 +431,8 @@ def kimad_mx4_server_apply(updates, u_hats, weights, layer_start, d: int, x=None
     for m, (codes, scales) in enumerate(updates):
         up[m].codes, up[m].scales = _holds(codes, words * 64, "uint8", "codes"), _holds(scales, words, "int32", "scales")
         uh[m] = _holds(u_hats[m], d, "float32", "u_hats")
-    args = (up, uh, w, M, _holds(layer_start, 2, "int64", "layer_start"), L, d, 0 if x is None else _holds(x, d, "float32", "x"), gamma, _ptr(status_out))
+    args = (up, uh, w, M, _holds(layer_start, 2, "int64", "layer_start"), L, d, 0 if x is None else _holds(x, d, "float32", "x"), gamma,
+            0 if status_out is None else _holds(status_out, 1, "int32", "status_out"))
     _on_device(layer_start, x, status_out, *u_hats, *(t for pair in updates for t in pair))
     _check(lib().kimad_mx4_server_apply(*args, _stream(stream)), "kimad_mx4_server_apply")
 

@@ -252,3 +252,14 @@ def test_the_binding_refuses_other_types_of_the_same_size():
     # whole numbers without a sign are the same numbers
     with pytest.raises(ValueError, match="device tensors are wanted"):
         kimad.kimad_mx4_compress_ef(flat, flat.clone(), starts.to(torch.uint64), up[0], up[1].view(torch.uint32), stream=0)
+
+
+def test_the_binding_refuses_a_status_that_is_no_int32():
+    import torch
+    starts, flat = torch.tensor([0, 512]), torch.zeros(512)
+    up = torch.zeros(5, 64, dtype=torch.uint8), torch.zeros(5, dtype=torch.int32)
+    for status in (torch.zeros(1, dtype=torch.uint8), torch.zeros(0, dtype=torch.int32), torch.zeros(1), torch.zeros(1, dtype=torch.int64)):
+        with pytest.raises(ValueError, match="status_out"):
+            kimad.kimad_mx4_compress_ef(flat, flat.clone(), starts, *up, status, stream=0)
+        with pytest.raises(ValueError, match="status_out"):
+            kimad.kimad_mx4_server_apply([up], [flat], [1.0], starts, 512, None, 0.0, status, stream=0)
