@@ -336,6 +336,15 @@ def _holds(t, count: int, kind: str, what: str) -> int:
     return t.data_ptr()
 
 
+def _room(workspace):
+    """Address and bytes of a workspace, a tensor of any type whose elements lie side by side; zeros without one."""
+    if workspace is None:
+        return 0, 0
+    if not workspace.is_contiguous():
+        raise ValueError(f"workspace: a contiguous tensor is wanted, got shape {tuple(workspace.shape)}, strides {workspace.stride()}")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
 def _on_device(*tensors) -> None:
     """Host memory is refused: a kernel that reads it faults."""
     for t in tensors:
@@ -392,15 +401,14 @@ def kimad_mx4_matmul(a_codes, a_scales, b_codes, b_scales, K: int, out, workspac
     a, sa = _holds_mx4(a_codes, a_scales, M, K, "A's codes and scales")
     b, sb = _holds_mx4(b_codes, b_scales, N, K, "B's codes and scales")
     kind = _type(out)
+    ws, nbytes = _room(workspace)
     _on_device(a_codes, a_scales, b_codes, b_scales, out, workspace)
     L = lib()
-    ws = nbytes = 0
     if workspace is None:
         nbytes = L.kimad_mx4_matmul_workspace_bytes(M, N, K)
         if nbytes:
             workspace = _scratch(nbytes, out.device, stream)
-    if workspace is not None:
-        ws, nbytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+            ws = workspace.data_ptr()
     _check(L.kimad_mx4_matmul(a, sa, M, b, sb, N, K, out.data_ptr(), kind, ld, ws, nbytes, _stream(stream)), "kimad_mx4_matmul")
 
 
@@ -466,15 +474,14 @@ def kimad_distill(logits, t_idx, t_val, temperature: float, loss=None, stats=Non
     _, _, rows, vocab, _, _, _, k = lead
     at_loss = 0 if loss is None else _holds(loss, rows, "float32", "loss")
     at_stats = 0 if stats is None else _holds(stats, 2 * rows, "float32", "stats")
+    ws, nbytes = _room(workspace)
     _on_device(logits, t_idx, t_val, loss, stats, grad, row_weight, workspace)
     L = lib()
-    ws = nbytes = 0
     if workspace is None:
         nbytes = L.kimad_distill_workspace_bytes(rows, vocab, k)
         if nbytes:
             workspace = _scratch(nbytes, logits.device, stream)
-    if workspace is not None:
-        ws, nbytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+            ws = workspace.data_ptr()
     _check(L.kimad_distill(*lead, temperature, weight, at_loss, at_stats, g, ld_grad, ws, nbytes, _stream(stream)), "kimad_distill")
 
 

@@ -263,3 +263,14 @@ def test_the_binding_refuses_a_status_that_is_no_int32():
             kimad.kimad_mx4_compress_ef(flat, flat.clone(), starts, *up, status, stream=0)
         with pytest.raises(ValueError, match="status_out"):
             kimad.kimad_mx4_server_apply([up], [flat], [1.0], starts, 512, None, 0.0, status, stream=0)
+
+
+def test_the_binding_refuses_a_workspace_with_less_memory_than_elements_or_gaps():
+    import torch
+    a, sa = kimad.mx4_empty(100, 16384, "cpu")
+    x, idx, val = torch.zeros(2, 70001), torch.zeros(2, 3, dtype=torch.int32), torch.zeros(2, 3)
+    for ws in (torch.zeros(1).expand(1 << 20), torch.zeros(1 << 12, 2)[:, 0]):
+        with pytest.raises(ValueError, match="workspace"):
+            kimad.kimad_mx4_matmul(a, sa, a, sa, 16384, torch.zeros(100, 100), workspace=ws, stream=0)
+        with pytest.raises(ValueError, match="workspace"):
+            kimad.kimad_distill(x, idx, val, 1.0, loss=torch.zeros(2), workspace=ws, stream=0)
