@@ -345,11 +345,26 @@ def _room(workspace):
     return workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
-def _on_device(*tensors) -> None:
-    """Host memory is refused: a kernel that reads it faults."""
+def _on_device(stream, *tensors) -> int:
+    """The handle of the stream that a call on these tensors (or None) goes to.  Host memory is refused, and memory of another device than the one that the
+    kernels run on: a kernel that reads it faults.  A given stream runs on its own device, the null stream and torch's current one on the
+    current device."""
+    where = None
     for t in tensors:
-        if t is not None and not t.is_cuda:
-            raise ValueError(f"device tensors are wanted, got one of shape {tuple(t.shape)} on {t.device}")
+        if t is not None:
+            device = t.get_device()
+            if device < 0:
+                raise ValueError(f"device tensors are wanted, got one of shape {tuple(t.shape)} on {t.device}")
+            if where is None:
+                where = device
+            elif device != where:
+                raise ValueError(f"tensors of one device are wanted, got devices {where} and {device}")
+    handle = _stream(stream)
+    if stream is None or handle == 0:
+        import torch
+        if where != torch.cuda.current_device():
+            raise ValueError(f"tensors of the current device are wanted, {torch.cuda.current_device()}, got device {where}")
+    return handle
 
 
 def _holds_mx4(codes, scales, rows: int, cols: int, what: str):
@@ -377,8 +392,8 @@ def kimad_mx4_quantise(x, codes=None, scales=None, codes_t=None, scales_t=None, 
     c, s = (0, 0) if codes is None else _holds_mx4(codes, scales, rows, cols, "codes and scales")
     ct, st = (0, 0) if codes_t is None else _holds_mx4(codes_t, scales_t, cols, rows, "codes_t and scales_t")
     kind = _type(x)
-    _on_device(x, codes, scales, codes_t, scales_t)
-    _check(lib().kimad_mx4_quantise(x.data_ptr(), kind, rows, cols, ld, c, s, ct, st, _stream(stream)), "kimad_mx4_quantise")
+    handle = _on_device(stream, x, codes, scales, codes_t, scales_t)
+    _check(lib().kimad_mx4_quantise(x.data_ptr(), kind, rows, cols, ld, c, s, ct, st, handle), "kimad_mx4_quantise")
 
 
 def kimad_mx4_dequantise(codes, scales, out, stream=None) -> None:
@@ -386,8 +401,8 @@ def kimad_mx4_dequantise(codes, scales, out, stream=None) -> None:
     rows, cols, ld = _rows(out, "out")
     c, s = _holds_mx4(codes, scales, rows, cols, "codes and scales")
     kind = _type(out)
-    _on_device(codes, scales, out)
-    _check(lib().kimad_mx4_dequantise(c, s, rows, cols, out.data_ptr(), kind, ld, _stream(stream)), "kimad_mx4_dequantise")
+    handle = _on_device(stream, codes, scales, out)
+    _check(lib().kimad_mx4_dequantise(c, s, rows, cols, out.data_ptr(), kind, ld, handle), "kimad_mx4_dequantise")
 
 
 def kimad_mx4_matmul_workspace_bytes(M: int, N: int, K: int) -> int:
@@ -402,14 +417,14 @@ def kimad_mx4_matmul(a_codes, a_scales, b_codes, b_scales, K: int, out, workspac
     b, sb = _holds_mx4(b_codes, b_scales, N, K, "B's codes and scales")
     kind = _type(out)
     ws, nbytes = _room(workspace)
-    _on_device(a_codes, a_scales, b_codes, b_scales, out, workspace)
+    handle = _on_device(stream, a_codes, a_scales, b_codes, b_scales, out, workspace)
     L = lib()
     if workspace is None:
         nbytes = L.kimad_mx4_matmul_workspace_bytes(M, N, K)
         if nbytes:
             workspace = _scratch(nbytes, out.device, stream)
             ws = workspace.data_ptr()
-    _check(L.kimad_mx4_matmul(a, sa, M, b, sb, N, K, out.data_ptr(), kind, ld, ws, nbytes, _stream(stream)), "kimad_mx4_matmul")
+    _check(L.kimad_mx4_matmul(a, sa, M, b, sb, N, K, out.data_ptr(), kind, ld, ws, nbytes, handle), "kimad_mx4_matmul")
 
 
 def kimad_mx4_update_words(L: int, d: int) -> int:
@@ -423,8 +438,8 @@ def kimad_mx4_compress_ef(g, h, layer_start, codes, scales, status_out=None, str
     words = d // 128 + L
     args = (_holds(g, d, "float32", "g"), _holds(h, d, "float32", "h"), _holds(layer_start, 2, "int64", "layer_start"), L, d,
             _holds(codes, words * 64, "uint8", "codes"), _holds(scales, words, "int32", "scales"), 0 if status_out is None else _holds(status_out, 1, "int32", "status_out"))
-    _on_device(g, h, layer_start, codes, scales, status_out)
-    _check(lib().kimad_mx4_compress_ef(*args, _stream(stream)), "kimad_mx4_compress_ef")
+    handle = _on_device(stream, g, h, layer_start, codes, scales, status_out)
+    _check(lib().kimad_mx4_compress_ef(*args, handle), "kimad_mx4_compress_ef")
 
 
 def kimad_mx4_server_apply(updates, u_hats, weights, layer_start, d: int, x=None, gamma: float = 0.0, status_out=None,
@@ -441,8 +456,8 @@ def kimad_mx4_server_apply(updates, u_hats, weights, layer_start, d: int, x=None
         uh[m] = _holds(u_hats[m], d, "float32", "u_hats")
     args = (up, uh, w, M, _holds(layer_start, 2, "int64", "layer_start"), L, d, 0 if x is None else _holds(x, d, "float32", "x"), gamma,
             0 if status_out is None else _holds(status_out, 1, "int32", "status_out"))
-    _on_device(layer_start, x, status_out, *u_hats, *(t for pair in updates for t in pair))
-    _check(lib().kimad_mx4_server_apply(*args, _stream(stream)), "kimad_mx4_server_apply")
+    handle = _on_device(stream, layer_start, x, status_out, *u_hats, *(t for pair in updates for t in pair))
+    _check(lib().kimad_mx4_server_apply(*args, handle), "kimad_mx4_server_apply")
 
 
 def kimad_distill_workspace_bytes(rows: int, vocab: int, k: int) -> int:
@@ -475,22 +490,22 @@ def kimad_distill(logits, t_idx, t_val, temperature: float, loss=None, stats=Non
     at_loss = 0 if loss is None else _holds(loss, rows, "float32", "loss")
     at_stats = 0 if stats is None else _holds(stats, 2 * rows, "float32", "stats")
     ws, nbytes = _room(workspace)
-    _on_device(logits, t_idx, t_val, loss, stats, grad, row_weight, workspace)
+    handle = _on_device(stream, logits, t_idx, t_val, loss, stats, grad, row_weight, workspace)
     L = lib()
     if workspace is None:
         nbytes = L.kimad_distill_workspace_bytes(rows, vocab, k)
         if nbytes:
             workspace = _scratch(nbytes, logits.device, stream)
             ws = workspace.data_ptr()
-    _check(L.kimad_distill(*lead, temperature, weight, at_loss, at_stats, g, ld_grad, ws, nbytes, _stream(stream)), "kimad_distill")
+    _check(L.kimad_distill(*lead, temperature, weight, at_loss, at_stats, g, ld_grad, ws, nbytes, handle), "kimad_distill")
 
 
 def kimad_distill_grad(logits, t_idx, t_val, temperature: float, stats, grad, row_weight=None, stream=None) -> None:
     """The gradient alone, from the statistics of an earlier kimad_distill."""
     lead, weight, g, ld_grad = _distill_inputs(logits, t_idx, t_val, row_weight, grad)
     at = _holds(stats, 2 * lead[2], "float32", "stats")
-    _on_device(logits, t_idx, t_val, stats, grad, row_weight)
-    _check(lib().kimad_distill_grad(*lead, temperature, weight, at, g, ld_grad, _stream(stream)), "kimad_distill_grad")
+    handle = _on_device(stream, logits, t_idx, t_val, stats, grad, row_weight)
+    _check(lib().kimad_distill_grad(*lead, temperature, weight, at, g, ld_grad, handle), "kimad_distill_grad")
 
 
 class Plan:

@@ -274,3 +274,28 @@ def test_the_binding_refuses_a_workspace_with_less_memory_than_elements_or_gaps(
             kimad.kimad_mx4_matmul(a, sa, a, sa, 16384, torch.zeros(100, 100), workspace=ws, stream=0)
         with pytest.raises(ValueError, match="workspace"):
             kimad.kimad_distill(x, idx, val, 1.0, loss=torch.zeros(2), workspace=ws, stream=0)
+
+
+class _Elsewhere:
+    """As much of a tensor as is asked where its memory is."""
+
+    def __init__(self, device):
+        self.index, self.shape, self.device, self.is_cuda = device, (4, 4), f"cuda:{device}", device >= 0
+
+    def get_device(self):
+        return self.index
+
+
+def test_the_binding_refuses_memory_of_another_device(monkeypatch):
+    import torch
+    from paper_2312_08053_amd import binding
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    here, there = _Elsewhere(1), _Elsewhere(0)
+    with pytest.raises(ValueError, match="one device"):
+        binding._on_device(0, here, None, there)
+    with pytest.raises(ValueError, match="current device"):
+        binding._on_device(0, there, there)
+    assert binding._on_device(0, here, None, here) == 0
+    assert binding._on_device(0x1234, there, there) == 0x1234      # a stream of that device, for all that a handle tells
+    with pytest.raises(ValueError, match="device tensors"):
+        binding._on_device(0, here, _Elsewhere(-1))
