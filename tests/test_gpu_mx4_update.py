@@ -205,3 +205,71 @@ def test_update_recorded_into_a_graph():
         torch.cuda.synchronize()
         assert torch.equal(h, h2) and torch.equal(hat, hat2) and torch.equal(x, x2)
         g.add_(0.25)
+
+
+def _apart(n, shift, gen, scale):
+    """Normal values times `scale`, `shift` elements into an allocation of their own."""
+    import torch
+    out = torch.empty(n + 8, device="cuda")[shift:shift + n]
+    out.copy_(torch.randn(n, generator=gen, device="cuda") * scale)
+    return out
+
+
+# Layers on cache lines and buffers too large for the cache (384 MiB) go by nontemporal accesses; the same values an element further go by ordinary ones.
+@pytest.mark.parametrize("M", [1, 3])
+def test_large_sets_on_cache_lines_give_what_they_give_off_them(M):
+    import torch
+    kimad = _kimad()
+    sizes = [32 * 5, 0, 128 * 1000, 32, 50_400_000, 32 * 77, 96 + 37]                 # the last word is partly filled
+    starts = _starts(sizes)
+    d, L = int(starts[-1]), len(sizes)
+    assert (starts[:-1] % 32 == 0).all() and 8 * d > 384 << 20
+    words = kimad.kimad_mx4_update_words(L, d)
+    st = torch.from_numpy(starts).cuda()
+    gen = torch.Generator(device="cuda").manual_seed(17 + M)
+    scale = torch.repeat_interleave(torch.tensor([1.0, 1.0, 1e-3, 4.0, 0.1, 1e-5, 2.0], device="cuda"), torch.tensor(sizes, device="cuda"))
+    g, h, x = (_apart(d, 0, gen, scale * f) for f in (1.0, 0.5, 0.1))
+    hats = [_apart(d, 0, gen, scale) for _ in range(M)]
+    for t in (g, h, x, *hats):
+        assert t.data_ptr() % 128 == 0
+    g[5], g[d - 1], g[3_000_000] = float("inf"), float("nan"), -float("inf")
+
+    def off(t):
+        return torch.empty(d + 8, device="cuda")[1:1 + d].copy_(t)
+
+    g0, h0 = g[:400].cpu().numpy(), h[:400].cpu().numpy()
+    tail = int(starts[-2])
+    g1, h1 = g[tail:].cpu().numpy(), h[tail:].cpu().numpy()
+    copies = off(g), off(h), off(x), [off(t) for t in hats]
+    sent = []
+    for gd, hd in ((g, h), copies[:2]):
+        codes = torch.full((words, 64), 0xEE, dtype=torch.uint8, device="cuda")
+        scales = torch.full((words,), -1, dtype=torch.int32, device="cuda")
+        status = torch.full((1,), -99, dtype=torch.int32, device="cuda")
+        kimad.kimad_mx4_compress_ef(gd, hd, st, codes, scales, status)
+        assert int(status.item()) == 0
+        sent.append((codes, scales))
+    assert torch.equal(sent[0][0], sent[1][0]) and torch.equal(sent[0][1], sent[1][1])
+    assert torch.equal(h.view(torch.int32), copies[1].clone().view(torch.int32))
+    # the first layers and the last one by the definition
+    _, _, want = ref.update(g0, h0, np.array([0, 160, 160, 400]))
+    assert _equal(h[:160].cpu().numpy(), want[:160]) and _equal(h[160:384].cpu().numpy(), want[160:384])
+    codes_t, bytes_t, want = ref.update(g1, h1, np.array([0, len(g1)]))
+    assert _equal(h[tail:].cpu().numpy(), want)
+    first = tail // 128 + L - 1
+    got_codes, got_bytes = ref.mx4_unpack(sent[0][0][first:].cpu().numpy(), _bits(sent[0][1])[first:][None, :])
+    assert np.array_equal(got_bytes[:2], bytes_t) and np.array_equal(ref.without_minus_zero(got_codes[:2]), ref.without_minus_zero(codes_t))
+    # the server, of which every worker sent the same
+    weights = [(1.0 + m) / 7 for m in range(M)]
+    before = [t[tail:].cpu().numpy() for t in hats], x[tail:].cpu().numpy()
+    kimad.kimad_mx4_server_apply([sent[0]] * M, hats, weights, st, d, x, 0.37)
+    kimad.kimad_mx4_server_apply([sent[1]] * M, copies[3], weights, st, d, copies[2], 0.37)
+    for a, b in zip([x, *hats], [copies[2], *copies[3]]):
+        assert torch.equal(a.view(torch.int32), b.clone().view(torch.int32))
+    q = ref.mx4_values(codes_t, bytes_t).reshape(-1)[:len(g1)].astype(np.float32)
+    total = np.zeros(len(g1))
+    for m in range(M):
+        want = before[0][m] + q
+        assert _equal(hats[m][tail:].cpu().numpy(), want)
+        total = total + weights[m] * want.astype(np.float64)
+    assert _equal(x[tail:].cpu().numpy(), (before[1].astype(np.float64) - 0.37 * total).astype(np.float32))
