@@ -285,3 +285,30 @@ def test_workspace_that_the_call_makes_stays_its_own_on_a_given_stream():
         loss.zero_()
         torch.cuda.synchronize()
         del others, busy
+
+
+# The longest rows of every kernel that holds them in registers, and a column more, as far off a 16-byte address as they may begin: not a group is to spare.
+@pytest.mark.parametrize("vocab", [505, 506, 1017, 1018, 2041, 2042, 4089, 4090, 8185, 8186, 16377, 16378, 32761, 32762, 53241, 53242, 60000, 65529, 65530])
+@pytest.mark.parametrize("kind", ["float32", "float16", "bfloat16"])
+def test_the_longest_rows_of_each_kernel(vocab, kind):
+    import torch
+    kimad = _kimad()
+    rows, k, T = 2, 20, 1.25
+    last = 16 // torch.empty(0, dtype=getattr(torch, kind)).element_size() - 1
+    for pad, offset in ((0, 0), ((-vocab) % 8, last)):                                # (the second: every row begins `last` elements in)
+        zd, idx, t, w = _inputs(rows, vocab, k, kind, vocab + offset, pad, offset)
+        idx[:, 0], w[:] = vocab - 1, (0.7, 1.3)
+        idx[:, 1:][idx[:, 1:] == vocab - 1] = 0
+        zd[0, vocab - 1], zd[1, 0] = 21.0, 21.0                                       # where a column left out would be seen
+        both = _run(zd, idx, t, T, w)
+        _check(zd, idx, t, T, w, both, kind)
+        forward = _run(zd, idx, t, T, w, grad=False)
+        assert torch.equal(forward["loss"], both["loss"]) and torch.equal(forward["stats"], both["stats"])
+        buf = torch.full((offset + rows * (vocab + pad) + 64,), 55.0, dtype=zd.dtype, device="cuda")
+        place = torch.as_strided(buf, (rows, vocab), (vocab + pad, 1), offset)
+        place.copy_(zd)
+        dev = torch.from_numpy(idx.astype(np.int32)).cuda(), torch.from_numpy(t).cuda()
+        kimad.kimad_distill(place, *dev, T, grad=place, row_weight=torch.from_numpy(w).cuda())
+        assert torch.equal(place, both["grad"])
+        place.fill_(55.0)
+        assert (buf == 55.0).all()                                                    # nothing around the rows was written
