@@ -375,3 +375,35 @@ def test_a_product_over_no_columns_is_zeros_at_every_size(M, N):
     out = torch.full((M, N), 3.0, device="cuda")
     kimad.kimad_mx4_matmul(a, sa, b, sb, 0, out)
     assert (_host(out) == 0).all()
+
+
+def test_every_rounding_case_at_scales_down_to_the_smallest_and_up_to_the_largest():
+    """All magnitudes, all ties and the numbers next to them, with both signs, through the conversions along rows, along columns, and of an update."""
+    import torch
+    kimad = _kimad()
+    ties = np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0])
+    blocks = []
+    for byte in (0, 1, 2, 23, 126, 127, 128, 251, 252):
+        scale = np.ldexp(1.0, byte - 127)
+        at = (ties * scale).astype(np.float32)
+        assert (at.astype(np.float64) == ties * scale).all()
+        v = np.concatenate([at, np.nextafter(at, np.float32(0)), np.nextafter(at, np.float32(np.inf)), (ref.MAGNITUDES * scale).astype(np.float32),
+                            (np.array([5.5, 7.0, 7.9375]) * scale).astype(np.float32)])
+        blocks += [v, -v]
+        assert ref.mx4_block(v.astype(np.float64))[1] == byte
+    x = np.stack(blocks)                                           # [18, 32]
+    codes, scales, _, _ = _quantise(torch.from_numpy(x).cuda())
+    _assert_form(codes, scales, x.astype(np.float64), "rows")
+    _, _, codes_t, scales_t = _quantise(torch.from_numpy(np.ascontiguousarray(x.T)).cuda(), False, True)
+    _assert_form(codes_t, scales_t, x.astype(np.float64), "columns")
+    out = torch.empty(18, 32, device="cuda")
+    kimad.kimad_mx4_dequantise(codes, scales, out)
+    assert np.array_equal(_host(out), ref.mx4_values(*ref.mx4_quantise(x.astype(np.float64)))[:, :32])
+    g, d = torch.from_numpy(x.reshape(-1)).cuda(), x.size
+    h, words = torch.zeros(d, device="cuda"), kimad.kimad_mx4_update_words(1, d)
+    up = torch.empty(words, 64, dtype=torch.uint8, device="cuda"), torch.empty(words, dtype=torch.int32, device="cuda")
+    kimad.kimad_mx4_compress_ef(g, h, torch.tensor([0, d], device="cuda"), *up)
+    want_codes, want_bytes, want_h = ref.update(x.reshape(-1), np.zeros(d, np.float32), np.array([0, d]))
+    got_codes, got_bytes = ref.mx4_unpack(up[0].cpu().numpy(), _words(up[1])[None, :])
+    assert np.array_equal(got_bytes, want_bytes) and np.array_equal(ref.without_minus_zero(got_codes), ref.without_minus_zero(want_codes))
+    assert np.array_equal(h.cpu().numpy(), want_h)
