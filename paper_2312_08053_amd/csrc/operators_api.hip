@@ -361,7 +361,9 @@ int kimad_distill(const void* logits, uint32_t type, uint64_t rows, uint64_t voc
         // Small workgroups with many groups a thread, for more of a row's phases run beside one another, as long as the registers leave two
         // workgroups a compute unit: loss and gradient, us, rows of 4000 elements by 64, 128 and 256 threads 35, 41, 51 (16 bits; 32 bits 62, 68, 69), of 8000
         // by 128 and 256 61, 64 (129, 114), of 12000 by 128 and 256 98, 87 (182, 167), of 32000 by 256 and 512 116, 109 (219, 208), of 50257 by 512 and
-        // 1024 335, 402 (by 512 with 32 bits: scratch memory).
+        // 1024 335, 402 (by 512 with 32 bits: scratch memory).  By 512 threads, up to ten groups a thread leave registers for a third workgroup, which
+        // helps shorter rows: with room for 10 and for 16 groups a thread 8192 rows of 34000 elements 222, 249, of 36000 231, 250, of 38000 250, 266, of 40953 264, 273;
+        // with room for 13 and for 16 of 42000 279, 279, of 44000 293, 287, of 48000 319, 309, of 53241 353, 330.
         constexpr bool WIDE = TYPE == TYPE_F32;
         if (groups <= 64) return launch_row<TYPE, 64, 1>(a, s);
         if (groups <= 128) return launch_row<TYPE, 64, 2>(a, s);
@@ -370,7 +372,7 @@ int kimad_distill(const void* logits, uint32_t type, uint64_t rows, uint64_t voc
         if (groups <= 1024) return launch_row<TYPE, WIDE ? 256 : 128, WIDE ? 4 : 8>(a, s);
         if (groups <= 2048) return launch_row<TYPE, 256, 8>(a, s);
         if (groups <= 4096) return launch_row<TYPE, 512, 8>(a, s);
-        if (!WIDE && groups <= 512 * 13) return launch_row<TYPE, WIDE ? 1024 : 512, WIDE ? 8 : 13>(a, s);
+        if (!WIDE && groups <= 512 * 10) return launch_row<TYPE, WIDE ? 1024 : 512, WIDE ? 8 : 10>(a, s);
         return launch_row<TYPE, WIDE ? 1024 : 512, WIDE ? 8 : 16>(a, s);
     });
 }

@@ -312,3 +312,9 @@ def test_the_longest_rows_of_each_kernel(vocab, kind):
         assert torch.equal(place, both["grad"])
         place.fill_(55.0)
         assert (buf == 55.0).all()                                                    # nothing around the rows was written
+
+
+@pytest.mark.parametrize("vocab", [40953, 40954])
+@pytest.mark.parametrize("kind", ["float32", "float16", "bfloat16"])
+def test_the_longest_rows_of_ten_groups_a_thread(vocab, kind):
+    test_the_longest_rows_of_each_kernel(vocab, kind)
