@@ -25,7 +25,7 @@ __global__ __launch_bounds__(256) void k_mx4_quantise_rows(const void* __restric
         for (uint32_t i = 0; i < QU; ++i) {
             const uint32_t u = u0 + 16u * i, r = u / nw, w = u - r * nw;
             const uint64_t col = (word0 + w) * MX4_WORD + 8u * lane16;
-            raw[i] = load8_first<TYPE>(x, (row0 + r) * ld + col, u < units ? (int64_t)cols - (int64_t)col : 0, 0u);
+            raw[i] = load8_first<TYPE>(x, (row0 + r) * ld + col, u < units ? (int64_t)cols - (int64_t)col : 0);
         }
 #pragma unroll
         for (uint32_t i = 0; i < QU; ++i) {
@@ -68,7 +68,7 @@ __global__ __launch_bounds__(256) void k_mx4_quantise_both(const void* __restric
 #pragma unroll
     for (uint32_t p = 0; p < 8; ++p) {
         const uint64_t row = row0 + 16u * p + g;
-        raw[p] = load8_first<TYPE>(x, row * ld + col0 + 8u * lane16, row < rows ? have : 0, 0u);
+        raw[p] = load8_first<TYPE>(x, row * ld + col0 + 8u * lane16, row < rows ? have : 0);
     }
 #pragma unroll
     for (uint32_t p = 0; p < 8; ++p) {

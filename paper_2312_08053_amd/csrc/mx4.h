@@ -70,16 +70,16 @@ __device__ __forceinline__ Raw8<TYPE> load8(const void* p, uint64_t i) {
     }
     return v;
 }
-// The first `n` of eight elements (n may be 0 or more than 8); the others become `fill` (a bit pattern of the type).
+// The first `n` of eight elements (n may be below 0 or more than 8); the others become zeros.
 template <uint32_t TYPE>
-__device__ __forceinline__ Raw8<TYPE> load8_first(const void* p, uint64_t i, int64_t n, uint32_t fill) {
+__device__ __forceinline__ Raw8<TYPE> load8_first(const void* p, uint64_t i, int64_t n) {
     if (n >= 8) return load8<TYPE>(p, i);
     Raw8<TYPE> v;
 #pragma unroll
     for (uint32_t k = 0; k < sizeof(v.r) / 4; ++k) v.r[k] = 0;
 #pragma unroll
     for (uint32_t k = 0; k < 8; ++k) {
-        uint32_t b = fill;
+        uint32_t b = 0;
         if ((int64_t)k < n) b = TYPE == TYPE_F32 ? static_cast<const uint32_t*>(p)[i + k] : (uint32_t)static_cast<const uint16_t*>(p)[i + k];
         v.set(k, b);
     }
