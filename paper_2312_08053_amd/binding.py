@@ -147,19 +147,23 @@ def _ptr(t) -> int:
     return 0 if t is None else int(t.data_ptr())
 
 
-_raw_stream = None
+_cuda = _current_stream = None                                  # torch.cuda, and the handle of a device's current stream
+
+
+def _with_torch() -> None:
+    global _cuda, _current_stream
+    import torch
+    _cuda = torch.cuda
+    # (the same number without an object around it)
+    _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: int(torch.cuda.current_stream(device).cuda_stream))
 
 
 def _stream(stream) -> int:
-    global _raw_stream
     if stream is not None:
         return int(getattr(stream, "cuda_stream", stream))
-    if _raw_stream is None:
-        import torch
-        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # the same number without an object around it
-        _raw_stream = ((lambda: raw(torch.cuda.current_device())) if raw is not None
-                       else lambda: int(torch.cuda.current_stream().cuda_stream))
-    return _raw_stream()
+    if _cuda is None:
+        _with_torch()
+    return _current_stream(_cuda.current_device())
 
 
 def _scratch(nbytes: int, device, stream):
@@ -321,17 +325,21 @@ def _rows(t, what: str):
     raise ValueError(f"{what}: a matrix with contiguous rows is wanted, got shape {tuple(shape)}, strides {strides}")
 
 
-_KINDS = {}
+class _Kinds(dict):
+    def __missing__(self, dtype):
+        import torch
+        self.update({torch.float32: "float32", torch.int32: "int32", torch.uint32: "int32", torch.int64: "int64", torch.uint64: "int64",
+                     torch.uint8: "uint8"})
+        return self.setdefault(dtype, None)
+
+
+_KINDS = _Kinds()                                                # torch is not imported before a tensor is there
 
 
 def _holds(t, count: int, kind: str, what: str) -> int:
     """The address of a contiguous tensor of at least `count` elements of a kind: "float32", or "int32", "int64", "uint8", the whole numbers
     of so many bits (of the two larger ones, unsigned ones too)."""
-    if not _KINDS:
-        import torch
-        _KINDS.update({torch.float32: "float32", torch.int32: "int32", torch.uint32: "int32", torch.int64: "int64", torch.uint64: "int64",
-                       torch.uint8: "uint8"})
-    if _KINDS.get(t.dtype) != kind or t.numel() < count or not t.is_contiguous():
+    if _KINDS[t.dtype] != kind or t.numel() < count or not t.is_contiguous():
         raise ValueError(f"{what}: {count} contiguous elements of {kind} are wanted, got {t.numel()} of {t.dtype}, strides {t.stride()}")
     return t.data_ptr()
 
@@ -353,25 +361,31 @@ def _on_device(stream, *tensors) -> int:
     for t in tensors:
         if t is not None:
             device = t.get_device()
-            if device < 0:
-                raise ValueError(f"device tensors are wanted, got one of shape {tuple(t.shape)} on {t.device}")
-            if where is None:
+            if device != where:
+                if device < 0:
+                    raise ValueError(f"device tensors are wanted, got one of shape {tuple(t.shape)} on {t.device}")
+                if where is not None:
+                    raise ValueError(f"tensors of one device are wanted, got devices {where} and {device}")
                 where = device
-            elif device != where:
-                raise ValueError(f"tensors of one device are wanted, got devices {where} and {device}")
-    handle = _stream(stream)
-    if stream is None or handle == 0:
-        import torch
-        if where != torch.cuda.current_device():
-            raise ValueError(f"tensors of the current device are wanted, {torch.cuda.current_device()}, got device {where}")
-    return handle
+    if stream is not None:
+        handle = _stream(stream)
+        if handle:
+            return handle
+    if _cuda is None:
+        _with_torch()
+    if where != _cuda.current_device():
+        raise ValueError(f"tensors of the current device are wanted, {_cuda.current_device()}, got device {where}")
+    return _current_stream(where) if stream is None else handle
 
 
 def _holds_mx4(codes, scales, rows: int, cols: int, what: str):
     """The addresses of a quantised matrix.  Its codes and scales have its own shape: both are laid out by it, so that a part of a
     larger matrix's is no smaller matrix.  One-dimensional ones are buffers with room for it, as through the C call."""
     words = (cols + 127) // 128
-    if (codes.shape != (rows, 64 * words) and codes.dim() != 1) or (scales.shape != (words, rows) and scales.dim() != 1):
+    if codes.shape == (rows, 64 * words) and scales.shape == (words, rows):
+        if _KINDS[codes.dtype] == "uint8" and _KINDS[scales.dtype] == "int32" and codes.is_contiguous() and scales.is_contiguous():
+            return codes.data_ptr(), scales.data_ptr()
+    elif codes.dim() != 1 or scales.dim() != 1:
         raise ValueError(f"{what}: shapes {(rows, 64 * words)} and {(words, rows)} are wanted, got {tuple(codes.shape)} and {tuple(scales.shape)}")
     return _holds(codes, rows * words * 64, "uint8", what), _holds(scales, rows * words, "int32", what)
 
@@ -393,7 +407,9 @@ def kimad_mx4_quantise(x, codes=None, scales=None, codes_t=None, scales_t=None, 
     ct, st = (0, 0) if codes_t is None else _holds_mx4(codes_t, scales_t, cols, rows, "codes_t and scales_t")
     kind = _type(x)
     handle = _on_device(stream, x, codes, scales, codes_t, scales_t)
-    _check(lib().kimad_mx4_quantise(x.data_ptr(), kind, rows, cols, ld, c, s, ct, st, handle), "kimad_mx4_quantise")
+    rc = lib().kimad_mx4_quantise(x.data_ptr(), kind, rows, cols, ld, c, s, ct, st, handle)
+    if rc:
+        _check(rc, "kimad_mx4_quantise")
 
 
 def kimad_mx4_dequantise(codes, scales, out, stream=None) -> None:
@@ -402,7 +418,9 @@ def kimad_mx4_dequantise(codes, scales, out, stream=None) -> None:
     c, s = _holds_mx4(codes, scales, rows, cols, "codes and scales")
     kind = _type(out)
     handle = _on_device(stream, codes, scales, out)
-    _check(lib().kimad_mx4_dequantise(c, s, rows, cols, out.data_ptr(), kind, ld, handle), "kimad_mx4_dequantise")
+    rc = lib().kimad_mx4_dequantise(c, s, rows, cols, out.data_ptr(), kind, ld, handle)
+    if rc:
+        _check(rc, "kimad_mx4_dequantise")
 
 
 def kimad_mx4_matmul_workspace_bytes(M: int, N: int, K: int) -> int:
@@ -424,7 +442,9 @@ def kimad_mx4_matmul(a_codes, a_scales, b_codes, b_scales, K: int, out, workspac
         if nbytes:
             workspace = _scratch(nbytes, out.device, stream)
             ws = workspace.data_ptr()
-    _check(L.kimad_mx4_matmul(a, sa, M, b, sb, N, K, out.data_ptr(), kind, ld, ws, nbytes, handle), "kimad_mx4_matmul")
+    rc = L.kimad_mx4_matmul(a, sa, M, b, sb, N, K, out.data_ptr(), kind, ld, ws, nbytes, handle)
+    if rc:
+        _check(rc, "kimad_mx4_matmul")
 
 
 def kimad_mx4_update_words(L: int, d: int) -> int:
@@ -437,9 +457,12 @@ def kimad_mx4_compress_ef(g, h, layer_start, codes, scales, status_out=None, str
     d, L = g.numel(), layer_start.numel() - 1
     words = d // 128 + L
     args = (_holds(g, d, "float32", "g"), _holds(h, d, "float32", "h"), _holds(layer_start, 2, "int64", "layer_start"), L, d,
-            _holds(codes, words * 64, "uint8", "codes"), _holds(scales, words, "int32", "scales"), 0 if status_out is None else _holds(status_out, 1, "int32", "status_out"))
+            _holds(codes, words * 64, "uint8", "codes"), _holds(scales, words, "int32", "scales"),
+            0 if status_out is None else _holds(status_out, 1, "int32", "status_out"))
     handle = _on_device(stream, g, h, layer_start, codes, scales, status_out)
-    _check(lib().kimad_mx4_compress_ef(*args, handle), "kimad_mx4_compress_ef")
+    rc = lib().kimad_mx4_compress_ef(*args, handle)
+    if rc:
+        _check(rc, "kimad_mx4_compress_ef")
 
 
 def kimad_mx4_server_apply(updates, u_hats, weights, layer_start, d: int, x=None, gamma: float = 0.0, status_out=None,
@@ -451,13 +474,17 @@ def kimad_mx4_server_apply(updates, u_hats, weights, layer_start, d: int, x=None
     if len(updates) != M or len(weights) != M:
         raise ValueError(f"{M} estimators, {len(updates)} updates and {len(weights)} weights")
     up, uh, w = (_Mx4Update * M)(), (C.c_void_p * M)(), (C.c_double * M)(*weights)
+    tensors = [layer_start, x, status_out, *u_hats]
     for m, (codes, scales) in enumerate(updates):
+        tensors += (codes, scales)
         up[m].codes, up[m].scales = _holds(codes, words * 64, "uint8", "codes"), _holds(scales, words, "int32", "scales")
         uh[m] = _holds(u_hats[m], d, "float32", "u_hats")
     args = (up, uh, w, M, _holds(layer_start, 2, "int64", "layer_start"), L, d, 0 if x is None else _holds(x, d, "float32", "x"), gamma,
             0 if status_out is None else _holds(status_out, 1, "int32", "status_out"))
-    handle = _on_device(stream, layer_start, x, status_out, *u_hats, *(t for pair in updates for t in pair))
-    _check(lib().kimad_mx4_server_apply(*args, handle), "kimad_mx4_server_apply")
+    handle = _on_device(stream, *tensors)
+    rc = lib().kimad_mx4_server_apply(*args, handle)
+    if rc:
+        _check(rc, "kimad_mx4_server_apply")
 
 
 def kimad_distill_workspace_bytes(rows: int, vocab: int, k: int) -> int:
@@ -468,9 +495,10 @@ def _distill_inputs(logits, t_idx, t_val, row_weight, grad):
     """The leading arguments of both calls, and the trailing ones for row_weight and grad."""
     rows, vocab, ld = _rows(logits, "logits")
     kind = _type(logits)
-    k = t_idx.shape[1] if t_idx.dim() == 2 else -1
-    if t_idx.shape != (rows, k) or t_val.shape != (rows, k):
-        raise ValueError(f"entries: [rows, k] is wanted twice, got {tuple(t_idx.shape)} and {tuple(t_val.shape)} for {rows} rows")
+    shape = t_idx.shape
+    if len(shape) != 2 or shape[0] != rows or t_val.shape != shape:
+        raise ValueError(f"entries: [rows, k] is wanted twice, got {tuple(shape)} and {tuple(t_val.shape)} for {rows} rows")
+    k = shape[1]
     lead = (logits.data_ptr(), kind, rows, vocab, ld, _holds(t_idx, rows * k, "int32", "t_idx"), _holds(t_val, rows * k, "float32", "t_val"), k)
     weight = 0 if row_weight is None else _holds(row_weight, rows, "float32", "row_weight")
     if grad is None:
@@ -497,7 +525,9 @@ def kimad_distill(logits, t_idx, t_val, temperature: float, loss=None, stats=Non
         if nbytes:
             workspace = _scratch(nbytes, logits.device, stream)
             ws = workspace.data_ptr()
-    _check(L.kimad_distill(*lead, temperature, weight, at_loss, at_stats, g, ld_grad, ws, nbytes, handle), "kimad_distill")
+    rc = L.kimad_distill(*lead, temperature, weight, at_loss, at_stats, g, ld_grad, ws, nbytes, handle)
+    if rc:
+        _check(rc, "kimad_distill")
 
 
 def kimad_distill_grad(logits, t_idx, t_val, temperature: float, stats, grad, row_weight=None, stream=None) -> None:
@@ -505,7 +535,9 @@ def kimad_distill_grad(logits, t_idx, t_val, temperature: float, stats, grad, ro
     lead, weight, g, ld_grad = _distill_inputs(logits, t_idx, t_val, row_weight, grad)
     at = _holds(stats, 2 * lead[2], "float32", "stats")
     handle = _on_device(stream, logits, t_idx, t_val, stats, grad, row_weight)
-    _check(lib().kimad_distill_grad(*lead, temperature, weight, at, g, ld_grad, handle), "kimad_distill_grad")
+    rc = lib().kimad_distill_grad(*lead, temperature, weight, at, g, ld_grad, handle)
+    if rc:
+        _check(rc, "kimad_distill_grad")
 
 
 class Plan:
