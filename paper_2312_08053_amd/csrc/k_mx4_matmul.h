@@ -62,9 +62,10 @@ __device__ __forceinline__ void tile_of(uint32_t id, uint32_t tm, uint32_t tn, u
 // A tile of BM by BN, WM by WN waves.  Two words of K are a stage, of which LDS holds two: codes (128 bytes a row, whole cache lines: a word at a time, four
 // stages, took 8 % longer) and scale words.  The blocks of a row are stored in an order that turns with the row (block b of row r at b ^ (r / 2 % 8)), so
 // that sixteen lanes that read one block of sixteen rows meet sixteen different groups of banks.
-// Bound by the loads of a compute unit, some 25 bytes a clock however they are made (K = 16384, a tile of 256 a unit, 64 stages: loads alone 78 us, products
-// alone 87, reads of LDS alone 43, all 117 where the codes are zeros), and by power where they are not (150 us).  8192 x 5632 x 2048 into bfloat16
-// 60 to 63 us by machine, 3.0 to 3.1 PFLOP/s; 50257 x 768 x 8192 into fp32 192 to 205 us, 3.1 to 3.3.
+// What bounds it: K = 16384, a tile of 256 a unit, 64 stages take a unit 220 thousand cycles by the counters, of which its matrix cores work in 131 thousand.  The loads
+// alone (a copy of the kernel without products) took some 187 thousand, 25 bytes a clock however they are made, reads of LDS alone 100: the loads, and
+// what of the products is not hidden beside them.  On codes of zero these cycles run at 2.5 GHz, 98 us, on random ones at 1.95, 130 us: that much is
+// the power limit's.  8192 x 5632 x 2048 into bfloat16 60 to 65 us by machine, 2.9 to 3.1 PFLOP/s; 50257 x 768 x 8192 into fp32 187 to 205 us, 3.1 to 3.4.
 template <uint32_t BM_, uint32_t BN_, uint32_t WM_, uint32_t WN_>
 struct MatmulTile {
     static constexpr uint32_t BM = BM_, BN = BN_, WM = WM_, WN = WN_;

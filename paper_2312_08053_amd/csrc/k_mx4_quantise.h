@@ -8,7 +8,7 @@ namespace kimad {
 constexpr uint32_t QROWS = 16, QWORDS = 8;    // rows and words of a workgroup's share
 constexpr uint32_t QU = 4;                   // words of a lane under way together
 
-// Along rows: a workgroup takes 16 rows of up to 64 words.  Its sixteen groups of sixteen lanes walk row by row through the share, so
+// Along rows: a workgroup takes 16 rows of up to eight words.  Its sixteen groups of sixteen lanes walk row by row through the share, so
 // that reads and codes run on without gaps; the scale words, whose neighbours in memory are other rows' words, are collected in LDS
 // and leave in runs of 16.  Bound by memory: 50257 x 768
 // in fp32 40 us, 4.4 TB/s, 8192 x 2048 in bfloat16 9.7 us.  (Shares of 4, 8, 16 and 64 words, 256 x 2048: 3.0, 5.4, 6.8 and 6.8 us; 8192 x 2048: 11.2, 9.7, 10.0, 10.0.)
