@@ -385,7 +385,7 @@ def _holds_mx4(codes, scales, rows: int, cols: int, what: str):
     if codes.shape == (rows, 64 * words) and scales.shape == (words, rows):
         if _KINDS[codes.dtype] == "uint8" and _KINDS[scales.dtype] == "int32" and codes.is_contiguous() and scales.is_contiguous():
             return codes.data_ptr(), scales.data_ptr()
-    elif codes.dim() != 1 or scales.dim() != 1:
+    elif (codes.shape != (rows, 64 * words) and codes.dim() != 1) or (scales.shape != (words, rows) and scales.dim() != 1):
         raise ValueError(f"{what}: shapes {(rows, 64 * words)} and {(words, rows)} are wanted, got {tuple(codes.shape)} and {tuple(scales.shape)}")
     return _holds(codes, rows * words * 64, "uint8", what), _holds(scales, rows * words, "int32", what)
 

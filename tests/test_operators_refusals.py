@@ -299,3 +299,15 @@ def test_the_binding_refuses_memory_of_another_device(monkeypatch):
     assert binding._on_device(0x1234, there, there) == 0x1234      # a stream of that device, for all that a handle tells
     with pytest.raises(ValueError, match="device tensors"):
         binding._on_device(0, here, _Elsewhere(-1))
+
+
+def test_the_binding_takes_either_part_of_a_quantised_matrix_flat():
+    import torch
+    codes, scales = kimad.mx4_empty(100, 512, "cpu")
+    out = torch.zeros(100, 512)
+    for pair in ((codes, scales), (codes.view(-1), scales), (codes, scales.view(-1)), (codes.view(-1), scales.view(-1))):
+        with pytest.raises(ValueError, match="device tensors are wanted"):       # all that is wrong with them
+            kimad.kimad_mx4_dequantise(*pair, out, stream=0)
+    for pair in ((codes.view(-1)[1:], scales), (codes, scales.view(-1)[1:])):
+        with pytest.raises(ValueError, match="contiguous elements of"):
+            kimad.kimad_mx4_dequantise(*pair, out, stream=0)
