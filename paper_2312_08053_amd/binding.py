@@ -399,7 +399,8 @@ def mx4_empty(rows: int, cols: int, device="cuda"):
 
 
 def kimad_mx4_quantise(x, codes=None, scales=None, codes_t=None, scales_t=None, stream=None) -> None:
-    """x [rows, cols] along rows into codes, scales, along columns into codes_t, scales_t (each pair from mx4_empty, or None)."""
+    """x [rows, cols] along rows into codes, scales, along columns into codes_t, scales_t (each pair from mx4_empty for
+    that shape, or flat buffers with room for it, or None)."""
     rows, cols, ld = _rows(x, "x")
     if (codes is None) != (scales is None) or (codes_t is None) != (scales_t is None):
         raise ValueError("codes and scales are wanted together")
