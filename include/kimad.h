@@ -467,6 +467,80 @@ int kimad_distill_grad(const void* logits, uint32_t type, uint64_t rows, uint64_
                        const float* t_val, uint32_t k, float temperature, const float* row_weight, const float* stats, void* grad,
                        uint64_t ld_grad, void* stream);
 
+/* ---- Layers in front of a loss: a linear layer, the cross entropy of a linear head, dropout ----------------------------------
+ *
+ * As for the operators above: no call allocates, waits or needs a plan, and all may be recorded into a HIP graph; arrays that are
+ * read must not overlap arrays that are written, but where stated; every array is aligned like its elements.  `type` is that of
+ * the operands, KIMAD_VALUES_F16 or _BF16 (the matrix cores' types; the dropout takes _F32 too); sums are fp32 and rounded once,
+ * where they are stored.  Matrices have contiguous rows, `ld` elements apart: at most 2^22 for operands of a product, 2^24 for its
+ * results and what is added to them.  At most 8388480 rows (tokens), 2^22 features, and fewer than 2^34 elements a matrix, its columns counted as seven more; more are
+ * refused.  Operands are read fastest where they begin at 16-byte addresses, ld is a multiple of 8 and so are the features; others
+ * are laid out anew in the workspace first, but for up to 32 rows of a forward product.
+ *   workspace   DEVICE, 16-byte aligned, as many bytes as the call's own ..._workspace_bytes says for the same arguments (of the pointers,
+ *               which may be NULL there for 16-byte aligned ones, only the alignment counts); a smaller one is refused
+ *               (KIMAD_ERR_WORKSPACE_TOO_SMALL), 0 bytes need none.  Its contents need not be kept between calls; calls
+ *               that may run at the same time need one each, and so do graphs that may.
+ *   wants       which gradients are asked for: a sum of KIMAD_WANT_... */
+#define KIMAD_ACT_NONE 0u
+#define KIMAD_ACT_RELU 1u
+#define KIMAD_ACT_GELU 2u               /* z / (1 + exp(-2 sqrt(2 / pi) (z + 0.044715 z^3))), the tanh form */
+#define KIMAD_ACT_SILU 3u               /* z / (1 + exp(-z)) */
+#define KIMAD_WANT_DX 1u
+#define KIMAD_WANT_DW 2u
+#define KIMAD_WANT_DB 4u
+
+/* A linear layer:  z = x w^T + bias,  out = act(z) + residual.
+ *   x         DEVICE [M, K];  w  DEVICE [N, K]
+ *   bias      DEVICE [N] of `type`, or NULL;  residual  DEVICE [M, N] of `type`, or NULL; may be out itself (of the same type and ld)
+ *   z         DEVICE [M, N] of `type`, or NULL: z rounded, for the gradient
+ *   out       DEVICE [M, N] of out_type, `type` or KIMAD_VALUES_F32
+ * The activation is of z in fp32; of an infinite z it is its limit.  K = 0 leaves bias, activation and residual. */
+uint64_t kimad_linear_workspace_bytes(const void* x, uint64_t ld_x, const void* w, uint64_t ld_w, uint64_t M, uint64_t N, uint64_t K);
+int kimad_linear(const void* x, uint64_t ld_x, const void* w, uint64_t ld_w, uint32_t type, uint64_t M, uint64_t N, uint64_t K,
+                 const void* bias, const void* residual, uint64_t ld_residual, uint32_t act, void* z, uint64_t ld_z, void* out,
+                 uint32_t out_type, uint64_t ld_out, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* Its gradient:  dz = dy act'(z),  dx = dz w,  dw = dz^T x,  db = the sum of dz's rows (the residual's gradient is dy itself).
+ *   dy        DEVICE [M, N] of `type`;  z  as kimad_linear left it (not read without an activation)
+ *   dx        DEVICE [M, K] of `type`, or NULL (then w is not read)
+ *   dw        DEVICE [N, K] of dw_type, `type` or KIMAD_VALUES_F32 (what a round compresses), or NULL (then x is not read)
+ *   db        DEVICE float[N], or NULL
+ * With an activation dz is rounded to `type` before the two products, not for db.  The slope of relu at 0 is 0.  Sums over no rows are 0. */
+uint64_t kimad_linear_grad_workspace_bytes(const void* dy, uint64_t ld_dy, const void* x, uint64_t ld_x, const void* w, uint64_t ld_w,
+                                           uint64_t M, uint64_t N, uint64_t K, uint32_t act, uint32_t wants);
+int kimad_linear_grad(const void* dy, uint64_t ld_dy, const void* x, uint64_t ld_x, const void* w, uint64_t ld_w, const void* z,
+                      uint64_t ld_z, uint32_t type, uint64_t M, uint64_t N, uint64_t K, uint32_t act, void* dx, uint64_t ld_dx,
+                      void* dw, uint32_t dw_type, uint64_t ld_dw, float* db, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* Softmax cross entropy of a linear head, loss and gradient in one call, without its logits z = x w^T being kept:
+ *     lse[r]  = ln sum_v exp(z[r, v])           loss[r] = row_weight[r] (lse[r] - z[r, target[r]])
+ *     G[r, v] = row_weight[r] (exp(z[r, v] - lse[r]) - (v == target[r]))     dx = G w     dw = G^T x
+ *   x           DEVICE [rows, dim];  w  DEVICE [vocab, dim];  vocab and dim at least 1, vocab at most 2^22 - 64
+ *   target      DEVICE int32[rows]; one below 0 or of vocab or more is none: the row does not count
+ *   row_weight  DEVICE float[rows] or NULL (1); 0: the row does not count.  What comes back from above is multiplied into it
+ *   loss, lse   DEVICE float[rows] or NULL
+ *   dx          DEVICE [rows, dim] of `type`, or NULL;  dw  DEVICE [vocab, dim] of dw_type, `type` or KIMAD_VALUES_F32, or NULL
+ * At least one output is wanted, unless there are no rows (then dw is 0).  A row that does not count has loss, lse and gradient 0, adds
+ * nothing to dw, and what it holds, Inf and NaN too, reaches nothing.  So does a row whose logits are all -Inf.  For a gradient the
+ * exponentials of a piece of the rows are kept, 512 MiB at most or 256 rows, and G, both in `type`: gradients are as exact
+ * as ones whose G is rounded twice.  (fp16: G is scaled by a power of two, so that weights need not be.) */
+uint64_t kimad_linear_xent_workspace_bytes(const void* x, uint64_t ld_x, const void* w, uint64_t ld_w, uint32_t type, uint64_t rows,
+                                           uint64_t vocab, uint64_t dim, uint32_t wants, uint32_t dw_type);
+int kimad_linear_xent(const void* x, uint64_t ld_x, const void* w, uint64_t ld_w, uint32_t type, uint64_t rows, uint64_t vocab,
+                      uint64_t dim, const int32_t* target, const float* row_weight, float* loss, float* lse, void* dx,
+                      uint64_t ld_dx, void* dw, uint32_t dw_type, uint64_t ld_dw, void* workspace, uint64_t workspace_bytes,
+                      void* stream);
+
+/* Dropout whose mask is never stored:  out[i] = residual[i] + (keep_i ? x[i] / (1 - p) : 0), i counting along the rows, r * cols + c.
+ * keep_i is decided by 16 bits: half i % 2 (0 the lower) of word (i / 2) % 4 of the Philox 4x32-10 block with key `seed` and counter
+ * (i / 8, offset), low words first; dropped where they are below floor(65536 p + 1/2), so that p counts in steps of 2^-16 and 1 - p is
+ * that of the p so rounded.  The gradient with regard to x is the same call on dy with the same p, seed and offset and no residual.
+ *   x, out      DEVICE [rows, cols] of `type` (fp32 too), rows ld, ld_out apart; residual the same or NULL.  out may be x or residual
+ *               (with the same ld).  At most 2^35 - 2048 elements; more are refused
+ *   p           0 .. 1; at 1 nothing of x is left.  A dropped Inf or NaN is gone. */
+int kimad_dropout(const void* x, uint32_t type, uint64_t rows, uint64_t cols, uint64_t ld, const void* residual, uint64_t ld_residual,
+                  double p, uint64_t seed, uint64_t offset, void* out, uint64_t ld_out, void* stream);
+
 const char* kimad_strerror(int status);
 const char* kimad_version(void);
 

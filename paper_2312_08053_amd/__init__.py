@@ -12,6 +12,9 @@ from .binding import (KimadError, Plan, lib, kimad_workspace_bytes, kimad_plan_c
                       kimad_mx4_quantise, kimad_mx4_dequantise, kimad_mx4_matmul, kimad_mx4_matmul_workspace_bytes,
                       kimad_mx4_update_words, kimad_mx4_compress_ef, kimad_mx4_server_apply, mx4_empty,
                       kimad_distill, kimad_distill_grad, kimad_distill_workspace_bytes,
+                      kimad_linear, kimad_linear_workspace_bytes, kimad_linear_grad, kimad_linear_grad_workspace_bytes,
+                      kimad_linear_xent, kimad_linear_xent_workspace_bytes, kimad_dropout,
+                      KIMAD_ACT_NONE, KIMAD_ACT_RELU, KIMAD_ACT_GELU, KIMAD_ACT_SILU,
                       EXPORTED_SYMBOLS, LIB_PATH)
 
 __all__ = ["KimadError", "Plan", "lib", "kimad_workspace_bytes", "kimad_plan_create",
@@ -20,4 +23,7 @@ __all__ = ["KimadError", "Plan", "lib", "kimad_workspace_bytes", "kimad_plan_cre
            "kimad_mx4_quantise", "kimad_mx4_dequantise", "kimad_mx4_matmul", "kimad_mx4_matmul_workspace_bytes",
            "kimad_mx4_update_words", "kimad_mx4_compress_ef", "kimad_mx4_server_apply", "mx4_empty",
            "kimad_distill", "kimad_distill_grad", "kimad_distill_workspace_bytes",
+           "kimad_linear", "kimad_linear_workspace_bytes", "kimad_linear_grad", "kimad_linear_grad_workspace_bytes",
+           "kimad_linear_xent", "kimad_linear_xent_workspace_bytes", "kimad_dropout",
+           "KIMAD_ACT_NONE", "KIMAD_ACT_RELU", "KIMAD_ACT_GELU", "KIMAD_ACT_SILU",
            "EXPORTED_SYMBOLS", "LIB_PATH"]

@@ -19,6 +19,13 @@ KIMAD_VALUES_F32 = 0
 KIMAD_VALUES_F16 = 1
 KIMAD_VALUES_BF16 = 2
 KIMAD_MAX_J = 64
+KIMAD_ACT_NONE = 0
+KIMAD_ACT_RELU = 1
+KIMAD_ACT_GELU = 2
+KIMAD_ACT_SILU = 3
+KIMAD_WANT_DX = 1
+KIMAD_WANT_DW = 2
+KIMAD_WANT_DB = 4
 
 EXPORTED_SYMBOLS = [
     "kimad_workspace_bytes", "kimad_plan_create", "kimad_plan_destroy", "kimad_plan_grid_sizes",
@@ -31,6 +38,8 @@ EXPORTED_SYMBOLS = [
     "kimad_mx4_quantise", "kimad_mx4_dequantise", "kimad_mx4_matmul", "kimad_mx4_matmul_workspace_bytes",
     "kimad_mx4_update_words", "kimad_mx4_compress_ef", "kimad_mx4_server_apply",
     "kimad_distill", "kimad_distill_grad", "kimad_distill_workspace_bytes",
+    "kimad_linear", "kimad_linear_workspace_bytes", "kimad_linear_grad", "kimad_linear_grad_workspace_bytes",
+    "kimad_linear_xent", "kimad_linear_xent_workspace_bytes", "kimad_dropout",
 ]
 
 
@@ -107,6 +116,13 @@ def lib() -> C.CDLL:
     L.kimad_distill_workspace_bytes.argtypes = [u64, u64, u32]
     L.kimad_distill.argtypes = [vp, u32, u64, u64, u64, vp, vp, u32, f32, vp, vp, vp, vp, u64, vp, u64, vp]
     L.kimad_distill_grad.argtypes = [vp, u32, u64, u64, u64, vp, vp, u32, f32, vp, vp, vp, u64, vp]
+    L.kimad_linear_workspace_bytes.argtypes = [vp, u64, vp, u64, u64, u64, u64]
+    L.kimad_linear.argtypes = [vp, u64, vp, u64, u32, u64, u64, u64, vp, vp, u64, u32, vp, u64, vp, u32, u64, vp, u64, vp]
+    L.kimad_linear_grad_workspace_bytes.argtypes = [vp, u64, vp, u64, vp, u64, u64, u64, u64, u32, u32]
+    L.kimad_linear_grad.argtypes = [vp, u64, vp, u64, vp, u64, vp, u64, u32, u64, u64, u64, u32, vp, u64, vp, u32, u64, vp, vp, u64, vp]
+    L.kimad_linear_xent_workspace_bytes.argtypes = [vp, u64, vp, u64, u32, u64, u64, u64, u32, u32]
+    L.kimad_linear_xent.argtypes = [vp, u64, vp, u64, u32, u64, u64, u64, vp, vp, vp, vp, vp, u64, vp, u32, u64, vp, u64, vp]
+    L.kimad_dropout.argtypes = [vp, u32, u64, u64, u64, vp, u64, C.c_double, u64, u64, vp, u64, vp]
     L.kimad_strerror.argtypes = [C.c_int]
     L.kimad_strerror.restype = C.c_char_p
     L.kimad_version.restype = C.c_char_p
@@ -114,7 +130,8 @@ def lib() -> C.CDLL:
         if name not in ("kimad_strerror", "kimad_version", "kimad_budget_bytes"):
             getattr(L, name).restype = C.c_int
     L.kimad_budget_bytes.argtypes = [C.c_double, C.c_double, C.c_double, C.c_double, C.c_uint64]
-    for name in ("kimad_budget_bytes", "kimad_mx4_matmul_workspace_bytes", "kimad_mx4_update_words", "kimad_distill_workspace_bytes"):
+    for name in ("kimad_budget_bytes", "kimad_mx4_matmul_workspace_bytes", "kimad_mx4_update_words", "kimad_distill_workspace_bytes",
+                 "kimad_linear_workspace_bytes", "kimad_linear_grad_workspace_bytes", "kimad_linear_xent_workspace_bytes"):
         getattr(L, name).restype = C.c_uint64
     _lib = L
     return L
@@ -539,6 +556,153 @@ def kimad_distill_grad(logits, t_idx, t_val, temperature: float, stats, grad, ro
     rc = lib().kimad_distill_grad(*lead, temperature, weight, at, g, ld_grad, handle)
     if rc:
         _check(rc, "kimad_distill_grad")
+
+
+def _half(t, what: str) -> int:
+    """KIMAD_VALUES_* of an operand of a product in 16 bits."""
+    kind = _type(t)
+    if kind == KIMAD_VALUES_F32:
+        raise TypeError(f"{what}: float16 or bfloat16 is wanted, got {t.dtype}")
+    return kind
+
+
+def _matrix(t, shape, dtypes, what: str):
+    """(address, elements from row to row) of a matrix of this shape and one of these types; zeros for None."""
+    if t is None:
+        return 0, 0
+    rows, cols, ld = _rows(t, what)
+    if (rows, cols) != shape or t.dtype not in dtypes:
+        raise ValueError(f"{what}: shape {tuple(shape)} of {' or '.join(str(d) for d in dtypes)} is wanted, got {tuple(t.shape)} of {t.dtype}")
+    return t.data_ptr(), ld
+
+
+def _for_call(workspace, nbytes: int, device, stream):
+    """(address, bytes, the tensor) of a call's workspace: the given one, or one from the stream's pool."""
+    if workspace is not None:
+        return *_room(workspace), workspace
+    if not nbytes:
+        return 0, 0, None
+    workspace = _scratch(nbytes, device, stream)
+    return workspace.data_ptr(), nbytes, workspace
+
+
+def kimad_linear_workspace_bytes(x, w) -> int:
+    """Bytes that kimad_linear of these operands needs."""
+    (M, K, ld_x), (N, K2, ld_w) = _rows(x, "x"), _rows(w, "w")
+    return int(lib().kimad_linear_workspace_bytes(x.data_ptr(), ld_x, w.data_ptr(), ld_w, M, N, K))
+
+
+def kimad_linear(x, w, out, bias=None, residual=None, act: int = KIMAD_ACT_NONE, z=None, workspace=None, stream=None) -> None:
+    """out [M, N] = act(x w^T + bias) + residual of x [M, K], w [N, K], bias [N], residual [M, N], all of one type, float16 or bfloat16; out
+    may be float32 too, and may be residual itself.  act: KIMAD_ACT_*.  z [M, N] or None: what the activation is of, kept for
+    kimad_linear_grad.  workspace: a device tensor (allocated here if None and one is needed)."""
+    (M, K, ld_x), (N, K2, ld_w) = _rows(x, "x"), _rows(w, "w")
+    kind, dtype = _half(x, "x"), x.dtype
+    if K2 != K or w.dtype != dtype:
+        raise ValueError(f"w: rows of {K} elements of {dtype} are wanted, got {K2} of {w.dtype}")
+    out_kind = _type(out)
+    at_out, ld_out = _matrix(out, (M, N), (dtype, out.dtype if out_kind == KIMAD_VALUES_F32 else dtype), "out")
+    at_res, ld_res = _matrix(residual, (M, N), (dtype,), "residual")
+    at_z, ld_z = _matrix(z, (M, N), (dtype,), "z")
+    if bias is not None and (bias.shape != (N,) or bias.dtype != dtype or not bias.is_contiguous()):
+        raise ValueError(f"bias: {N} contiguous elements of {dtype} are wanted, got {tuple(bias.shape)} of {bias.dtype}")
+    handle = _on_device(stream, x, w, out, bias, residual, z, workspace)
+    L = lib()
+    need = 0 if workspace is not None else L.kimad_linear_workspace_bytes(x.data_ptr(), ld_x, w.data_ptr(), ld_w, M, N, K)
+    ws, nbytes, kept = _for_call(workspace, need, x.device, stream)
+    rc = L.kimad_linear(x.data_ptr(), ld_x, w.data_ptr(), ld_w, kind, M, N, K, _ptr(bias), at_res, ld_res, act, at_z, ld_z, at_out, out_kind, ld_out, ws, nbytes, handle)
+    if rc:
+        _check(rc, "kimad_linear")
+
+
+def _linear_grad_inputs(dy, x, w, dx, dw, db):
+    """(M, N, K, the six leading arguments, wants): x may be None where dw is, w where dx is."""
+    M, N, ld_dy = _rows(dy, "dy")
+    if (dx is not None and w is None) or (dw is not None and x is None):
+        raise ValueError("w is wanted with dx, x with dw")
+    K = w.shape[-1] if w is not None else x.shape[-1] if x is not None else 0
+    at_x, ld_x = _matrix(x, (M, K), (dy.dtype,), "x")
+    at_w, ld_w = _matrix(w, (N, K), (dy.dtype,), "w")
+    wants = (KIMAD_WANT_DX if dx is not None else 0) | (KIMAD_WANT_DW if dw is not None else 0) | (KIMAD_WANT_DB if db is not None else 0)
+    return M, N, K, (dy.data_ptr(), ld_dy, at_x, max(ld_x, K), at_w, max(ld_w, K)), wants
+
+
+def kimad_linear_grad_workspace_bytes(dy, x, w, act: int = KIMAD_ACT_NONE, dx=None, dw=None, db=None) -> int:
+    """Bytes that kimad_linear_grad with these arguments needs."""
+    M, N, K, lead, wants = _linear_grad_inputs(dy, x, w, dx, dw, db)
+    return int(lib().kimad_linear_grad_workspace_bytes(*lead, M, N, K, act, wants))
+
+
+def kimad_linear_grad(dy, x, w, z=None, act: int = KIMAD_ACT_NONE, dx=None, dw=None, db=None, workspace=None, stream=None) -> None:
+    """The gradient of kimad_linear: dx [M, K], dw [N, K] (float32 too), db float32 [N] from dy [M, N]; an output that is None is left out.  x may be
+    None without dw, w without dx, z (as kimad_linear left it) without an activation.  The residual's gradient is dy."""
+    M, N, K, lead, wants = _linear_grad_inputs(dy, x, w, dx, dw, db)
+    kind, dtype = _half(dy, "dy"), dy.dtype
+    if act and z is None:
+        raise ValueError("z is wanted with an activation")
+    at_z, ld_z = _matrix(z, (M, N), (dtype,), "z")
+    at_dx, ld_dx = _matrix(dx, (M, K), (dtype,), "dx")
+    dw_kind = kind if dw is None else _type(dw)
+    at_dw, ld_dw = _matrix(dw, (N, K), (dtype, dw.dtype if dw_kind == KIMAD_VALUES_F32 else dtype) if dw is not None else (), "dw")
+    at_db = 0 if db is None else _holds(db, N, "float32", "db")
+    handle = _on_device(stream, dy, x, w, z, dx, dw, db, workspace)
+    L = lib()
+    need = 0 if workspace is not None else L.kimad_linear_grad_workspace_bytes(*lead, M, N, K, act, wants)
+    ws, nbytes, kept = _for_call(workspace, need, dy.device, stream)
+    rc = L.kimad_linear_grad(*lead, at_z, ld_z, kind, M, N, K, act, at_dx, ld_dx, at_dw, dw_kind, ld_dw, at_db, ws, nbytes, handle)
+    if rc:
+        _check(rc, "kimad_linear_grad")
+
+
+def _xent_inputs(x, w, dx, dw):
+    (rows, dim, ld_x), (vocab, dim2, ld_w) = _rows(x, "x"), _rows(w, "w")
+    kind = _half(x, "x")
+    if dim2 != dim or w.dtype != x.dtype:
+        raise ValueError(f"w: rows of {dim} elements of {x.dtype} are wanted, got {dim2} of {w.dtype}")
+    wants = (KIMAD_WANT_DX if dx is not None else 0) | (KIMAD_WANT_DW if dw is not None else 0)
+    return rows, vocab, dim, (x.data_ptr(), ld_x, w.data_ptr(), ld_w, kind, rows, vocab, dim), wants, kind if dw is None else _type(dw)
+
+
+def kimad_linear_xent_workspace_bytes(x, w, dx=None, dw=None) -> int:
+    """Bytes that kimad_linear_xent with these arguments needs."""
+    _, _, _, lead, wants, dw_kind = _xent_inputs(x, w, dx, dw)
+    return int(lib().kimad_linear_xent_workspace_bytes(*lead, wants, dw_kind))
+
+
+def kimad_linear_xent(x, w, target, loss=None, lse=None, dx=None, dw=None, row_weight=None, workspace=None, stream=None) -> None:
+    """Cross entropy of the head w [vocab, dim] on x [rows, dim] (one type, float16 or bfloat16) against target int32 [rows] (none: below 0, or vocab and
+    more), each row's times row_weight float32 [rows]: loss and lse float32 [rows], dx [rows, dim], dw [vocab, dim] (float32 too);
+    an output that is None is left out.  workspace: a device tensor (allocated here if None)."""
+    rows, vocab, dim, lead, wants, dw_kind = _xent_inputs(x, w, dx, dw)
+    at_target = _holds(target, rows, "int32", "target")
+    at_weight = 0 if row_weight is None else _holds(row_weight, rows, "float32", "row_weight")
+    at_loss = 0 if loss is None else _holds(loss, rows, "float32", "loss")
+    at_lse = 0 if lse is None else _holds(lse, rows, "float32", "lse")
+    at_dx, ld_dx = _matrix(dx, (rows, dim), (x.dtype,), "dx")
+    at_dw, ld_dw = _matrix(dw, (vocab, dim), (x.dtype, dw.dtype if dw_kind == KIMAD_VALUES_F32 else x.dtype) if dw is not None else (), "dw")
+    handle = _on_device(stream, x, w, target, loss, lse, dx, dw, row_weight, workspace)
+    L = lib()
+    need = 0 if workspace is not None else L.kimad_linear_xent_workspace_bytes(*lead, wants, dw_kind)
+    ws, nbytes, kept = _for_call(workspace, need, x.device, stream)
+    rc = L.kimad_linear_xent(*lead, at_target, at_weight, at_loss, at_lse, at_dx, ld_dx, at_dw, dw_kind, ld_dw, ws, nbytes, handle)
+    if rc:
+        _check(rc, "kimad_linear_xent")
+
+
+def kimad_dropout(x, out, p: float, seed: int, offset: int = 0, residual=None, stream=None) -> None:
+    """out = residual + (x where it is kept, else 0) / (1 - p) of matrices of one type (float32 too), elements counted along the rows; the same seed and offset (whole
+    numbers of 64 bits) keep the same elements, so that the gradient is the same call on dy without residual.  out may be x or
+    residual."""
+    rows, cols, ld = _rows(x, "x")
+    kind = _type(x)
+    at_out, ld_out = _matrix(out, (rows, cols), (x.dtype,), "out")
+    at_res, ld_res = _matrix(residual, (rows, cols), (x.dtype,), "residual")
+    if not (0 <= seed < 1 << 64 and 0 <= offset < 1 << 64):
+        raise ValueError(f"seed and offset: whole numbers of 64 bits are wanted, got {seed} and {offset}")
+    handle = _on_device(stream, x, out, residual)
+    rc = lib().kimad_dropout(x.data_ptr(), kind, rows, cols, ld, at_res, ld_res, p, seed, offset, at_out, ld_out, handle)
+    if rc:
+        _check(rc, "kimad_dropout")
 
 
 class Plan:

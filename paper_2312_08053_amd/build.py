@@ -9,7 +9,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libkimad.so")
 
-SOURCES = ["kimad_api.hip", "operators_api.hip"]
+SOURCES = ["kimad_api.hip", "operators_api.hip", "layers_api.hip"]
 
 # -packed-fp32-ops is switched off: hipcc must not form packed fp32 instructions from the
 # scalar float code.  Contraction is off so that x = g - h and h + x stay single IEEE operations.

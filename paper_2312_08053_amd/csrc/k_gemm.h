@@ -1,0 +1,480 @@
+// Products of 16-bit matrices with fp32 sums, C [M, N] = A B, and what is done with a sum on its way out.
+//
+// An operand is stored along K (rows of K elements: A [M, K], B [N, K]) or across it (rows of M or N elements: A [K, M], B [K, N]), so that a layer's
+// forward product and both of its gradients read activations, weights and gradients as they lie:
+//   x W^T      A along K,  B along K
+//   dz W       A along K,  B across K
+//   dz^T x     A across K, B across K
+// v_mfma_f32_32x32x16: lane l holds elements k = 8 (l / 32) .. + 7 of row l % 32, of A and of B; element i of the result's lane l is
+// C[8 (i / 4) + 4 (l / 32) + i % 4][l % 32].
+#pragma once
+#include "k_mx4_matmul.h"
+
+namespace kimad {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+
+template <uint32_t TYPE>
+__device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
+    if constexpr (TYPE == TYPE_BF16) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+template <uint32_t TYPE>
+__device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
+    if constexpr (TYPE == TYPE_BF16) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+
+// ---- activations ---------------------------------------------------------------------------------------------------------------
+
+enum : uint32_t { ACT_NONE = 0, ACT_RELU = 1, ACT_GELU = 2, ACT_SILU = 3 };     // KIMAD_ACT_* of the public header
+
+constexpr float LOG2E = 1.4426950408889634f;
+// What the sigmoid of gelu (its tanh form, z sigmoid(2 sqrt(2 / pi) (z + 0.044715 z^3))) is taken of.
+constexpr float GELU_A = 1.5957691216057308f, GELU_B = 0.044715f;
+__device__ __forceinline__ float sigmoid(float x) { return 1.f / (1.f + __builtin_amdgcn_exp2f(-LOG2E * x)); }
+__device__ __forceinline__ float act_inner(float z, uint32_t act) { return act == ACT_GELU ? GELU_A * fmaf(GELU_B * z * z, z, z) : z; }
+__device__ __forceinline__ float act_of(float z, uint32_t act) {
+    if (act == ACT_NONE) return z;
+    if (act == ACT_RELU) return z < 0.f ? 0.f : z;                            // (a NaN stays one)
+    const float s = sigmoid(act_inner(z, act));
+    return s == 0.f ? 0.f : z * s;                                            // (of -Inf: its limit)
+}
+__device__ __forceinline__ float act_slope(float z, uint32_t act) {
+    if (act == ACT_NONE) return 1.f;
+    if (act == ACT_RELU) return z > 0.f ? 1.f : z <= 0.f ? 0.f : z;
+    const float s = sigmoid(act_inner(z, act)), d = s * (1.f - s);
+    const float inner = act == ACT_GELU ? GELU_A * fmaf(3.f * GELU_B * z, z, 1.f) : 1.f;
+    return d == 0.f ? s : fmaf(z * d, inner, s);                              // (far out: the limits)
+}
+
+// ---- tiles ---------------------------------------------------------------------------------------------------------------------
+
+// What becomes of a sum s:  z = scale s + bias, z kept, act(z) + residual.
+struct GemmEnd {
+    void* out;                   // fp32 or of the operands' type
+    const void* bias;            // [N], or null
+    const void* residual;        // [M, N], or null
+    void* z;                     // [M, N], or null
+    const float* scale;          // one number on the device, or null: 1
+    uint64_t ld, ld_res, ld_z;
+    uint32_t act, res32;         // res32: the residual is fp32
+};
+// Or, for the cross entropy: exponentials and their sums (see k_xent.h).
+struct SoftmaxEnd {
+    f32x2* strips;               // [M][strips]: largest sum of a strip's columns, and the sum of exp(s - largest)
+    void* e;                     // [M, pitch] exp(s - largest), or null
+    const int32_t* target;       // [M]
+    float* picked;               // [M]: the sum at the target
+    uint64_t pitch;
+    uint32_t strips_row;
+};
+struct GemmArgs {
+    const uint8_t *a, *b;
+    uint64_t lda, ldb;           // elements from row to row as stored
+    uint64_t M, N, K;            // K: a multiple of 8 where an operand is stored along it
+    uint64_t k_rows_a, k_rows_b; // rows that an operand across K has (beyond them: zeros)
+    uint32_t tiles_m, tiles_n;
+    uint32_t splits, share;      // parts of the sum, `share` stages each (the last one fewer); more than one: part p goes to out + p M ld
+    GemmEnd end;
+    SoftmaxEnd soft;
+};
+
+// A tile of BM by BN, WM by WN waves.  64 of K are a stage, 128 bytes of a row that is stored along K, of which LDS holds two.
+//   Along K, 16 bytes b of row r stand at b ^ (r / 2 % 8), so that sixteen lanes that read one b of sixteen rows meet different banks.
+//   Across K, LDS has rows of one k, BM elements each, and a read that transposes: sixteen lanes bring 4 k of 16 elements, and each gets
+//   one element's four.  Of a row the 64-byte pieces stand turned by its k, so that the four rows of such a read lie in different banks.
+template <uint32_t BM_, uint32_t BN_, uint32_t WM_, uint32_t WN_>
+struct GemmTile {
+    static constexpr uint32_t BM = BM_, BN = BN_, WM = WM_, WN = WN_;
+    static constexpr uint32_t WAVES = WM * WN, TI = BM / WM / 32, TJ = BN / WN / 32;
+    static constexpr uint32_t LA = BM / 8 / WAVES, LB = BN / 8 / WAVES, LOADS = LA + LB;
+    static constexpr uint32_t STAGE = (BM + BN) * 128;
+    static constexpr uint32_t COLS = 32 * TJ, PITCH = COLS + 8;
+    static constexpr uint32_t OUT = 8 * PITCH * 4, LDS = 2 * STAGE + WAVES * OUT;
+    static constexpr uint32_t STRIP = COLS;                                   // columns of a strip of the softmax's end
+};
+constexpr uint32_t GEMM_STAGE_K = 64;
+
+// An operand's side of a tile's loads.  E: elements of the tile's edge, ACROSS: stored across K.
+template <uint32_t E, uint32_t WAVES, bool ACROSS>
+struct GemmSide {
+    static constexpr uint32_t LOADS = E / 8 / WAVES;
+    static constexpr uint32_t LANES_ROW = ACROSS ? E / 8 : 8, ROWS_LOAD = 64 / LANES_ROW;   // lanes of a stored row's part, rows of a load
+    const uint8_t* base;
+    uint64_t ld_bytes;
+    uint32_t offset;             // of the lane, in its first load
+    uint32_t block;              // along K: which 16 bytes of a row's 128
+
+    static __device__ __forceinline__ uint32_t turned(uint32_t k) { return E >= 128 ? k & 3u : (k >> 1) & 1u; }
+    __device__ __forceinline__ void begin(uint32_t wave, uint32_t lane, uint64_t ld) {
+        ld_bytes = 2 * ld;
+        const uint32_t row = wave * ROWS_LOAD + lane / LANES_ROW, at = lane % LANES_ROW;
+        // (the loads of a wave are WAVES * ROWS_LOAD rows apart, and turned alike)
+        static_assert(ACROSS ? WAVES * ROWS_LOAD % 4 == 0 : WAVES * ROWS_LOAD % 16 == 0, "one order for all loads of a lane");
+        block = ACROSS ? ((at >> 2) ^ turned(row)) << 2 | (at & 3u) : at ^ ((row >> 1) & 7u);
+        offset = row * (uint32_t)ld_bytes + 16u * block;
+    }
+    // Where stage k0 / 64 begins, and how many bytes from there on are the operand's.
+    __device__ __forceinline__ void aim(const uint8_t* p, uint64_t first, uint64_t k0) { base = p + (ACROSS ? k0 * ld_bytes + 2 * first : first * ld_bytes + 2 * k0); }
+    __device__ __forceinline__ uint32_t bytes(uint64_t left, uint64_t k_left) const {
+        if (ACROSS) {
+            if (k_left == 0) return 0;
+            const uint32_t rows = k_left < GEMM_STAGE_K ? (uint32_t)k_left : GEMM_STAGE_K;
+            // (whole words: half of the last one may be beyond the array, never of another page)
+            return (rows - 1) * (uint32_t)ld_bytes + (2 * (uint32_t)(left < E ? left : E) + 3 & ~3u);
+        }
+        const uint32_t rows = left < E ? (uint32_t)left : E, part = k_left < GEMM_STAGE_K ? (uint32_t)k_left : GEMM_STAGE_K;
+        return (rows - 1) * (uint32_t)ld_bytes + 2 * part;
+    }
+};
+
+template <uint32_t E, bool ACROSS>
+__device__ __forceinline__ u32x4 gemm_operand(const uint8_t* at, uint32_t k) {
+    if constexpr (ACROSS) {
+        typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
+        u32x4 v;
+#pragma unroll
+        for (uint32_t t = 0; t < 2; ++t) {
+            const i16x4 h = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(at + (k + 4 * t) * E * 2));
+            const u32x2 w = __builtin_bit_cast(u32x2, h);
+            v[2 * t] = w[0];
+            v[2 * t + 1] = w[1];
+        }
+        return v;
+    } else {
+        return *reinterpret_cast<const u32x4*>(at);
+    }
+}
+
+enum : uint32_t { END_TYPE = 0, END_F32 = 1, END_SOFTMAX = 2 };
+
+template <uint32_t TYPE, class T, bool ACROSS_A, bool ACROSS_B, uint32_t END>
+__global__ __launch_bounds__(64 * T::WAVES, 2) void k_gemm_tile(GemmArgs g) {
+    constexpr uint32_t BM = T::BM, BN = T::BN, WM = T::WM, WN = T::WN;
+    __shared__ __attribute__((aligned(1024))) uint8_t s_mem[T::LDS];
+    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t lds0 = lds_address(s_mem), tiles = g.tiles_m * g.tiles_n, items = tiles * g.splits;
+    const uint64_t stages = (g.K + GEMM_STAGE_K - 1) / GEMM_STAGE_K;
+
+    GemmSide<BM, T::WAVES, ACROSS_A> sa;
+    GemmSide<BN, T::WAVES, ACROSS_B> sb;
+    sa.begin(wave, lane, g.lda);
+    sb.begin(wave, lane, g.ldb);
+    uint64_t stage_in, stage_end, left_a, left_b;
+    auto aim = [&](uint32_t item) {
+        uint32_t tm = 0, tn = 0;
+        const bool none = item >= items;                                      // (behind the last one the loads go on, of nothing)
+        if (!none) tile_of(item % tiles, g.tiles_m, g.tiles_n, tm, tn);
+        stage_in = none ? 0 : (uint64_t)(item / tiles) * g.share;
+        stage_end = stage_in + g.share < stages ? stage_in + g.share : stages;
+        const uint64_t m0 = (uint64_t)tm * BM, n0 = (uint64_t)tn * BN;
+        left_a = none ? 0 : g.M - m0;
+        left_b = none ? 0 : g.N - n0;
+        sa.aim(g.a, m0, stage_in * GEMM_STAGE_K);
+        sb.aim(g.b, n0, stage_in * GEMM_STAGE_K);
+    };
+    uint32_t item_in = blockIdx.x, buffer_in = 0;
+    aim(item_in);
+    // part `k` of `n` of a stage's loads
+    auto bring = [&](uint32_t k, uint32_t n) {
+        const uint32_t stage = lds0 + buffer_in * T::STAGE;
+        const uint64_t k0 = stage_in * GEMM_STAGE_K, k_left = g.K - k0;
+        const uint64_t k_left_a = !ACROSS_A ? k_left : g.k_rows_a > k0 ? g.k_rows_a - k0 : 0, k_left_b = !ACROSS_B ? k_left : g.k_rows_b > k0 ? g.k_rows_b - k0 : 0;
+        const __amdgpu_buffer_rsrc_t from_a = buffer_of(sa.base, left_a ? sa.bytes(left_a, k_left_a) : 0u), from_b = buffer_of(sb.base, left_b ? sb.bytes(left_b, k_left_b) : 0u);
+        // (along K, a row's end would run into the next row)
+        const bool past_a = !ACROSS_A && 8ull * sa.block >= k_left, past_b = !ACROSS_B && 8ull * sb.block >= k_left;
+#pragma unroll
+        for (uint32_t i = k * T::LOADS / n; i < (k + 1) * T::LOADS / n; ++i) {
+            if (i < T::LA) load_lds16(from_a, past_a ? 0xFFFFFFF0u : sa.offset + i * (T::WAVES * sa.ROWS_LOAD * (uint32_t)sa.ld_bytes), 0, stage + (i * T::WAVES + wave) * 1024u);
+            else load_lds16(from_b, past_b ? 0xFFFFFFF0u : sb.offset + (i - T::LA) * (T::WAVES * sb.ROWS_LOAD * (uint32_t)sb.ld_bytes), 0, stage + BM * 128 + ((i - T::LA) * T::WAVES + wave) * 1024u);
+        }
+    };
+    auto brought = [&]() {
+        buffer_in ^= 1u;
+        sa.base += ACROSS_A ? GEMM_STAGE_K * sa.ld_bytes : 2 * GEMM_STAGE_K;
+        sb.base += ACROSS_B ? GEMM_STAGE_K * sb.ld_bytes : 2 * GEMM_STAGE_K;
+        if (++stage_in == stage_end) {
+            item_in += gridDim.x;
+            aim(item_in);
+        }
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+    };
+
+    const uint32_t wm = wave / WN, wn = wave % WN, r32 = lane & 31u, kb = lane >> 5;
+    f32x16 acc[T::TI][T::TJ];
+    struct Half {                                                             // the operands of 16 of K
+        u32x4 a[T::TI], b[T::TJ];
+    } half0, half1;
+    // Where a lane reads: along K its row's 16 bytes, across K its four elements of a row of one k.
+    const uint32_t turn = (r32 >> 1) & 7u, k_lane = 8 * kb + ((lane & 15u) >> 2), in_piece = 32 * ((lane >> 4) & 1u) + 8 * (lane & 3u);
+    auto lane_at = [&](uint32_t edge, uint32_t first, bool across) {          // of 32 rows of the tile from `first` on
+        return across ? k_lane * edge * 2 + (((first >> 5) ^ (edge >= 128 ? k_lane & 3u : (k_lane >> 1) & 1u)) << 6) + in_piece : (first + r32) * 128;
+    };
+    auto read = [&](uint32_t buffer, uint32_t step, Half& h) {
+        const uint8_t *at_a = s_mem + buffer * T::STAGE, *at_b = at_a + BM * 128;
+        const uint32_t along = 16u * ((2 * step + kb) ^ turn);
+#pragma unroll
+        for (uint32_t i = 0; i < T::TI; ++i) h.a[i] = gemm_operand<BM, ACROSS_A>(at_a + lane_at(BM, wm * (BM / WM) + 32 * i, ACROSS_A) + (ACROSS_A ? 0 : along), 16 * step);
+#pragma unroll
+        for (uint32_t j = 0; j < T::TJ; ++j) h.b[j] = gemm_operand<BN, ACROSS_B>(at_b + lane_at(BN, wn * (BN / WN) + 32 * j, ACROSS_B) + (ACROSS_B ? 0 : along), 16 * step);
+    };
+    auto multiply = [&](const Half& h, auto between) {
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (uint32_t i = 0; i < T::TI; ++i)
+#pragma unroll
+            for (uint32_t j = 0; j < T::TJ; ++j) {
+                acc[i][j] = mfma32<TYPE>(h.a[i], h.b[j], acc[i][j]);
+                // (used here: the compiler would otherwise move the products behind the branches and waits that follow, where no reads are left to hide)
+                asm volatile("" : "+v"(acc[i][j]));
+                between(i * T::TJ + j);
+            }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto nothing = [](uint32_t) {};
+    // The reads of one half are under way while the other is multiplied, across stages and items too; the barrier in front of a stage's last 16 of K waits
+    // for the next stage, and behind it this stage's buffer takes the one after the next.  A tile is stored while the next item's first stage
+    // comes; the next barrier lets these stores be.
+    constexpr uint32_t STORES = END == END_F32 ? 4 * T::TI * T::TJ : 4 * T::TI;
+    bring(0, 1);
+    brought();
+    bring(0, 1);
+    brought();
+    vm_wait_barrier<T::LOADS, 0>(0);
+    uint32_t buffer = 0;
+    read(0, 0, half0);
+    uint32_t stores_behind = 0;                                               // 1: a tile's stores, STORES or more, are the wave's last accesses
+    for (uint32_t item = blockIdx.x; item < items; item += gridDim.x) {
+        const uint64_t first = (uint64_t)(item / tiles) * g.share, here = stages - first < g.share ? stages - first : g.share;
+#pragma unroll
+        for (uint32_t i = 0; i < T::TI; ++i)
+#pragma unroll
+            for (uint32_t j = 0; j < T::TJ; ++j) acc[i][j] = f32x16{};
+#pragma nounroll
+        for (uint64_t s = 0; s < here; ++s) {
+            read(buffer, 1, half1);
+            multiply(half0, nothing);
+            read(buffer, 2, half0);
+            multiply(half1, nothing);
+            read(buffer, 3, half1);
+            multiply(half0, nothing);
+            vm_wait_barrier<0, STORES>(stores_behind);
+            stores_behind = 0;
+            buffer ^= 1u;
+            read(buffer, 0, half0);                                           // (behind the last item: of a buffer, and for nothing)
+            multiply(half1, [&](uint32_t k) { bring(k, T::TI * T::TJ); });    // the loads between the products: what sets them up costs no time
+            brought();
+        }
+
+        uint32_t tm, tn;
+        tile_of(item % tiles, g.tiles_m, g.tiles_n, tm, tn);
+        const uint64_t tile_m = (uint64_t)tm * BM, tile_n = (uint64_t)tn * BN;
+        // Eight rows at a time through LDS, so that stores run along the rows: 16 bytes a lane, whole cache lines.
+        constexpr uint32_t BYTES = END == END_F32 ? 4 : 2, BEYOND = 0xFFFFFFF0u, EACH = 16 / BYTES, LANES = T::COLS / EACH;   // elements of a lane, lanes of a row
+        constexpr uint32_t PASSES = 8 * LANES > 64 ? 8 * LANES / 64 : 1, PASS_ROWS = 8 / PASSES;
+        uint32_t l;                                                           // the lane, found anew: kept through the loop, it would cost a register
+        asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(l));
+        float* mine = reinterpret_cast<float*>(s_mem + 2 * T::STAGE + wave * T::OUT);
+        const uint32_t rows = g.M - tile_m < BM ? (uint32_t)(g.M - tile_m) : BM, cols = g.N - tile_n < BN ? (uint32_t)(g.N - tile_n) : BN;
+        const uint32_t row = l / LANES, wcol = wn * T::COLS + EACH * (l % LANES), col = EACH * (l % LANES);
+        const bool row_in = PASSES > 1 || row < 8, whole = wcol + EACH <= cols, cut = wcol < cols && !whole;
+        // eight rows of the wave's sums through LDS, pass by pass
+        auto through = [&](uint32_t i, uint32_t e, f32x4 (&v)[PASSES][EACH / 4]) {
+#pragma unroll
+            for (uint32_t j = 0; j < T::TJ; ++j) {
+                const f32x16 x = acc[i][j];
+#pragma unroll
+                for (uint32_t k = 0; k < 4; ++k) mine[(4 * (l >> 5) + k) * T::PITCH + 32 * j + (l & 31u)] = x[4 * e + k];
+            }
+            wave_sync_lds();
+#pragma unroll
+            for (uint32_t p = 0; p < PASSES; ++p)
+#pragma unroll
+                for (uint32_t q = 0; q < EACH / 4; ++q) v[p][q] = *reinterpret_cast<const f32x4*>(mine + ((p * PASS_ROWS + row) & 7u) * T::PITCH + col + 4 * q);
+            wave_sync_lds();
+        };
+        if constexpr (END == END_SOFTMAX) {
+            const SoftmaxEnd& o = g.soft;
+            int32_t target[4 * T::TI];
+#pragma unroll
+            for (uint32_t x = 0; x < 4 * T::TI; ++x) {
+                const uint32_t r = wm * (BM / WM) + 8 * x + row;
+                target[x] = row_in && r < rows ? o.target[tile_m + r] : -1;
+            }
+#pragma unroll
+            for (uint32_t i = 0; i < T::TI; ++i) {
+                const uint32_t first = wm * (BM / WM) + 32 * i;
+                const __amdgpu_buffer_rsrc_t to = buffer_of(static_cast<uint8_t*>(o.e) + ((tile_m + first) * o.pitch + tile_n) * 2, 0xFFFFFF00u);
+#pragma unroll
+                for (uint32_t e = 0; e < 4; ++e) {
+                    f32x4 v[PASSES][EACH / 4];
+                    through(i, e, v);
+                    const uint32_t r = first + 8 * e + row;
+                    const bool in = row_in && r < rows;
+                    float m = -INFINITY, s = 0.f, x[EACH];
+#pragma unroll
+                    for (uint32_t k = 0; k < EACH; ++k) {
+                        x[k] = v[0][k / 4][k % 4];
+                        const uint32_t at = (uint32_t)(target[4 * i + e] - (int32_t)(tile_n + wcol));
+                        if (at == k && in && wcol + k < cols) o.picked[tile_m + r] = x[k];
+                        if (wcol + k >= cols) x[k] = -INFINITY;
+                        m = fmaxf(m, x[k]);
+                    }
+                    m = fmaxf(m, __uint_as_float(dpp_u32<DPP_XOR1>(__float_as_uint(m))));
+                    m = fmaxf(m, __uint_as_float(dpp_u32<DPP_XOR2>(__float_as_uint(m))));
+                    if (LANES == 8) m = fmaxf(m, __uint_as_float(dpp_u32<DPP_HALF_MIRROR>(__float_as_uint(m))));
+                    const float from = m == -INFINITY ? 0.f : m;
+                    u32x4 out;
+#pragma unroll
+                    for (uint32_t k = 0; k < EACH; ++k) {
+                        x[k] = __builtin_amdgcn_exp2f((x[k] - from) * LOG2E);
+                        s += x[k];
+                    }
+#pragma unroll
+                    for (uint32_t k = 0; k < 4; ++k) out[k] = pack2<TYPE>(x[2 * k], x[2 * k + 1]);
+                    s += __uint_as_float(dpp_u32<DPP_XOR1>(__float_as_uint(s)));
+                    s += __uint_as_float(dpp_u32<DPP_XOR2>(__float_as_uint(s)));
+                    if (LANES == 8) s += __uint_as_float(dpp_u32<DPP_HALF_MIRROR>(__float_as_uint(s)));
+                    if (o.e) __builtin_amdgcn_raw_buffer_store_b128(out, to, in && tile_n + wcol < o.pitch ? ((8 * e + row) * (uint32_t)o.pitch + wcol) * 2 : BEYOND, 0, 0);
+                    if (in && l % LANES == 0 && wn * T::COLS < cols) o.strips[(tile_m + r) * o.strips_row + tn * WN + wn] = f32x2{m, s};
+                }
+            }
+            stores_behind = o.e ? 1u : 0u;
+        } else {
+            const GemmEnd& o = g.end;
+            const float scale = o.scale ? *o.scale : 1.f;
+            const uint64_t part = item / tiles;
+            float bias[EACH];
+#pragma unroll
+            for (uint32_t k = 0; k < EACH; ++k) bias[k] = o.bias && wcol + k < cols ? load1<TYPE>(o.bias, tile_n + wcol + k) : 0.f;
+            const uint32_t at = (row * (uint32_t)o.ld + wcol) * BYTES;
+#pragma unroll
+            for (uint32_t i = 0; i < T::TI; ++i) {
+                const uint32_t first = wm * (BM / WM) + 32 * i;               // the store's rows begin here: the lanes' offsets are those of 32 rows, below 2^32
+                const __amdgpu_buffer_rsrc_t to = buffer_of(static_cast<uint8_t*>(o.out) + ((part * g.M + tile_m + first) * o.ld + tile_n) * BYTES, 0xFFFFFF00u);
+                // A residual of 16 bits: that of the 32 rows is under way before the first is used.
+                const uint8_t* res_base = static_cast<const uint8_t*>(o.residual) + ((tile_m + first + row) * o.ld_res + tile_n + wcol) * (o.res32 ? 4 : 2);
+                uint32_t res[4][PASSES][EACH / 2];
+                if (o.residual && !o.res32) {
+#pragma unroll
+                    for (uint32_t e = 0; e < 4; ++e)
+#pragma unroll
+                        for (uint32_t p = 0; p < PASSES; ++p) {
+                            const uint32_t r = 8 * e + p * PASS_ROWS;
+                            const uint16_t* q = reinterpret_cast<const uint16_t*>(res_base) + r * o.ld_res;
+                            if (row_in && first + r + row < rows) {
+                                if (whole) {
+#pragma unroll
+                                    for (uint32_t k = 0; k < EACH / 2; k += 2) {
+                                        const u32x2_any w = *reinterpret_cast<const u32x2_any*>(q + 2 * k);
+                                        res[e][p][k] = w[0];
+                                        res[e][p][k + 1] = w[1];
+                                    }
+                                } else {
+#pragma unroll
+                                    for (uint32_t k = 0; k < EACH; k += 2)
+                                        res[e][p][k / 2] = (wcol + k < cols ? (uint32_t)q[k] : 0u) | (wcol + k + 1 < cols ? (uint32_t)q[k + 1] << 16 : 0u);
+                                }
+                            }
+                        }
+                }
+#pragma unroll
+                for (uint32_t e = 0; e < 4; ++e) {
+                    f32x4 v[PASSES][EACH / 4], res32[PASSES][EACH / 4];
+                    if (o.residual && o.res32) {
+#pragma unroll
+                        for (uint32_t p = 0; p < PASSES; ++p) {
+                            const uint32_t r = 8 * e + p * PASS_ROWS;
+                            const float* q = reinterpret_cast<const float*>(res_base) + r * o.ld_res;
+                            if (row_in && first + r + row < rows)
+#pragma unroll
+                                for (uint32_t k = 0; k < EACH; k += 4) {
+                                    if (whole) res32[p][k / 4] = *reinterpret_cast<const f32x4_any*>(q + k);
+                                    else
+#pragma unroll
+                                        for (uint32_t h = 0; h < 4; ++h) res32[p][k / 4][h] = wcol + k + h < cols ? q[k + h] : 0.f;
+                                }
+                        }
+                    }
+                    through(i, e, v);
+#pragma unroll
+                    for (uint32_t p = 0; p < PASSES; ++p) {
+                        // (the whole offset in the lane's register: a 16-byte store with a scalar offset as well has stored values that the next instructions
+                        // wrote into its data registers, in rows with such an offset and in no others)
+                        const uint32_t r = 8 * e + p * PASS_ROWS, to_at = at + r * (uint32_t)o.ld * BYTES;
+                        const bool in = row_in && first + r + row < rows;
+                        float x[EACH];
+#pragma unroll
+                        for (uint32_t k = 0; k < EACH; ++k) x[k] = fmaf(v[p][k / 4][k % 4], scale, bias[k]);
+                        if (o.z && in) {
+                            uint16_t* q = static_cast<uint16_t*>(o.z) + (tile_m + first + r + row) * o.ld_z + tile_n + wcol;
+                            if (whole) {
+#pragma unroll
+                                for (uint32_t k = 0; k < EACH; k += 4) *reinterpret_cast<u32x2_any*>(q + k) = u32x2_any{pack2<TYPE>(x[k], x[k + 1]), pack2<TYPE>(x[k + 2], x[k + 3])};
+                            } else if (cut) {
+#pragma unroll
+                                for (uint32_t k = 0; k < EACH; ++k)
+                                    if (wcol + k < cols) store1<TYPE>(q, k, x[k]);
+                            }
+                        }
+                        if (o.act != ACT_NONE)
+#pragma unroll
+                            for (uint32_t k = 0; k < EACH; ++k) x[k] = act_of(x[k], o.act);
+                        if (o.residual)
+#pragma unroll
+                            for (uint32_t k = 0; k < EACH; ++k) {
+                                const uint32_t w = res[e][p][k / 2] >> (16 * (k % 2)) & 0xFFFFu;
+                                x[k] += o.res32 ? res32[p][k / 4][k % 4] : TYPE == TYPE_BF16 ? __uint_as_float(w << 16) : half_to_float(w);
+                            }
+                        u32x4 out;
+#pragma unroll
+                        for (uint32_t k = 0; k < 4; ++k) out[k] = BYTES == 4 ? __float_as_uint(x[k]) : pack2<TYPE>(x[2 * k % EACH], x[(2 * k + 1) % EACH]);
+                        __builtin_amdgcn_raw_buffer_store_b128(out, to, in && whole ? to_at : BEYOND, 0, 0);
+                        if (in && cut) {
+#pragma unroll
+                            for (uint32_t k = 0; k < EACH; ++k) {
+                                const uint32_t ok = wcol + k < cols ? to_at + k * BYTES : BEYOND;
+                                if (BYTES == 4) __builtin_amdgcn_raw_buffer_store_b32(out[k % 4], to, ok, 0, 0);
+                                else __builtin_amdgcn_raw_buffer_store_b16((uint16_t)(out[k / 2 % 4] >> (16 * (k % 2))), to, ok, 0, 0);
+                            }
+                        }
+                    }
+                }
+            }
+            stores_behind = 1u;
+            if (cols % EACH != 0) {                                           // (so many more stores that the counter would not tell)
+                stores_behind = 0;
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            }
+        }
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                          // no load may reach LDS that is another workgroup's by then
+}
+
+// The parts of a sum, in their order, and its end.  A thread takes four columns.
+template <uint32_t TYPE, bool OUT32>
+__global__ __launch_bounds__(256) void k_gemm_join(const float* __restrict__ parts, uint32_t splits, uint64_t M, uint64_t N, GemmEnd o) {
+    const uint64_t each = (N + 3) / 4, i = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= M * each) return;
+    const uint64_t m = i / each, n = 4 * (i % each);
+    const float scale = o.scale ? *o.scale : 1.f;
+#pragma unroll
+    for (uint32_t k = 0; k < 4; ++k) {
+        if (n + k >= N) break;
+        float v = 0.f;
+        for (uint32_t p = 0; p < splits; ++p) v += parts[(p * M + m) * N + n + k];
+        v = fmaf(v, scale, o.bias ? load1<TYPE>(o.bias, n + k) : 0.f);
+        if (o.z) store1<TYPE>(o.z, m * o.ld_z + n + k, v);
+        v = act_of(v, o.act);
+        if (o.residual) v += o.res32 ? static_cast<const float*>(o.residual)[m * o.ld_res + n + k] : load1<TYPE>(o.residual, m * o.ld_res + n + k);
+        store1<OUT32 ? TYPE_F32 : TYPE>(o.out, m * o.ld + n + k, v);
+    }
+}
+
+}  // namespace kimad

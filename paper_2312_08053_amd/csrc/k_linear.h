@@ -1,0 +1,159 @@
+// A linear layer's products beside the tiles of k_gemm.h: few rows, rows laid out anew, and what its gradient is made of.
+#pragma once
+#include "k_distill.h"
+#include "k_gemm.h"
+
+namespace kimad {
+
+// Few rows of A (16 MT at most): sixteen rows of B by a workgroup, whose waves take a quarter of K each, straight from memory to registers, U times 32 of K
+// under way.  Rows may begin anywhere.  Bound by the reads of B.
+template <uint32_t TYPE, uint32_t MT, uint32_t END>
+__global__ __launch_bounds__(256) void k_gemm_few(GemmArgs g) {
+    __shared__ f32x4 s_part[3][MT][64];
+    constexpr uint32_t U = 8 / MT;
+    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15u, blk = lane >> 4;
+    const uint64_t n0 = (uint64_t)blockIdx.x * 16, n = n0 + r < g.N ? n0 + r : g.N - 1;
+    // (whole cache lines)
+    const uint64_t quarter = (g.K + 255) / 256 * 64, begin = wave * quarter < g.K ? wave * quarter : g.K, end = begin + quarter < g.K ? begin + quarter : g.K;
+    const uint64_t b = n * g.ldb + 8 * blk;
+    uint64_t a[MT];
+    f32x4 acc[MT];
+#pragma unroll
+    for (uint32_t t = 0; t < MT; ++t) {
+        a[t] = (16 * t + r < g.M ? 16 * t + r : g.M - 1) * g.lda + 8 * blk;
+        acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    auto words = [](const Raw8<TYPE>& v) { return u32x4{v.r[0], v.r[1], v.r[2], v.r[3]}; };
+    uint64_t k = begin;
+    for (; k + 32 * U <= end; k += 32 * U) {
+        Raw8<TYPE> vb[U], va[U][MT];
+#pragma unroll
+        for (uint32_t u = 0; u < U; ++u) {
+            vb[u] = load8<TYPE>(g.b, b + k + 32 * u);
+#pragma unroll
+            for (uint32_t t = 0; t < MT; ++t) va[u][t] = load8<TYPE>(g.a, a[t] + k + 32 * u);
+        }
+#pragma unroll
+        for (uint32_t u = 0; u < U; ++u)
+#pragma unroll
+            for (uint32_t t = 0; t < MT; ++t) acc[t] = mfma16<TYPE>(words(va[u][t]), words(vb[u]), acc[t]);
+    }
+    for (; k < end; k += 32) {
+        const int64_t left = (int64_t)(end - k) - 8 * blk;
+        const u32x4 vb = words(load8_first<TYPE>(g.b, b + k, left));
+#pragma unroll
+        for (uint32_t t = 0; t < MT; ++t) acc[t] = mfma16<TYPE>(words(load8_first<TYPE>(g.a, a[t] + k, left)), vb, acc[t]);
+    }
+    if (wave)
+#pragma unroll
+        for (uint32_t t = 0; t < MT; ++t) s_part[wave - 1][t][lane] = acc[t];
+    __syncthreads();
+    if (wave) return;
+#pragma unroll
+    for (uint32_t t = 0; t < MT; ++t) {
+        acc[t] = acc[t] + s_part[0][t][lane] + s_part[1][t][lane] + s_part[2][t][lane];
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) {
+            const uint64_t m = 16 * t + 4 * blk + i;
+            const bool in = m < g.M && n0 + r < g.N;
+            if constexpr (END == END_SOFTMAX) {
+                // sixteen lanes have a row's strip of sixteen columns
+                const SoftmaxEnd& o = g.soft;
+                if (in && (uint64_t)(int64_t)o.target[m] == n0 + r) o.picked[m] = acc[t][i];
+                const float x = in ? acc[t][i] : -INFINITY;
+                Softmax v = {x, x == -INFINITY ? 0.f : 1.f + (x - x)};            // (of +Inf and NaN a NaN)
+#pragma unroll
+                for (uint32_t h = 1; h < 16; h <<= 1) v = join(v, Softmax{__shfl_xor(v.m, h), __shfl_xor(v.s, h)}, LOG2E);
+                if (r == 0 && m < g.M) o.strips[m * o.strips_row + blockIdx.x] = f32x2{v.m, v.s};
+            } else if (in) {
+                const GemmEnd& o = g.end;
+                float v = acc[t][i] + (o.bias ? load1<TYPE>(o.bias, n) : 0.f);
+                if (o.z) store1<TYPE>(o.z, m * o.ld_z + n, v);
+                v = act_of(v, o.act);
+                if (o.residual) v += load1<TYPE>(o.residual, m * o.ld_res + n);
+                store1<END == END_F32 ? TYPE_F32 : TYPE>(o.out, m * o.ld + n, v);
+            }
+        }
+    }
+}
+
+// A product over nothing: its end alone.
+template <uint32_t TYPE, bool OUT32>
+__global__ __launch_bounds__(256) void k_gemm_none(uint64_t M, uint64_t N, GemmEnd o) {
+    for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < M * N; i += (uint64_t)gridDim.x * 256) {
+        const uint64_t m = i / N, n = i % N;
+        float v = o.bias ? load1<TYPE>(o.bias, n) : 0.f;
+        if (o.z) store1<TYPE>(o.z, m * o.ld_z + n, v);
+        v = act_of(v, o.act);
+        if (o.residual) v += load1<TYPE>(o.residual, m * o.ld_res + n);
+        store1<OUT32 ? TYPE_F32 : TYPE>(o.out, m * o.ld + n, v);
+    }
+}
+
+// Rows of 16-bit elements laid out anew, `pitch` (a multiple of 8) apart and filled up with zeros: for operands whose rows do not begin at 16-byte addresses or
+// end inside 16 bytes.  Rows that do not count (weight 0, no target) become zeros: a NaN there would reach every sum over rows.
+__global__ __launch_bounds__(256) void k_rows_copy(const void* __restrict__ from, uint64_t ld, uint64_t rows, uint64_t cols, void* __restrict__ to, uint64_t pitch,
+                                                   const int32_t* __restrict__ target, int64_t vocab, const float* __restrict__ weight) {
+    const uint64_t each = pitch / 8, i = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= rows * each) return;
+    const uint64_t r = i / each, c = i % each * 8;
+    const bool live = (!target || (target[r] >= 0 && target[r] < vocab)) && (!weight || weight[r] != 0.f);
+    const Raw8<TYPE_BF16> v = load8_first<TYPE_BF16>(from, r * ld + c, live ? (int64_t)(cols - c) : 0);
+    reinterpret_cast<u32x4*>(to)[i] = u32x4{v.r[0], v.r[1], v.r[2], v.r[3]};
+}
+
+// dz = dy act'(z), rounded to the type, and the sums of its columns in fp32 (of what was not rounded): of 128 rows a workgroup, 512 columns.  Bound by memory.
+constexpr uint32_t SUM_ROWS = 128, SUM_COLS = 512;
+struct ActGradArgs {
+    const void *dy, *z;          // z null: no activation
+    void* dz;                    // or null; pitch elements from row to row, filled up with zeros
+    float* sums;                 // [ceil(M / 128)][N], or null
+    uint64_t M, N, ld_dy, ld_z, pitch;
+    uint32_t act;
+};
+template <uint32_t TYPE>
+__global__ __launch_bounds__(256) void k_act_grad(ActGradArgs a) {
+    __shared__ float s_sum[4][SUM_COLS];
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
+    const uint64_t c = (uint64_t)blockIdx.x * SUM_COLS + 8 * lane, m0 = (uint64_t)blockIdx.y * SUM_ROWS, m1 = m0 + SUM_ROWS < a.M ? m0 + SUM_ROWS : a.M;
+    const int64_t n = (int64_t)a.N - (int64_t)c;
+    float sum[8] = {};
+    if (c < a.pitch)
+        for (uint64_t m = m0 + wave; m < m1; m += 4) {
+            const Raw8<TYPE> g = load8_first<TYPE>(a.dy, m * a.ld_dy + c, n);
+            float v[8];
+            if (a.z) {
+                const Raw8<TYPE> z = load8_first<TYPE>(a.z, m * a.ld_z + c, n);
+#pragma unroll
+                for (uint32_t k = 0; k < 8; ++k) v[k] = (int64_t)k < n ? g.at(k) * act_slope(z.at(k), a.act) : 0.f;
+            } else {
+#pragma unroll
+                for (uint32_t k = 0; k < 8; ++k) v[k] = g.at(k);
+            }
+            if (a.dz) store8<TYPE>(a.dz, m * a.pitch + c, v);
+#pragma unroll
+            for (uint32_t k = 0; k < 8; ++k) sum[k] += v[k];
+        }
+    if (!a.sums) return;
+#pragma unroll
+    for (uint32_t k = 0; k < 8; ++k) s_sum[wave][8 * lane + k] = sum[k];
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < SUM_COLS; i += 256) {
+        const uint64_t col = (uint64_t)blockIdx.x * SUM_COLS + i;
+        if (col < a.N) a.sums[blockIdx.y * a.N + col] = s_sum[0][i] + s_sum[1][i] + s_sum[2][i] + s_sum[3][i];
+    }
+}
+// The sums of all rows from those of 128 each: a wave of a workgroup takes every fourth.
+__global__ __launch_bounds__(256) void k_sum_join(const float* __restrict__ sums, uint64_t parts, uint64_t N, float* __restrict__ out) {
+    __shared__ float s_sum[4][64];
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
+    const uint64_t n = (uint64_t)blockIdx.x * 64 + lane;
+    float v = 0.f;
+    if (n < N)
+        for (uint64_t p = wave; p < parts; p += 4) v += sums[p * N + n];
+    s_sum[wave][lane] = v;
+    __syncthreads();
+    if (wave == 0 && n < N) out[n] = s_sum[0][lane] + s_sum[1][lane] + s_sum[2][lane] + s_sum[3][lane];
+}
+
+}  // namespace kimad

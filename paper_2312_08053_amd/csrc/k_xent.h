@@ -1,0 +1,100 @@
+// Softmax cross entropy of a linear head without its logits.  With z = x W^T, lse_r = ln sum_v exp(z_rv) and p = exp(z - lse),
+//     loss_r = w_r (lse_r - z_{r, t_r}),   G = w (p - onehot(t)),   dx = G W,   dW = G^T x.
+// The product z goes by tiles (k_gemm.h) whose end is END_SOFTMAX: of a strip of a row's columns (32 or 64) only its largest sum m and s = sum exp(z - m)
+// are kept, and for a gradient e = exp(z - m) in 16 bits, of a piece of the rows at a time.  With lse known, e becomes G in its place, e exp(m - lse) w: a
+// rounding of e and one of G, each as large as that of a p that is rounded once.  At the target, where p - 1 may be much smaller than p, it is taken from the fp32
+// logit.  A second product for z in the place of e would cost 2 R V D operations more; e costs 4 bytes of traffic an element.
+#pragma once
+#include "k_linear.h"
+
+namespace kimad {
+
+struct XentArgs {
+    const f32x2* strips;
+    const float* picked;
+    const int32_t* target;
+    const float* weight;         // or null: 1
+    float *loss, *lse;           // or null
+    f32x2* rows_out;             // [rows]: lse, and the row's weight times `scale` (0: the row does not count)
+    void* e;                     // [rows, pitch]: exp(z - m), and then G
+    const float* scale;          // two numbers on the device: what G is multiplied by, and its inverse; or null
+    uint64_t rows, pitch;
+    uint32_t vocab, strips_row, strip;
+};
+
+// G in 16 bits of fp16 is multiplied by a power of two that takes the largest weight to 2^12: a p of 2^-26 is then no subnormal.
+__global__ __launch_bounds__(1024) void k_xent_scale(const int32_t* __restrict__ target, const float* __restrict__ weight, uint64_t rows, uint32_t vocab, float* __restrict__ out) {
+    __shared__ float s_max[16];
+    float m = 0.f;
+    for (uint64_t r = threadIdx.x; r < rows; r += 1024) {
+        const float w = weight ? fabsf(weight[r]) : 1.f;
+        if ((uint32_t)target[r] < vocab && w < INFINITY) m = fmaxf(m, w);
+    }
+#pragma unroll
+    for (uint32_t o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
+    if ((threadIdx.x & 63u) == 0) s_max[threadIdx.x >> 6] = m;
+    __syncthreads();
+    if (threadIdx.x) return;
+    for (uint32_t i = 1; i < 16; ++i) m = fmaxf(m, s_max[i]);
+    int32_t k = 12 - ((int32_t)(__float_as_uint(m) >> 23) - 126);             // (the largest weight is below 2^(exponent - 126))
+    k = m == 0.f ? 0 : k > 100 ? 100 : k < -100 ? -100 : k;
+    out[0] = __uint_as_float((uint32_t)(127 + k) << 23);
+    out[1] = __uint_as_float((uint32_t)(127 - k) << 23);
+}
+
+// A row's sums from its strips, by a workgroup: the loss and lse.
+__global__ __launch_bounds__(256) void k_xent_rows(XentArgs a) {
+    __shared__ Softmax room[4];
+    const uint64_t row = blockIdx.x;
+    const int32_t t = a.target[row];
+    const float w = a.weight ? a.weight[row] : 1.f;
+    bool live = (uint32_t)t < a.vocab && w != 0.f;
+    Softmax q = {-INFINITY, 0.f};
+    if (live) {
+        for (uint32_t i = threadIdx.x; i < a.strips_row; i += 256) {
+            const f32x2 v = a.strips[row * a.strips_row + i];
+            q = join(q, Softmax{v[0], v[1]}, LOG2E);
+        }
+        q = join_block<256>(q, LOG2E, room);
+        live = q.s != 0.f;                                                    // (every logit -Inf: the row leaves nothing)
+    }
+    if (threadIdx.x) return;
+    const float lse = live ? q.m + logf(q.s) : 0.f;
+    if (a.loss) a.loss[row] = live ? w * ((q.m - a.picked[row]) + logf(q.s)) : 0.f;
+    if (a.lse) a.lse[row] = lse;
+    if (a.rows_out) a.rows_out[row] = f32x2{lse, live ? w * (a.scale ? a.scale[0] : 1.f) : 0.f};
+}
+
+// e becomes G.  A thread takes eight columns.  Bound by memory.
+template <uint32_t TYPE>
+__global__ __launch_bounds__(256) void k_xent_gradient(XentArgs a, uint32_t chunks) {
+    const uint64_t row = blockIdx.x / chunks;
+    const uint64_t col = ((uint64_t)(blockIdx.x % chunks) * 256 + threadIdx.x) * 8;
+    if (col >= a.pitch) return;
+    const f32x2 of = a.rows_out[row];
+    u32x4* at = reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.e) + row * a.pitch + col);
+    const bool live = of[1] != 0.f && col < a.vocab;
+    u32x4 out = {0u, 0u, 0u, 0u};
+    if (live) {
+        const u32x4 w = *at;
+        Raw8<TYPE> e;
+#pragma unroll
+        for (uint32_t k = 0; k < 4; ++k) e.r[k] = w[k];
+        const float m = a.strips[row * a.strips_row + col / a.strip][0], f = __builtin_amdgcn_exp2f((m - of[0]) * LOG2E) * of[1];
+        const uint32_t t = (uint32_t)a.target[row] - (uint32_t)col;
+        float v[8];
+#pragma unroll
+        for (uint32_t k = 0; k < 8; ++k) v[k] = col + k < a.vocab ? e.at(k) * f : 0.f;
+        if (t < 8) {
+            const float p = expm1f(a.picked[row] - of[0]) * of[1];
+#pragma unroll
+            for (uint32_t k = 0; k < 8; ++k)
+                if (t == k) v[k] = p;
+        }
+#pragma unroll
+        for (uint32_t k = 0; k < 4; ++k) out[k] = pack2<TYPE>(v[2 * k], v[2 * k + 1]);
+    }
+    *at = out;
+}
+
+}  // namespace kimad

@@ -5,7 +5,7 @@
 #include <cmath>
 #include <type_traits>
 
-#include "../../include/kimad.h"
+#include "operators_host.h"
 #include "k_mx4_quantise.h"
 #include "k_mx4_matmul.h"
 #include "k_mx4_update.h"
@@ -19,23 +19,14 @@ static_assert(TYPE_F32 == KIMAD_VALUES_F32 && TYPE_F16 == KIMAD_VALUES_F16 && TY
 
 static_assert(UPDATE_MAX_WORKERS == KIMAD_MAX_WORKERS, "header and kernel constants");
 
-constexpr uint64_t MOST = 1ull << 40;                    // elements along an axis that the checks below let through
 constexpr uint64_t FEW_ROWS = 32;                        // products of so many rows may go by k_mx4_matmul_few
-constexpr uint64_t UNITS = 256;                         // compute units of the device
 constexpr uint64_t MATMUL_MOST_K = 1ull << 25, MATMUL_MOST_LD = 1ull << 24;     // eight rows of codes and 32 rows of the result are reached by 32-bit offsets
-constexpr uint64_t GRID_MOST = 0x7FFFFFFFull, GRID_Y_MOST = 65535;
 constexpr uint32_t UPDATE_MOST_L = 0x7FFFFFFFu;          // layers of an update: the kernels count them, and search among them, in 32 bits
-// a launch's workgroups along x: their threads are counted in 32 bits
-inline bool grid_ok(uint64_t wgs, uint64_t threads) { return wgs <= GRID_MOST && wgs <= 0xFFFFFFFFull / threads; }
-
-inline bool aligned(const void* p, uintptr_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
 inline uint64_t words_of(uint64_t cols) { return (cols + MX4_WORD - 1) / MX4_WORD; }
-inline int launched() { return hipGetLastError() == hipSuccess ? KIMAD_OK : KIMAD_ERR_HIP; }
 // codes and scales are both given or both missing
 inline bool pair_ok(const void* codes, const uint32_t* scales) {
     return !codes == !scales && (!codes || (aligned(codes, 16) && aligned(scales, 4)));
 }
-inline uint64_t type_bytes(uint32_t type) { return type == KIMAD_VALUES_F32 ? 4 : 2; }
 
 // Calls f with the type as a compile-time constant.
 template <class F>

@@ -1,0 +1,222 @@
+"""The cross entropy of a linear head, loss and gradients, on the GPU."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2312_08053_amd as kimad
+from tests import layers_reference as ref
+
+pytestmark = pytest.mark.gpu
+F32, F16, BF16 = torch.float32, torch.float16, torch.bfloat16
+HALF = {F32: 2.0 ** -24, F16: 2.0 ** -11, BF16: 2.0 ** -8}             # half a step, relative
+
+
+def inputs(rows, vocab, dim, dtype, seed, spread=2.0):
+    rng = np.random.default_rng(seed)
+    x = torch.from_numpy(rng.normal(size=(rows, dim))).to(dtype)
+    w = torch.from_numpy(rng.normal(size=(vocab, dim)) * spread / dim ** 0.5).to(dtype)
+    target = rng.integers(0, vocab, rows).astype(np.int32)
+    target[rng.random(rows) < 0.1] = -1
+    weight = rng.choice([0.0, 0.25, 1.0, 3.0], rows).astype(np.float32)
+    return x, w, target, weight
+
+
+def check(x, w, target, weight, got, dtype, dw_dtype, span=None):
+    """Bounds: a logit is off by dim 2^-23 of its products' magnitudes, d in all; so are lse and the loss, and a few roundings of numbers no larger than lse and the
+    logits.  G is off by that, by an exponential of an argument a (4 |a| 2^-24), and by three roundings to the type (e, G, and what is stored); products sum as many terms as
+    there are.  In fp16 an exponential below 2^-14 of its strip's largest is off by 2^-25 of that instead."""
+    X, W = x.double().numpy(), w.double().numpy()
+    loss, lse, dx, dw, G = ref.xent(X, W, target, weight)
+    size = np.abs(X) @ np.abs(W).T
+    dim, vocab, rows = X.shape[1], len(W), len(X)
+    z = X @ W.T
+    wt = np.ones(rows) if weight is None else np.abs(weight.astype(np.float64))
+    d = dim * 2.0 ** -23 * size.max(1)
+    a = np.abs(z).max(1) + np.abs(lse)
+    row = 2 * d + 2.0 ** -21 * (a + 1) + vocab * 2.0 ** -24
+    if "lse" in got:
+        assert (np.abs(got["lse"] - lse) <= row).all()
+    if "loss" in got:
+        assert (np.abs(got["loss"] - loss) <= wt * row * 2).all()
+    u = HALF[dtype]
+    off = np.abs(G) * (2 * u + u * u + (2 * row + 8 * a * 2.0 ** -24 + 2.0 ** -21)[:, None]) + 2 * row[:, None] * (wt * (lse != 0))[:, None] * (np.arange(vocab)[None, :] == target[:, None])
+    if dtype == F16:
+        off += (2.0 ** -24 * wt * (lse != 0))[:, None] * np.ones(vocab)
+    for name, true, terms, ulp in (("dx", dx, off @ np.abs(W) + vocab * 2.0 ** -23 * (np.abs(G) @ np.abs(W)), u),
+                                   ("dw", dw, off.T @ np.abs(X) + rows * 2.0 ** -23 * (np.abs(G).T @ np.abs(X)), HALF[dw_dtype])):
+        if name in got:
+            bound = terms + ulp * (np.abs(true) + terms) + (2.0 ** -24 if dtype == F16 else 2.0 ** -120)
+            assert (np.abs(got[name] - true) <= bound).all(), (name, np.abs(got[name] - true).max(), bound.max())
+
+
+def call(x, w, target, weight, outs, dw_dtype=None, **kw):
+    x, w = x.cuda() if not x.is_cuda else x, w.cuda() if not w.is_cuda else w
+    rows, dim, vocab = x.shape[0], x.shape[1], w.shape[0]
+    nan = float("nan")
+    t = {"loss": torch.full((rows,), nan, device="cuda"), "lse": torch.full((rows,), nan, device="cuda"), "dx": torch.full((rows, dim), nan, dtype=x.dtype, device="cuda"),
+         "dw": torch.full((vocab, dim), nan, dtype=dw_dtype or x.dtype, device="cuda")}
+    out = {n: t[n] for n in outs}
+    kimad.kimad_linear_xent(x, w, torch.from_numpy(target).cuda(), row_weight=None if weight is None else torch.from_numpy(weight).cuda(), **out, **kw)
+    return out
+
+
+def numbers(out):
+    return {n: t.double().cpu().numpy() for n, t in out.items()}
+
+
+# few rows; one and several tiles of each size; odd widths, strips that end in a tile; one column
+SHAPES = [(1, 1, 1), (1, 1000, 64), (5, 77, 100), (16, 3001, 128), (32, 500, 33), (33, 31, 8), (64, 64, 64), (100, 65, 72), (130, 1003, 513), (300, 2000, 200), (600, 4099, 96)]
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("rows,vocab,dim", SHAPES)
+def test_loss(rows, vocab, dim, dtype):
+    x, w, target, weight = inputs(rows, vocab, dim, dtype, rows + vocab)
+    got = numbers(call(x, w, target, weight, ("loss", "lse")))
+    check(x, w, target, weight, got, dtype, dtype)
+    assert np.array_equal(numbers(call(x, w, target, weight, ("loss",)))["loss"], got["loss"])
+
+
+@pytest.mark.parametrize("dtype,dw_dtype", [(F16, F16), (BF16, BF16), (BF16, F32)])
+@pytest.mark.parametrize("rows,vocab,dim", SHAPES)
+def test_gradients(rows, vocab, dim, dtype, dw_dtype):
+    x, w, target, weight = inputs(rows, vocab, dim, dtype, rows + vocab + 1)
+    got = call(x, w, target, weight, ("loss", "lse", "dx", "dw"), dw_dtype)
+    check(x, w, target, weight, numbers(got), dtype, dw_dtype)
+    for some in (("dx",), ("dw",), ("loss", "dw")):
+        again = call(x, w, target, weight, some, dw_dtype)
+        assert all(torch.equal(again[n], got[n]) for n in some), some
+    got = numbers(call(x, w, target, None, ("loss", "dx", "dw"), dw_dtype))       # every weight 1
+    check(x, w, target, None, got, dtype, dw_dtype)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_a_sure_row(dtype):
+    """Where the target's probability is nearly one, p - 1 is what counts: by a p in 16 bits it would be 0, or off by many times itself."""
+    rows, vocab, dim = 40, 300, 64
+    x, w, target, _ = inputs(rows, vocab, dim, dtype, 5, spread=0.5)
+    target = np.arange(rows, dtype=np.int32)
+    w[:rows] = 0
+    for r in range(rows):
+        x[r, r], w[r, r] = 4.0, 4.0
+    got = numbers(call(x, w, target, None, ("loss", "dx", "dw")))
+    check(x, w, target, None, got, dtype, dtype)
+    G = ref.xent(x.double().numpy(), w.double().numpy(), target)[4]
+    assert (np.abs(G[np.arange(rows), target]) < 1e-2).any()
+
+
+@pytest.mark.parametrize("grad", [False, True])
+@pytest.mark.parametrize("rows", [3, 70])
+def test_rows_that_do_not_count_reach_nothing(rows, grad):
+    """Rows without a target or of weight 0 hold Inf and NaN."""
+    x, w, target, weight = inputs(rows, 150, 72, BF16, 3)
+    target[0], weight[1:] = -1, 1.0
+    weight[2] = 0.0
+    target[1] = 7
+    dirty = x.clone()
+    dirty[0], dirty[2] = float("nan"), float("inf")
+    outs = ("loss", "lse", "dx", "dw") if grad else ("loss", "lse")
+    clean_x = x.clone()
+    got, want = call(dirty, w, target, weight, outs), call(clean_x, w, target, weight, outs)
+    for n in outs:
+        assert torch.equal(got[n], want[n]), n
+    check(x, w, target, weight, numbers(got), BF16, BF16)
+    for bad in (-1, 150, 2 ** 31 - 1, -2 ** 31):                           # none of these is a target
+        target[:] = bad
+        got = call(x, w, target, weight, outs)
+        assert not any(t.any() for t in got.values())
+
+
+def test_infinite_and_nan_rows():
+    x, w, target, _ = inputs(70, 100, 64, BF16, 8)
+    target[:] = 5
+    x[4, 3], x[6, 3] = float("nan"), float("inf")
+    got = call(x, w, target, None, ("loss", "dx"))
+    others = [r for r in range(70) if r not in (4, 6)]
+    assert got["loss"][[4, 6]].isnan().all() and got["dx"][[4, 6]].isnan().all()
+    want = call(x[others], w, target[others], None, ("loss", "dx"))
+    assert torch.equal(got["loss"][others], want["loss"]) and got["dx"][others].isfinite().all()
+    assert call(x[:7], w, target[:7], None, ("loss",))["loss"].isnan().tolist() == [False] * 4 + [True, False, True]   # (few rows)
+
+
+@pytest.mark.parametrize("scale", [1e-30, 2.0 ** -20, 1.0, 2.0 ** 12])
+def test_weights_of_any_size(scale):
+    """fp16: G is scaled by the largest weight, so that small weights lose nothing but what the result's own type does."""
+    x, w, target, weight = inputs(50, 200, 64, F16, 4)
+    weight = (weight * scale).astype(np.float32)
+    got = numbers(call(x, w, target, weight, ("loss", "dw"), F32))
+    loss, _, _, dw, _ = ref.xent(x.double().numpy(), w.double().numpy(), target, weight)
+    assert np.abs(got["dw"] - dw).max() <= 2.0 ** -9 * np.abs(dw).max() and np.abs(got["loss"] - loss).max() <= 2.0 ** -18 * np.abs(loss).max()
+
+
+@pytest.mark.parametrize("rows,vocab,dim", [(20, 77, 100), (90, 333, 104), (150, 200, 65)])
+@pytest.mark.parametrize("pad,shift", [(1, 0), (8, 0), (24, 1)])
+def test_strides_and_addresses(rows, vocab, dim, pad, shift):
+    from tests.test_gpu_linear import buffer, outside_is_nan
+    x, w, target, weight = inputs(rows, vocab, dim, F16, pad)
+    (xb, _), (wb, _) = buffer(x.cuda(), pad, shift), buffer(w.cuda(), pad, shift)
+    dx, dx_full = buffer(torch.zeros(rows, dim, dtype=F16, device="cuda"), pad, shift)
+    dw, dw_full = buffer(torch.zeros(vocab, dim, device="cuda"), pad, shift)
+    loss = torch.empty(rows, device="cuda")
+    kimad.kimad_linear_xent(xb, wb, torch.from_numpy(target).cuda(), loss=loss, dx=dx, dw=dw, row_weight=torch.from_numpy(weight).cuda())
+    check(x, w, target, weight, numbers({"loss": loss, "dx": dx, "dw": dw}), F16, F32)
+    assert outside_is_nan(dx, dx_full, shift, pad) and outside_is_nan(dw, dw_full, shift, pad)
+
+
+@pytest.mark.parametrize("dw_dtype", [BF16, F32])
+def test_pieces_of_the_rows(dw_dtype):
+    """A vocabulary of 262144 leaves a piece 1024 rows: 2100 rows are three.  One row in a hundred counts, which can be checked on its own; the others must add nothing."""
+    rows, vocab, dim = 2100, 262144, 32
+    rng = np.random.default_rng(0)
+    x, w = torch.from_numpy(rng.normal(size=(rows, dim))).to(BF16), torch.from_numpy(rng.normal(size=(vocab, dim)) * 0.5).to(BF16)
+    target = np.full(rows, -1, dtype=np.int32)
+    some = np.arange(50, rows, 100)
+    target[some] = rng.integers(0, vocab, len(some))
+    got = call(x, w, target, None, ("loss", "lse", "dx", "dw"), dw_dtype)
+    alone = {n: v for n, v in numbers(got).items()}
+    for n in ("loss", "lse", "dx"):
+        assert not np.delete(alone[n], some, 0).any()
+        alone[n] = alone[n][some]
+    check(x[some], w, target[some], None, alone, BF16, dw_dtype)
+
+
+def test_streams_graphs_and_the_same_bits():
+    rows, vocab, dim = 300, 1000, 136
+    x, w, target, weight = inputs(rows, vocab, dim, BF16, 6)
+    xg, wg, tg, wt = x.cuda(), w.cuda(), torch.from_numpy(target).cuda(), torch.from_numpy(weight).cuda()
+    want = call(x, w, target, weight, ("loss", "dx", "dw"))
+    out = {n: torch.empty_like(t) for n, t in want.items()}
+    workspace = torch.empty(kimad.kimad_linear_xent_workspace_bytes(xg, wg, dx=out["dx"], dw=out["dw"]), dtype=torch.uint8, device="cuda")
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    kimad.kimad_linear_xent(xg, wg, tg, row_weight=wt, workspace=workspace, stream=side, **out)
+    side.synchronize()
+    assert all(torch.equal(out[n], want[n]) for n in want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        kimad.kimad_linear_xent(xg, wg, tg, row_weight=wt, workspace=workspace, **out)
+    for k in range(4):
+        x2, w2, target2, weight2 = inputs(rows, vocab, dim, BF16, 10 + k)
+        xg.copy_(x2), wg.copy_(w2), tg.copy_(torch.from_numpy(target2)), wt.copy_(torch.from_numpy(weight2))
+        workspace.fill_(255)
+        graph.replay()
+        eager = call(x2, w2, target2, weight2, ("loss", "dx", "dw"))
+        torch.cuda.synchronize()
+        assert all(torch.equal(out[n], eager[n]) for n in out), k
+
+
+def test_gradients_against_differences():
+    """Of the loss as the call itself gives it, along random directions; steps are whole multiples of the inputs' own, so that both ends are the type's numbers.  The loss in
+    fp32 is off by 2^-20 or so of ten, which over the step's 2^-4 is 2e-4, and by a third derivative times the step squared."""
+    rows, vocab, dim = 60, 120, 64
+    rng = np.random.default_rng(2)
+    x = torch.from_numpy(rng.integers(-16, 17, (rows, dim)) / 16.0).to(F16)
+    w = torch.from_numpy(rng.integers(-16, 17, (vocab, dim)) / 16.0).to(F16)
+    target, weight = rng.integers(0, vocab, rows).astype(np.int32), np.ones(rows, dtype=np.float32)
+    got = numbers(call(x, w, target, weight, ("loss", "dx", "dw")))
+    for k in range(4):
+        ux, uw = torch.from_numpy(rng.integers(-1, 2, x.shape) / 64.0).to(F16), torch.from_numpy(rng.integers(-1, 2, w.shape) / 64.0).to(F16)
+        for name, grad, ends in (("dx", ux, [(x + ux, w), (x - ux, w)]), ("dw", uw, [(x, w + uw), (x, w - uw)])):
+            a, b = (numbers(call(p, q, target, weight, ("loss",)))["loss"].sum() for p, q in ends)
+            slope = (got[name] * grad.double().numpy()).sum()
+            assert abs((a - b) / 2 - slope) <= 0.01 * np.abs(got[name] * grad.double().numpy()).sum() + 1e-3, (name, k)
