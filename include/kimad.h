@@ -473,7 +473,7 @@ int kimad_distill_grad(const void* logits, uint32_t type, uint64_t rows, uint64_
  * read must not overlap arrays that are written, but where stated; every array is aligned like its elements.  `type` is that of
  * the operands, KIMAD_VALUES_F16 or _BF16 (the matrix cores' types; the dropout takes _F32 too); sums are fp32 and rounded once,
  * where they are stored.  Matrices have contiguous rows, `ld` elements apart: at most 2^22 for operands of a product, 2^24 for its
- * results and what is added to them.  At most 8388480 rows (tokens), 2^22 features, and fewer than 2^34 elements a matrix, its columns counted as seven more; more are
+ * results and what is added to them.  At most 4194240 rows (tokens), 2^22 features, and fewer than 2^34 elements a matrix, its columns counted as seven more; more are
  * refused.  Operands are read fastest where they begin at 16-byte addresses, ld is a multiple of 8 and so are the features; others
  * are laid out anew in the workspace first, but for up to 32 rows of a forward product.
  *   workspace   DEVICE, 16-byte aligned, as many bytes as the call's own ..._workspace_bytes says for the same arguments (of the pointers,

@@ -36,23 +36,51 @@ enum : uint32_t { ACT_NONE = 0, ACT_RELU = 1, ACT_GELU = 2, ACT_SILU = 3 };     
 constexpr float LOG2E = 1.4426950408889634f;
 // What the sigmoid of gelu (its tanh form, z sigmoid(2 sqrt(2 / pi) (z + 0.044715 z^3))) is taken of.
 constexpr float GELU_A = 1.5957691216057308f, GELU_B = 0.044715f;
-__device__ __forceinline__ float sigmoid(float x) { return 1.f / (1.f + __builtin_amdgcn_exp2f(-LOG2E * x)); }
-__device__ __forceinline__ float act_inner(float z, uint32_t act) { return act == ACT_GELU ? GELU_A * fmaf(GELU_B * z * z, z, z) : z; }
-__device__ __forceinline__ float act_of(float z, uint32_t act) {
-    if (act == ACT_NONE) return z;
-    if (act == ACT_RELU) return z < 0.f ? 0.f : z;                            // (a NaN stays one)
-    const float s = sigmoid(act_inner(z, act));
-    return s == 0.f ? 0.f : z * s;                                            // (of -Inf: its limit)
+__device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-LOG2E * x)); }
+template <uint32_t ACT>
+__device__ __forceinline__ float act_inner(float z) { return ACT == ACT_GELU ? GELU_A * fmaf(GELU_B * z * z, z, z) : z; }
+// (Comparisons, through which a NaN stays one, keep infinite z from meeting a sigmoid of 0, and their limits.)
+template <uint32_t ACT>
+__device__ __forceinline__ float act_as(float z) {
+    if (ACT == ACT_NONE) return z;
+    if (ACT == ACT_RELU) return z < 0.f ? 0.f : z;
+    const float s = sigmoid(act_inner<ACT>(z));
+    return (z < -1e30f ? -1e30f : z) * s;
 }
-__device__ __forceinline__ float act_slope(float z, uint32_t act) {
-    if (act == ACT_NONE) return 1.f;
-    if (act == ACT_RELU) return z > 0.f ? 1.f : z <= 0.f ? 0.f : z;
-    const float s = sigmoid(act_inner(z, act)), d = s * (1.f - s);
-    const float inner = act == ACT_GELU ? GELU_A * fmaf(3.f * GELU_B * z, z, 1.f) : 1.f;
-    return d == 0.f ? s : fmaf(z * d, inner, s);                              // (far out: the limits)
+template <uint32_t ACT>
+__device__ __forceinline__ float slope_as(float z) {
+    if (ACT == ACT_NONE) return 1.f;
+    if (ACT == ACT_RELU) return z > 0.f ? 1.f : z <= 0.f ? 0.f : z;
+    z = z > 100.f ? 100.f : z < -100.f ? -100.f : z;                          // (the slope is 1 or 0 from there on)
+    const float s = sigmoid(act_inner<ACT>(z)), zd = z * (s * (1.f - s));
+    return s + (ACT == ACT_GELU ? zd * (GELU_A * fmaf(3.f * GELU_B * z, z, 1.f)) : zd);
+}
+// Calls f with the activation as a compile-time constant.
+template <class F>
+__device__ __forceinline__ void with_act(uint32_t act, F f) {
+    if (act == ACT_NONE) f(std::integral_constant<uint32_t, ACT_NONE>{});
+    else if (act == ACT_RELU) f(std::integral_constant<uint32_t, ACT_RELU>{});
+    else if (act == ACT_GELU) f(std::integral_constant<uint32_t, ACT_GELU>{});
+    else f(std::integral_constant<uint32_t, ACT_SILU>{});
+}
+__device__ __forceinline__ float act_of(float z, uint32_t act) {
+    with_act(act, [&](auto a) { z = act_as<decltype(a)::value>(z); });
+    return z;
 }
 
 // ---- tiles ---------------------------------------------------------------------------------------------------------------------
+
+// Exponentials e = exp(s - m), 0 to 1, in 16 bits without a sign: M of mantissa, 16 - M of exponent.  A product in fp16 takes M = 12, exact to 2^-13 of e down to 2^-14 and to
+// 2^-28 below, one in bfloat16 M = 11, 2^-12 down to 2^-30 and 2^-43 below: small beside the roundings of those types.  The float e 2^-(128 - 2^(16 - M))
+// has such an exponent, and its bits, rounded, are the code.
+template <uint32_t TYPE>
+struct SmallFloat {
+    static constexpr uint32_t SHIFT = TYPE == TYPE_F16 ? 11 : 12;             // 23 - M
+    static constexpr float DOWN = TYPE == TYPE_F16 ? 0x1p-112f : 0x1p-96f, UP = TYPE == TYPE_F16 ? 0x1p112f : 0x1p96f;
+    static __device__ __forceinline__ uint32_t bits(float e) { return __float_as_uint(e * DOWN) + (1u << (SHIFT - 1)); }
+    static __device__ __forceinline__ uint32_t pack(float a, float b) { return bits(a) >> SHIFT | (bits(b) >> SHIFT) << 16; }
+    static __device__ __forceinline__ float at(uint32_t word, uint32_t half) { return __uint_as_float((half ? word >> 16 : word & 0xFFFFu) << SHIFT) * UP; }
+};
 
 // What becomes of a sum s:  z = scale s + bias, z kept, act(z) + residual.
 struct GemmEnd {
@@ -67,7 +95,7 @@ struct GemmEnd {
 // Or, for the cross entropy: exponentials and their sums (see k_xent.h).
 struct SoftmaxEnd {
     f32x2* strips;               // [M][strips]: largest sum of a strip's columns, and the sum of exp(s - largest)
-    void* e;                     // [M, pitch] exp(s - largest), or null
+    void* e;                     // [M, pitch] exp(s - largest) as a SmallFloat, or null
     const int32_t* target;       // [M]
     float* picked;               // [M]: the sum at the target
     uint64_t pitch;
@@ -88,49 +116,62 @@ struct GemmArgs {
 //   Along K, 16 bytes b of row r stand at b ^ (r / 2 % 8), so that sixteen lanes that read one b of sixteen rows meet different banks.
 //   Across K, LDS has rows of one k, BM elements each, and a read that transposes: sixteen lanes bring 4 k of 16 elements, and each gets
 //   one element's four.  Of a row the 64-byte pieces stand turned by its k, so that the four rows of such a read lie in different banks.
-template <uint32_t BM_, uint32_t BN_, uint32_t WM_, uint32_t WN_>
+template <uint32_t BM_, uint32_t BN_, uint32_t WM_, uint32_t WN_, uint32_t SK_, uint32_t NB_>
 struct GemmTile {
-    static constexpr uint32_t BM = BM_, BN = BN_, WM = WM_, WN = WN_;
-    static constexpr uint32_t WAVES = WM * WN, TI = BM / WM / 32, TJ = BN / WN / 32;
-    static constexpr uint32_t LA = BM / 8 / WAVES, LB = BN / 8 / WAVES, LOADS = LA + LB;
-    static constexpr uint32_t STAGE = (BM + BN) * 128;
+    static constexpr uint32_t BM = BM_, BN = BN_, WM = WM_, WN = WN_, SK = SK_, NB = NB_;
+    static constexpr uint32_t WAVES = WM * WN, TI = BM / WM / 32, TJ = BN / WN / 32, STEPS = SK / 16;
+    static constexpr uint32_t LA = BM * SK / 512 / WAVES, LB = BN * SK / 512 / WAVES, LOADS = LA + LB;
+    static constexpr uint32_t STAGE = (BM + BN) * SK * 2;
     static constexpr uint32_t COLS = 32 * TJ, PITCH = COLS + 8;
-    static constexpr uint32_t OUT = 8 * PITCH * 4, LDS = 2 * STAGE + WAVES * OUT;
+    static constexpr uint32_t OUT = 8 * PITCH * 4, LDS = NB * STAGE + WAVES * OUT;
     static constexpr uint32_t STRIP = COLS;                                   // columns of a strip of the softmax's end
 };
-constexpr uint32_t GEMM_STAGE_K = 64;
 
 // An operand's side of a tile's loads.  E: elements of the tile's edge, ACROSS: stored across K.
-template <uint32_t E, uint32_t WAVES, bool ACROSS>
+template <uint32_t E, uint32_t WAVES, uint32_t SK, bool ACROSS>
 struct GemmSide {
-    static constexpr uint32_t LOADS = E / 8 / WAVES;
-    static constexpr uint32_t LANES_ROW = ACROSS ? E / 8 : 8, ROWS_LOAD = 64 / LANES_ROW;   // lanes of a stored row's part, rows of a load
+    static constexpr uint32_t LANES_ROW = ACROSS ? E / 8 : SK / 8, ROWS_LOAD = 64 / LANES_ROW;   // lanes of a stored row's part, rows of a load
+    // What is brought next: a stage of K, of `rows` rows along K or elements across it.
     const uint8_t* base;
     uint64_t ld_bytes;
+    uint32_t rows, k_left;       // k_left: of K (rows of it, across) from this stage on
+    uint32_t bytes;
     uint32_t offset;             // of the lane, in its first load
-    uint32_t block;              // along K: which 16 bytes of a row's 128
+    uint32_t block;              // along K: which 16 bytes of a row's part
 
     static __device__ __forceinline__ uint32_t turned(uint32_t k) { return E >= 128 ? k & 3u : (k >> 1) & 1u; }
+    // along K: of a row whose part is SK / 8 times 16 bytes
+    static __device__ __forceinline__ uint32_t turn(uint32_t row) { return SK == 64 ? (row >> 1) & 7u : (row >> 2) & 3u; }
     __device__ __forceinline__ void begin(uint32_t wave, uint32_t lane, uint64_t ld) {
         ld_bytes = 2 * ld;
         const uint32_t row = wave * ROWS_LOAD + lane / LANES_ROW, at = lane % LANES_ROW;
         // (the loads of a wave are WAVES * ROWS_LOAD rows apart, and turned alike)
         static_assert(ACROSS ? WAVES * ROWS_LOAD % 4 == 0 : WAVES * ROWS_LOAD % 16 == 0, "one order for all loads of a lane");
-        block = ACROSS ? ((at >> 2) ^ turned(row)) << 2 | (at & 3u) : at ^ ((row >> 1) & 7u);
+        block = ACROSS ? ((at >> 2) ^ turned(row)) << 2 | (at & 3u) : at ^ turn(row);
         offset = row * (uint32_t)ld_bytes + 16u * block;
     }
-    // Where stage k0 / 64 begins, and how many bytes from there on are the operand's.
-    __device__ __forceinline__ void aim(const uint8_t* p, uint64_t first, uint64_t k0) { base = p + (ACROSS ? k0 * ld_bytes + 2 * first : first * ld_bytes + 2 * k0); }
-    __device__ __forceinline__ uint32_t bytes(uint64_t left, uint64_t k_left) const {
-        if (ACROSS) {
-            if (k_left == 0) return 0;
-            const uint32_t rows = k_left < GEMM_STAGE_K ? (uint32_t)k_left : GEMM_STAGE_K;
-            // (whole words: half of the last one may be beyond the array, never of another page)
-            return (rows - 1) * (uint32_t)ld_bytes + (2 * (uint32_t)(left < E ? left : E) + 3 & ~3u);
-        }
-        const uint32_t rows = left < E ? (uint32_t)left : E, part = k_left < GEMM_STAGE_K ? (uint32_t)k_left : GEMM_STAGE_K;
-        return (rows - 1) * (uint32_t)ld_bytes + 2 * part;
+    // At row or element `first` of `all`, and at k0 of K.
+    __device__ __forceinline__ void aim(const uint8_t* p, uint64_t first, uint64_t all, uint32_t k0, uint32_t K) {
+        base = p + (ACROSS ? k0 * ld_bytes + 2 * first : first * ld_bytes + 2 * k0);
+        rows = __builtin_amdgcn_readfirstlane(first >= all ? 0u : all - first < E ? (uint32_t)(all - first) : E);
+        k_left = __builtin_amdgcn_readfirstlane(K > k0 ? K - k0 : 0u);
+        measure();
     }
+    __device__ __forceinline__ void next() {
+        base += ACROSS ? SK * ld_bytes : 2 * SK;
+        k_left = k_left > SK ? k_left - SK : 0u;
+        measure();
+    }
+    // Bytes of the stage, beyond which are zeros.  (Across, whole words: half of the last one may be beyond the array, never of another page.)
+    __device__ __forceinline__ void measure() {
+        const uint32_t k = k_left < SK ? k_left : SK, lines = ACROSS ? k : rows, line = ACROSS ? (2 * rows + 3) & ~3u : 2 * k;
+        bytes = ((lines - 1) * (uint32_t)ld_bytes + line) & (lines == 0 || line == 0 ? 0u : ~0u);
+        bytes = __builtin_amdgcn_readfirstlane(bytes);                        // (made once, not with every load)
+    }
+    __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer() const { return buffer_of(base, bytes); }
+    // The lane's offset in its first load; along K, a row's end would run into the next row: such lanes are beyond every buffer, in all of their loads.
+    __device__ __forceinline__ uint32_t lane_offset() const { return !ACROSS && 8 * block >= k_left ? 0x80000000u : offset; }
+    __device__ __forceinline__ uint32_t step() const { return WAVES * ROWS_LOAD * (uint32_t)ld_bytes; }
 };
 
 template <uint32_t E, bool ACROSS>
@@ -151,6 +192,10 @@ __device__ __forceinline__ u32x4 gemm_operand(const uint8_t* at, uint32_t k) {
     }
 }
 
+// The cache policy of a tile's stores: nontemporal, since operands that are read again and again should keep the L2 (4096 x 50304 x 768 into exponentials 410 us
+// without, 362 with; into bfloat16 368 and 332).
+constexpr int STREAM = 2;
+
 enum : uint32_t { END_TYPE = 0, END_F32 = 1, END_SOFTMAX = 2 };
 
 template <uint32_t TYPE, class T, bool ACROSS_A, bool ACROSS_B, uint32_t END>
@@ -159,46 +204,40 @@ __global__ __launch_bounds__(64 * T::WAVES, 2) void k_gemm_tile(GemmArgs g) {
     __shared__ __attribute__((aligned(1024))) uint8_t s_mem[T::LDS];
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t lds0 = lds_address(s_mem), tiles = g.tiles_m * g.tiles_n, items = tiles * g.splits;
-    const uint64_t stages = (g.K + GEMM_STAGE_K - 1) / GEMM_STAGE_K;
+    const uint32_t stages = (uint32_t)((g.K + T::SK - 1) / T::SK);
 
-    GemmSide<BM, T::WAVES, ACROSS_A> sa;
-    GemmSide<BN, T::WAVES, ACROSS_B> sb;
+    GemmSide<BM, T::WAVES, T::SK, ACROSS_A> sa;
+    GemmSide<BN, T::WAVES, T::SK, ACROSS_B> sb;
     sa.begin(wave, lane, g.lda);
     sb.begin(wave, lane, g.ldb);
-    uint64_t stage_in, stage_end, left_a, left_b;
+    uint32_t stages_in;                                                       // of the item, this one counted
     auto aim = [&](uint32_t item) {
         uint32_t tm = 0, tn = 0;
         const bool none = item >= items;                                      // (behind the last one the loads go on, of nothing)
         if (!none) tile_of(item % tiles, g.tiles_m, g.tiles_n, tm, tn);
-        stage_in = none ? 0 : (uint64_t)(item / tiles) * g.share;
-        stage_end = stage_in + g.share < stages ? stage_in + g.share : stages;
-        const uint64_t m0 = (uint64_t)tm * BM, n0 = (uint64_t)tn * BN;
-        left_a = none ? 0 : g.M - m0;
-        left_b = none ? 0 : g.N - n0;
-        sa.aim(g.a, m0, stage_in * GEMM_STAGE_K);
-        sb.aim(g.b, n0, stage_in * GEMM_STAGE_K);
+        const uint32_t first = none ? 0 : item / tiles * g.share, k0 = first * T::SK;
+        stages_in = stages - first < g.share ? stages - first : g.share;
+        sa.aim(g.a, (uint64_t)tm * BM, none ? 0 : g.M, k0, ACROSS_A ? (uint32_t)g.k_rows_a : (uint32_t)g.K);
+        sb.aim(g.b, (uint64_t)tn * BN, none ? 0 : g.N, k0, ACROSS_B ? (uint32_t)g.k_rows_b : (uint32_t)g.K);
     };
     uint32_t item_in = blockIdx.x, buffer_in = 0;
     aim(item_in);
     // part `k` of `n` of a stage's loads
     auto bring = [&](uint32_t k, uint32_t n) {
-        const uint32_t stage = lds0 + buffer_in * T::STAGE;
-        const uint64_t k0 = stage_in * GEMM_STAGE_K, k_left = g.K - k0;
-        const uint64_t k_left_a = !ACROSS_A ? k_left : g.k_rows_a > k0 ? g.k_rows_a - k0 : 0, k_left_b = !ACROSS_B ? k_left : g.k_rows_b > k0 ? g.k_rows_b - k0 : 0;
-        const __amdgpu_buffer_rsrc_t from_a = buffer_of(sa.base, left_a ? sa.bytes(left_a, k_left_a) : 0u), from_b = buffer_of(sb.base, left_b ? sb.bytes(left_b, k_left_b) : 0u);
-        // (along K, a row's end would run into the next row)
-        const bool past_a = !ACROSS_A && 8ull * sa.block >= k_left, past_b = !ACROSS_B && 8ull * sb.block >= k_left;
+        const uint32_t stage = lds0 + buffer_in * T::STAGE + wave * 1024u;
+        const __amdgpu_buffer_rsrc_t from_a = sa.buffer(), from_b = sb.buffer();
+        const uint32_t off_a = sa.lane_offset(), off_b = sb.lane_offset();
 #pragma unroll
         for (uint32_t i = k * T::LOADS / n; i < (k + 1) * T::LOADS / n; ++i) {
-            if (i < T::LA) load_lds16(from_a, past_a ? 0xFFFFFFF0u : sa.offset + i * (T::WAVES * sa.ROWS_LOAD * (uint32_t)sa.ld_bytes), 0, stage + (i * T::WAVES + wave) * 1024u);
-            else load_lds16(from_b, past_b ? 0xFFFFFFF0u : sb.offset + (i - T::LA) * (T::WAVES * sb.ROWS_LOAD * (uint32_t)sb.ld_bytes), 0, stage + BM * 128 + ((i - T::LA) * T::WAVES + wave) * 1024u);
+            if (i < T::LA) load_lds16(from_a, off_a + i * sa.step(), 0, stage + i * T::WAVES * 1024u);
+            else load_lds16(from_b, off_b + (i - T::LA) * sb.step(), 0, stage + BM * T::SK * 2 + (i - T::LA) * T::WAVES * 1024u);
         }
     };
     auto brought = [&]() {
-        buffer_in ^= 1u;
-        sa.base += ACROSS_A ? GEMM_STAGE_K * sa.ld_bytes : 2 * GEMM_STAGE_K;
-        sb.base += ACROSS_B ? GEMM_STAGE_K * sb.ld_bytes : 2 * GEMM_STAGE_K;
-        if (++stage_in == stage_end) {
+        buffer_in = buffer_in + 1 == T::NB ? 0u : buffer_in + 1;
+        sa.next();
+        sb.next();
+        if (--stages_in == 0) {
             item_in += gridDim.x;
             aim(item_in);
         }
@@ -212,12 +251,12 @@ __global__ __launch_bounds__(64 * T::WAVES, 2) void k_gemm_tile(GemmArgs g) {
         u32x4 a[T::TI], b[T::TJ];
     } half0, half1;
     // Where a lane reads: along K its row's 16 bytes, across K its four elements of a row of one k.
-    const uint32_t turn = (r32 >> 1) & 7u, k_lane = 8 * kb + ((lane & 15u) >> 2), in_piece = 32 * ((lane >> 4) & 1u) + 8 * (lane & 3u);
+    const uint32_t turn = sa.turn(r32), k_lane = 8 * kb + ((lane & 15u) >> 2), in_piece = 32 * ((lane >> 4) & 1u) + 8 * (lane & 3u);
     auto lane_at = [&](uint32_t edge, uint32_t first, bool across) {          // of 32 rows of the tile from `first` on
-        return across ? k_lane * edge * 2 + (((first >> 5) ^ (edge >= 128 ? k_lane & 3u : (k_lane >> 1) & 1u)) << 6) + in_piece : (first + r32) * 128;
+        return across ? k_lane * edge * 2 + (((first >> 5) ^ (edge >= 128 ? k_lane & 3u : (k_lane >> 1) & 1u)) << 6) + in_piece : (first + r32) * T::SK * 2;
     };
     auto read = [&](uint32_t buffer, uint32_t step, Half& h) {
-        const uint8_t *at_a = s_mem + buffer * T::STAGE, *at_b = at_a + BM * 128;
+        const uint8_t *at_a = s_mem + buffer * T::STAGE, *at_b = at_a + BM * T::SK * 2;
         const uint32_t along = 16u * ((2 * step + kb) ^ turn);
 #pragma unroll
         for (uint32_t i = 0; i < T::TI; ++i) h.a[i] = gemm_operand<BM, ACROSS_A>(at_a + lane_at(BM, wm * (BM / WM) + 32 * i, ACROSS_A) + (ACROSS_A ? 0 : along), 16 * step);
@@ -239,34 +278,34 @@ __global__ __launch_bounds__(64 * T::WAVES, 2) void k_gemm_tile(GemmArgs g) {
     };
     auto nothing = [](uint32_t) {};
     // The reads of one half are under way while the other is multiplied, across stages and items too; the barrier in front of a stage's last 16 of K waits
-    // for the next stage, and behind it this stage's buffer takes the one after the next.  A tile is stored while the next item's first stage
-    // comes; the next barrier lets these stores be.
+    // for the next stage, and behind it this stage's buffer takes the one NB further on.  A tile is stored while the next item's first stages
+    // come; the next barriers let these stores be.
     constexpr uint32_t STORES = END == END_F32 ? 4 * T::TI * T::TJ : 4 * T::TI;
-    bring(0, 1);
-    brought();
-    bring(0, 1);
-    brought();
-    vm_wait_barrier<T::LOADS, 0>(0);
+#pragma unroll
+    for (uint32_t i = 0; i < T::NB; ++i) {
+        bring(0, 1);
+        brought();
+    }
+    vm_wait_barrier<(T::NB - 1) * T::LOADS, 0>(0);
     uint32_t buffer = 0;
     read(0, 0, half0);
-    uint32_t stores_behind = 0;                                               // 1: a tile's stores, STORES or more, are the wave's last accesses
+    uint32_t stores_behind = 0;                                               // not 0: a tile's stores, STORES or more, are behind the loads that the next barrier waits for
     for (uint32_t item = blockIdx.x; item < items; item += gridDim.x) {
-        const uint64_t first = (uint64_t)(item / tiles) * g.share, here = stages - first < g.share ? stages - first : g.share;
+        const uint32_t first = item / tiles * g.share, here = stages - first < g.share ? stages - first : g.share;
 #pragma unroll
         for (uint32_t i = 0; i < T::TI; ++i)
 #pragma unroll
             for (uint32_t j = 0; j < T::TJ; ++j) acc[i][j] = f32x16{};
 #pragma nounroll
-        for (uint64_t s = 0; s < here; ++s) {
-            read(buffer, 1, half1);
-            multiply(half0, nothing);
-            read(buffer, 2, half0);
-            multiply(half1, nothing);
-            read(buffer, 3, half1);
-            multiply(half0, nothing);
-            vm_wait_barrier<0, STORES>(stores_behind);
-            stores_behind = 0;
-            buffer ^= 1u;
+        for (uint32_t s = 0; s < here; ++s) {
+#pragma unroll
+            for (uint32_t step = 1; step < T::STEPS; ++step) {
+                read(buffer, step, step % 2 ? half1 : half0);
+                multiply(step % 2 ? half0 : half1, nothing);
+            }
+            vm_wait_barrier<(T::NB - 2) * T::LOADS, STORES>(stores_behind);
+            stores_behind = stores_behind ? stores_behind - 1 : 0;
+            buffer = buffer + 1 == T::NB ? 0u : buffer + 1;
             read(buffer, 0, half0);                                           // (behind the last item: of a buffer, and for nothing)
             multiply(half1, [&](uint32_t k) { bring(k, T::TI * T::TJ); });    // the loads between the products: what sets them up costs no time
             brought();
@@ -280,7 +319,7 @@ __global__ __launch_bounds__(64 * T::WAVES, 2) void k_gemm_tile(GemmArgs g) {
         constexpr uint32_t PASSES = 8 * LANES > 64 ? 8 * LANES / 64 : 1, PASS_ROWS = 8 / PASSES;
         uint32_t l;                                                           // the lane, found anew: kept through the loop, it would cost a register
         asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(l));
-        float* mine = reinterpret_cast<float*>(s_mem + 2 * T::STAGE + wave * T::OUT);
+        float* mine = reinterpret_cast<float*>(s_mem + T::NB * T::STAGE + wave * T::OUT);
         const uint32_t rows = g.M - tile_m < BM ? (uint32_t)(g.M - tile_m) : BM, cols = g.N - tile_n < BN ? (uint32_t)(g.N - tile_n) : BN;
         const uint32_t row = l / LANES, wcol = wn * T::COLS + EACH * (l % LANES), col = EACH * (l % LANES);
         const bool row_in = PASSES > 1 || row < 8, whole = wcol + EACH <= cols, cut = wcol < cols && !whole;
@@ -301,51 +340,59 @@ __global__ __launch_bounds__(64 * T::WAVES, 2) void k_gemm_tile(GemmArgs g) {
         };
         if constexpr (END == END_SOFTMAX) {
             const SoftmaxEnd& o = g.soft;
-            int32_t target[4 * T::TI];
+            static_assert(PASSES == 1, "a lane's row of eight");
+            const bool tile_cut = cols < BN;
+            uint32_t target[4 * T::TI];                                       // as the lane's column, where it is one of the lane's
 #pragma unroll
             for (uint32_t x = 0; x < 4 * T::TI; ++x) {
                 const uint32_t r = wm * (BM / WM) + 8 * x + row;
-                target[x] = row_in && r < rows ? o.target[tile_m + r] : -1;
+                target[x] = row_in && r < rows ? (uint32_t)o.target[tile_m + r] - (uint32_t)(tile_n + wcol) : EACH;
             }
+            f32x4 next[1][2];
+            through(0, 0, next);
 #pragma unroll
-            for (uint32_t i = 0; i < T::TI; ++i) {
-                const uint32_t first = wm * (BM / WM) + 32 * i;
-                const __amdgpu_buffer_rsrc_t to = buffer_of(static_cast<uint8_t*>(o.e) + ((tile_m + first) * o.pitch + tile_n) * 2, 0xFFFFFF00u);
+            for (uint32_t x = 0; x < 4 * T::TI; ++x) {
+                const uint32_t i = x / 4, e = x % 4, r = wm * (BM / WM) + 8 * x + row;
+                float v[EACH];
 #pragma unroll
-                for (uint32_t e = 0; e < 4; ++e) {
-                    f32x4 v[PASSES][EACH / 4];
-                    through(i, e, v);
-                    const uint32_t r = first + 8 * e + row;
-                    const bool in = row_in && r < rows;
-                    float m = -INFINITY, s = 0.f, x[EACH];
+                for (uint32_t k = 0; k < EACH; ++k) v[k] = next[0][k / 4][k % 4];
+                if (x + 1 < 4 * T::TI) through((x + 1) / 4, (x + 1) % 4, next);
+                const bool in = row_in && r < rows;
+                if (target[x] < EACH && target[x] + wcol < cols) {
+                    float at = v[0];
 #pragma unroll
-                    for (uint32_t k = 0; k < EACH; ++k) {
-                        x[k] = v[0][k / 4][k % 4];
-                        const uint32_t at = (uint32_t)(target[4 * i + e] - (int32_t)(tile_n + wcol));
-                        if (at == k && in && wcol + k < cols) o.picked[tile_m + r] = x[k];
-                        if (wcol + k >= cols) x[k] = -INFINITY;
-                        m = fmaxf(m, x[k]);
-                    }
-                    m = fmaxf(m, __uint_as_float(dpp_u32<DPP_XOR1>(__float_as_uint(m))));
-                    m = fmaxf(m, __uint_as_float(dpp_u32<DPP_XOR2>(__float_as_uint(m))));
-                    if (LANES == 8) m = fmaxf(m, __uint_as_float(dpp_u32<DPP_HALF_MIRROR>(__float_as_uint(m))));
-                    const float from = m == -INFINITY ? 0.f : m;
+                    for (uint32_t k = 1; k < EACH; ++k) at = target[x] == k ? v[k] : at;
+                    o.picked[tile_m + r] = at;
+                }
+                if (tile_cut)
+#pragma unroll
+                    for (uint32_t k = 0; k < EACH; ++k) v[k] = wcol + k < cols ? v[k] : -INFINITY;
+                float m = v[0], sum = 0.f;
+#pragma unroll
+                for (uint32_t k = 1; k < EACH; ++k) m = fmaxf(m, v[k]);
+                m = fmaxf(m, __uint_as_float(dpp_u32<DPP_XOR1>(__float_as_uint(m))));
+                m = fmaxf(m, __uint_as_float(dpp_u32<DPP_XOR2>(__float_as_uint(m))));
+                if (LANES == 8) m = fmaxf(m, __uint_as_float(dpp_u32<DPP_HALF_MIRROR>(__float_as_uint(m))));
+                const float from = (m == -INFINITY ? 0.f : m) * LOG2E;
+#pragma unroll
+                for (uint32_t k = 0; k < EACH; ++k) {
+                    v[k] = __builtin_amdgcn_exp2f(fmaf(v[k], LOG2E, -from));
+                    sum += v[k];
+                }
+                sum += __uint_as_float(dpp_u32<DPP_XOR1>(__float_as_uint(sum)));
+                sum += __uint_as_float(dpp_u32<DPP_XOR2>(__float_as_uint(sum)));
+                if (LANES == 8) sum += __uint_as_float(dpp_u32<DPP_HALF_MIRROR>(__float_as_uint(sum)));
+                if (o.e) {
                     u32x4 out;
 #pragma unroll
-                    for (uint32_t k = 0; k < EACH; ++k) {
-                        x[k] = __builtin_amdgcn_exp2f((x[k] - from) * LOG2E);
-                        s += x[k];
-                    }
-#pragma unroll
-                    for (uint32_t k = 0; k < 4; ++k) out[k] = pack2<TYPE>(x[2 * k], x[2 * k + 1]);
-                    s += __uint_as_float(dpp_u32<DPP_XOR1>(__float_as_uint(s)));
-                    s += __uint_as_float(dpp_u32<DPP_XOR2>(__float_as_uint(s)));
-                    if (LANES == 8) s += __uint_as_float(dpp_u32<DPP_HALF_MIRROR>(__float_as_uint(s)));
-                    if (o.e) __builtin_amdgcn_raw_buffer_store_b128(out, to, in && tile_n + wcol < o.pitch ? ((8 * e + row) * (uint32_t)o.pitch + wcol) * 2 : BEYOND, 0, 0);
-                    if (in && l % LANES == 0 && wn * T::COLS < cols) o.strips[(tile_m + r) * o.strips_row + tn * WN + wn] = f32x2{m, s};
+                    for (uint32_t k = 0; k < 4; ++k) out[k] = SmallFloat<TYPE>::pack(v[2 * k], v[2 * k + 1]);
+                    const uint32_t first = wm * (BM / WM) + 32 * i;
+                    const __amdgpu_buffer_rsrc_t to = buffer_of(static_cast<uint8_t*>(o.e) + ((tile_m + first) * o.pitch + tile_n) * 2, 0xFFFFFF00u);
+                    __builtin_amdgcn_raw_buffer_store_b128(out, to, in && tile_n + wcol < o.pitch ? ((8 * e + row) * (uint32_t)o.pitch + wcol) * 2 : BEYOND, 0, STREAM);
                 }
+                if (in && l % LANES == 0 && wn * T::COLS < cols) o.strips[(tile_m + r) * o.strips_row + tn * WN + wn] = f32x2{m, sum};
             }
-            stores_behind = o.e ? 1u : 0u;
+            stores_behind = o.e ? T::NB - 1 : 0u;
         } else {
             const GemmEnd& o = g.end;
             const float scale = o.scale ? *o.scale : 1.f;
@@ -354,6 +401,7 @@ __global__ __launch_bounds__(64 * T::WAVES, 2) void k_gemm_tile(GemmArgs g) {
 #pragma unroll
             for (uint32_t k = 0; k < EACH; ++k) bias[k] = o.bias && wcol + k < cols ? load1<TYPE>(o.bias, tile_n + wcol + k) : 0.f;
             const uint32_t at = (row * (uint32_t)o.ld + wcol) * BYTES;
+            f32x4 next[PASSES][EACH / 4];                                     // the sums of the pass after this one, on their way
 #pragma unroll
             for (uint32_t i = 0; i < T::TI; ++i) {
                 const uint32_t first = wm * (BM / WM) + 32 * i;               // the store's rows begin here: the lanes' offsets are those of 32 rows, below 2^32
@@ -387,6 +435,11 @@ __global__ __launch_bounds__(64 * T::WAVES, 2) void k_gemm_tile(GemmArgs g) {
 #pragma unroll
                 for (uint32_t e = 0; e < 4; ++e) {
                     f32x4 v[PASSES][EACH / 4], res32[PASSES][EACH / 4];
+                    if (i + e == 0) through(0, 0, next);
+#pragma unroll
+                    for (uint32_t p = 0; p < PASSES; ++p)
+#pragma unroll
+                        for (uint32_t k = 0; k < EACH / 4; ++k) v[p][k] = next[p][k];
                     if (o.residual && o.res32) {
 #pragma unroll
                         for (uint32_t p = 0; p < PASSES; ++p) {
@@ -402,7 +455,7 @@ __global__ __launch_bounds__(64 * T::WAVES, 2) void k_gemm_tile(GemmArgs g) {
                                 }
                         }
                     }
-                    through(i, e, v);
+                    if (4 * i + e + 1 < 4 * T::TI) through((4 * i + e + 1) / 4, (e + 1) % 4, next);
 #pragma unroll
                     for (uint32_t p = 0; p < PASSES; ++p) {
                         // (the whole offset in the lane's register: a 16-byte store with a scalar offset as well has stored values that the next instructions
@@ -411,21 +464,25 @@ __global__ __launch_bounds__(64 * T::WAVES, 2) void k_gemm_tile(GemmArgs g) {
                         const bool in = row_in && first + r + row < rows;
                         float x[EACH];
 #pragma unroll
-                        for (uint32_t k = 0; k < EACH; ++k) x[k] = fmaf(v[p][k / 4][k % 4], scale, bias[k]);
+                        for (uint32_t k = 0; k < EACH; ++k) x[k] = v[p][k / 4][k % 4];
+                        if (o.bias || o.scale)
+#pragma unroll
+                            for (uint32_t k = 0; k < EACH; ++k) x[k] = fmaf(x[k], scale, bias[k]);
                         if (o.z && in) {
                             uint16_t* q = static_cast<uint16_t*>(o.z) + (tile_m + first + r + row) * o.ld_z + tile_n + wcol;
                             if (whole) {
 #pragma unroll
-                                for (uint32_t k = 0; k < EACH; k += 4) *reinterpret_cast<u32x2_any*>(q + k) = u32x2_any{pack2<TYPE>(x[k], x[k + 1]), pack2<TYPE>(x[k + 2], x[k + 3])};
+                                for (uint32_t k = 0; k < EACH; k += 4) __builtin_nontemporal_store((u32x2_any{pack2<TYPE>(x[k], x[k + 1]), pack2<TYPE>(x[k + 2], x[k + 3])}), reinterpret_cast<u32x2_any*>(q + k));
                             } else if (cut) {
 #pragma unroll
                                 for (uint32_t k = 0; k < EACH; ++k)
                                     if (wcol + k < cols) store1<TYPE>(q, k, x[k]);
                             }
                         }
-                        if (o.act != ACT_NONE)
+                        with_act(o.act, [&](auto kind) {
 #pragma unroll
-                            for (uint32_t k = 0; k < EACH; ++k) x[k] = act_of(x[k], o.act);
+                            for (uint32_t k = 0; k < EACH; ++k) x[k] = act_as<decltype(kind)::value>(x[k]);
+                        });
                         if (o.residual)
 #pragma unroll
                             for (uint32_t k = 0; k < EACH; ++k) {
@@ -435,7 +492,7 @@ __global__ __launch_bounds__(64 * T::WAVES, 2) void k_gemm_tile(GemmArgs g) {
                         u32x4 out;
 #pragma unroll
                         for (uint32_t k = 0; k < 4; ++k) out[k] = BYTES == 4 ? __float_as_uint(x[k]) : pack2<TYPE>(x[2 * k % EACH], x[(2 * k + 1) % EACH]);
-                        __builtin_amdgcn_raw_buffer_store_b128(out, to, in && whole ? to_at : BEYOND, 0, 0);
+                        __builtin_amdgcn_raw_buffer_store_b128(out, to, in && whole ? to_at : BEYOND, 0, STREAM);
                         if (in && cut) {
 #pragma unroll
                             for (uint32_t k = 0; k < EACH; ++k) {
@@ -447,7 +504,7 @@ __global__ __launch_bounds__(64 * T::WAVES, 2) void k_gemm_tile(GemmArgs g) {
                     }
                 }
             }
-            stores_behind = 1u;
+            stores_behind = T::NB - 1;
             if (cols % EACH != 0) {                                           // (so many more stores that the counter would not tell)
                 stores_behind = 0;
                 asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -457,23 +514,31 @@ __global__ __launch_bounds__(64 * T::WAVES, 2) void k_gemm_tile(GemmArgs g) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                          // no load may reach LDS that is another workgroup's by then
 }
 
-// The parts of a sum, in their order, and its end.  A thread takes four columns.
-template <uint32_t TYPE, bool OUT32>
+// The parts of a sum, in their order, and its end.  A thread takes four columns, together where the parts' rows lie at 16-byte addresses (VEC).  Bound by memory.
+template <uint32_t TYPE, bool OUT32, bool VEC>
 __global__ __launch_bounds__(256) void k_gemm_join(const float* __restrict__ parts, uint32_t splits, uint64_t M, uint64_t N, GemmEnd o) {
     const uint64_t each = (N + 3) / 4, i = (uint64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= M * each) return;
     const uint64_t m = i / each, n = 4 * (i % each);
     const float scale = o.scale ? *o.scale : 1.f;
+    float v[4] = {};
+    if (VEC) {
+        f32x4 sum = *reinterpret_cast<const f32x4*>(parts + m * N + n);
+#pragma unroll 4
+        for (uint32_t p = 1; p < splits; ++p) sum = sum + *reinterpret_cast<const f32x4*>(parts + (p * M + m) * N + n);
+#pragma unroll
+        for (uint32_t k = 0; k < 4; ++k) v[k] = sum[k];
+    }
 #pragma unroll
     for (uint32_t k = 0; k < 4; ++k) {
         if (n + k >= N) break;
-        float v = 0.f;
-        for (uint32_t p = 0; p < splits; ++p) v += parts[(p * M + m) * N + n + k];
-        v = fmaf(v, scale, o.bias ? load1<TYPE>(o.bias, n + k) : 0.f);
-        if (o.z) store1<TYPE>(o.z, m * o.ld_z + n + k, v);
-        v = act_of(v, o.act);
-        if (o.residual) v += o.res32 ? static_cast<const float*>(o.residual)[m * o.ld_res + n + k] : load1<TYPE>(o.residual, m * o.ld_res + n + k);
-        store1<OUT32 ? TYPE_F32 : TYPE>(o.out, m * o.ld + n + k, v);
+        if (!VEC)
+            for (uint32_t p = 0; p < splits; ++p) v[k] += parts[(p * M + m) * N + n + k];
+        v[k] = fmaf(v[k], scale, o.bias ? load1<TYPE>(o.bias, n + k) : 0.f);
+        if (o.z) store1<TYPE>(o.z, m * o.ld_z + n + k, v[k]);
+        v[k] = act_of(v[k], o.act);
+        if (o.residual) v[k] += o.res32 ? static_cast<const float*>(o.residual)[m * o.ld_res + n + k] : load1<TYPE>(o.residual, m * o.ld_res + n + k);
+        store1<OUT32 ? TYPE_F32 : TYPE>(o.out, m * o.ld + n + k, v[k]);
     }
 }
 

@@ -102,12 +102,12 @@ __global__ __launch_bounds__(256) void k_rows_copy(const void* __restrict__ from
     reinterpret_cast<u32x4*>(to)[i] = u32x4{v.r[0], v.r[1], v.r[2], v.r[3]};
 }
 
-// dz = dy act'(z), rounded to the type, and the sums of its columns in fp32 (of what was not rounded): of 128 rows a workgroup, 512 columns.  Bound by memory.
-constexpr uint32_t SUM_ROWS = 128, SUM_COLS = 512;
+// dz = dy act'(z), rounded to the type, and the sums of its columns in fp32 (of what was not rounded): of 64 rows a workgroup, 512 columns.  Bound by memory.
+constexpr uint32_t SUM_ROWS = 64, SUM_COLS = 512;
 struct ActGradArgs {
     const void *dy, *z;          // z null: no activation
     void* dz;                    // or null; pitch elements from row to row, filled up with zeros
-    float* sums;                 // [ceil(M / 128)][N], or null
+    float* sums;                 // [ceil(M / 64)][N], or null
     uint64_t M, N, ld_dy, ld_z, pitch;
     uint32_t act;
 };
@@ -118,22 +118,30 @@ __global__ __launch_bounds__(256) void k_act_grad(ActGradArgs a) {
     const uint64_t c = (uint64_t)blockIdx.x * SUM_COLS + 8 * lane, m0 = (uint64_t)blockIdx.y * SUM_ROWS, m1 = m0 + SUM_ROWS < a.M ? m0 + SUM_ROWS : a.M;
     const int64_t n = (int64_t)a.N - (int64_t)c;
     float sum[8] = {};
+    constexpr uint32_t U = 4;                            // rows of a wave under way together
     if (c < a.pitch)
-        for (uint64_t m = m0 + wave; m < m1; m += 4) {
-            const Raw8<TYPE> g = load8_first<TYPE>(a.dy, m * a.ld_dy + c, n);
-            float v[8];
-            if (a.z) {
-                const Raw8<TYPE> z = load8_first<TYPE>(a.z, m * a.ld_z + c, n);
+        with_act(a.z ? a.act : (uint32_t)ACT_NONE, [&](auto kind) {
+            constexpr uint32_t ACT = decltype(kind)::value;
+            for (uint64_t m = m0 + wave; m < m1; m += 4 * U) {
+                Raw8<TYPE> g[U], z[U];
 #pragma unroll
-                for (uint32_t k = 0; k < 8; ++k) v[k] = (int64_t)k < n ? g.at(k) * act_slope(z.at(k), a.act) : 0.f;
-            } else {
+                for (uint32_t u = 0; u < U; ++u) {
+                    const uint64_t r = m + 4 * u < m1 ? m + 4 * u : m;
+                    g[u] = load8_first<TYPE>(a.dy, r * a.ld_dy + c, n);
+                    if (ACT != ACT_NONE) z[u] = load8_first<TYPE>(a.z, r * a.ld_z + c, n);
+                }
 #pragma unroll
-                for (uint32_t k = 0; k < 8; ++k) v[k] = g.at(k);
+                for (uint32_t u = 0; u < U; ++u) {
+                    if (m + 4 * u >= m1) break;
+                    float v[8];
+#pragma unroll
+                    for (uint32_t k = 0; k < 8; ++k) v[k] = ACT == ACT_NONE ? g[u].at(k) : (int64_t)k < n ? g[u].at(k) * slope_as<ACT>(z[u].at(k)) : 0.f;
+                    if (a.dz) store8<TYPE>(a.dz, (m + 4 * u) * a.pitch + c, v);
+#pragma unroll
+                    for (uint32_t k = 0; k < 8; ++k) sum[k] += v[k];
+                }
             }
-            if (a.dz) store8<TYPE>(a.dz, m * a.pitch + c, v);
-#pragma unroll
-            for (uint32_t k = 0; k < 8; ++k) sum[k] += v[k];
-        }
+        });
     if (!a.sums) return;
 #pragma unroll
     for (uint32_t k = 0; k < 8; ++k) s_sum[wave][8 * lane + k] = sum[k];
@@ -143,7 +151,7 @@ __global__ __launch_bounds__(256) void k_act_grad(ActGradArgs a) {
         if (col < a.N) a.sums[blockIdx.y * a.N + col] = s_sum[0][i] + s_sum[1][i] + s_sum[2][i] + s_sum[3][i];
     }
 }
-// The sums of all rows from those of 128 each: a wave of a workgroup takes every fourth.
+// The sums of all rows from those of 64 each: a wave of a workgroup takes every fourth.
 __global__ __launch_bounds__(256) void k_sum_join(const float* __restrict__ sums, uint64_t parts, uint64_t N, float* __restrict__ out) {
     __shared__ float s_sum[4][64];
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;

@@ -1,8 +1,8 @@
 // Softmax cross entropy of a linear head without its logits.  With z = x W^T, lse_r = ln sum_v exp(z_rv) and p = exp(z - lse),
 //     loss_r = w_r (lse_r - z_{r, t_r}),   G = w (p - onehot(t)),   dx = G W,   dW = G^T x.
 // The product z goes by tiles (k_gemm.h) whose end is END_SOFTMAX: of a strip of a row's columns (32 or 64) only its largest sum m and s = sum exp(z - m)
-// are kept, and for a gradient e = exp(z - m) in 16 bits, of a piece of the rows at a time.  With lse known, e becomes G in its place, e exp(m - lse) w: a
-// rounding of e and one of G, each as large as that of a p that is rounded once.  At the target, where p - 1 may be much smaller than p, it is taken from the fp32
+// are kept, and for a gradient e = exp(z - m) in 16 bits (SmallFloat, whose rounding is small beside the type's), of a piece of the rows at a time.  With lse known, e
+// becomes G in its place, e exp(m - lse) w, in the type of the products.  At the target, where p - 1 may be much smaller than p, it is taken from the fp32
 // logit.  A second product for z in the place of e would cost 2 R V D operations more; e costs 4 bytes of traffic an element.
 #pragma once
 #include "k_linear.h"
@@ -16,7 +16,7 @@ struct XentArgs {
     const float* weight;         // or null: 1
     float *loss, *lse;           // or null
     f32x2* rows_out;             // [rows]: lse, and the row's weight times `scale` (0: the row does not count)
-    void* e;                     // [rows, pitch]: exp(z - m), and then G
+    void* e;                     // [rows, pitch]: exp(z - m) as a SmallFloat, and then G
     const float* scale;          // two numbers on the device: what G is multiplied by, and its inverse; or null
     uint64_t rows, pitch;
     uint32_t vocab, strips_row, strip;
@@ -77,14 +77,11 @@ __global__ __launch_bounds__(256) void k_xent_gradient(XentArgs a, uint32_t chun
     u32x4 out = {0u, 0u, 0u, 0u};
     if (live) {
         const u32x4 w = *at;
-        Raw8<TYPE> e;
-#pragma unroll
-        for (uint32_t k = 0; k < 4; ++k) e.r[k] = w[k];
         const float m = a.strips[row * a.strips_row + col / a.strip][0], f = __builtin_amdgcn_exp2f((m - of[0]) * LOG2E) * of[1];
         const uint32_t t = (uint32_t)a.target[row] - (uint32_t)col;
         float v[8];
 #pragma unroll
-        for (uint32_t k = 0; k < 8; ++k) v[k] = col + k < a.vocab ? e.at(k) * f : 0.f;
+        for (uint32_t k = 0; k < 8; ++k) v[k] = col + k < a.vocab ? SmallFloat<TYPE>::at(w[k / 2], k % 2) * f : 0.f;
         if (t < 8) {
             const float p = expm1f(a.picked[row] - of[0]) * of[1];
 #pragma unroll

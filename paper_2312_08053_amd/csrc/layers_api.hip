@@ -20,12 +20,14 @@ static_assert(ACT_NONE == KIMAD_ACT_NONE && ACT_RELU == KIMAD_ACT_RELU && ACT_GE
 constexpr uint64_t FEW_ROWS = 32;                        // products of so many rows may go by k_gemm_few
 constexpr uint64_t LD_MOST = 1ull << 22;                 // operands: 256 rows are reached by 32-bit offsets
 constexpr uint64_t OUT_LD_MOST = 1ull << 24;             // results: 32 rows
-constexpr uint64_t ROWS_MOST = 65535ull * SUM_ROWS;      // 8388480: the column sums' grid
+constexpr uint64_t ROWS_MOST = 65535ull * SUM_ROWS;      // 4194240: the column sums' grid
 constexpr uint64_t MATRIX_MOST = 1ull << 34;             // elements of a matrix, less one: the grids of what lays it out or joins its parts
 
-typedef GemmTile<256, 256, 2, 4> Gemm256;
-typedef GemmTile<128, 128, 2, 2> Gemm128;
-typedef GemmTile<64, 64, 2, 2> Gemm64;
+typedef GemmTile<256, 256, 2, 4, 64, 2> Gemm256;
+typedef GemmTile<128, 128, 2, 2, 64, 2> Gemm128;
+typedef GemmTile<64, 64, 2, 2, 64, 2> Gemm64;
+constexpr uint64_t STAGE_K = 64;
+static_assert(Gemm256::SK == STAGE_K && Gemm128::SK == STAGE_K && Gemm64::SK == STAGE_K, "stages of the tiles");
 
 template <class F>
 int with_half_type(uint32_t type, F f) {
@@ -56,7 +58,7 @@ struct GemmPlan {
 GemmPlan gemm_plan(uint64_t M, uint64_t N, uint64_t K, bool wide, bool may_split, bool may_few) {
     GemmPlan best{};
     best.splits = 1;
-    const uint64_t stages = (K + GEMM_STAGE_K - 1) / GEMM_STAGE_K;
+    const uint64_t stages = (K + STAGE_K - 1) / STAGE_K;
     best.share = (uint32_t)stages;
     if (may_few && M <= FEW_ROWS) {
         best.kind = GemmPlan::FEW;
@@ -90,7 +92,7 @@ uint64_t gemm_edge(const GemmPlan& p) { return p.kind == GemmPlan::T256 ? 256 : 
 // The same way of sharing out for a product with fewer rows or a shorter sum (it needs no more room).
 GemmPlan fewer(GemmPlan p, uint64_t M, uint64_t K) {
     if (p.kind == GemmPlan::FEW) return p;
-    const uint64_t stages = (K + GEMM_STAGE_K - 1) / GEMM_STAGE_K;
+    const uint64_t stages = (K + STAGE_K - 1) / STAGE_K;
     p.tiles_m = (M + gemm_edge(p) - 1) / gemm_edge(p);
     p.share = (uint32_t)((stages + p.splits - 1) / p.splits);
     p.splits = (uint32_t)((stages + p.share - 1) / p.share);
@@ -131,8 +133,13 @@ int launch_gemm(GemmArgs g, const GemmPlan& p, bool out32, float* parts, hipStre
     g.end.out = parts; g.end.ld = g.N;
     const int rc = launch_kind<TYPE, XA, XB, END_F32>(g, p, s);
     if (rc) return rc;
-    if (out32) hipLaunchKernelGGL((k_gemm_join<TYPE, true>), dim3((uint32_t)wgs), dim3(256), 0, s, parts, p.splits, g.M, g.N, end);
-    else hipLaunchKernelGGL((k_gemm_join<TYPE, false>), dim3((uint32_t)wgs), dim3(256), 0, s, parts, p.splits, g.M, g.N, end);
+    auto join = [&](auto o32, auto vec) {
+        hipLaunchKernelGGL((k_gemm_join<TYPE, decltype(o32)::value, decltype(vec)::value>), dim3((uint32_t)wgs), dim3(256), 0, s, parts, p.splits, g.M, g.N, end);
+    };
+    constexpr std::true_type yes{};
+    constexpr std::false_type no{};
+    if (g.N % 4 == 0) out32 ? join(yes, yes) : join(no, yes);
+    else out32 ? join(yes, no) : join(no, no);
     return launched();
 }
 

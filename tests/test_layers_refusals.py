@@ -28,7 +28,7 @@ def dropout(x=P, kind=F32, rows=4, cols=8, ld=8, res=0, ld_res=8, p=0.5, seed=1,
 @pytest.mark.parametrize("bad", [
     dict(kind=F32), dict(kind=3), dict(out_kind=F16), dict(out_kind=3), dict(act=4), dict(ld_x=63), dict(ld_w=63), dict(ld_out=47), dict(x=0), dict(w=0), dict(out=0),
     dict(x=P + 1), dict(w=P + 1), dict(out=P + 1), dict(out=P + 2, out_kind=F32), dict(bias=P + 1), dict(res=P + 1), dict(res=P, ld_res=47), dict(z=P + 1), dict(z=P, ld_z=47),
-    dict(M=8388481), dict(ld_x=(1 << 22) + 1), dict(ld_out=(1 << 24) + 1), dict(N=(1 << 22) + 1, ld_out=1 << 23), dict(M=1 << 20, N=1 << 14, ld_out=1 << 14)])
+    dict(M=4194241), dict(ld_x=(1 << 22) + 1), dict(ld_out=(1 << 24) + 1), dict(N=(1 << 22) + 1, ld_out=1 << 23), dict(M=1 << 20, N=1 << 14, ld_out=1 << 14)])
 def test_linear_refuses(bad):
     assert linear(**bad) == BAD
 
@@ -45,7 +45,7 @@ def test_linear_asks_for_its_workspace():
 
 @pytest.mark.parametrize("bad", [
     dict(kind=F32), dict(dw_kind=F16), dict(act=4), dict(act=1), dict(act=1, z=P + 1), dict(act=1, z=P, ld_z=47), dict(dy=0), dict(dy=P + 1), dict(ld_dy=47), dict(x=0), dict(w=0),
-    dict(dx=P + 1), dict(dw=P + 1), dict(dw=P + 2, dw_kind=F32), dict(db=P + 2), dict(ld_dx=63), dict(ld_dw=63), dict(M=8388481), dict(ld_dy=(1 << 22) + 1)])
+    dict(dx=P + 1), dict(dw=P + 1), dict(dw=P + 2, dw_kind=F32), dict(db=P + 2), dict(ld_dx=63), dict(ld_dw=63), dict(M=4194241), dict(ld_dy=(1 << 22) + 1)])
 def test_linear_grad_refuses(bad):
     assert linear_grad(**bad) == BAD
 
@@ -55,7 +55,7 @@ def test_linear_grad_asks_for_its_workspace():
     assert need(P, 48, P, 64, P, 64, 40, 48, 64, 0, 7) == 0
     assert need(P, 48, P, 64, P, 64, 40, 48, 64, 1, 1) == 2 * 40 * 48                                           # dz
     assert need(P, 48, P, 64, P, 64, 40, 48, 64, 1, 4) == 0                                                     # the bias alone
-    assert need(P, 48, P, 64, P, 64, 400, 48, 64, 0, 4) == 4 * 4 * 48                                           # sums of 128 rows each
+    assert need(P, 48, P, 64, P, 64, 400, 48, 64, 0, 4) == 7 * 4 * 48 + 192                                        # sums of 64 rows each, in whole 256 bytes
     assert linear_grad(act=1, z=P) == SMALL and linear_grad(act=1, z=P, ws=P + 8, nbytes=BIG) == SMALL
     assert linear_grad(x=0, dw=0, ws=0, dx=0, w=0) == OK                                                        # nothing wanted
 
@@ -63,7 +63,7 @@ def test_linear_grad_asks_for_its_workspace():
 @pytest.mark.parametrize("bad", [
     dict(kind=F32), dict(dw=P, dw_kind=F16), dict(vocab=0), dict(vocab=(1 << 22) - 63), dict(dim=0, ld_x=64), dict(ld_x=63), dict(ld_w=63), dict(x=0), dict(w=0), dict(x=P + 1),
     dict(target=0), dict(target=P + 2), dict(weight=P + 2), dict(loss=P + 2), dict(lse=P + 2), dict(dx=P + 1), dict(dx=P, ld_dx=63), dict(dw=P + 1), dict(dw=P, ld_dw=63),
-    dict(dw=P + 2, dw_kind=F32), dict(rows=8388481), dict(loss=0)])
+    dict(dw=P + 2, dw_kind=F32), dict(rows=4194241), dict(loss=0)])
 def test_cross_entropy_refuses(bad):
     assert xent(**bad, nbytes=BIG) == BAD
 
