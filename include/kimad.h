@@ -475,7 +475,7 @@ int kimad_distill_grad(const void* logits, uint32_t type, uint64_t rows, uint64_
  * where they are stored.  Matrices have contiguous rows, `ld` elements apart: at most 2^22 for operands of a product, 2^24 for its
  * results and what is added to them.  At most 4194240 rows (tokens), 2^22 features, and fewer than 2^34 elements a matrix, its columns counted as seven more; more are
  * refused.  Operands are read fastest where they begin at 16-byte addresses, ld is a multiple of 8 and so are the features; others
- * are laid out anew in the workspace first, but for up to 32 rows of a forward product.
+ * are laid out anew in the workspace first, but for forward products of few rows.
  *   workspace   DEVICE, 16-byte aligned, as many bytes as the call's own ..._workspace_bytes says for the same arguments (of the pointers,
  *               which may be NULL there for 16-byte aligned ones, only the alignment counts); a smaller one is refused
  *               (KIMAD_ERR_WORKSPACE_TOO_SMALL), 0 bytes need none.  Its contents need not be kept between calls; calls
@@ -522,8 +522,8 @@ int kimad_linear_grad(const void* dy, uint64_t ld_dy, const void* x, uint64_t ld
  *   dx          DEVICE [rows, dim] of `type`, or NULL;  dw  DEVICE [vocab, dim] of dw_type, `type` or KIMAD_VALUES_F32, or NULL
  * At least one output is wanted, unless there are no rows (then dw is 0).  A row that does not count has loss, lse and gradient 0, adds
  * nothing to dw, and what it holds, Inf and NaN too, reaches nothing.  So does a row whose logits are all -Inf.  For a gradient the
- * exponentials of a piece of the rows are kept, 512 MiB at most or 256 rows, and G, both in `type`: gradients are as exact
- * as ones whose G is rounded twice.  (fp16: G is scaled by a power of two, so that weights need not be.) */
+ * exponentials of a piece of the rows are kept, 512 MiB at most or 256 rows, and turned into G, divided by the largest weight and rounded to
+ * `type`, for the two products. */
 uint64_t kimad_linear_xent_workspace_bytes(const void* x, uint64_t ld_x, const void* w, uint64_t ld_w, uint32_t type, uint64_t rows,
                                            uint64_t vocab, uint64_t dim, uint32_t wants, uint32_t dw_type);
 int kimad_linear_xent(const void* x, uint64_t ld_x, const void* w, uint64_t ld_w, uint32_t type, uint64_t rows, uint64_t vocab,

@@ -107,7 +107,9 @@ struct GemmArgs {
     uint64_t M, N, K;            // K: a multiple of 8 where an operand is stored along it
     uint64_t k_rows_a, k_rows_b; // rows that an operand across K has (beyond them: zeros)
     uint32_t tiles_m, tiles_n;
-    uint32_t splits, share;      // parts of the sum, `share` stages each (the last one fewer); more than one: part p goes to out + p M ld
+    uint32_t whole;              // the first so many tiles are summed by one workgroup each; the others' sums are shared out,
+    uint32_t splits, share;      // in parts of `share` stages each (the last one fewer), part p of the t-th of them at parts + (p * (tiles - whole) + t) tiles
+    float* parts;                // (as the waves' registers lie), which k_gemm_join adds
     GemmEnd end;
     SoftmaxEnd soft;
 };
@@ -198,25 +200,230 @@ constexpr int STREAM = 2;
 
 enum : uint32_t { END_TYPE = 0, END_F32 = 1, END_SOFTMAX = 2 };
 
+// What is done with a wave's sums, TI times 32 rows from row0 of the tile on and its wn-th strip of columns.  `mine`: LDS of the wave's own, T::OUT bytes.  Whether the
+// wave's last accesses are stores, 4 TI or more (fp32: 4 TI TJ).
+template <uint32_t TYPE, class T, uint32_t TI, uint32_t END>
+__device__ __forceinline__ bool gemm_end(const GemmArgs& g, const f32x16 (&acc)[TI][T::TJ], float* mine, uint64_t tile_m, uint64_t tile_n, uint32_t row0, uint32_t wn) {
+    constexpr uint32_t BM = T::BM, BN = T::BN;
+    // Eight rows at a time through LDS, so that stores run along the rows: 16 bytes a lane, whole cache lines.
+    constexpr uint32_t BYTES = END == END_F32 ? 4 : 2, BEYOND = 0xFFFFFFF0u, EACH = 16 / BYTES, LANES = T::COLS / EACH;   // elements of a lane, lanes of a row
+    constexpr uint32_t PASSES = 8 * LANES > 64 ? 8 * LANES / 64 : 1, PASS_ROWS = 8 / PASSES;
+    uint32_t l;                                                           // the lane, found anew: kept through the loop, it would cost a register
+    asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(l));
+    const uint32_t rows = g.M - tile_m < BM ? (uint32_t)(g.M - tile_m) : BM, cols = g.N - tile_n < BN ? (uint32_t)(g.N - tile_n) : BN;
+    const uint32_t row = l / LANES, wcol = wn * T::COLS + EACH * (l % LANES), col = EACH * (l % LANES);
+    const bool row_in = PASSES > 1 || row < 8, whole = wcol + EACH <= cols, cut = wcol < cols && !whole;
+    // eight rows of the wave's sums through LDS, pass by pass
+    auto through = [&](uint32_t i, uint32_t e, f32x4 (&v)[PASSES][EACH / 4]) {
+#pragma unroll
+        for (uint32_t j = 0; j < T::TJ; ++j) {
+            const f32x16 x = acc[i][j];
+#pragma unroll
+            for (uint32_t k = 0; k < 4; ++k) mine[(4 * (l >> 5) + k) * T::PITCH + 32 * j + (l & 31u)] = x[4 * e + k];
+        }
+        wave_sync_lds();
+#pragma unroll
+        for (uint32_t p = 0; p < PASSES; ++p)
+#pragma unroll
+            for (uint32_t q = 0; q < EACH / 4; ++q) v[p][q] = *reinterpret_cast<const f32x4*>(mine + ((p * PASS_ROWS + row) & 7u) * T::PITCH + col + 4 * q);
+        wave_sync_lds();
+    };
+    if constexpr (END == END_SOFTMAX) {
+        const SoftmaxEnd& o = g.soft;
+        static_assert(PASSES == 1, "a lane's row of eight");
+        const bool tile_cut = cols < BN;
+        uint32_t target[4 * TI];                                       // as the lane's column, where it is one of the lane's
+#pragma unroll
+        for (uint32_t x = 0; x < 4 * TI; ++x) {
+            const uint32_t r = row0 + 8 * x + row;
+            target[x] = row_in && r < rows ? (uint32_t)o.target[tile_m + r] - (uint32_t)(tile_n + wcol) : EACH;
+        }
+        f32x4 next[1][2];
+        through(0, 0, next);
+#pragma unroll
+        for (uint32_t x = 0; x < 4 * TI; ++x) {
+            const uint32_t i = x / 4, e = x % 4, r = row0 + 8 * x + row;
+            float v[EACH];
+#pragma unroll
+            for (uint32_t k = 0; k < EACH; ++k) v[k] = next[0][k / 4][k % 4];
+            if (x + 1 < 4 * TI) through((x + 1) / 4, (x + 1) % 4, next);
+            const bool in = row_in && r < rows;
+            if (target[x] < EACH && target[x] + wcol < cols) {
+                float at = v[0];
+#pragma unroll
+                for (uint32_t k = 1; k < EACH; ++k) at = target[x] == k ? v[k] : at;
+                o.picked[tile_m + r] = at;
+            }
+            if (tile_cut)
+#pragma unroll
+                for (uint32_t k = 0; k < EACH; ++k) v[k] = wcol + k < cols ? v[k] : -INFINITY;
+            float m = v[0], sum = 0.f;
+#pragma unroll
+            for (uint32_t k = 1; k < EACH; ++k) m = fmaxf(m, v[k]);
+            m = fmaxf(m, __uint_as_float(dpp_u32<DPP_XOR1>(__float_as_uint(m))));
+            m = fmaxf(m, __uint_as_float(dpp_u32<DPP_XOR2>(__float_as_uint(m))));
+            if (LANES == 8) m = fmaxf(m, __uint_as_float(dpp_u32<DPP_HALF_MIRROR>(__float_as_uint(m))));
+            const float from = (m == -INFINITY ? 0.f : m) * LOG2E;
+#pragma unroll
+            for (uint32_t k = 0; k < EACH; ++k) {
+                v[k] = __builtin_amdgcn_exp2f(fmaf(v[k], LOG2E, -from));
+                sum += v[k];
+            }
+            sum += __uint_as_float(dpp_u32<DPP_XOR1>(__float_as_uint(sum)));
+            sum += __uint_as_float(dpp_u32<DPP_XOR2>(__float_as_uint(sum)));
+            if (LANES == 8) sum += __uint_as_float(dpp_u32<DPP_HALF_MIRROR>(__float_as_uint(sum)));
+            if (o.e) {
+                u32x4 out;
+#pragma unroll
+                for (uint32_t k = 0; k < 4; ++k) out[k] = SmallFloat<TYPE>::pack(v[2 * k], v[2 * k + 1]);
+                const uint32_t first = row0 + 32 * i;
+                const __amdgpu_buffer_rsrc_t to = buffer_of(static_cast<uint8_t*>(o.e) + ((tile_m + first) * o.pitch + tile_n) * 2, 0xFFFFFF00u);
+                __builtin_amdgcn_raw_buffer_store_b128(out, to, in && tile_n + wcol < o.pitch ? ((8 * e + row) * (uint32_t)o.pitch + wcol) * 2 : BEYOND, 0, STREAM);
+            }
+            if (in && l % LANES == 0 && wn * T::COLS < cols) o.strips[(tile_m + r) * o.strips_row + tile_n / T::STRIP + wn] = f32x2{m, sum};
+        }
+        return o.e != nullptr;
+    } else {
+        const GemmEnd& o = g.end;
+        const float scale = o.scale ? *o.scale : 1.f;
+        Raw8<TYPE> bias;                                                      // as it lies
+#pragma unroll
+        for (uint32_t k = 0; k < EACH / 2; ++k) bias.r[k] = 0;
+        if (o.bias)
+#pragma unroll
+            for (uint32_t k = 0; k < EACH; ++k)
+                if (wcol + k < cols) bias.set(k, static_cast<const uint16_t*>(o.bias)[tile_n + wcol + k]);
+        const uint32_t at = (row * (uint32_t)o.ld + wcol) * BYTES;
+        f32x4 next[PASSES][EACH / 4];                                     // the sums of the pass after this one, on their way
+#pragma unroll
+        for (uint32_t i = 0; i < TI; ++i) {
+            const uint32_t first = row0 + 32 * i;               // the store's rows begin here: the lanes' offsets are those of 32 rows, below 2^32
+            const __amdgpu_buffer_rsrc_t to = buffer_of(static_cast<uint8_t*>(o.out) + ((tile_m + first) * o.ld + tile_n) * BYTES, 0xFFFFFF00u);
+            // A residual of 16 bits: that of the 32 rows is under way before the first is used.
+            const uint8_t* res_base = static_cast<const uint8_t*>(o.residual) + ((tile_m + first + row) * o.ld_res + tile_n + wcol) * (o.res32 ? 4 : 2);
+            uint32_t res[4][PASSES][EACH / 2];
+            if (o.residual && !o.res32) {
+#pragma unroll
+                for (uint32_t e = 0; e < 4; ++e)
+#pragma unroll
+                    for (uint32_t p = 0; p < PASSES; ++p) {
+                        const uint32_t r = 8 * e + p * PASS_ROWS;
+                        const uint16_t* q = reinterpret_cast<const uint16_t*>(res_base) + r * o.ld_res;
+                        if (row_in && first + r + row < rows) {
+                            if (whole) {
+#pragma unroll
+                                for (uint32_t k = 0; k < EACH / 2; k += 2) {
+                                    const u32x2_any w = *reinterpret_cast<const u32x2_any*>(q + 2 * k);
+                                    res[e][p][k] = w[0];
+                                    res[e][p][k + 1] = w[1];
+                                }
+                            } else {
+#pragma unroll
+                                for (uint32_t k = 0; k < EACH; k += 2)
+                                    res[e][p][k / 2] = (wcol + k < cols ? (uint32_t)q[k] : 0u) | (wcol + k + 1 < cols ? (uint32_t)q[k + 1] << 16 : 0u);
+                            }
+                        }
+                    }
+            }
+#pragma unroll
+            for (uint32_t e = 0; e < 4; ++e) {
+                f32x4 v[PASSES][EACH / 4], res32[PASSES][EACH / 4];
+                if (i + e == 0) through(0, 0, next);
+#pragma unroll
+                for (uint32_t p = 0; p < PASSES; ++p)
+#pragma unroll
+                    for (uint32_t k = 0; k < EACH / 4; ++k) v[p][k] = next[p][k];
+                if (o.residual && o.res32) {
+#pragma unroll
+                    for (uint32_t p = 0; p < PASSES; ++p) {
+                        const uint32_t r = 8 * e + p * PASS_ROWS;
+                        const float* q = reinterpret_cast<const float*>(res_base) + r * o.ld_res;
+                        if (row_in && first + r + row < rows)
+#pragma unroll
+                            for (uint32_t k = 0; k < EACH; k += 4) {
+                                if (whole) res32[p][k / 4] = *reinterpret_cast<const f32x4_any*>(q + k);
+                                else
+#pragma unroll
+                                    for (uint32_t h = 0; h < 4; ++h) res32[p][k / 4][h] = wcol + k + h < cols ? q[k + h] : 0.f;
+                            }
+                    }
+                }
+                if (4 * i + e + 1 < 4 * TI) through((4 * i + e + 1) / 4, (e + 1) % 4, next);
+#pragma unroll
+                for (uint32_t p = 0; p < PASSES; ++p) {
+                    // (the whole offset in the lane's register: a 16-byte store with a scalar offset as well has stored values that the next instructions
+                    // wrote into its data registers, in rows with such an offset and in no others)
+                    const uint32_t r = 8 * e + p * PASS_ROWS, to_at = at + r * (uint32_t)o.ld * BYTES;
+                    const bool in = row_in && first + r + row < rows;
+                    float x[EACH];
+#pragma unroll
+                    for (uint32_t k = 0; k < EACH; ++k) x[k] = v[p][k / 4][k % 4];
+                    if (o.bias || o.scale)
+#pragma unroll
+                        for (uint32_t k = 0; k < EACH; ++k) x[k] = fmaf(x[k], scale, bias.at(k));
+                    if (o.z && in) {
+                        uint16_t* q = static_cast<uint16_t*>(o.z) + (tile_m + first + r + row) * o.ld_z + tile_n + wcol;
+                        if (whole) {
+#pragma unroll
+                            for (uint32_t k = 0; k < EACH; k += 4) __builtin_nontemporal_store((u32x2_any{pack2<TYPE>(x[k], x[k + 1]), pack2<TYPE>(x[k + 2], x[k + 3])}), reinterpret_cast<u32x2_any*>(q + k));
+                        } else if (cut) {
+#pragma unroll
+                            for (uint32_t k = 0; k < EACH; ++k)
+                                if (wcol + k < cols) store1<TYPE>(q, k, x[k]);
+                        }
+                    }
+                    with_act(o.act, [&](auto kind) {
+#pragma unroll
+                        for (uint32_t k = 0; k < EACH; ++k) x[k] = act_as<decltype(kind)::value>(x[k]);
+                    });
+                    if (o.residual)
+#pragma unroll
+                        for (uint32_t k = 0; k < EACH; ++k) {
+                            const uint32_t w = res[e][p][k / 2] >> (16 * (k % 2)) & 0xFFFFu;
+                            x[k] += o.res32 ? res32[p][k / 4][k % 4] : TYPE == TYPE_BF16 ? __uint_as_float(w << 16) : half_to_float(w);
+                        }
+                    u32x4 out;
+#pragma unroll
+                    for (uint32_t k = 0; k < 4; ++k) out[k] = BYTES == 4 ? __float_as_uint(x[k]) : pack2<TYPE>(x[2 * k % EACH], x[(2 * k + 1) % EACH]);
+                    __builtin_amdgcn_raw_buffer_store_b128(out, to, in && whole ? to_at : BEYOND, 0, STREAM);
+                    if (in && cut) {
+#pragma unroll
+                        for (uint32_t k = 0; k < EACH; ++k) {
+                            const uint32_t ok = wcol + k < cols ? to_at + k * BYTES : BEYOND;
+                            if (BYTES == 4) __builtin_amdgcn_raw_buffer_store_b32(out[k % 4], to, ok, 0, 0);
+                            else __builtin_amdgcn_raw_buffer_store_b16((uint16_t)(out[k / 2 % 4] >> (16 * (k % 2))), to, ok, 0, 0);
+                        }
+                    }
+                }
+            }
+        }
+        if (cols % EACH == 0) return true;
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                  // (so many more stores that the counter would not tell)
+        return false;
+    }
+}
+
 template <uint32_t TYPE, class T, bool ACROSS_A, bool ACROSS_B, uint32_t END>
 __global__ __launch_bounds__(64 * T::WAVES, 2) void k_gemm_tile(GemmArgs g) {
     constexpr uint32_t BM = T::BM, BN = T::BN, WM = T::WM, WN = T::WN;
     __shared__ __attribute__((aligned(1024))) uint8_t s_mem[T::LDS];
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t lds0 = lds_address(s_mem), tiles = g.tiles_m * g.tiles_n, items = tiles * g.splits;
+    const uint32_t lds0 = lds_address(s_mem), tiles = g.tiles_m * g.tiles_n, shared = tiles - g.whole, items = g.whole + shared * g.splits;
     const uint32_t stages = (uint32_t)((g.K + T::SK - 1) / T::SK);
 
     GemmSide<BM, T::WAVES, T::SK, ACROSS_A> sa;
     GemmSide<BN, T::WAVES, T::SK, ACROSS_B> sb;
     sa.begin(wave, lane, g.lda);
     sb.begin(wave, lane, g.ldb);
+    auto stage_first = [&](uint32_t item) { return item < g.whole ? 0u : (item - g.whole) / shared * g.share; };
+    auto stages_of = [&](uint32_t item, uint32_t first) { return item < g.whole || stages - first < g.share ? stages - first : g.share; };
     uint32_t stages_in;                                                       // of the item, this one counted
     auto aim = [&](uint32_t item) {
         uint32_t tm = 0, tn = 0;
         const bool none = item >= items;                                      // (behind the last one the loads go on, of nothing)
-        if (!none) tile_of(item % tiles, g.tiles_m, g.tiles_n, tm, tn);
-        const uint32_t first = none ? 0 : item / tiles * g.share, k0 = first * T::SK;
-        stages_in = stages - first < g.share ? stages - first : g.share;
+        if (!none) tile_of(item < g.whole ? item : g.whole + (item - g.whole) % shared, g.tiles_m, g.tiles_n, tm, tn);
+        const uint32_t first = none ? 0 : stage_first(item), k0 = first * T::SK;
+        stages_in = none ? stages : stages_of(item, first);
         sa.aim(g.a, (uint64_t)tm * BM, none ? 0 : g.M, k0, ACROSS_A ? (uint32_t)g.k_rows_a : (uint32_t)g.K);
         sb.aim(g.b, (uint64_t)tn * BN, none ? 0 : g.N, k0, ACROSS_B ? (uint32_t)g.k_rows_b : (uint32_t)g.K);
     };
@@ -255,13 +462,17 @@ __global__ __launch_bounds__(64 * T::WAVES, 2) void k_gemm_tile(GemmArgs g) {
     auto lane_at = [&](uint32_t edge, uint32_t first, bool across) {          // of 32 rows of the tile from `first` on
         return across ? k_lane * edge * 2 + (((first >> 5) ^ (edge >= 128 ? k_lane & 3u : (k_lane >> 1) & 1u)) << 6) + in_piece : (first + r32) * T::SK * 2;
     };
-    auto read = [&](uint32_t buffer, uint32_t step, Half& h) {
+    // The k-th of the operands of 16 of K, in the order in which the products want them.
+    constexpr uint32_t READS = T::TI + T::TJ;
+    auto read = [&](uint32_t buffer, uint32_t step, uint32_t k, Half& h) {
         const uint8_t *at_a = s_mem + buffer * T::STAGE, *at_b = at_a + BM * T::SK * 2;
-        const uint32_t along = 16u * ((2 * step + kb) ^ turn);
+        const uint32_t along = 16u * ((2 * step + kb) ^ turn), i = k == 0 ? 0 : k - T::TJ, j = k - 1;
+        if (k == 0 || k > T::TJ) h.a[i] = gemm_operand<BM, ACROSS_A>(at_a + lane_at(BM, wm * (BM / WM) + 32 * i, ACROSS_A) + (ACROSS_A ? 0 : along), 16 * step);
+        else h.b[j] = gemm_operand<BN, ACROSS_B>(at_b + lane_at(BN, wn * (BN / WN) + 32 * j, ACROSS_B) + (ACROSS_B ? 0 : along), 16 * step);
+    };
+    auto read_all = [&](uint32_t buffer, uint32_t step, Half& h) {
 #pragma unroll
-        for (uint32_t i = 0; i < T::TI; ++i) h.a[i] = gemm_operand<BM, ACROSS_A>(at_a + lane_at(BM, wm * (BM / WM) + 32 * i, ACROSS_A) + (ACROSS_A ? 0 : along), 16 * step);
-#pragma unroll
-        for (uint32_t j = 0; j < T::TJ; ++j) h.b[j] = gemm_operand<BN, ACROSS_B>(at_b + lane_at(BN, wn * (BN / WN) + 32 * j, ACROSS_B) + (ACROSS_B ? 0 : along), 16 * step);
+        for (uint32_t k = 0; k < READS; ++k) read(buffer, step, k, h);
     };
     auto multiply = [&](const Half& h, auto between) {
         __builtin_amdgcn_sched_barrier(0);
@@ -276,7 +487,15 @@ __global__ __launch_bounds__(64 * T::WAVES, 2) void k_gemm_tile(GemmArgs g) {
             }
         __builtin_amdgcn_sched_barrier(0);
     };
-    auto nothing = [](uint32_t) {};
+    constexpr uint32_t PRODUCTS = T::TI * T::TJ;
+    // Reads along K go between the products that they run beside, those across K before them (8192 x 2048 x 5632: along 174 us before, 170 between; both across
+    // 8192 x 8192 x 8192 870 and 1278: a read that transposes is two).
+    constexpr bool BETWEEN = !ACROSS_A && !ACROSS_B;
+    auto read_beside = [&](uint32_t buffer, uint32_t step, uint32_t k, Half& h) {
+        if (!BETWEEN) return;
+#pragma unroll
+        for (uint32_t r = k * READS / PRODUCTS; r < (k + 1) * READS / PRODUCTS; ++r) read(buffer, step, r, h);
+    };
     // The reads of one half are under way while the other is multiplied, across stages and items too; the barrier in front of a stage's last 16 of K waits
     // for the next stage, and behind it this stage's buffer takes the one NB further on.  A tile is stored while the next item's first stages
     // come; the next barriers let these stores be.
@@ -288,10 +507,10 @@ __global__ __launch_bounds__(64 * T::WAVES, 2) void k_gemm_tile(GemmArgs g) {
     }
     vm_wait_barrier<(T::NB - 1) * T::LOADS, 0>(0);
     uint32_t buffer = 0;
-    read(0, 0, half0);
+    read_all(0, 0, half0);
     uint32_t stores_behind = 0;                                               // not 0: a tile's stores, STORES or more, are behind the loads that the next barrier waits for
     for (uint32_t item = blockIdx.x; item < items; item += gridDim.x) {
-        const uint32_t first = item / tiles * g.share, here = stages - first < g.share ? stages - first : g.share;
+        const uint32_t here = stages_of(item, stage_first(item));
 #pragma unroll
         for (uint32_t i = 0; i < T::TI; ++i)
 #pragma unroll
@@ -300,246 +519,80 @@ __global__ __launch_bounds__(64 * T::WAVES, 2) void k_gemm_tile(GemmArgs g) {
         for (uint32_t s = 0; s < here; ++s) {
 #pragma unroll
             for (uint32_t step = 1; step < T::STEPS; ++step) {
-                read(buffer, step, step % 2 ? half1 : half0);
-                multiply(step % 2 ? half0 : half1, nothing);
+                if (!BETWEEN) read_all(buffer, step, step % 2 ? half1 : half0);
+                multiply(step % 2 ? half0 : half1, [&](uint32_t k) { read_beside(buffer, step, k, step % 2 ? half1 : half0); });
             }
             vm_wait_barrier<(T::NB - 2) * T::LOADS, STORES>(stores_behind);
             stores_behind = stores_behind ? stores_behind - 1 : 0;
             buffer = buffer + 1 == T::NB ? 0u : buffer + 1;
-            read(buffer, 0, half0);                                           // (behind the last item: of a buffer, and for nothing)
-            multiply(half1, [&](uint32_t k) { bring(k, T::TI * T::TJ); });    // the loads between the products: what sets them up costs no time
+            if (!BETWEEN) read_all(buffer, 0, half0);                         // (behind the last item reads and loads go on, of a buffer and of nothing)
+            multiply(half1, [&](uint32_t k) {
+                read_beside(buffer, 0, k, half0);
+                bring(k, PRODUCTS);                                           // (between the products, what sets up the loads costs no time)
+            });
             brought();
         }
 
-        uint32_t tm, tn;
-        tile_of(item % tiles, g.tiles_m, g.tiles_n, tm, tn);
-        const uint64_t tile_m = (uint64_t)tm * BM, tile_n = (uint64_t)tn * BN;
-        // Eight rows at a time through LDS, so that stores run along the rows: 16 bytes a lane, whole cache lines.
-        constexpr uint32_t BYTES = END == END_F32 ? 4 : 2, BEYOND = 0xFFFFFFF0u, EACH = 16 / BYTES, LANES = T::COLS / EACH;   // elements of a lane, lanes of a row
-        constexpr uint32_t PASSES = 8 * LANES > 64 ? 8 * LANES / 64 : 1, PASS_ROWS = 8 / PASSES;
-        uint32_t l;                                                           // the lane, found anew: kept through the loop, it would cost a register
-        asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(l));
-        float* mine = reinterpret_cast<float*>(s_mem + T::NB * T::STAGE + wave * T::OUT);
-        const uint32_t rows = g.M - tile_m < BM ? (uint32_t)(g.M - tile_m) : BM, cols = g.N - tile_n < BN ? (uint32_t)(g.N - tile_n) : BN;
-        const uint32_t row = l / LANES, wcol = wn * T::COLS + EACH * (l % LANES), col = EACH * (l % LANES);
-        const bool row_in = PASSES > 1 || row < 8, whole = wcol + EACH <= cols, cut = wcol < cols && !whole;
-        // eight rows of the wave's sums through LDS, pass by pass
-        auto through = [&](uint32_t i, uint32_t e, f32x4 (&v)[PASSES][EACH / 4]) {
+        const bool part = item >= g.whole;
+        const uint32_t tile = part ? g.whole + (item - g.whole) % shared : item;
+        if (END != END_SOFTMAX && part && g.splits > 1) {
+            uint32_t l;                                                       // the lane, found anew: kept through the loop, it would cost a register
+            asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(l));
+            f32x4* to = reinterpret_cast<f32x4*>(g.parts + (uint64_t)(item - g.whole) * (BM * BN)) + wave * (T::TI * T::TJ * 256) + l;
 #pragma unroll
-            for (uint32_t j = 0; j < T::TJ; ++j) {
-                const f32x16 x = acc[i][j];
+            for (uint32_t i = 0; i < T::TI; ++i)
 #pragma unroll
-                for (uint32_t k = 0; k < 4; ++k) mine[(4 * (l >> 5) + k) * T::PITCH + 32 * j + (l & 31u)] = x[4 * e + k];
-            }
-            wave_sync_lds();
+                for (uint32_t j = 0; j < T::TJ; ++j) {
+                    const f32x16 x = acc[i][j];
 #pragma unroll
-            for (uint32_t p = 0; p < PASSES; ++p)
-#pragma unroll
-                for (uint32_t q = 0; q < EACH / 4; ++q) v[p][q] = *reinterpret_cast<const f32x4*>(mine + ((p * PASS_ROWS + row) & 7u) * T::PITCH + col + 4 * q);
-            wave_sync_lds();
-        };
-        if constexpr (END == END_SOFTMAX) {
-            const SoftmaxEnd& o = g.soft;
-            static_assert(PASSES == 1, "a lane's row of eight");
-            const bool tile_cut = cols < BN;
-            uint32_t target[4 * T::TI];                                       // as the lane's column, where it is one of the lane's
-#pragma unroll
-            for (uint32_t x = 0; x < 4 * T::TI; ++x) {
-                const uint32_t r = wm * (BM / WM) + 8 * x + row;
-                target[x] = row_in && r < rows ? (uint32_t)o.target[tile_m + r] - (uint32_t)(tile_n + wcol) : EACH;
-            }
-            f32x4 next[1][2];
-            through(0, 0, next);
-#pragma unroll
-            for (uint32_t x = 0; x < 4 * T::TI; ++x) {
-                const uint32_t i = x / 4, e = x % 4, r = wm * (BM / WM) + 8 * x + row;
-                float v[EACH];
-#pragma unroll
-                for (uint32_t k = 0; k < EACH; ++k) v[k] = next[0][k / 4][k % 4];
-                if (x + 1 < 4 * T::TI) through((x + 1) / 4, (x + 1) % 4, next);
-                const bool in = row_in && r < rows;
-                if (target[x] < EACH && target[x] + wcol < cols) {
-                    float at = v[0];
-#pragma unroll
-                    for (uint32_t k = 1; k < EACH; ++k) at = target[x] == k ? v[k] : at;
-                    o.picked[tile_m + r] = at;
+                    for (uint32_t e = 0; e < 4; ++e) to[(4 * (i * T::TJ + j) + e) * 64] = f32x4{x[4 * e], x[4 * e + 1], x[4 * e + 2], x[4 * e + 3]};
                 }
-                if (tile_cut)
-#pragma unroll
-                    for (uint32_t k = 0; k < EACH; ++k) v[k] = wcol + k < cols ? v[k] : -INFINITY;
-                float m = v[0], sum = 0.f;
-#pragma unroll
-                for (uint32_t k = 1; k < EACH; ++k) m = fmaxf(m, v[k]);
-                m = fmaxf(m, __uint_as_float(dpp_u32<DPP_XOR1>(__float_as_uint(m))));
-                m = fmaxf(m, __uint_as_float(dpp_u32<DPP_XOR2>(__float_as_uint(m))));
-                if (LANES == 8) m = fmaxf(m, __uint_as_float(dpp_u32<DPP_HALF_MIRROR>(__float_as_uint(m))));
-                const float from = (m == -INFINITY ? 0.f : m) * LOG2E;
-#pragma unroll
-                for (uint32_t k = 0; k < EACH; ++k) {
-                    v[k] = __builtin_amdgcn_exp2f(fmaf(v[k], LOG2E, -from));
-                    sum += v[k];
-                }
-                sum += __uint_as_float(dpp_u32<DPP_XOR1>(__float_as_uint(sum)));
-                sum += __uint_as_float(dpp_u32<DPP_XOR2>(__float_as_uint(sum)));
-                if (LANES == 8) sum += __uint_as_float(dpp_u32<DPP_HALF_MIRROR>(__float_as_uint(sum)));
-                if (o.e) {
-                    u32x4 out;
-#pragma unroll
-                    for (uint32_t k = 0; k < 4; ++k) out[k] = SmallFloat<TYPE>::pack(v[2 * k], v[2 * k + 1]);
-                    const uint32_t first = wm * (BM / WM) + 32 * i;
-                    const __amdgpu_buffer_rsrc_t to = buffer_of(static_cast<uint8_t*>(o.e) + ((tile_m + first) * o.pitch + tile_n) * 2, 0xFFFFFF00u);
-                    __builtin_amdgcn_raw_buffer_store_b128(out, to, in && tile_n + wcol < o.pitch ? ((8 * e + row) * (uint32_t)o.pitch + wcol) * 2 : BEYOND, 0, STREAM);
-                }
-                if (in && l % LANES == 0 && wn * T::COLS < cols) o.strips[(tile_m + r) * o.strips_row + tn * WN + wn] = f32x2{m, sum};
-            }
-            stores_behind = o.e ? T::NB - 1 : 0u;
-        } else {
-            const GemmEnd& o = g.end;
-            const float scale = o.scale ? *o.scale : 1.f;
-            const uint64_t part = item / tiles;
-            float bias[EACH];
-#pragma unroll
-            for (uint32_t k = 0; k < EACH; ++k) bias[k] = o.bias && wcol + k < cols ? load1<TYPE>(o.bias, tile_n + wcol + k) : 0.f;
-            const uint32_t at = (row * (uint32_t)o.ld + wcol) * BYTES;
-            f32x4 next[PASSES][EACH / 4];                                     // the sums of the pass after this one, on their way
-#pragma unroll
-            for (uint32_t i = 0; i < T::TI; ++i) {
-                const uint32_t first = wm * (BM / WM) + 32 * i;               // the store's rows begin here: the lanes' offsets are those of 32 rows, below 2^32
-                const __amdgpu_buffer_rsrc_t to = buffer_of(static_cast<uint8_t*>(o.out) + ((part * g.M + tile_m + first) * o.ld + tile_n) * BYTES, 0xFFFFFF00u);
-                // A residual of 16 bits: that of the 32 rows is under way before the first is used.
-                const uint8_t* res_base = static_cast<const uint8_t*>(o.residual) + ((tile_m + first + row) * o.ld_res + tile_n + wcol) * (o.res32 ? 4 : 2);
-                uint32_t res[4][PASSES][EACH / 2];
-                if (o.residual && !o.res32) {
-#pragma unroll
-                    for (uint32_t e = 0; e < 4; ++e)
-#pragma unroll
-                        for (uint32_t p = 0; p < PASSES; ++p) {
-                            const uint32_t r = 8 * e + p * PASS_ROWS;
-                            const uint16_t* q = reinterpret_cast<const uint16_t*>(res_base) + r * o.ld_res;
-                            if (row_in && first + r + row < rows) {
-                                if (whole) {
-#pragma unroll
-                                    for (uint32_t k = 0; k < EACH / 2; k += 2) {
-                                        const u32x2_any w = *reinterpret_cast<const u32x2_any*>(q + 2 * k);
-                                        res[e][p][k] = w[0];
-                                        res[e][p][k + 1] = w[1];
-                                    }
-                                } else {
-#pragma unroll
-                                    for (uint32_t k = 0; k < EACH; k += 2)
-                                        res[e][p][k / 2] = (wcol + k < cols ? (uint32_t)q[k] : 0u) | (wcol + k + 1 < cols ? (uint32_t)q[k + 1] << 16 : 0u);
-                                }
-                            }
-                        }
-                }
-#pragma unroll
-                for (uint32_t e = 0; e < 4; ++e) {
-                    f32x4 v[PASSES][EACH / 4], res32[PASSES][EACH / 4];
-                    if (i + e == 0) through(0, 0, next);
-#pragma unroll
-                    for (uint32_t p = 0; p < PASSES; ++p)
-#pragma unroll
-                        for (uint32_t k = 0; k < EACH / 4; ++k) v[p][k] = next[p][k];
-                    if (o.residual && o.res32) {
-#pragma unroll
-                        for (uint32_t p = 0; p < PASSES; ++p) {
-                            const uint32_t r = 8 * e + p * PASS_ROWS;
-                            const float* q = reinterpret_cast<const float*>(res_base) + r * o.ld_res;
-                            if (row_in && first + r + row < rows)
-#pragma unroll
-                                for (uint32_t k = 0; k < EACH; k += 4) {
-                                    if (whole) res32[p][k / 4] = *reinterpret_cast<const f32x4_any*>(q + k);
-                                    else
-#pragma unroll
-                                        for (uint32_t h = 0; h < 4; ++h) res32[p][k / 4][h] = wcol + k + h < cols ? q[k + h] : 0.f;
-                                }
-                        }
-                    }
-                    if (4 * i + e + 1 < 4 * T::TI) through((4 * i + e + 1) / 4, (e + 1) % 4, next);
-#pragma unroll
-                    for (uint32_t p = 0; p < PASSES; ++p) {
-                        // (the whole offset in the lane's register: a 16-byte store with a scalar offset as well has stored values that the next instructions
-                        // wrote into its data registers, in rows with such an offset and in no others)
-                        const uint32_t r = 8 * e + p * PASS_ROWS, to_at = at + r * (uint32_t)o.ld * BYTES;
-                        const bool in = row_in && first + r + row < rows;
-                        float x[EACH];
-#pragma unroll
-                        for (uint32_t k = 0; k < EACH; ++k) x[k] = v[p][k / 4][k % 4];
-                        if (o.bias || o.scale)
-#pragma unroll
-                            for (uint32_t k = 0; k < EACH; ++k) x[k] = fmaf(x[k], scale, bias[k]);
-                        if (o.z && in) {
-                            uint16_t* q = static_cast<uint16_t*>(o.z) + (tile_m + first + r + row) * o.ld_z + tile_n + wcol;
-                            if (whole) {
-#pragma unroll
-                                for (uint32_t k = 0; k < EACH; k += 4) __builtin_nontemporal_store((u32x2_any{pack2<TYPE>(x[k], x[k + 1]), pack2<TYPE>(x[k + 2], x[k + 3])}), reinterpret_cast<u32x2_any*>(q + k));
-                            } else if (cut) {
-#pragma unroll
-                                for (uint32_t k = 0; k < EACH; ++k)
-                                    if (wcol + k < cols) store1<TYPE>(q, k, x[k]);
-                            }
-                        }
-                        with_act(o.act, [&](auto kind) {
-#pragma unroll
-                            for (uint32_t k = 0; k < EACH; ++k) x[k] = act_as<decltype(kind)::value>(x[k]);
-                        });
-                        if (o.residual)
-#pragma unroll
-                            for (uint32_t k = 0; k < EACH; ++k) {
-                                const uint32_t w = res[e][p][k / 2] >> (16 * (k % 2)) & 0xFFFFu;
-                                x[k] += o.res32 ? res32[p][k / 4][k % 4] : TYPE == TYPE_BF16 ? __uint_as_float(w << 16) : half_to_float(w);
-                            }
-                        u32x4 out;
-#pragma unroll
-                        for (uint32_t k = 0; k < 4; ++k) out[k] = BYTES == 4 ? __float_as_uint(x[k]) : pack2<TYPE>(x[2 * k % EACH], x[(2 * k + 1) % EACH]);
-                        __builtin_amdgcn_raw_buffer_store_b128(out, to, in && whole ? to_at : BEYOND, 0, STREAM);
-                        if (in && cut) {
-#pragma unroll
-                            for (uint32_t k = 0; k < EACH; ++k) {
-                                const uint32_t ok = wcol + k < cols ? to_at + k * BYTES : BEYOND;
-                                if (BYTES == 4) __builtin_amdgcn_raw_buffer_store_b32(out[k % 4], to, ok, 0, 0);
-                                else __builtin_amdgcn_raw_buffer_store_b16((uint16_t)(out[k / 2 % 4] >> (16 * (k % 2))), to, ok, 0, 0);
-                            }
-                        }
-                    }
-                }
-            }
             stores_behind = T::NB - 1;
-            if (cols % EACH != 0) {                                           // (so many more stores that the counter would not tell)
-                stores_behind = 0;
-                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            }
+        } else {
+            uint32_t tm, tn;
+            tile_of(tile, g.tiles_m, g.tiles_n, tm, tn);
+            float* mine = reinterpret_cast<float*>(s_mem + T::NB * T::STAGE + wave * T::OUT);
+            const bool counted = gemm_end<TYPE, T, T::TI, END>(g, acc, mine, (uint64_t)tm * BM, (uint64_t)tn * BN, wm * (BM / WM), wn);
+            stores_behind = counted ? T::NB - 1 : 0u;
         }
+        read_all(buffer, 0, half0);                                           // (once more: kept through the end, it would cost 24 registers)
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                          // no load may reach LDS that is another workgroup's by then
 }
 
-// The parts of a sum, in their order, and its end.  A thread takes four columns, together where the parts' rows lie at 16-byte addresses (VEC).  Bound by memory.
-template <uint32_t TYPE, bool OUT32, bool VEC>
-__global__ __launch_bounds__(256) void k_gemm_join(const float* __restrict__ parts, uint32_t splits, uint64_t M, uint64_t N, GemmEnd o) {
-    const uint64_t each = (N + 3) / 4, i = (uint64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= M * each) return;
-    const uint64_t m = i / each, n = 4 * (i % each);
-    const float scale = o.scale ? *o.scale : 1.f;
-    float v[4] = {};
-    if (VEC) {
-        f32x4 sum = *reinterpret_cast<const f32x4*>(parts + m * N + n);
-#pragma unroll 4
-        for (uint32_t p = 1; p < splits; ++p) sum = sum + *reinterpret_cast<const f32x4*>(parts + (p * M + m) * N + n);
+// The parts of the shared tiles' sums, in their order, and their end: a wave takes 32 rows of one wave's part of a tile.  Bound by memory.
+template <uint32_t TYPE, class T, uint32_t END>
+__global__ __launch_bounds__(256) void k_gemm_join(GemmArgs g) {
+    __shared__ __attribute__((aligned(16))) uint8_t s_mem[4 * T::OUT];
+    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t shared = g.tiles_m * g.tiles_n - g.whole, unit = blockIdx.x * 4 + wave, t = unit / (T::WAVES * T::TI);
+    if (t >= shared) return;
+    const uint32_t w = unit / T::TI % T::WAVES, i = unit % T::TI;
+    uint32_t tm, tn;
+    tile_of(g.whole + t, g.tiles_m, g.tiles_n, tm, tn);
+    const uint64_t tile_m = (uint64_t)tm * T::BM, tile_n = (uint64_t)tn * T::BN;
+    const uint32_t row0 = w / T::WN * (T::BM / T::WM) + 32 * i, wn = w % T::WN;
+    if (tile_m + row0 >= g.M || tile_n + wn * T::COLS >= g.N) return;
+    const f32x4* from = reinterpret_cast<const f32x4*>(g.parts + (uint64_t)t * (T::BM * T::BN)) + (w * T::TI + i) * (T::TJ * 256) + lane;
+    const uint64_t step = (uint64_t)shared * (T::BM * T::BN / 4);
+    f32x16 acc[1][T::TJ];
 #pragma unroll
-        for (uint32_t k = 0; k < 4; ++k) v[k] = sum[k];
-    }
+    for (uint32_t j = 0; j < T::TJ; ++j) acc[0][j] = f32x16{};
+    constexpr uint32_t U = 4;                                                 // parts under way together
+    for (uint32_t p = 0; p < g.splits; p += U) {
+        f32x4 v[U][T::TJ * 4];
 #pragma unroll
-    for (uint32_t k = 0; k < 4; ++k) {
-        if (n + k >= N) break;
-        if (!VEC)
-            for (uint32_t p = 0; p < splits; ++p) v[k] += parts[(p * M + m) * N + n + k];
-        v[k] = fmaf(v[k], scale, o.bias ? load1<TYPE>(o.bias, n + k) : 0.f);
-        if (o.z) store1<TYPE>(o.z, m * o.ld_z + n + k, v[k]);
-        v[k] = act_of(v[k], o.act);
-        if (o.residual) v[k] += o.res32 ? static_cast<const float*>(o.residual)[m * o.ld_res + n + k] : load1<TYPE>(o.residual, m * o.ld_res + n + k);
-        store1<OUT32 ? TYPE_F32 : TYPE>(o.out, m * o.ld + n + k, v[k]);
+        for (uint32_t u = 0; u < U; ++u)
+#pragma unroll
+            for (uint32_t k = 0; k < T::TJ * 4; ++k)
+                if (p + u < g.splits) v[u][k] = from[(p + u) * step + k * 64];
+#pragma unroll
+        for (uint32_t u = 0; u < U; ++u)
+            if (p + u < g.splits)
+#pragma unroll
+                for (uint32_t k = 0; k < T::TJ * 16; ++k) acc[0][k / 16][k % 16] += v[u][k / 4][k % 4];
     }
+    gemm_end<TYPE, T, 1, END>(g, acc, reinterpret_cast<float*>(s_mem + wave * T::OUT), tile_m, tile_n, row0, wn);
 }
 
 }  // namespace kimad

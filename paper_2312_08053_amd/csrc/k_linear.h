@@ -10,7 +10,7 @@ namespace kimad {
 template <uint32_t TYPE, uint32_t MT, uint32_t END>
 __global__ __launch_bounds__(256) void k_gemm_few(GemmArgs g) {
     __shared__ f32x4 s_part[3][MT][64];
-    constexpr uint32_t U = 8 / MT;
+    constexpr uint32_t U = MT == 1 ? 8 : MT == 2 ? 4 : 2;
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15u, blk = lane >> 4;
     const uint64_t n0 = (uint64_t)blockIdx.x * 16, n = n0 + r < g.N ? n0 + r : g.N - 1;
     // (whole cache lines)
@@ -91,31 +91,65 @@ __global__ __launch_bounds__(256) void k_gemm_none(uint64_t M, uint64_t N, GemmE
 }
 
 // Rows of 16-bit elements laid out anew, `pitch` (a multiple of 8) apart and filled up with zeros: for operands whose rows do not begin at 16-byte addresses or
-// end inside 16 bytes.  Rows that do not count (weight 0, no target) become zeros: a NaN there would reach every sum over rows.
-__global__ __launch_bounds__(256) void k_rows_copy(const void* __restrict__ from, uint64_t ld, uint64_t rows, uint64_t cols, void* __restrict__ to, uint64_t pitch,
-                                                   const int32_t* __restrict__ target, int64_t vocab, const float* __restrict__ weight) {
-    const uint64_t each = pitch / 8, i = (uint64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= rows * each) return;
+// end inside 16 bytes.  Rows that do not count (weight 0, no target) become zeros: a NaN there would reach every sum over rows.  Two matrices in one launch.
+struct CopyArgs {
+    const void* from[2];
+    void* to[2];                 // or null
+    uint64_t ld[2], rows[2], cols[2], pitch[2];
+    uint32_t wgs0;               // workgroups of the first
+    const int32_t* target;       // of the first matrix's rows, or null
+    const float* weight;
+    uint32_t vocab;
+    float* scale;                // two numbers, or null
+    float largest;               // what the largest weight is to become
+};
+// The cross entropy's G in 16 bits holds w / max |w| times `largest`: equal weights, however many rows share one, then cost no rounding that is the same for all rows, and
+// fp16's small numbers reach further.  (By one workgroup; weights that are not finite leave nothing finite anyway.)
+__device__ __forceinline__ void scale_of_weights(const CopyArgs& a) {
+    __shared__ float s_max[4];
+    float m = 0.f;
+    for (uint64_t r = threadIdx.x; r < a.rows[0]; r += 256) {
+        const float w = a.weight ? fabsf(a.weight[r]) : 1.f;
+        if ((uint32_t)a.target[r] < a.vocab && w < INFINITY) m = fmaxf(m, w);
+    }
+#pragma unroll
+    for (uint32_t o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
+    if ((threadIdx.x & 63u) == 0) s_max[threadIdx.x >> 6] = m;
+    __syncthreads();
+    if (threadIdx.x) return;
+    m = fmaxf(fmaxf(s_max[0], s_max[1]), fmaxf(s_max[2], s_max[3]));
+    m = m == 0.f ? 1.f : fmaxf(m, 0x1p-100f);
+    a.scale[0] = a.largest / m;
+    a.scale[1] = m / a.largest;
+}
+__global__ __launch_bounds__(256) void k_rows_copy(CopyArgs a) {
+    if (a.scale && blockIdx.x + 1 == gridDim.x) {
+        scale_of_weights(a);
+        return;
+    }
+    const uint32_t which = blockIdx.x >= a.wgs0;
+    const uint64_t each = a.pitch[which] / 8, i = (uint64_t)(blockIdx.x - (which ? a.wgs0 : 0)) * 256 + threadIdx.x;
+    if (i >= a.rows[which] * each) return;
     const uint64_t r = i / each, c = i % each * 8;
-    const bool live = (!target || (target[r] >= 0 && target[r] < vocab)) && (!weight || weight[r] != 0.f);
-    const Raw8<TYPE_BF16> v = load8_first<TYPE_BF16>(from, r * ld + c, live ? (int64_t)(cols - c) : 0);
-    reinterpret_cast<u32x4*>(to)[i] = u32x4{v.r[0], v.r[1], v.r[2], v.r[3]};
+    const bool live = which || ((!a.target || (uint32_t)a.target[r] < a.vocab) && (!a.weight || a.weight[r] != 0.f));
+    const Raw8<TYPE_BF16> v = load8_first<TYPE_BF16>(a.from[which], r * a.ld[which] + c, live ? (int64_t)(a.cols[which] - c) : 0);
+    reinterpret_cast<u32x4*>(a.to[which])[i] = u32x4{v.r[0], v.r[1], v.r[2], v.r[3]};
 }
 
-// dz = dy act'(z), rounded to the type, and the sums of its columns in fp32 (of what was not rounded): of 64 rows a workgroup, 512 columns.  Bound by memory.
+// dz = dy act'(z), rounded to the type, and the sums of its columns in fp32 (of what was not rounded): of 64 rows a workgroup (128, if there are no more), 512 columns.  Bound by memory.
 constexpr uint32_t SUM_ROWS = 64, SUM_COLS = 512;
 struct ActGradArgs {
     const void *dy, *z;          // z null: no activation
     void* dz;                    // or null; pitch elements from row to row, filled up with zeros
-    float* sums;                 // [ceil(M / 64)][N], or null
+    float* sums;                 // [ceil(M / rows)][N], or null
     uint64_t M, N, ld_dy, ld_z, pitch;
-    uint32_t act;
+    uint32_t act, rows;          // rows of a workgroup
 };
 template <uint32_t TYPE>
 __global__ __launch_bounds__(256) void k_act_grad(ActGradArgs a) {
     __shared__ float s_sum[4][SUM_COLS];
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
-    const uint64_t c = (uint64_t)blockIdx.x * SUM_COLS + 8 * lane, m0 = (uint64_t)blockIdx.y * SUM_ROWS, m1 = m0 + SUM_ROWS < a.M ? m0 + SUM_ROWS : a.M;
+    const uint64_t c = (uint64_t)blockIdx.x * SUM_COLS + 8 * lane, m0 = (uint64_t)blockIdx.y * a.rows, m1 = m0 + a.rows < a.M ? m0 + a.rows : a.M;
     const int64_t n = (int64_t)a.N - (int64_t)c;
     float sum[8] = {};
     constexpr uint32_t U = 4;                            // rows of a wave under way together
@@ -151,7 +185,7 @@ __global__ __launch_bounds__(256) void k_act_grad(ActGradArgs a) {
         if (col < a.N) a.sums[blockIdx.y * a.N + col] = s_sum[0][i] + s_sum[1][i] + s_sum[2][i] + s_sum[3][i];
     }
 }
-// The sums of all rows from those of 64 each: a wave of a workgroup takes every fourth.
+// The sums of all rows from the workgroups': a wave of a workgroup takes every fourth.
 __global__ __launch_bounds__(256) void k_sum_join(const float* __restrict__ sums, uint64_t parts, uint64_t N, float* __restrict__ out) {
     __shared__ float s_sum[4][64];
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;

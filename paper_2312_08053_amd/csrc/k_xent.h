@@ -17,30 +17,10 @@ struct XentArgs {
     float *loss, *lse;           // or null
     f32x2* rows_out;             // [rows]: lse, and the row's weight times `scale` (0: the row does not count)
     void* e;                     // [rows, pitch]: exp(z - m) as a SmallFloat, and then G
-    const float* scale;          // two numbers on the device: what G is multiplied by, and its inverse; or null
+    const float* scale;          // two numbers on the device: what G is multiplied by, and its inverse (k_rows_copy)
     uint64_t rows, pitch;
     uint32_t vocab, strips_row, strip;
 };
-
-// G in 16 bits of fp16 is multiplied by a power of two that takes the largest weight to 2^12: a p of 2^-26 is then no subnormal.
-__global__ __launch_bounds__(1024) void k_xent_scale(const int32_t* __restrict__ target, const float* __restrict__ weight, uint64_t rows, uint32_t vocab, float* __restrict__ out) {
-    __shared__ float s_max[16];
-    float m = 0.f;
-    for (uint64_t r = threadIdx.x; r < rows; r += 1024) {
-        const float w = weight ? fabsf(weight[r]) : 1.f;
-        if ((uint32_t)target[r] < vocab && w < INFINITY) m = fmaxf(m, w);
-    }
-#pragma unroll
-    for (uint32_t o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
-    if ((threadIdx.x & 63u) == 0) s_max[threadIdx.x >> 6] = m;
-    __syncthreads();
-    if (threadIdx.x) return;
-    for (uint32_t i = 1; i < 16; ++i) m = fmaxf(m, s_max[i]);
-    int32_t k = 12 - ((int32_t)(__float_as_uint(m) >> 23) - 126);             // (the largest weight is below 2^(exponent - 126))
-    k = m == 0.f ? 0 : k > 100 ? 100 : k < -100 ? -100 : k;
-    out[0] = __uint_as_float((uint32_t)(127 + k) << 23);
-    out[1] = __uint_as_float((uint32_t)(127 - k) << 23);
-}
 
 // A row's sums from its strips, by a workgroup: the loss and lse.
 __global__ __launch_bounds__(256) void k_xent_rows(XentArgs a) {
@@ -62,7 +42,7 @@ __global__ __launch_bounds__(256) void k_xent_rows(XentArgs a) {
     const float lse = live ? q.m + logf(q.s) : 0.f;
     if (a.loss) a.loss[row] = live ? w * ((q.m - a.picked[row]) + logf(q.s)) : 0.f;
     if (a.lse) a.lse[row] = lse;
-    if (a.rows_out) a.rows_out[row] = f32x2{lse, live ? w * (a.scale ? a.scale[0] : 1.f) : 0.f};
+    if (a.rows_out) a.rows_out[row] = f32x2{lse, live ? w * a.scale[0] : 0.f};
 }
 
 // e becomes G.  A thread takes eight columns.  Bound by memory.

@@ -17,7 +17,7 @@ using namespace kimad;
 
 static_assert(ACT_NONE == KIMAD_ACT_NONE && ACT_RELU == KIMAD_ACT_RELU && ACT_GELU == KIMAD_ACT_GELU && ACT_SILU == KIMAD_ACT_SILU, "header and kernel constants");
 
-constexpr uint64_t FEW_ROWS = 32;                        // products of so many rows may go by k_gemm_few
+constexpr uint64_t FEW_MOST = 96;                        // products of so many rows may go by k_gemm_few
 constexpr uint64_t LD_MOST = 1ull << 22;                 // operands: 256 rows are reached by 32-bit offsets
 constexpr uint64_t OUT_LD_MOST = 1ull << 24;             // results: 32 rows
 constexpr uint64_t ROWS_MOST = 65535ull * SUM_ROWS;      // 4194240: the column sums' grid
@@ -47,72 +47,78 @@ struct Room {
     }
 };
 
-// How a product is shared out (as in the 4-bit product: rounds of as many tiles as compute units, and with few tiles and long sums parts of a sum).
+// How a product is shared out: by the least of the times below, which are fits (us) to measurements of each tile alone: rounds of as many tiles as compute units, and a
+// last one that costs less the fewer units it fills.  The tiles of a last round may be shared out along the sum too (`splits` parts, which are of fp32 and are added by a
+// second launch).
 struct GemmPlan {
     enum { FEW, T64, T128, T256 } kind;
-    uint64_t tiles_m, tiles_n;
+    uint64_t tiles_m, tiles_n, whole;
     uint32_t splits, share;
     double us;
     uint32_t strip() const { return kind == FEW ? 16 : kind == T64 ? Gemm64::STRIP : kind == T128 ? Gemm128::STRIP : Gemm256::STRIP; }
+    uint64_t edge() const { return kind == T256 ? 256 : kind == T128 ? 128 : 64; }
+    uint64_t shared() const { return kind == FEW ? 0 : tiles_m * tiles_n - whole; }
+    uint64_t parts_count() const { return shared() * splits * edge() * edge(); }
 };
-GemmPlan gemm_plan(uint64_t M, uint64_t N, uint64_t K, bool wide, bool may_split, bool may_few) {
+GemmPlan gemm_plan(uint64_t M, uint64_t N, uint64_t K, bool wide, bool may_split, uint32_t few) {
     GemmPlan best{};
     best.splits = 1;
     const uint64_t stages = (K + STAGE_K - 1) / STAGE_K;
     best.share = (uint32_t)stages;
-    if (may_few && M <= FEW_ROWS) {
+    // k_gemm_few, whose waves read all of A each; rows that begin off 16-byte addresses cost it over three times as much, but a copy costs the tiles more.
+    const double copy = few == 2 ? 4.0 + (double)((M + N) * K) * 4.0 / 4.5e6 : 0.0;
+    if (few && M <= FEW_MOST) {
         best.kind = GemmPlan::FEW;
-        return best;
+        best.us = 2.5 + (double)(N * K) * (0.26e-6 + 1.5e-8 * (double)M) * (few == 2 ? 3.3 : 1.0) - copy;
+        if (best.us <= 0) best.us = 1e-3;
     }
     const double read = 2.0 + (double)((M + N) * K) * 2.0 / 4.5e6;            // both operands from memory
     // of one tile: a stage with nothing beside it on its compute unit, what comes from beyond the L2; among others, where few units have one and where all do;
     // its end in 16 bits and in 32; the launch
     struct { decltype(best.kind) kind; uint64_t edge; double alone, lone, stage, end16, end32, launch; } const kinds[] = {
-        {GemmPlan::T256, 256, 1.3, 1.3, 1.6, 3.0, 6.0, 5.0}, {GemmPlan::T128, 128, 0.69, 0.64, 0.64, 1.0, 1.5, 5.0}, {GemmPlan::T64, 64, 0.45, 0.24, 0.24, 0.35, 0.35, 4.5}};
+        {GemmPlan::T256, 256, 1.3, 1.3, 1.6, 6.0, 8.0, 5.0}, {GemmPlan::T128, 128, 0.72, 0.66, 0.70, 1.0, 1.5, 5.0}, {GemmPlan::T64, 64, 0.45, 0.24, 0.24, 0.35, 0.35, 4.5}};
     for (const auto& k : kinds) {
-        const uint64_t tm = (M + k.edge - 1) / k.edge, tn = (N + k.edge - 1) / k.edge;
-        for (uint64_t splits = 1; splits == 1 || (may_split && splits <= 16 && 4 * splits <= stages && tm * tn * splits <= 4 * UNITS); splits *= 2) {
+        const uint64_t tm = (M + k.edge - 1) / k.edge, tn = (N + k.edge - 1) / k.edge, tiles = tm * tn, full = tiles / UNITS * UNITS, rest = tiles - full;
+        for (uint64_t splits = 1; splits == 1 || (may_split && rest && splits <= 16 && 4 * splits <= stages); ++splits) {
             const uint64_t share = (stages + splits - 1) / splits, parts = (stages + share - 1) / share;
-            const uint64_t items = tm * tn * parts, rounds = items / UNITS;
-            const double part = (double)(items % UNITS) / UNITS, end = wide || parts > 1 ? k.end32 : k.end16;
-            double us = (double)rounds * ((double)share * k.stage + end) + k.launch;
-            if (part > 0) us += (double)share * (k.lone + part * (k.stage - k.lone)) + end;
-            if (parts > 1) us += 4.0 + (double)(parts * M * N) * 8.0 / 4e6;     // 4 bytes written and read, at 4 TB/s
+            if (parts != splits) continue;
+            const uint64_t items = rest * parts, rounds = items / UNITS;
+            const double part = (double)(items % UNITS) / UNITS, end = wide ? k.end32 : k.end16, part_end = parts > 1 ? k.end32 : end;
+            double us = k.launch + (double)(full / UNITS) * ((double)stages * k.stage + end) + (double)rounds * ((double)share * k.stage + part_end);
+            if (part > 0) us += (double)share * (k.lone + part * (k.stage - k.lone)) + part_end;
+            if (parts > 1) us += 4.0 + (double)(items * k.edge * k.edge) * 8.0 / 4e6;   // 4 bytes written and read, at 4 TB/s
             us = std::max(std::max(us, k.launch + (double)share * k.alone + end), read);
             if (best.us == 0 || us < best.us) {
                 best.us = us;
-                best.kind = k.kind; best.tiles_m = tm; best.tiles_n = tn;
+                best.kind = k.kind; best.tiles_m = tm; best.tiles_n = tn; best.whole = parts > 1 ? full : tiles;
                 best.splits = (uint32_t)parts; best.share = (uint32_t)share;
             }
         }
     }
     return best;
 }
-uint64_t gemm_edge(const GemmPlan& p) { return p.kind == GemmPlan::T256 ? 256 : p.kind == GemmPlan::T128 ? 128 : 64; }
-// The same way of sharing out for a product with fewer rows or a shorter sum (it needs no more room).
-GemmPlan fewer(GemmPlan p, uint64_t M, uint64_t K) {
-    if (p.kind == GemmPlan::FEW) return p;
-    const uint64_t stages = (K + STAGE_K - 1) / STAGE_K;
-    p.tiles_m = (M + gemm_edge(p) - 1) / gemm_edge(p);
-    p.share = (uint32_t)((stages + p.splits - 1) / p.splits);
-    p.splits = (uint32_t)((stages + p.share - 1) / p.share);
-    return p;
-}
-uint64_t parts_count(const GemmPlan& p, uint64_t M, uint64_t N) { return p.splits > 1 ? p.splits * M * N : 0; }
 
 template <uint32_t TYPE, class T, bool XA, bool XB, uint32_t END>
 int launch_tile(GemmArgs g, const GemmPlan& p, hipStream_t s) {
-    const uint64_t items = p.tiles_m * p.tiles_n * p.splits;                  // (below 2^28 for matrices of fewer than 2^34 elements and rows of 2^22)
+    const uint64_t items = p.whole + p.shared() * p.splits;                   // (below 2^28 for matrices of fewer than 2^34 elements and rows of 2^22)
     constexpr uint64_t slots = UNITS * ((160 * 1024) / T::LDS);
-    g.tiles_m = (uint32_t)p.tiles_m; g.tiles_n = (uint32_t)p.tiles_n; g.splits = p.splits; g.share = p.share;
+    g.tiles_m = (uint32_t)p.tiles_m; g.tiles_n = (uint32_t)p.tiles_n; g.whole = (uint32_t)p.whole; g.splits = p.splits; g.share = p.share;
     hipLaunchKernelGGL((k_gemm_tile<TYPE, T, XA, XB, END>), dim3((uint32_t)std::min<uint64_t>(items, slots)), dim3(64 * T::WAVES), 0, s, g);
+    if constexpr (END != END_SOFTMAX)
+        if (p.splits > 1) {
+            const uint64_t units = p.shared() * (T::WAVES * T::TI);
+            if (const int rc = launched()) return rc;
+            hipLaunchKernelGGL((k_gemm_join<TYPE, T, END>), dim3((uint32_t)((units + 3) / 4)), dim3(256), 0, s, g);
+        }
     return launched();
 }
 template <uint32_t TYPE, uint32_t END>
 int launch_few(const GemmArgs& g, hipStream_t s) {
     const uint64_t groups = (g.N + 15) / 16;
     if (g.M <= 16) hipLaunchKernelGGL((k_gemm_few<TYPE, 1, END>), dim3((uint32_t)groups), dim3(256), 0, s, g);
-    else hipLaunchKernelGGL((k_gemm_few<TYPE, 2, END>), dim3((uint32_t)groups), dim3(256), 0, s, g);
+    else if (g.M <= 32) hipLaunchKernelGGL((k_gemm_few<TYPE, 2, END>), dim3((uint32_t)groups), dim3(256), 0, s, g);
+    else if (g.M <= 64) hipLaunchKernelGGL((k_gemm_few<TYPE, 4, END>), dim3((uint32_t)groups), dim3(256), 0, s, g);
+    else hipLaunchKernelGGL((k_gemm_few<TYPE, 6, END>), dim3((uint32_t)groups), dim3(256), 0, s, g);
     return launched();
 }
 template <uint32_t TYPE, bool XA, bool XB, uint32_t END>
@@ -123,24 +129,11 @@ int launch_kind(const GemmArgs& g, const GemmPlan& p, hipStream_t s) {
     if (p.kind == GemmPlan::T128) return launch_tile<TYPE, Gemm128, XA, XB, END>(g, p, s);
     return launch_tile<TYPE, Gemm64, XA, XB, END>(g, p, s);
 }
-// A product and its end; parts: room for parts_count() numbers.
+// A product and its end; parts: room for the plan's parts_count() numbers.
 template <uint32_t TYPE, bool XA, bool XB>
 int launch_gemm(GemmArgs g, const GemmPlan& p, bool out32, float* parts, hipStream_t s) {
-    if (p.splits == 1) return out32 ? launch_kind<TYPE, XA, XB, END_F32>(g, p, s) : launch_kind<TYPE, XA, XB, END_TYPE>(g, p, s);
-    const uint64_t wgs = (g.M * ((g.N + 3) / 4) + 255) / 256;
-    const GemmEnd end = g.end;
-    g.end = GemmEnd{};
-    g.end.out = parts; g.end.ld = g.N;
-    const int rc = launch_kind<TYPE, XA, XB, END_F32>(g, p, s);
-    if (rc) return rc;
-    auto join = [&](auto o32, auto vec) {
-        hipLaunchKernelGGL((k_gemm_join<TYPE, decltype(o32)::value, decltype(vec)::value>), dim3((uint32_t)wgs), dim3(256), 0, s, parts, p.splits, g.M, g.N, end);
-    };
-    constexpr std::true_type yes{};
-    constexpr std::false_type no{};
-    if (g.N % 4 == 0) out32 ? join(yes, yes) : join(no, yes);
-    else out32 ? join(yes, no) : join(no, no);
-    return launched();
+    g.parts = parts;
+    return out32 ? launch_kind<TYPE, XA, XB, END_F32>(g, p, s) : launch_kind<TYPE, XA, XB, END_TYPE>(g, p, s);
 }
 
 // A sum over nothing, and its end.
@@ -161,9 +154,24 @@ int zeros(void* out, uint32_t type, uint64_t rows, uint64_t cols, uint64_t ld, h
 // Whether the tiles' loads reach an operand as it lies: rows at 16-byte addresses, and for one that is stored along K rows that end at one.
 bool lies_well(const void* p, uint64_t ld, uint64_t rows, uint64_t cols, bool along) { return aligned(p, 16) && (ld % 8 == 0 || rows <= 1) && (!along || cols % 8 == 0); }
 uint64_t pitch_of(uint64_t cols) { return (cols + 7) / 8 * 8; }
-int copy_rows(const void* from, uint64_t ld, uint64_t rows, uint64_t cols, void* to, const int32_t* target, uint64_t vocab, const float* weight, hipStream_t s) {
-    const uint64_t wgs = (rows * (pitch_of(cols) / 8) + 255) / 256;
-    hipLaunchKernelGGL(k_rows_copy, dim3((uint32_t)wgs), dim3(256), 0, s, from, ld, rows, cols, to, pitch_of(cols), target, (int64_t)vocab, weight);
+// Two matrices (either may stay where it is: `to` null) laid out anew; the first one's rows that do not count become zeros.  scale: as k_rows_copy makes it.
+struct CopyOf {
+    const void* from;
+    uint64_t ld, rows, cols;
+    void* to;
+};
+int copy_rows(const CopyOf& first, const CopyOf& second, const int32_t* target, uint64_t vocab, const float* weight, float* scale, float largest, hipStream_t s) {
+    CopyArgs a{};
+    const CopyOf* of[2] = {&first, &second};
+    uint64_t wgs[2];
+    for (uint32_t i = 0; i < 2; ++i) {
+        a.from[i] = of[i]->from; a.to[i] = of[i]->to; a.ld[i] = of[i]->ld; a.rows[i] = of[i]->rows; a.cols[i] = of[i]->cols; a.pitch[i] = pitch_of(of[i]->cols);
+        wgs[i] = of[i]->to ? (of[i]->rows * (a.pitch[i] / 8) + 255) / 256 : 0;
+    }
+    if (wgs[0] + wgs[1] == 0 && !scale) return KIMAD_OK;
+    a.scale = scale; a.largest = largest;
+    a.wgs0 = (uint32_t)wgs[0]; a.target = target; a.weight = weight; a.vocab = (uint32_t)vocab;
+    hipLaunchKernelGGL(k_rows_copy, dim3((uint32_t)(wgs[0] + wgs[1] + (scale ? 1 : 0))), dim3(256), 0, s, a);
     return launched();
 }
 // an operand: its address and leading dimension, in place or copied
@@ -187,11 +195,12 @@ struct LinearRoom {
 };
 LinearRoom linear_room(Room& room, const void* x, uint64_t ld_x, const void* w, uint64_t ld_w, uint64_t M, uint64_t N, uint64_t K) {
     LinearRoom r{};
-    r.plan = gemm_plan(M, N, K, true, true, true);
+    const bool x_well = lies_well(x, ld_x, M, K, true), w_well = lies_well(w, ld_w, N, K, true);
+    r.plan = gemm_plan(M, N, K, true, true, x_well && w_well ? 1 : 2);
     if (r.plan.kind == GemmPlan::FEW) return r;
-    if (!lies_well(x, ld_x, M, K, true) || K % 8) r.x = room.take<uint16_t>(M * pitch_of(K));
-    if (!lies_well(w, ld_w, N, K, true) || K % 8) r.w = room.take<uint16_t>(N * pitch_of(K));
-    r.parts = room.take<float>(parts_count(r.plan, M, N));
+    if (!x_well) r.x = room.take<uint16_t>(M * pitch_of(K));
+    if (!w_well) r.w = room.take<uint16_t>(N * pitch_of(K));
+    r.parts = room.take<float>(r.plan.parts_count());
     return r;
 }
 bool linear_sizes_ok(uint64_t M, uint64_t N, uint64_t K) { return M <= ROWS_MOST && N <= LD_MOST && K <= LD_MOST && fits(M, N + 7) && fits(M, K + 7) && fits(N, K + 7); }
@@ -202,7 +211,7 @@ struct LinearGradRoom {
     bool dz_made;                // else dy itself is dz
     uint16_t *dz, *x, *w;
     float *sums, *parts;
-    uint64_t sum_parts;
+    uint64_t sum_rows, sum_parts;
     GemmPlan dx, dw;
 };
 LinearGradRoom linear_grad_room(Room& room, const void* dy, uint64_t ld_dy, const void* x, uint64_t ld_x, const void* w, uint64_t ld_w, uint64_t M, uint64_t N, uint64_t K, uint32_t act,
@@ -213,16 +222,17 @@ LinearGradRoom linear_grad_room(Room& room, const void* dy, uint64_t ld_dy, cons
     if (r.dz_made) r.dz = room.take<uint16_t>(M * pitch_of(N));
     if (dw && !lies_well(x, ld_x, M, K, false)) r.x = room.take<uint16_t>(M * pitch_of(K));
     if (dx && !lies_well(w, ld_w, N, K, false)) r.w = room.take<uint16_t>(N * pitch_of(K));
-    r.sum_parts = (M + SUM_ROWS - 1) / SUM_ROWS;
+    r.sum_rows = M <= 2 * SUM_ROWS ? 2 * SUM_ROWS : SUM_ROWS;
+    r.sum_parts = (M + r.sum_rows - 1) / r.sum_rows;
     if ((wants & KIMAD_WANT_DB) && r.sum_parts > 1) r.sums = room.take<float>(r.sum_parts * N);
     uint64_t parts = 0;
     if (dx) {
-        r.dx = gemm_plan(M, K, pitch_of(N), false, true, false);
-        parts = std::max(parts, parts_count(r.dx, M, K));
+        r.dx = gemm_plan(M, K, pitch_of(N), false, true, 0);
+        parts = std::max(parts, r.dx.parts_count());
     }
     if (dw) {
-        r.dw = gemm_plan(N, K, M, true, true, false);
-        parts = std::max(parts, parts_count(r.dw, N, K));
+        r.dw = gemm_plan(N, K, M, true, true, 0);
+        parts = std::max(parts, r.dw.parts_count());
     }
     r.parts = room.take<float>(parts);
     return r;
@@ -232,11 +242,11 @@ LinearGradRoom linear_grad_room(Room& room, const void* dy, uint64_t ld_dy, cons
 
 constexpr uint64_t PIECE_BYTES = 1ull << 29;             // of the exponentials that a gradient's piece of rows keeps
 struct XentRoom {
-    uint64_t piece, pieces, pitch, strips_row;
+    uint64_t piece, pieces, pitch;
     uint16_t *x, *w, *e;
     f32x2 *strips, *rows_out;
     float *picked, *scale, *sum, *parts;
-    GemmPlan z, dx, dw;
+    struct { GemmPlan z, dx, dw; } plans[2];             // of a piece, and of the last one, which may have fewer rows
 };
 XentRoom xent_room(Room& room, const void* x, uint64_t ld_x, const void* w, uint64_t ld_w, uint32_t type, uint64_t rows, uint64_t vocab, uint64_t dim, uint32_t wants, uint32_t dw_type) {
     XentRoom r{};
@@ -247,27 +257,27 @@ XentRoom xent_room(Room& room, const void* x, uint64_t ld_x, const void* w, uint
     r.pieces = (rows + most - 1) / most;
     r.piece = r.pieces <= 1 ? rows : std::min(most, ((rows + r.pieces - 1) / r.pieces + 255) / 256 * 256);
     r.pieces = (rows + r.piece - 1) / r.piece;
-    r.z = gemm_plan(r.piece, vocab, dim, false, false, !grad);
-    const bool few = r.z.kind == GemmPlan::FEW;
-    if (grad || (!few && !lies_well(x, ld_x, rows, dim, true))) r.x = room.take<uint16_t>(rows * pitch_of(dim));
-    if (!few && !lies_well(w, ld_w, vocab, dim, true)) r.w = room.take<uint16_t>(vocab * pitch_of(dim));
-    r.strips_row = (vocab + r.z.strip() - 1) / r.z.strip();
-    r.strips = room.take<f32x2>(r.piece * r.strips_row);
+    const bool x_well = lies_well(x, ld_x, rows, dim, true), w_well = lies_well(w, ld_w, vocab, dim, true);
+    uint64_t parts = 0, strips = 0;
+    for (uint32_t last = 0; last < 2; ++last) {
+        const uint64_t n = last ? rows - (r.pieces - 1) * r.piece : r.piece;
+        auto& p = r.plans[last];
+        p.z = gemm_plan(n, vocab, dim, false, false, grad ? 0 : x_well && w_well ? 1 : 2);
+        strips = std::max(strips, n * ((vocab + p.z.strip() - 1) / p.z.strip()));
+        if (dx) p.dx = gemm_plan(n, dim, r.pitch, false, true, 0);
+        if (dw) p.dw = gemm_plan(vocab, dim, n, r.pieces > 1, true, 0);
+        parts = std::max(parts, std::max(dx ? p.dx.parts_count() : 0, dw ? p.dw.parts_count() : 0));
+    }
+    const bool few = r.plans[0].z.kind == GemmPlan::FEW && r.plans[1].z.kind == GemmPlan::FEW;
+    if (grad || (!few && !x_well)) r.x = room.take<uint16_t>(rows * pitch_of(dim));
+    if (!few && !w_well) r.w = room.take<uint16_t>(vocab * pitch_of(dim));
+    r.strips = room.take<f32x2>(strips);
     r.picked = room.take<float>(r.piece);
     if (!grad) return r;
     r.rows_out = room.take<f32x2>(r.piece);
-    if (type == KIMAD_VALUES_F16) r.scale = room.take<float>(2);
+    r.scale = room.take<float>(2);
     r.e = room.take<uint16_t>(r.piece * r.pitch);
-    uint64_t parts = 0;
-    if (dx) {
-        r.dx = gemm_plan(r.piece, dim, r.pitch, false, true, false);
-        parts = std::max(parts, parts_count(r.dx, r.piece, dim));
-    }
-    if (dw) {
-        r.dw = gemm_plan(vocab, dim, r.piece, r.pieces > 1, true, false);
-        parts = std::max(parts, parts_count(r.dw, vocab, dim));
-        if (r.pieces > 1 && dw_type != KIMAD_VALUES_F32) r.sum = room.take<float>(vocab * dim);
-    }
+    if (dw && r.pieces > 1 && dw_type != KIMAD_VALUES_F32) r.sum = room.take<float>(vocab * dim);
     r.parts = room.take<float>(parts);
     return r;
 }
@@ -299,15 +309,8 @@ int kimad_linear(const void* x, uint64_t ld_x, const void* w, uint64_t ld_w, uin
     Room room{static_cast<uint8_t*>(workspace), 0};
     const LinearRoom r = linear_room(room, x, ld_x, w, ld_w, M, N, K);
     if (room.used && (!workspace || workspace_bytes < room.used || !aligned(workspace, 16))) return KIMAD_ERR_WORKSPACE_TOO_SMALL;
-    Operand ox{x, ld_x}, ow{w, ld_w};
-    if (r.x) {
-        if (const int rc = copy_rows(x, ld_x, M, K, r.x, nullptr, 0, nullptr, s)) return rc;
-        ox = {r.x, pitch_of(K)};
-    }
-    if (r.w) {
-        if (const int rc = copy_rows(w, ld_w, N, K, r.w, nullptr, 0, nullptr, s)) return rc;
-        ow = {r.w, pitch_of(K)};
-    }
+    if (const int rc = copy_rows({x, ld_x, M, K, r.x}, {w, ld_w, N, K, r.w}, nullptr, 0, nullptr, nullptr, 0.f, s)) return rc;
+    const Operand ox = r.x ? Operand{r.x, pitch_of(K)} : Operand{x, ld_x}, ow = r.w ? Operand{r.w, pitch_of(K)} : Operand{w, ld_w};
     g.a = static_cast<const uint8_t*>(ox.p); g.lda = ox.ld; g.b = static_cast<const uint8_t*>(ow.p); g.ldb = ow.ld;
     if (r.plan.kind != GemmPlan::FEW) g.K = pitch_of(K);
     return with_half_type(type, [&](auto t) { return launch_gemm<decltype(t)::value, false, false>(g, r.plan, out32, r.parts, s); });
@@ -338,11 +341,12 @@ int kimad_linear_grad(const void* dy, uint64_t ld_dy, const void* x, uint64_t ld
     const uint32_t wants = (dx ? KIMAD_WANT_DX : 0u) | (dw ? KIMAD_WANT_DW : 0u) | (db ? KIMAD_WANT_DB : 0u);
     const LinearGradRoom r = linear_grad_room(room, dy, ld_dy, x, ld_x, w, ld_w, M, N, K, act, wants);
     if (room.used && (!workspace || workspace_bytes < room.used || !aligned(workspace, 16))) return KIMAD_ERR_WORKSPACE_TOO_SMALL;
-    Operand odz{dy, ld_dy}, ox{x, ld_x}, ow{w, ld_w};
-    if (r.dz_made) odz = {r.dz, pitch_of(N)};
+    if (const int rc = copy_rows({x, ld_x, M, K, r.x}, {w, ld_w, N, K, r.w}, nullptr, 0, nullptr, nullptr, 0.f, s)) return rc;
+    const Operand odz = r.dz_made ? Operand{r.dz, pitch_of(N)} : Operand{dy, ld_dy};
+    const Operand ox = r.x ? Operand{r.x, pitch_of(K)} : Operand{x, ld_x}, ow = r.w ? Operand{r.w, pitch_of(K)} : Operand{w, ld_w};
     if (r.dz_made || db) {
         ActGradArgs a{};
-        a.dy = dy; a.z = act == KIMAD_ACT_NONE ? nullptr : z; a.dz = r.dz; a.M = M; a.N = N; a.ld_dy = ld_dy; a.ld_z = ld_z; a.pitch = pitch_of(N); a.act = act;
+        a.dy = dy; a.z = act == KIMAD_ACT_NONE ? nullptr : z; a.dz = r.dz; a.M = M; a.N = N; a.ld_dy = ld_dy; a.ld_z = ld_z; a.pitch = pitch_of(N); a.act = act; a.rows = (uint32_t)r.sum_rows;
         a.sums = db ? (r.sum_parts > 1 ? r.sums : db) : nullptr;
         const uint64_t gx = (a.pitch + SUM_COLS - 1) / SUM_COLS;
         const int rc = with_half_type(type, [&](auto t) {
@@ -354,14 +358,6 @@ int kimad_linear_grad(const void* dy, uint64_t ld_dy, const void* x, uint64_t ld
             hipLaunchKernelGGL(k_sum_join, dim3((uint32_t)((N + 63) / 64)), dim3(256), 0, s, r.sums, r.sum_parts, N, db);
             if (const int rc2 = launched()) return rc2;
         }
-    }
-    if (r.x) {
-        if (const int rc = copy_rows(x, ld_x, M, K, r.x, nullptr, 0, nullptr, s)) return rc;
-        ox = {r.x, pitch_of(K)};
-    }
-    if (r.w) {
-        if (const int rc = copy_rows(w, ld_w, N, K, r.w, nullptr, 0, nullptr, s)) return rc;
-        ow = {r.w, pitch_of(K)};
     }
     if (dx) {
         GemmArgs g{};
@@ -403,34 +399,24 @@ int kimad_linear_xent(const void* x, uint64_t ld_x, const void* w, uint64_t ld_w
     Room room{static_cast<uint8_t*>(workspace), 0};
     const XentRoom r = xent_room(room, x, ld_x, w, ld_w, type, rows, vocab, dim, wants, dw_type);
     if (!workspace || workspace_bytes < room.used || !aligned(workspace, 16)) return KIMAD_ERR_WORKSPACE_TOO_SMALL;
-    const bool few = r.z.kind == GemmPlan::FEW;
-    Operand ox{x, ld_x}, ow{w, ld_w};
-    if (r.x) {
-        if (const int rc = copy_rows(x, ld_x, rows, dim, r.x, target, vocab, row_weight, s)) return rc;
-        ox = {r.x, pitch_of(dim)};
-    }
-    if (r.w) {
-        if (const int rc = copy_rows(w, ld_w, vocab, dim, r.w, nullptr, 0, nullptr, s)) return rc;
-        ow = {r.w, pitch_of(dim)};
-    }
-    if (r.scale) {
-        hipLaunchKernelGGL(k_xent_scale, dim3(1), dim3(1024), 0, s, target, row_weight, rows, (uint32_t)vocab, r.scale);
-        if (const int rc = launched()) return rc;
-    }
+    if (const int rc = copy_rows({x, ld_x, rows, dim, r.x}, {w, ld_w, vocab, dim, r.w}, target, vocab, row_weight, r.scale, type == KIMAD_VALUES_F16 ? 4096.f : 1.f, s)) return rc;
+    const Operand ox = r.x ? Operand{r.x, pitch_of(dim)} : Operand{x, ld_x}, ow = r.w ? Operand{r.w, pitch_of(dim)} : Operand{w, ld_w};
     const bool dw32 = dw_type == KIMAD_VALUES_F32;
     return with_half_type(type, [&](auto t) {
         constexpr uint32_t TYPE = decltype(t)::value;
         for (uint64_t p = 0; p < r.pieces; ++p) {
             const uint64_t row = p * r.piece, n = std::min(r.piece, rows - row);
+            const auto& plan = r.plans[p + 1 == r.pieces];
+            const uint32_t strip = plan.z.strip(), strips_row = (uint32_t)((vocab + strip - 1) / strip);
             GemmArgs g{};
             g.a = static_cast<const uint8_t*>(ox.p) + row * ox.ld * 2; g.lda = ox.ld; g.b = static_cast<const uint8_t*>(ow.p); g.ldb = ow.ld;
-            g.M = n; g.N = vocab; g.K = few ? dim : pitch_of(dim);
-            g.soft.strips = r.strips; g.soft.e = r.e; g.soft.target = target + row; g.soft.picked = r.picked; g.soft.pitch = r.pitch; g.soft.strips_row = (uint32_t)r.strips_row;
-            if (const int rc = launch_kind<TYPE, false, false, END_SOFTMAX>(g, fewer(r.z, n, g.K), s)) return rc;
+            g.M = n; g.N = vocab; g.K = plan.z.kind == GemmPlan::FEW ? dim : pitch_of(dim);
+            g.soft.strips = r.strips; g.soft.e = r.e; g.soft.target = target + row; g.soft.picked = r.picked; g.soft.pitch = r.pitch; g.soft.strips_row = strips_row;
+            if (const int rc = launch_kind<TYPE, false, false, END_SOFTMAX>(g, plan.z, s)) return rc;
             XentArgs a{};
             a.strips = r.strips; a.picked = r.picked; a.target = target + row; a.weight = row_weight ? row_weight + row : nullptr;
             a.loss = loss ? loss + row : nullptr; a.lse = lse ? lse + row : nullptr; a.rows_out = r.rows_out; a.e = r.e; a.scale = r.scale;
-            a.rows = n; a.pitch = r.pitch; a.vocab = (uint32_t)vocab; a.strips_row = (uint32_t)r.strips_row; a.strip = r.z.strip();
+            a.rows = n; a.pitch = r.pitch; a.vocab = (uint32_t)vocab; a.strips_row = strips_row; a.strip = strip;
             hipLaunchKernelGGL(k_xent_rows, dim3((uint32_t)n), dim3(256), 0, s, a);
             if (const int rc = launched()) return rc;
             if (!wants) continue;
@@ -441,21 +427,21 @@ int kimad_linear_xent(const void* x, uint64_t ld_x, const void* w, uint64_t ld_w
                 GemmArgs d{};
                 d.a = reinterpret_cast<const uint8_t*>(r.e); d.lda = r.pitch; d.b = static_cast<const uint8_t*>(ow.p); d.ldb = ow.ld;
                 d.M = n; d.N = dim; d.K = r.pitch; d.k_rows_b = vocab;
-                d.end.out = static_cast<uint8_t*>(dx) + row * ld_dx * 2; d.end.ld = ld_dx; d.end.scale = r.scale ? r.scale + 1 : nullptr;
-                if (const int rc = launch_gemm<TYPE, false, true>(d, fewer(r.dx, n, d.K), false, r.parts, s)) return rc;
+                d.end.out = static_cast<uint8_t*>(dx) + row * ld_dx * 2; d.end.ld = ld_dx; d.end.scale = r.scale + 1;
+                if (const int rc = launch_gemm<TYPE, false, true>(d, plan.dx, false, r.parts, s)) return rc;
             }
             if (dw) {
                 GemmArgs d{};
                 d.a = reinterpret_cast<const uint8_t*>(r.e); d.lda = r.pitch; d.b = static_cast<const uint8_t*>(ox.p) + row * ox.ld * 2; d.ldb = ox.ld;
                 d.M = vocab; d.N = dim; d.K = n; d.k_rows_a = n; d.k_rows_b = n;
-                d.end.scale = r.scale ? r.scale + 1 : nullptr;
+                d.end.scale = r.scale + 1;
                 // the pieces' sums in fp32, in dw itself where it is
                 void* sum = dw32 ? dw : r.sum;
                 const uint64_t ld_sum = dw32 ? ld_dw : dim;
                 const bool last = p + 1 == r.pieces;
                 if (p) { d.end.residual = sum; d.end.ld_res = ld_sum; d.end.res32 = 1; }
                 d.end.out = last ? dw : sum; d.end.ld = last ? ld_dw : ld_sum;
-                if (const int rc = launch_gemm<TYPE, true, true>(d, fewer(r.dw, vocab, n), dw32 || !last, r.parts, s)) return rc;
+                if (const int rc = launch_gemm<TYPE, true, true>(d, plan.dw, dw32 || !last, r.parts, s)) return rc;
             }
         }
         return (int)KIMAD_OK;

@@ -36,10 +36,10 @@ def test_linear_refuses(bad):
 def test_linear_asks_for_its_workspace():
     need = kimad.lib().kimad_linear_workspace_bytes
     assert need(P, 64, P, 64, 40, 48, 64) == 0
-    assert need(P, 65, P, 65, 40, 48, 65) == -(-2 * 40 * 72 // 256) * 256 + -(-2 * 48 * 72 // 256) * 256        # both laid out anew
-    assert need(P + 2, 64, P, 64, 40, 48, 64) == 2 * 40 * 64                                                    # one of them
+    assert need(P, 65, P, 65, 200, 48, 65) == -(-2 * 200 * 72 // 256) * 256 + -(-2 * 48 * 72 // 256) * 256      # both laid out anew
+    assert need(P + 2, 64, P, 64, 200, 48, 64) == 2 * 200 * 64                                                  # one of them
     assert need(P + 2, 65, P, 65, 32, 48, 65) == 0                                                              # few rows: read as they lie
-    assert linear(x=P + 2) == SMALL and linear(x=P + 2, ws=0, nbytes=BIG) == SMALL and linear(x=P + 2, ws=P + 8, nbytes=BIG) == SMALL
+    assert linear(x=P + 2, M=200) == SMALL and linear(x=P + 2, M=200, ws=0, nbytes=BIG) == SMALL and linear(x=P + 2, M=200, ws=P + 8, nbytes=BIG) == SMALL
     assert linear(M=0) == OK and linear(N=0) == OK and linear(M=0, x=0, out=0, w=0) == BAD and linear(M=0, x=0, out=0) == OK
 
 
@@ -55,7 +55,7 @@ def test_linear_grad_asks_for_its_workspace():
     assert need(P, 48, P, 64, P, 64, 40, 48, 64, 0, 7) == 0
     assert need(P, 48, P, 64, P, 64, 40, 48, 64, 1, 1) == 2 * 40 * 48                                           # dz
     assert need(P, 48, P, 64, P, 64, 40, 48, 64, 1, 4) == 0                                                     # the bias alone
-    assert need(P, 48, P, 64, P, 64, 400, 48, 64, 0, 4) == 7 * 4 * 48 + 192                                        # sums of 64 rows each, in whole 256 bytes
+    assert need(P, 48, P, 64, P, 64, 400, 48, 64, 0, 4) == 7 * 4 * 48 + 192                                     # sums of 64 rows each, in whole 256 bytes
     assert linear_grad(act=1, z=P) == SMALL and linear_grad(act=1, z=P, ws=P + 8, nbytes=BIG) == SMALL
     assert linear_grad(x=0, dw=0, ws=0, dx=0, w=0) == OK                                                        # nothing wanted
 
