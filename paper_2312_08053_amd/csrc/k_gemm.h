@@ -106,7 +106,7 @@ struct GemmArgs {
     uint64_t lda, ldb;           // elements from row to row as stored
     uint64_t M, N, K;            // K: a multiple of 8 where an operand is stored along it
     uint64_t k_rows_a, k_rows_b; // rows that an operand across K has (beyond them: zeros)
-    uint32_t tiles_m, tiles_n;
+    uint32_t tiles_m, tiles_n, band;   // band: rows of tiles that are taken together, so that what an XCD reads at a time is shared
     uint32_t whole;              // the first so many tiles are summed by one workgroup each; the others' sums are shared out,
     uint32_t splits, share;      // in parts of `share` stages each (the last one fewer), part p of the t-th of them at parts + (p * (tiles - whole) + t) tiles
     float* parts;                // (as the waves' registers lie), which k_gemm_join adds
@@ -199,6 +199,18 @@ __device__ __forceinline__ u32x4 gemm_operand(const uint8_t* at, uint32_t k) {
 constexpr int STREAM = 2;
 
 enum : uint32_t { END_TYPE = 0, END_F32 = 1, END_SOFTMAX = 2 };
+
+// Workgroups go to the eight XCDs in turn: the items are numbered so that an XCD takes a run of them.
+__device__ __forceinline__ uint32_t in_runs(uint32_t id, uint32_t total) {
+    const uint32_t xcd = id & 7u, each = total >> 3, more = total & 7u;
+    return xcd * each + (xcd < more ? xcd : more) + (id >> 3);
+}
+// A tile by its number, in bands of `band` rows of tiles.
+__device__ __forceinline__ void tile_at(uint32_t id, uint32_t tm, uint32_t tn, uint32_t band, uint32_t& m, uint32_t& n) {
+    const uint32_t first = id / (band * tn) * band, high = tm - first < band ? tm - first : band, r = id % (band * tn);
+    m = first + r % high;
+    n = r / high;
+}
 
 // What is done with a wave's sums, TI times 32 rows from row0 of the tile on and its wn-th strip of columns.  `mine`: LDS of the wave's own, T::OUT bytes.  Whether the
 // wave's last accesses are stores, 4 TI or more (fp32: 4 TI TJ).
@@ -415,15 +427,23 @@ __global__ __launch_bounds__(64 * T::WAVES, 2) void k_gemm_tile(GemmArgs g) {
     GemmSide<BN, T::WAVES, T::SK, ACROSS_B> sb;
     sa.begin(wave, lane, g.lda);
     sb.begin(wave, lane, g.ldb);
-    auto stage_first = [&](uint32_t item) { return item < g.whole ? 0u : (item - g.whole) / shared * g.share; };
-    auto stages_of = [&](uint32_t item, uint32_t first) { return item < g.whole || stages - first < g.share ? stages - first : g.share; };
+    // An item's tile, and the part of its sum that it is: the whole tiles come first, then the shared ones' first parts and so on.
+    struct Item {
+        uint32_t tile, part, first, count;                                    // first, count: stages
+    };
+    auto item_at = [&](uint32_t id) {
+        if (id < g.whole) return Item{in_runs(id, g.whole), 0u, 0u, stages};
+        const uint32_t i = in_runs(id - g.whole, shared * g.splits), part = i / shared, first = part * g.share;
+        return Item{g.whole + i % shared, part, first, stages - first < g.share ? stages - first : g.share};
+    };
     uint32_t stages_in;                                                       // of the item, this one counted
     auto aim = [&](uint32_t item) {
         uint32_t tm = 0, tn = 0;
         const bool none = item >= items;                                      // (behind the last one the loads go on, of nothing)
-        if (!none) tile_of(item < g.whole ? item : g.whole + (item - g.whole) % shared, g.tiles_m, g.tiles_n, tm, tn);
-        const uint32_t first = none ? 0 : stage_first(item), k0 = first * T::SK;
-        stages_in = none ? stages : stages_of(item, first);
+        const Item it = none ? Item{0u, 0u, 0u, stages} : item_at(item);
+        if (!none) tile_at(it.tile, g.tiles_m, g.tiles_n, g.band, tm, tn);
+        const uint32_t k0 = it.first * T::SK;
+        stages_in = it.count;
         sa.aim(g.a, (uint64_t)tm * BM, none ? 0 : g.M, k0, ACROSS_A ? (uint32_t)g.k_rows_a : (uint32_t)g.K);
         sb.aim(g.b, (uint64_t)tn * BN, none ? 0 : g.N, k0, ACROSS_B ? (uint32_t)g.k_rows_b : (uint32_t)g.K);
     };
@@ -510,7 +530,7 @@ __global__ __launch_bounds__(64 * T::WAVES, 2) void k_gemm_tile(GemmArgs g) {
     read_all(0, 0, half0);
     uint32_t stores_behind = 0;                                               // not 0: a tile's stores, STORES or more, are behind the loads that the next barrier waits for
     for (uint32_t item = blockIdx.x; item < items; item += gridDim.x) {
-        const uint32_t here = stages_of(item, stage_first(item));
+        const uint32_t here = item_at(item).count;
 #pragma unroll
         for (uint32_t i = 0; i < T::TI; ++i)
 #pragma unroll
@@ -533,12 +553,11 @@ __global__ __launch_bounds__(64 * T::WAVES, 2) void k_gemm_tile(GemmArgs g) {
             brought();
         }
 
-        const bool part = item >= g.whole;
-        const uint32_t tile = part ? g.whole + (item - g.whole) % shared : item;
-        if (END != END_SOFTMAX && part && g.splits > 1) {
+        const Item it = item_at(item);
+        if (END != END_SOFTMAX && item >= g.whole) {
             uint32_t l;                                                       // the lane, found anew: kept through the loop, it would cost a register
             asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(l));
-            f32x4* to = reinterpret_cast<f32x4*>(g.parts + (uint64_t)(item - g.whole) * (BM * BN)) + wave * (T::TI * T::TJ * 256) + l;
+            f32x4* to = reinterpret_cast<f32x4*>(g.parts + ((uint64_t)it.part * shared + it.tile - g.whole) * (BM * BN)) + wave * (T::TI * T::TJ * 256) + l;
 #pragma unroll
             for (uint32_t i = 0; i < T::TI; ++i)
 #pragma unroll
@@ -550,7 +569,7 @@ __global__ __launch_bounds__(64 * T::WAVES, 2) void k_gemm_tile(GemmArgs g) {
             stores_behind = T::NB - 1;
         } else {
             uint32_t tm, tn;
-            tile_of(tile, g.tiles_m, g.tiles_n, tm, tn);
+            tile_at(it.tile, g.tiles_m, g.tiles_n, g.band, tm, tn);
             float* mine = reinterpret_cast<float*>(s_mem + T::NB * T::STAGE + wave * T::OUT);
             const bool counted = gemm_end<TYPE, T, T::TI, END>(g, acc, mine, (uint64_t)tm * BM, (uint64_t)tn * BN, wm * (BM / WM), wn);
             stores_behind = counted ? T::NB - 1 : 0u;
@@ -569,7 +588,7 @@ __global__ __launch_bounds__(256) void k_gemm_join(GemmArgs g) {
     if (t >= shared) return;
     const uint32_t w = unit / T::TI % T::WAVES, i = unit % T::TI;
     uint32_t tm, tn;
-    tile_of(g.whole + t, g.tiles_m, g.tiles_n, tm, tn);
+    tile_at(g.whole + t, g.tiles_m, g.tiles_n, g.band, tm, tn);
     const uint64_t tile_m = (uint64_t)tm * T::BM, tile_n = (uint64_t)tn * T::BN;
     const uint32_t row0 = w / T::WN * (T::BM / T::WM) + 32 * i, wn = w % T::WN;
     if (tile_m + row0 >= g.M || tile_n + wn * T::COLS >= g.N) return;

@@ -108,9 +108,10 @@ struct CopyArgs {
 __device__ __forceinline__ void scale_of_weights(const CopyArgs& a) {
     __shared__ float s_max[4];
     float m = 0.f;
+#pragma unroll 8
     for (uint64_t r = threadIdx.x; r < a.rows[0]; r += 256) {
         const float w = a.weight ? fabsf(a.weight[r]) : 1.f;
-        if ((uint32_t)a.target[r] < a.vocab && w < INFINITY) m = fmaxf(m, w);
+        m = fmaxf(m, (uint32_t)a.target[r] < a.vocab && w < INFINITY ? w : 0.f);
     }
 #pragma unroll
     for (uint32_t o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));

@@ -79,7 +79,7 @@ GemmPlan gemm_plan(uint64_t M, uint64_t N, uint64_t K, bool wide, bool may_split
         {GemmPlan::T256, 256, 1.3, 1.3, 1.6, 6.0, 8.0, 5.0}, {GemmPlan::T128, 128, 0.72, 0.66, 0.70, 1.0, 1.5, 5.0}, {GemmPlan::T64, 64, 0.45, 0.24, 0.24, 0.35, 0.35, 4.5}};
     for (const auto& k : kinds) {
         const uint64_t tm = (M + k.edge - 1) / k.edge, tn = (N + k.edge - 1) / k.edge, tiles = tm * tn, full = tiles / UNITS * UNITS, rest = tiles - full;
-        for (uint64_t splits = 1; splits == 1 || (may_split && rest && splits <= 16 && 4 * splits <= stages); ++splits) {
+        for (uint64_t splits = 1; splits == 1 || (may_split && rest && splits <= 256 && 4 * splits <= stages && (splits <= 4 || rest * splits <= 8 * UNITS)); splits += splits < 16 ? 1 : splits / 4) {
             const uint64_t share = (stages + splits - 1) / splits, parts = (stages + share - 1) / share;
             if (parts != splits) continue;
             const uint64_t items = rest * parts, rounds = items / UNITS;
@@ -98,11 +98,18 @@ GemmPlan gemm_plan(uint64_t M, uint64_t N, uint64_t K, bool wide, bool may_split
     return best;
 }
 
+// Rows of tiles in a band: about as many as columns among the tiles that an XCD has at a time, so that these share most of what they read.
+uint32_t band_rows(const GemmPlan& p) {
+    const uint64_t run = std::min<uint64_t>(UNITS / 8, (p.tiles_m * p.tiles_n * p.splits + 7) / 8);
+    const uint64_t across = std::max<uint64_t>(1, std::min(p.tiles_n, (uint64_t)std::sqrt((double)run)));
+    return (uint32_t)std::min(p.tiles_m, (run + across - 1) / across);
+}
+
 template <uint32_t TYPE, class T, bool XA, bool XB, uint32_t END>
 int launch_tile(GemmArgs g, const GemmPlan& p, hipStream_t s) {
     const uint64_t items = p.whole + p.shared() * p.splits;                   // (below 2^28 for matrices of fewer than 2^34 elements and rows of 2^22)
     constexpr uint64_t slots = UNITS * ((160 * 1024) / T::LDS);
-    g.tiles_m = (uint32_t)p.tiles_m; g.tiles_n = (uint32_t)p.tiles_n; g.whole = (uint32_t)p.whole; g.splits = p.splits; g.share = p.share;
+    g.tiles_m = (uint32_t)p.tiles_m; g.tiles_n = (uint32_t)p.tiles_n; g.band = band_rows(p); g.whole = (uint32_t)p.whole; g.splits = p.splits; g.share = p.share;
     hipLaunchKernelGGL((k_gemm_tile<TYPE, T, XA, XB, END>), dim3((uint32_t)std::min<uint64_t>(items, slots)), dim3(64 * T::WAVES), 0, s, g);
     if constexpr (END != END_SOFTMAX)
         if (p.splits > 1) {
