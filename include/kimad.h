@@ -522,7 +522,7 @@ int kimad_linear_grad(const void* dy, uint64_t ld_dy, const void* x, uint64_t ld
  *   dx          DEVICE [rows, dim] of `type`, or NULL;  dw  DEVICE [vocab, dim] of dw_type, `type` or KIMAD_VALUES_F32, or NULL
  * At least one output is wanted, unless there are no rows (then dw is 0).  A row that does not count has loss, lse and gradient 0, adds
  * nothing to dw, and what it holds, Inf and NaN too, reaches nothing.  So does a row whose logits are all -Inf.  For a gradient the
- * exponentials of a piece of the rows are kept, 512 MiB at most or 256 rows, and turned into G, divided by the largest weight and rounded to
+ * exponentials of a piece of the rows are kept, 1 GiB at most or 256 rows, and turned into G, divided by the largest weight and rounded to
  * `type`, for the two products. */
 uint64_t kimad_linear_xent_workspace_bytes(const void* x, uint64_t ld_x, const void* w, uint64_t ld_w, uint32_t type, uint64_t rows,
                                            uint64_t vocab, uint64_t dim, uint32_t wants, uint32_t dw_type);

@@ -5,9 +5,53 @@
 
 namespace kimad {
 
+// Eight 16-bit elements at a time of a row that may begin at any of them.  SHIFTED: from the one or two whole 16 bytes that they lie in, by selections and shifts; loads from
+// addresses off 16 bytes take longer (one row by 32000 x 2049 64 us, so 36, and 20 where rows lie at such addresses).  (Whole 16 bytes with an element of the row are never of another page.)
+template <bool SHIFTED>
+struct RowReader {
+    const uint8_t* at;
+    uint32_t shift;              // bytes from a 16-byte address to the row's first element
+    __device__ __forceinline__ void begin(const uint8_t* p) {
+        shift = SHIFTED ? (uint32_t)(reinterpret_cast<uintptr_t>(p) & 15u) : 0u;
+        at = p - shift;
+    }
+    struct Raw {
+        u32x4 v[SHIFTED ? 2 : 1];
+    };
+    __device__ __forceinline__ Raw load(uint64_t i) const {                   // i: a multiple of 8
+        Raw r;
+        const u32x4* q = reinterpret_cast<const u32x4*>(at + 2 * i);
+        r.v[0] = q[0];
+        if constexpr (SHIFTED) r.v[1] = q[shift ? 1 : 0];
+        return r;
+    }
+    __device__ __forceinline__ u32x4 words(const Raw& r) const {
+        if constexpr (!SHIFTED) return r.v[0];
+        else {
+            // (by masks: of selections the compiler makes addresses)
+            const uint32_t by4 = shift & 4u ? ~0u : 0u, by8 = shift & 8u ? ~0u : 0u;
+            uint32_t d[8], t[7], u[5];
+            u32x4 out;
+#pragma unroll
+            for (uint32_t k = 0; k < 8; ++k) d[k] = r.v[k / 4][k % 4];
+#pragma unroll
+            for (uint32_t k = 0; k < 7; ++k) t[k] = (d[k + 1] & by4) | (d[k] & ~by4);
+#pragma unroll
+            for (uint32_t k = 0; k < 5; ++k) u[k] = (t[k + 2] & by8) | (t[k] & ~by8);
+#pragma unroll
+            for (uint32_t k = 0; k < 4; ++k) out[k] = __builtin_amdgcn_alignbyte(u[k + 1], u[k], shift & 2u);
+            return out;
+        }
+    }
+    __device__ __forceinline__ u32x4 first(uint64_t i, int64_t n) const {     // the first n of them, the others zeros
+        const Raw8<TYPE_BF16> v = load8_first<TYPE_BF16>(at + shift, i, n);
+        return u32x4{v.r[0], v.r[1], v.r[2], v.r[3]};
+    }
+};
+
 // Few rows of A (16 MT at most): sixteen rows of B by a workgroup, whose waves take a quarter of K each, straight from memory to registers, U times 32 of K
-// under way.  Rows may begin anywhere.  Bound by the reads of B.
-template <uint32_t TYPE, uint32_t MT, uint32_t END>
+// under way.  SHIFTED: rows may begin anywhere.  Bound by the reads of B.
+template <uint32_t TYPE, uint32_t MT, uint32_t END, bool SHIFTED>
 __global__ __launch_bounds__(256) void k_gemm_few(GemmArgs g) {
     __shared__ f32x4 s_part[3][MT][64];
     constexpr uint32_t U = MT == 1 ? 8 : MT == 2 ? 4 : 2;
@@ -15,34 +59,33 @@ __global__ __launch_bounds__(256) void k_gemm_few(GemmArgs g) {
     const uint64_t n0 = (uint64_t)blockIdx.x * 16, n = n0 + r < g.N ? n0 + r : g.N - 1;
     // (whole cache lines)
     const uint64_t quarter = (g.K + 255) / 256 * 64, begin = wave * quarter < g.K ? wave * quarter : g.K, end = begin + quarter < g.K ? begin + quarter : g.K;
-    const uint64_t b = n * g.ldb + 8 * blk;
-    uint64_t a[MT];
+    RowReader<SHIFTED> b, a[MT];
+    b.begin(g.b + 2 * n * g.ldb);
     f32x4 acc[MT];
 #pragma unroll
     for (uint32_t t = 0; t < MT; ++t) {
-        a[t] = (16 * t + r < g.M ? 16 * t + r : g.M - 1) * g.lda + 8 * blk;
+        a[t].begin(g.a + 2 * (16 * t + r < g.M ? 16 * t + r : g.M - 1) * g.lda);
         acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    auto words = [](const Raw8<TYPE>& v) { return u32x4{v.r[0], v.r[1], v.r[2], v.r[3]}; };
     uint64_t k = begin;
     for (; k + 32 * U <= end; k += 32 * U) {
-        Raw8<TYPE> vb[U], va[U][MT];
+        typename RowReader<SHIFTED>::Raw vb[U], va[U][MT];
 #pragma unroll
         for (uint32_t u = 0; u < U; ++u) {
-            vb[u] = load8<TYPE>(g.b, b + k + 32 * u);
+            vb[u] = b.load(k + 32 * u + 8 * blk);
 #pragma unroll
-            for (uint32_t t = 0; t < MT; ++t) va[u][t] = load8<TYPE>(g.a, a[t] + k + 32 * u);
+            for (uint32_t t = 0; t < MT; ++t) va[u][t] = a[t].load(k + 32 * u + 8 * blk);
         }
 #pragma unroll
         for (uint32_t u = 0; u < U; ++u)
 #pragma unroll
-            for (uint32_t t = 0; t < MT; ++t) acc[t] = mfma16<TYPE>(words(va[u][t]), words(vb[u]), acc[t]);
+            for (uint32_t t = 0; t < MT; ++t) acc[t] = mfma16<TYPE>(a[t].words(va[u][t]), b.words(vb[u]), acc[t]);
     }
     for (; k < end; k += 32) {
         const int64_t left = (int64_t)(end - k) - 8 * blk;
-        const u32x4 vb = words(load8_first<TYPE>(g.b, b + k, left));
+        const u32x4 vb = b.first(k + 8 * blk, left);
 #pragma unroll
-        for (uint32_t t = 0; t < MT; ++t) acc[t] = mfma16<TYPE>(words(load8_first<TYPE>(g.a, a[t] + k, left)), vb, acc[t]);
+        for (uint32_t t = 0; t < MT; ++t) acc[t] = mfma16<TYPE>(a[t].first(k + 8 * blk, left), vb, acc[t]);
     }
     if (wave)
 #pragma unroll
@@ -144,46 +187,50 @@ struct ActGradArgs {
     void* dz;                    // or null; pitch elements from row to row, filled up with zeros
     float* sums;                 // [ceil(M / rows)][N], or null
     uint64_t M, N, ld_dy, ld_z, pitch;
-    uint32_t act, rows;          // rows of a workgroup
+    uint32_t act, rows, lanes;   // rows of a workgroup; lanes of a row, a power of two, 8 columns each
 };
 template <uint32_t TYPE>
 __global__ __launch_bounds__(256) void k_act_grad(ActGradArgs a) {
-    __shared__ float s_sum[4][SUM_COLS];
-    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
-    const uint64_t c = (uint64_t)blockIdx.x * SUM_COLS + 8 * lane, m0 = (uint64_t)blockIdx.y * a.rows, m1 = m0 + a.rows < a.M ? m0 + a.rows : a.M;
+    __shared__ float s_sum[4 * SUM_COLS];
+    // (a wave takes 64 / lanes rows at a time: of narrow matrices several)
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, per = 64u / a.lanes, group = wave * per + lane / a.lanes, at = lane % a.lanes;
+    const uint64_t c = (uint64_t)blockIdx.x * SUM_COLS + 8 * at, m0 = (uint64_t)blockIdx.y * a.rows, m1 = m0 + a.rows < a.M ? m0 + a.rows : a.M;
     const int64_t n = (int64_t)a.N - (int64_t)c;
     float sum[8] = {};
-    constexpr uint32_t U = 4;                            // rows of a wave under way together
+    constexpr uint32_t U = 4;                            // rows of a lane under way together
     if (c < a.pitch)
         with_act(a.z ? a.act : (uint32_t)ACT_NONE, [&](auto kind) {
             constexpr uint32_t ACT = decltype(kind)::value;
-            for (uint64_t m = m0 + wave; m < m1; m += 4 * U) {
+            for (uint64_t m = m0 + group; m < m1; m += 4 * per * U) {
                 Raw8<TYPE> g[U], z[U];
 #pragma unroll
                 for (uint32_t u = 0; u < U; ++u) {
-                    const uint64_t r = m + 4 * u < m1 ? m + 4 * u : m;
+                    const uint64_t r = m + 4 * per * u < m1 ? m + 4 * per * u : m;
                     g[u] = load8_first<TYPE>(a.dy, r * a.ld_dy + c, n);
                     if (ACT != ACT_NONE) z[u] = load8_first<TYPE>(a.z, r * a.ld_z + c, n);
                 }
 #pragma unroll
                 for (uint32_t u = 0; u < U; ++u) {
-                    if (m + 4 * u >= m1) break;
+                    if (m + 4 * per * u >= m1) break;
                     float v[8];
 #pragma unroll
                     for (uint32_t k = 0; k < 8; ++k) v[k] = ACT == ACT_NONE ? g[u].at(k) : (int64_t)k < n ? g[u].at(k) * slope_as<ACT>(z[u].at(k)) : 0.f;
-                    if (a.dz) store8<TYPE>(a.dz, (m + 4 * u) * a.pitch + c, v);
+                    if (a.dz) store8<TYPE>(a.dz, (m + 4 * per * u) * a.pitch + c, v);
 #pragma unroll
                     for (uint32_t k = 0; k < 8; ++k) sum[k] += v[k];
                 }
             }
         });
     if (!a.sums) return;
+    const uint32_t cols = 8 * a.lanes;
 #pragma unroll
-    for (uint32_t k = 0; k < 8; ++k) s_sum[wave][8 * lane + k] = sum[k];
+    for (uint32_t k = 0; k < 8; ++k) s_sum[group * cols + 8 * at + k] = sum[k];
     __syncthreads();
-    for (uint32_t i = threadIdx.x; i < SUM_COLS; i += 256) {
+    for (uint32_t i = threadIdx.x; i < cols; i += 256) {
         const uint64_t col = (uint64_t)blockIdx.x * SUM_COLS + i;
-        if (col < a.N) a.sums[blockIdx.y * a.N + col] = s_sum[0][i] + s_sum[1][i] + s_sum[2][i] + s_sum[3][i];
+        float v = 0.f;
+        for (uint32_t q = 0; q < 4 * per; ++q) v += s_sum[q * cols + i];
+        if (col < a.N) a.sums[blockIdx.y * a.N + col] = v;
     }
 }
 // The sums of all rows from the workgroups': a wave of a workgroup takes every fourth.
@@ -193,6 +240,7 @@ __global__ __launch_bounds__(256) void k_sum_join(const float* __restrict__ sums
     const uint64_t n = (uint64_t)blockIdx.x * 64 + lane;
     float v = 0.f;
     if (n < N)
+#pragma unroll 8
         for (uint64_t p = wave; p < parts; p += 4) v += sums[p * N + n];
     s_sum[wave][lane] = v;
     __syncthreads();

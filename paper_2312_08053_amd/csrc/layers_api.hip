@@ -65,29 +65,32 @@ GemmPlan gemm_plan(uint64_t M, uint64_t N, uint64_t K, bool wide, bool may_split
     best.splits = 1;
     const uint64_t stages = (K + STAGE_K - 1) / STAGE_K;
     best.share = (uint32_t)stages;
-    // k_gemm_few, whose waves read all of A each; rows that begin off 16-byte addresses cost it over three times as much, but a copy costs the tiles more.
+    // k_gemm_few, whose waves read all of A each; rows that begin off 16-byte addresses cost it nearly twice as much, and the tiles a copy.
     const double copy = few == 2 ? 4.0 + (double)((M + N) * K) * 4.0 / 4.5e6 : 0.0;
     if (few && M <= FEW_MOST) {
         best.kind = GemmPlan::FEW;
-        best.us = 2.5 + (double)(N * K) * (0.26e-6 + 1.5e-8 * (double)M) * (few == 2 ? 3.3 : 1.0) - copy;
+        best.us = 2.5 + (double)(N * K) * (0.26e-6 + 1.5e-8 * (double)M) * (few == 2 ? 1.8 : 1.0) - copy;
         if (best.us <= 0) best.us = 1e-3;
     }
     const double read = 2.0 + (double)((M + N) * K) * 2.0 / 4.5e6;            // both operands from memory
-    // of one tile: a stage with nothing beside it on its compute unit, what comes from beyond the L2; among others, where few units have one and where all do;
-    // its end in 16 bits and in 32; the launch
-    struct { decltype(best.kind) kind; uint64_t edge; double alone, lone, stage, end16, end32, launch; } const kinds[] = {
-        {GemmPlan::T256, 256, 1.3, 1.3, 1.6, 6.0, 8.0, 5.0}, {GemmPlan::T128, 128, 0.72, 0.66, 0.70, 1.0, 1.5, 5.0}, {GemmPlan::T64, 64, 0.45, 0.24, 0.24, 0.35, 0.35, 4.5}};
+    // of one tile: a stage with nothing beside it on its compute unit, and a unit's time for one among others; its end in 16 bits and in 32; the launch; tiles that
+    // a compute unit holds
+    struct { decltype(best.kind) kind; uint64_t edge; double alone, stage, end16, end32, launch; uint64_t held; } const kinds[] = {
+        {GemmPlan::T256, 256, 1.5, 1.65, 6.0, 8.0, 4.0, 1}, {GemmPlan::T128, 128, 0.87, 0.56, 1.0, 1.5, 5.0, 2}, {GemmPlan::T64, 64, 0.5, 0.21, 0.35, 0.35, 4.5, 4}};
     for (const auto& k : kinds) {
-        const uint64_t tm = (M + k.edge - 1) / k.edge, tn = (N + k.edge - 1) / k.edge, tiles = tm * tn, full = tiles / UNITS * UNITS, rest = tiles - full;
-        for (uint64_t splits = 1; splits == 1 || (may_split && rest && splits <= 256 && 4 * splits <= stages && (splits <= 4 || rest * splits <= 8 * UNITS)); splits += splits < 16 ? 1 : splits / 4) {
+        const uint64_t tm = (M + k.edge - 1) / k.edge, tn = (N + k.edge - 1) / k.edge, tiles = tm * tn, slots = UNITS * k.held, full = tiles / slots * slots, rest = tiles - full;
+        auto rounds = [&](uint64_t items, uint64_t each, double end) {        // of `each` stages a tile
+            const uint64_t left = (items % slots + UNITS - 1) / UNITS;
+            const double whole = (double)(items / slots * k.held) * ((double)each * k.stage + end);
+            return left ? whole + (double)each * std::max(k.alone, (double)left * k.stage) + (double)left * end : whole;
+        };
+        for (uint64_t splits = 1; splits == 1 || (may_split && rest && splits <= 256 && 4 * splits <= stages && (splits <= 4 || rest * splits <= 2 * slots)); splits += splits < 16 ? 1 : splits / 4) {
             const uint64_t share = (stages + splits - 1) / splits, parts = (stages + share - 1) / share;
             if (parts != splits) continue;
-            const uint64_t items = rest * parts, rounds = items / UNITS;
-            const double part = (double)(items % UNITS) / UNITS, end = wide ? k.end32 : k.end16, part_end = parts > 1 ? k.end32 : end;
-            double us = k.launch + (double)(full / UNITS) * ((double)stages * k.stage + end) + (double)rounds * ((double)share * k.stage + part_end);
-            if (part > 0) us += (double)share * (k.lone + part * (k.stage - k.lone)) + part_end;
-            if (parts > 1) us += 4.0 + (double)(items * k.edge * k.edge) * 8.0 / 4e6;   // 4 bytes written and read, at 4 TB/s
-            us = std::max(std::max(us, k.launch + (double)share * k.alone + end), read);
+            const double end = wide ? k.end32 : k.end16;
+            double us = k.launch + rounds(full, stages, end) + rounds(rest * parts, share, parts > 1 ? k.end32 : end);
+            if (parts > 1) us += 6.5 + 0.1 * (double)parts + (double)(rest * parts * k.edge * k.edge) * 8.0 / 8e6;   // 4 bytes written and read, much of them beyond memory
+            us = std::max(us, read);
             if (best.us == 0 || us < best.us) {
                 best.us = us;
                 best.kind = k.kind; best.tiles_m = tm; best.tiles_n = tn; best.whole = parts > 1 ? full : tiles;
@@ -121,12 +124,17 @@ int launch_tile(GemmArgs g, const GemmPlan& p, hipStream_t s) {
 }
 template <uint32_t TYPE, uint32_t END>
 int launch_few(const GemmArgs& g, hipStream_t s) {
-    const uint64_t groups = (g.N + 15) / 16;
-    if (g.M <= 16) hipLaunchKernelGGL((k_gemm_few<TYPE, 1, END>), dim3((uint32_t)groups), dim3(256), 0, s, g);
-    else if (g.M <= 32) hipLaunchKernelGGL((k_gemm_few<TYPE, 2, END>), dim3((uint32_t)groups), dim3(256), 0, s, g);
-    else if (g.M <= 64) hipLaunchKernelGGL((k_gemm_few<TYPE, 4, END>), dim3((uint32_t)groups), dim3(256), 0, s, g);
-    else hipLaunchKernelGGL((k_gemm_few<TYPE, 6, END>), dim3((uint32_t)groups), dim3(256), 0, s, g);
-    return launched();
+    const uint32_t groups = (uint32_t)((g.N + 15) / 16);
+    const bool shifted = !aligned(g.a, 16) || !aligned(g.b, 16) || (g.lda % 8 && g.M > 1) || (g.ldb % 8 && g.N > 1);
+    auto go = [&](auto mt) {
+        if (shifted) hipLaunchKernelGGL((k_gemm_few<TYPE, decltype(mt)::value, END, true>), dim3(groups), dim3(256), 0, s, g);
+        else hipLaunchKernelGGL((k_gemm_few<TYPE, decltype(mt)::value, END, false>), dim3(groups), dim3(256), 0, s, g);
+        return launched();
+    };
+    if (g.M <= 16) return go(std::integral_constant<uint32_t, 1>{});
+    if (g.M <= 32) return go(std::integral_constant<uint32_t, 2>{});
+    if (g.M <= 64) return go(std::integral_constant<uint32_t, 4>{});
+    return go(std::integral_constant<uint32_t, 6>{});
 }
 template <uint32_t TYPE, bool XA, bool XB, uint32_t END>
 int launch_kind(const GemmArgs& g, const GemmPlan& p, hipStream_t s) {
@@ -247,7 +255,9 @@ LinearGradRoom linear_grad_room(Room& room, const void* dy, uint64_t ld_dy, cons
 
 // ---- cross entropy ----
 
-constexpr uint64_t PIECE_BYTES = 1ull << 29;             // of the exponentials that a gradient's piece of rows keeps
+// Of the exponentials that a gradient's piece of rows keeps: 8192 rows of 50257, width 768, in one piece 2398 us, in two 2536, in four (which the memory-side cache would hold)
+// 2821, for every piece adds to all of dw.
+constexpr uint64_t PIECE_BYTES = 1ull << 30;
 struct XentRoom {
     uint64_t piece, pieces, pitch;
     uint16_t *x, *w, *e;
@@ -354,6 +364,8 @@ int kimad_linear_grad(const void* dy, uint64_t ld_dy, const void* x, uint64_t ld
     if (r.dz_made || db) {
         ActGradArgs a{};
         a.dy = dy; a.z = act == KIMAD_ACT_NONE ? nullptr : z; a.dz = r.dz; a.M = M; a.N = N; a.ld_dy = ld_dy; a.ld_z = ld_z; a.pitch = pitch_of(N); a.act = act; a.rows = (uint32_t)r.sum_rows;
+        a.lanes = 1;
+        while (a.lanes < 64 && 8 * a.lanes < a.pitch) a.lanes *= 2;
         a.sums = db ? (r.sum_parts > 1 ? r.sums : db) : nullptr;
         const uint64_t gx = (a.pitch + SUM_COLS - 1) / SUM_COLS;
         const int rc = with_half_type(type, [&](auto t) {

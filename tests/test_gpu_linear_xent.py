@@ -165,8 +165,8 @@ def test_strides_and_addresses(rows, vocab, dim, pad, shift):
 
 @pytest.mark.parametrize("dw_dtype", [BF16, F32])
 def test_pieces_of_the_rows(dw_dtype):
-    """A vocabulary of 262144 leaves a piece 1024 rows: 2100 rows are three.  One row in a hundred counts, which can be checked on its own; the others must add nothing."""
-    rows, vocab, dim = 2100, 262144, 32
+    """A vocabulary of 262144 leaves a piece 2048 rows: 4200 rows are three.  One row in a hundred counts, which can be checked on its own; the others must add nothing."""
+    rows, vocab, dim = 4200, 262144, 32
     rng = np.random.default_rng(0)
     x, w = torch.from_numpy(rng.normal(size=(rows, dim))).to(BF16), torch.from_numpy(rng.normal(size=(vocab, dim)) * 0.5).to(BF16)
     target = np.full(rows, -1, dtype=np.int32)
