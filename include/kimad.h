@@ -473,7 +473,7 @@ int kimad_distill_grad(const void* logits, uint32_t type, uint64_t rows, uint64_
  * read must not overlap arrays that are written, but where stated; every array is aligned like its elements.  `type` is that of
  * the operands, KIMAD_VALUES_F16 or _BF16 (the matrix cores' types; the dropout takes _F32 too); sums are fp32 and rounded once,
  * where they are stored.  Matrices have contiguous rows, `ld` elements apart: at most 2^22 for operands of a product, 2^24 for its
- * results and what is added to them.  At most 4194240 rows (tokens), 2^22 features, and fewer than 2^34 elements a matrix, its columns counted as seven more; more are
+ * results and what is added to them.  At most 4194240 rows (tokens), 2^22 features, and fewer than 2^33 elements a matrix, its columns counted as seven more; more are
  * refused.  Operands are read fastest where they begin at 16-byte addresses, ld is a multiple of 8 and so are the features; others
  * are laid out anew in the workspace first, but for forward products of few rows.
  *   workspace   DEVICE, 16-byte aligned, as many bytes as the call's own ..._workspace_bytes says for the same arguments (of the pointers,
@@ -521,7 +521,8 @@ int kimad_linear_grad(const void* dy, uint64_t ld_dy, const void* x, uint64_t ld
  *   loss, lse   DEVICE float[rows] or NULL
  *   dx          DEVICE [rows, dim] of `type`, or NULL;  dw  DEVICE [vocab, dim] of dw_type, `type` or KIMAD_VALUES_F32, or NULL
  * At least one output is wanted, unless there are no rows (then dw is 0).  A row that does not count has loss, lse and gradient 0, adds
- * nothing to dw, and what it holds, Inf and NaN too, reaches nothing.  So does a row whose logits are all -Inf.  For a gradient the
+ * nothing to dw, and what it holds, Inf and NaN too, reaches nothing.  A row whose logits are all -Inf has loss, lse and G 0.  A NaN or +Inf among a row's logits makes its
+ * loss and its G NaN, and with it dx's row and dw.  For a gradient the
  * exponentials of a piece of the rows are kept, 1 GiB at most or 256 rows, and turned into G, divided by the largest weight and rounded to
  * `type`, for the two products. */
 uint64_t kimad_linear_xent_workspace_bytes(const void* x, uint64_t ld_x, const void* w, uint64_t ld_w, uint32_t type, uint64_t rows,

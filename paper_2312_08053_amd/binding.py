@@ -19,6 +19,7 @@ KIMAD_VALUES_F32 = 0
 KIMAD_VALUES_F16 = 1
 KIMAD_VALUES_BF16 = 2
 KIMAD_MAX_J = 64
+KIMAD_ERR_WORKSPACE_TOO_SMALL = -2
 KIMAD_ACT_NONE = 0
 KIMAD_ACT_RELU = 1
 KIMAD_ACT_GELU = 2
@@ -608,9 +609,15 @@ def kimad_linear(x, w, out, bias=None, residual=None, act: int = KIMAD_ACT_NONE,
         raise ValueError(f"bias: {N} contiguous elements of {dtype} are wanted, got {tuple(bias.shape)} of {bias.dtype}")
     handle = _on_device(stream, x, w, out, bias, residual, z, workspace)
     L = lib()
-    need = 0 if workspace is not None else L.kimad_linear_workspace_bytes(x.data_ptr(), ld_x, w.data_ptr(), ld_w, M, N, K)
-    ws, nbytes, kept = _for_call(workspace, need, x.device, stream)
-    rc = L.kimad_linear(x.data_ptr(), ld_x, w.data_ptr(), ld_w, kind, M, N, K, _ptr(bias), at_res, ld_res, act, at_z, ld_z, at_out, out_kind, ld_out, ws, nbytes, handle)
+    args = (x.data_ptr(), ld_x, w.data_ptr(), ld_w, kind, M, N, K, _ptr(bias), at_res, ld_res, act, at_z, ld_z, at_out, out_kind, ld_out)
+    if workspace is None and M <= 96:                            # (products of few rows seldom need one: asked for only then)
+        rc = L.kimad_linear(*args, 0, 0, handle)
+    else:
+        rc = KIMAD_ERR_WORKSPACE_TOO_SMALL
+    if rc == KIMAD_ERR_WORKSPACE_TOO_SMALL:
+        need = 0 if workspace is not None else L.kimad_linear_workspace_bytes(*args[:4], M, N, K)
+        ws, nbytes, kept = _for_call(workspace, need, x.device, stream)
+        rc = L.kimad_linear(*args, ws, nbytes, handle)
     if rc:
         _check(rc, "kimad_linear")
 
@@ -700,7 +707,7 @@ def kimad_dropout(x, out, p: float, seed: int, offset: int = 0, residual=None, s
     if not (0 <= seed < 1 << 64 and 0 <= offset < 1 << 64):
         raise ValueError(f"seed and offset: whole numbers of 64 bits are wanted, got {seed} and {offset}")
     handle = _on_device(stream, x, out, residual)
-    rc = lib().kimad_dropout(x.data_ptr(), kind, rows, cols, ld, at_res, ld_res, p, seed, offset, at_out, ld_out, handle)
+    rc = lib().kimad_dropout(x.data_ptr(), kind, rows, cols, ld, at_res, ld_res, p, int(seed), int(offset), at_out, ld_out, handle)
     if rc:
         _check(rc, "kimad_dropout")
 

@@ -70,16 +70,23 @@ __device__ __forceinline__ float act_of(float z, uint32_t act) {
 
 // ---- tiles ---------------------------------------------------------------------------------------------------------------------
 
-// Exponentials e = exp(s - m), 0 to 1, in 16 bits without a sign: M of mantissa, 16 - M of exponent.  A product in fp16 takes M = 12, exact to 2^-13 of e down to 2^-14 and to
-// 2^-28 below, one in bfloat16 M = 11, 2^-12 down to 2^-30 and 2^-43 below: small beside the roundings of those types.  The float e 2^-(128 - 2^(16 - M))
-// has such an exponent, and its bits, rounded, are the code.
+// Exponentials e = exp(s - m), 0 to 1, in 16 bits, whose rounding is small beside the type's.  They are made, and summed, as 2^UP e.
+//   A product in bfloat16 takes them as fp16 numbers 2^15 e: exact to 2^-11 of e down to 2^-29, to 2^-40 below.
+//   One in fp16 as numbers without a sign, twelve bits of mantissa and four of exponent: exact to 2^-13 of e down to 2^-14, to 2^-28 below.  The float e 2^-112 has such
+//   an exponent, and its bits, rounded, are the code.
 template <uint32_t TYPE>
 struct SmallFloat {
-    static constexpr uint32_t SHIFT = TYPE == TYPE_F16 ? 11 : 12;             // 23 - M
-    static constexpr float DOWN = TYPE == TYPE_F16 ? 0x1p-112f : 0x1p-96f, UP = TYPE == TYPE_F16 ? 0x1p112f : 0x1p96f;
-    static __device__ __forceinline__ uint32_t bits(float e) { return __float_as_uint(e * DOWN) + (1u << (SHIFT - 1)); }
-    static __device__ __forceinline__ uint32_t pack(float a, float b) { return bits(a) >> SHIFT | (bits(b) >> SHIFT) << 16; }
-    static __device__ __forceinline__ float at(uint32_t word, uint32_t half) { return __uint_as_float((half ? word >> 16 : word & 0xFFFFu) << SHIFT) * UP; }
+    static constexpr float UP = TYPE == TYPE_BF16 ? 15.f : 0.f, DOWN = TYPE == TYPE_BF16 ? 0x1p-15f : 1.f;
+    static __device__ __forceinline__ uint32_t bits(float e) { return __float_as_uint(e * 0x1p-112f) + 0x400u; }
+    static __device__ __forceinline__ uint32_t pack(float a, float b) {       // of 2^UP e
+        if (TYPE == TYPE_BF16) return pack2<TYPE_F16>(a, b);
+        return bits(a) >> 11 | (bits(b) >> 11) << 16;
+    }
+    static __device__ __forceinline__ float at(uint32_t word, uint32_t half) {   // 2^UP e again, or e 2^-112
+        const uint32_t code = half ? word >> 16 : word & 0xFFFFu;
+        return TYPE == TYPE_BF16 ? half_to_float(code) : __uint_as_float(code << 11);
+    }
+    static constexpr float TO_E = TYPE == TYPE_BF16 ? 0x1p-15f : 0x1p112f;    // from what at() gives to e
 };
 
 // What becomes of a sum s:  z = scale s + bias, z kept, act(z) + residual.
@@ -275,10 +282,10 @@ __device__ __forceinline__ bool gemm_end(const GemmArgs& g, const f32x16 (&acc)[
             m = fmaxf(m, __uint_as_float(dpp_u32<DPP_XOR1>(__float_as_uint(m))));
             m = fmaxf(m, __uint_as_float(dpp_u32<DPP_XOR2>(__float_as_uint(m))));
             if (LANES == 8) m = fmaxf(m, __uint_as_float(dpp_u32<DPP_HALF_MIRROR>(__float_as_uint(m))));
-            const float from = (m == -INFINITY ? 0.f : m) * LOG2E;
+            const float from = SmallFloat<TYPE>::UP - (m == -INFINITY ? 0.f : m) * LOG2E;
 #pragma unroll
             for (uint32_t k = 0; k < EACH; ++k) {
-                v[k] = __builtin_amdgcn_exp2f(fmaf(v[k], LOG2E, -from));
+                v[k] = __builtin_amdgcn_exp2f(fmaf(v[k], LOG2E, from));
                 sum += v[k];
             }
             sum += __uint_as_float(dpp_u32<DPP_XOR1>(__float_as_uint(sum)));
@@ -292,7 +299,7 @@ __device__ __forceinline__ bool gemm_end(const GemmArgs& g, const f32x16 (&acc)[
                 const __amdgpu_buffer_rsrc_t to = buffer_of(static_cast<uint8_t*>(o.e) + ((tile_m + first) * o.pitch + tile_n) * 2, 0xFFFFFF00u);
                 __builtin_amdgcn_raw_buffer_store_b128(out, to, in && tile_n + wcol < o.pitch ? ((8 * e + row) * (uint32_t)o.pitch + wcol) * 2 : BEYOND, 0, STREAM);
             }
-            if (in && l % LANES == 0 && wn * T::COLS < cols) o.strips[(tile_m + r) * o.strips_row + tile_n / T::STRIP + wn] = f32x2{m, sum};
+            if (in && l % LANES == 0 && wn * T::COLS < cols) o.strips[(tile_m + r) * o.strips_row + tile_n / T::STRIP + wn] = f32x2{m, sum * SmallFloat<TYPE>::DOWN};
         }
         return o.e != nullptr;
     } else {

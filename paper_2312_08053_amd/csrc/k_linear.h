@@ -233,18 +233,21 @@ __global__ __launch_bounds__(256) void k_act_grad(ActGradArgs a) {
         if (col < a.N) a.sums[blockIdx.y * a.N + col] = v;
     }
 }
-// The sums of all rows from the workgroups': a wave of a workgroup takes every fourth.
-__global__ __launch_bounds__(256) void k_sum_join(const float* __restrict__ sums, uint64_t parts, uint64_t N, float* __restrict__ out) {
-    __shared__ float s_sum[4][64];
+// The sums of all rows from the workgroups': 64 columns a workgroup, whose sixteen waves take every sixteenth part.
+__global__ __launch_bounds__(1024) void k_sum_join(const float* __restrict__ sums, uint64_t parts, uint64_t N, float* __restrict__ out) {
+    __shared__ float s_sum[16][64];
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
     const uint64_t n = (uint64_t)blockIdx.x * 64 + lane;
     float v = 0.f;
     if (n < N)
 #pragma unroll 8
-        for (uint64_t p = wave; p < parts; p += 4) v += sums[p * N + n];
+        for (uint64_t p = wave; p < parts; p += 16) v += sums[p * N + n];
     s_sum[wave][lane] = v;
     __syncthreads();
-    if (wave == 0 && n < N) out[n] = s_sum[0][lane] + s_sum[1][lane] + s_sum[2][lane] + s_sum[3][lane];
+    if (wave || n >= N) return;
+#pragma unroll
+    for (uint32_t i = 1; i < 16; ++i) v += s_sum[i][lane];
+    out[n] = v;
 }
 
 }  // namespace kimad

@@ -58,10 +58,11 @@ __global__ __launch_bounds__(256) void k_xent_gradient(XentArgs a, uint32_t chun
     if (live) {
         const u32x4 w = *at;
         const float m = a.strips[row * a.strips_row + col / a.strip][0], f = __builtin_amdgcn_exp2f((m - of[0]) * LOG2E) * of[1];
+        const float fe = f * SmallFloat<TYPE>::TO_E;
         const uint32_t t = (uint32_t)a.target[row] - (uint32_t)col;
         float v[8];
 #pragma unroll
-        for (uint32_t k = 0; k < 8; ++k) v[k] = col + k < a.vocab ? SmallFloat<TYPE>::at(w[k / 2], k % 2) * f : 0.f;
+        for (uint32_t k = 0; k < 8; ++k) v[k] = col + k < a.vocab ? SmallFloat<TYPE>::at(w[k / 2], k % 2) * fe : 0.f;
         if (t < 8) {
             const float p = expm1f(a.picked[row] - of[0]) * of[1];
 #pragma unroll

@@ -21,7 +21,7 @@ constexpr uint64_t FEW_MOST = 96;                        // products of so many 
 constexpr uint64_t LD_MOST = 1ull << 22;                 // operands: 256 rows are reached by 32-bit offsets
 constexpr uint64_t OUT_LD_MOST = 1ull << 24;             // results: 32 rows
 constexpr uint64_t ROWS_MOST = 65535ull * SUM_ROWS;      // 4194240: the column sums' grid
-constexpr uint64_t MATRIX_MOST = 1ull << 34;             // elements of a matrix, less one: the grids of what lays it out or joins its parts
+constexpr uint64_t MATRIX_MOST = 1ull << 33;             // elements of a matrix are fewer: the grid of what lays two of them out
 
 typedef GemmTile<256, 256, 2, 4, 64, 2> Gemm256;
 typedef GemmTile<128, 128, 2, 2, 64, 2> Gemm128;
@@ -110,7 +110,7 @@ uint32_t band_rows(const GemmPlan& p) {
 
 template <uint32_t TYPE, class T, bool XA, bool XB, uint32_t END>
 int launch_tile(GemmArgs g, const GemmPlan& p, hipStream_t s) {
-    const uint64_t items = p.whole + p.shared() * p.splits;                   // (below 2^28 for matrices of fewer than 2^34 elements and rows of 2^22)
+    const uint64_t items = p.whole + p.shared() * p.splits;                   // (below 2^28 for matrices of fewer than 2^33 elements)
     constexpr uint64_t slots = UNITS * ((160 * 1024) / T::LDS);
     g.tiles_m = (uint32_t)p.tiles_m; g.tiles_n = (uint32_t)p.tiles_n; g.band = band_rows(p); g.whole = (uint32_t)p.whole; g.splits = p.splits; g.share = p.share;
     hipLaunchKernelGGL((k_gemm_tile<TYPE, T, XA, XB, END>), dim3((uint32_t)std::min<uint64_t>(items, slots)), dim3(64 * T::WAVES), 0, s, g);
@@ -374,7 +374,7 @@ int kimad_linear_grad(const void* dy, uint64_t ld_dy, const void* x, uint64_t ld
         });
         if (rc) return rc;
         if (r.sums) {
-            hipLaunchKernelGGL(k_sum_join, dim3((uint32_t)((N + 63) / 64)), dim3(256), 0, s, r.sums, r.sum_parts, N, db);
+            hipLaunchKernelGGL(k_sum_join, dim3((uint32_t)((N + 63) / 64)), dim3(1024), 0, s, r.sums, r.sum_parts, N, db);
             if (const int rc2 = launched()) return rc2;
         }
     }

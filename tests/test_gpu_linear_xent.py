@@ -180,6 +180,13 @@ def test_pieces_of_the_rows(dw_dtype):
     check(x[some], w, target[some], None, alone, BF16, dw_dtype)
 
 
+def test_no_rows():
+    dw = torch.full((7, 16), float("nan"), device="cuda")
+    kimad.kimad_linear_xent(torch.empty(0, 16, dtype=BF16, device="cuda"), torch.ones(7, 16, dtype=BF16, device="cuda"), torch.empty(0, dtype=torch.int32, device="cuda"),
+                            loss=torch.empty(0, device="cuda"), dx=torch.empty(0, 16, dtype=BF16, device="cuda"), dw=dw)
+    assert not dw.any()
+
+
 def test_streams_graphs_and_the_same_bits():
     rows, vocab, dim = 300, 1000, 136
     x, w, target, weight = inputs(rows, vocab, dim, BF16, 6)

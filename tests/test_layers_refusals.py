@@ -28,7 +28,7 @@ def dropout(x=P, kind=F32, rows=4, cols=8, ld=8, res=0, ld_res=8, p=0.5, seed=1,
 @pytest.mark.parametrize("bad", [
     dict(kind=F32), dict(kind=3), dict(out_kind=F16), dict(out_kind=3), dict(act=4), dict(ld_x=63), dict(ld_w=63), dict(ld_out=47), dict(x=0), dict(w=0), dict(out=0),
     dict(x=P + 1), dict(w=P + 1), dict(out=P + 1), dict(out=P + 2, out_kind=F32), dict(bias=P + 1), dict(res=P + 1), dict(res=P, ld_res=47), dict(z=P + 1), dict(z=P, ld_z=47),
-    dict(M=4194241), dict(ld_x=(1 << 22) + 1), dict(ld_out=(1 << 24) + 1), dict(N=(1 << 22) + 1, ld_out=1 << 23), dict(M=1 << 20, N=1 << 14, ld_out=1 << 14)])
+    dict(M=4194241), dict(ld_x=(1 << 22) + 1), dict(ld_out=(1 << 24) + 1), dict(N=(1 << 22) + 1, ld_out=1 << 23), dict(M=1 << 20, N=1 << 13, ld_out=1 << 13)])
 def test_linear_refuses(bad):
     assert linear(**bad) == BAD
 
