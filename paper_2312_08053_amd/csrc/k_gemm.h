@@ -121,25 +121,31 @@ struct GemmArgs {
     SoftmaxEnd soft;
 };
 
+constexpr uint32_t GEMM_STAGE_K = 64;
 // A tile of BM by BN, WM by WN waves.  64 of K are a stage, 128 bytes of a row that is stored along K, of which LDS holds two.
 //   Along K, 16 bytes b of row r stand at b ^ (r / 2 % 8), so that sixteen lanes that read one b of sixteen rows meet different banks.
 //   Across K, LDS has rows of one k, BM elements each, and a read that transposes: sixteen lanes bring 4 k of 16 elements, and each gets
 //   one element's four.  Of a row the 64-byte pieces stand turned by its k, so that the four rows of such a read lie in different banks.
-template <uint32_t BM_, uint32_t BN_, uint32_t WM_, uint32_t WN_, uint32_t SK_, uint32_t NB_>
+//
+// What bounds it, by copies with parts left out (8192 x 2048 x 5632 along K, one tile of 256 a unit, 88 stages; microseconds): products and reads of LDS alone 101, loads
+// alone 94 (64 KB a stage and unit, 16 TB/s in all), together on zeros 119 to 126, on random numbers 154 to 175 by machine: the matrix cores work in half of the cycles, and with numbers in
+// them the power limit, not the schedule, sets the pace; a library's product of these sizes takes 139.  Across K both (8192 x 8192 x 8192) 541, 661 and 870 on zeros as on random
+// numbers: loads and transposing reads, which share LDS.  8192 x 8192 x 8192 along K 811 to 880, 1250 to 1360 TFLOP/s.
+template <uint32_t BM_, uint32_t BN_, uint32_t WM_, uint32_t WN_>
 struct GemmTile {
-    static constexpr uint32_t BM = BM_, BN = BN_, WM = WM_, WN = WN_, SK = SK_, NB = NB_;
-    static constexpr uint32_t WAVES = WM * WN, TI = BM / WM / 32, TJ = BN / WN / 32, STEPS = SK / 16;
-    static constexpr uint32_t LA = BM * SK / 512 / WAVES, LB = BN * SK / 512 / WAVES, LOADS = LA + LB;
-    static constexpr uint32_t STAGE = (BM + BN) * SK * 2;
+    static constexpr uint32_t BM = BM_, BN = BN_, WM = WM_, WN = WN_;
+    static constexpr uint32_t WAVES = WM * WN, TI = BM / WM / 32, TJ = BN / WN / 32, STEPS = GEMM_STAGE_K / 16;
+    static constexpr uint32_t LA = BM / 8 / WAVES, LB = BN / 8 / WAVES, LOADS = LA + LB;
+    static constexpr uint32_t STAGE = (BM + BN) * GEMM_STAGE_K * 2;
     static constexpr uint32_t COLS = 32 * TJ, PITCH = COLS + 8;
-    static constexpr uint32_t OUT = 8 * PITCH * 4, LDS = NB * STAGE + WAVES * OUT;
+    static constexpr uint32_t OUT = 8 * PITCH * 4, LDS = 2 * STAGE + WAVES * OUT;
     static constexpr uint32_t STRIP = COLS;                                   // columns of a strip of the softmax's end
 };
 
 // An operand's side of a tile's loads.  E: elements of the tile's edge, ACROSS: stored across K.
-template <uint32_t E, uint32_t WAVES, uint32_t SK, bool ACROSS>
+template <uint32_t E, uint32_t WAVES, bool ACROSS>
 struct GemmSide {
-    static constexpr uint32_t LANES_ROW = ACROSS ? E / 8 : SK / 8, ROWS_LOAD = 64 / LANES_ROW;   // lanes of a stored row's part, rows of a load
+    static constexpr uint32_t SK = GEMM_STAGE_K, LANES_ROW = ACROSS ? E / 8 : SK / 8, ROWS_LOAD = 64 / LANES_ROW;   // lanes of a stored row's part, rows of a load
     // What is brought next: a stage of K, of `rows` rows along K or elements across it.
     const uint8_t* base;
     uint64_t ld_bytes;
@@ -149,8 +155,7 @@ struct GemmSide {
     uint32_t block;              // along K: which 16 bytes of a row's part
 
     static __device__ __forceinline__ uint32_t turned(uint32_t k) { return E >= 128 ? k & 3u : (k >> 1) & 1u; }
-    // along K: of a row whose part is SK / 8 times 16 bytes
-    static __device__ __forceinline__ uint32_t turn(uint32_t row) { return SK == 64 ? (row >> 1) & 7u : (row >> 2) & 3u; }
+    static __device__ __forceinline__ uint32_t turn(uint32_t row) { return (row >> 1) & 7u; }   // along K
     __device__ __forceinline__ void begin(uint32_t wave, uint32_t lane, uint64_t ld) {
         ld_bytes = 2 * ld;
         const uint32_t row = wave * ROWS_LOAD + lane / LANES_ROW, at = lane % LANES_ROW;
@@ -428,10 +433,10 @@ __global__ __launch_bounds__(64 * T::WAVES, 2) void k_gemm_tile(GemmArgs g) {
     __shared__ __attribute__((aligned(1024))) uint8_t s_mem[T::LDS];
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t lds0 = lds_address(s_mem), tiles = g.tiles_m * g.tiles_n, shared = tiles - g.whole, items = g.whole + shared * g.splits;
-    const uint32_t stages = (uint32_t)((g.K + T::SK - 1) / T::SK);
+    const uint32_t stages = (uint32_t)((g.K + GEMM_STAGE_K - 1) / GEMM_STAGE_K);
 
-    GemmSide<BM, T::WAVES, T::SK, ACROSS_A> sa;
-    GemmSide<BN, T::WAVES, T::SK, ACROSS_B> sb;
+    GemmSide<BM, T::WAVES, ACROSS_A> sa;
+    GemmSide<BN, T::WAVES, ACROSS_B> sb;
     sa.begin(wave, lane, g.lda);
     sb.begin(wave, lane, g.ldb);
     // An item's tile, and the part of its sum that it is: the whole tiles come first, then the shared ones' first parts and so on.
@@ -449,7 +454,7 @@ __global__ __launch_bounds__(64 * T::WAVES, 2) void k_gemm_tile(GemmArgs g) {
         const bool none = item >= items;                                      // (behind the last one the loads go on, of nothing)
         const Item it = none ? Item{0u, 0u, 0u, stages} : item_at(item);
         if (!none) tile_at(it.tile, g.tiles_m, g.tiles_n, g.band, tm, tn);
-        const uint32_t k0 = it.first * T::SK;
+        const uint32_t k0 = it.first * GEMM_STAGE_K;
         stages_in = it.count;
         sa.aim(g.a, (uint64_t)tm * BM, none ? 0 : g.M, k0, ACROSS_A ? (uint32_t)g.k_rows_a : (uint32_t)g.K);
         sb.aim(g.b, (uint64_t)tn * BN, none ? 0 : g.N, k0, ACROSS_B ? (uint32_t)g.k_rows_b : (uint32_t)g.K);
@@ -464,11 +469,11 @@ __global__ __launch_bounds__(64 * T::WAVES, 2) void k_gemm_tile(GemmArgs g) {
 #pragma unroll
         for (uint32_t i = k * T::LOADS / n; i < (k + 1) * T::LOADS / n; ++i) {
             if (i < T::LA) load_lds16(from_a, off_a + i * sa.step(), 0, stage + i * T::WAVES * 1024u);
-            else load_lds16(from_b, off_b + (i - T::LA) * sb.step(), 0, stage + BM * T::SK * 2 + (i - T::LA) * T::WAVES * 1024u);
+            else load_lds16(from_b, off_b + (i - T::LA) * sb.step(), 0, stage + BM * GEMM_STAGE_K * 2 + (i - T::LA) * T::WAVES * 1024u);
         }
     };
     auto brought = [&]() {
-        buffer_in = buffer_in + 1 == T::NB ? 0u : buffer_in + 1;
+        buffer_in ^= 1u;
         sa.next();
         sb.next();
         if (--stages_in == 0) {
@@ -487,12 +492,12 @@ __global__ __launch_bounds__(64 * T::WAVES, 2) void k_gemm_tile(GemmArgs g) {
     // Where a lane reads: along K its row's 16 bytes, across K its four elements of a row of one k.
     const uint32_t turn = sa.turn(r32), k_lane = 8 * kb + ((lane & 15u) >> 2), in_piece = 32 * ((lane >> 4) & 1u) + 8 * (lane & 3u);
     auto lane_at = [&](uint32_t edge, uint32_t first, bool across) {          // of 32 rows of the tile from `first` on
-        return across ? k_lane * edge * 2 + (((first >> 5) ^ (edge >= 128 ? k_lane & 3u : (k_lane >> 1) & 1u)) << 6) + in_piece : (first + r32) * T::SK * 2;
+        return across ? k_lane * edge * 2 + (((first >> 5) ^ (edge >= 128 ? k_lane & 3u : (k_lane >> 1) & 1u)) << 6) + in_piece : (first + r32) * GEMM_STAGE_K * 2;
     };
     // The k-th of the operands of 16 of K, in the order in which the products want them.
     constexpr uint32_t READS = T::TI + T::TJ;
     auto read = [&](uint32_t buffer, uint32_t step, uint32_t k, Half& h) {
-        const uint8_t *at_a = s_mem + buffer * T::STAGE, *at_b = at_a + BM * T::SK * 2;
+        const uint8_t *at_a = s_mem + buffer * T::STAGE, *at_b = at_a + BM * GEMM_STAGE_K * 2;
         const uint32_t along = 16u * ((2 * step + kb) ^ turn), i = k == 0 ? 0 : k - T::TJ, j = k - 1;
         if (k == 0 || k > T::TJ) h.a[i] = gemm_operand<BM, ACROSS_A>(at_a + lane_at(BM, wm * (BM / WM) + 32 * i, ACROSS_A) + (ACROSS_A ? 0 : along), 16 * step);
         else h.b[j] = gemm_operand<BN, ACROSS_B>(at_b + lane_at(BN, wn * (BN / WN) + 32 * j, ACROSS_B) + (ACROSS_B ? 0 : along), 16 * step);
@@ -524,18 +529,17 @@ __global__ __launch_bounds__(64 * T::WAVES, 2) void k_gemm_tile(GemmArgs g) {
         for (uint32_t r = k * READS / PRODUCTS; r < (k + 1) * READS / PRODUCTS; ++r) read(buffer, step, r, h);
     };
     // The reads of one half are under way while the other is multiplied, across stages and items too; the barrier in front of a stage's last 16 of K waits
-    // for the next stage, and behind it this stage's buffer takes the one NB further on.  A tile is stored while the next item's first stages
-    // come; the next barriers let these stores be.
+    // for the next stage, and behind it this stage's buffer takes the one after the next.  A tile is stored while the next item's first stage
+    // comes; the next barrier lets these stores be.
     constexpr uint32_t STORES = END == END_F32 ? 4 * T::TI * T::TJ : 4 * T::TI;
-#pragma unroll
-    for (uint32_t i = 0; i < T::NB; ++i) {
-        bring(0, 1);
-        brought();
-    }
-    vm_wait_barrier<(T::NB - 1) * T::LOADS, 0>(0);
+    bring(0, 1);
+    brought();
+    bring(0, 1);
+    brought();
+    vm_wait_barrier<T::LOADS, 0>(0);
     uint32_t buffer = 0;
     read_all(0, 0, half0);
-    uint32_t stores_behind = 0;                                               // not 0: a tile's stores, STORES or more, are behind the loads that the next barrier waits for
+    uint32_t stores_behind = 0;                                               // 1: a tile's stores, STORES or more, are behind the loads that the next barrier waits for
     for (uint32_t item = blockIdx.x; item < items; item += gridDim.x) {
         const uint32_t here = item_at(item).count;
 #pragma unroll
@@ -549,9 +553,9 @@ __global__ __launch_bounds__(64 * T::WAVES, 2) void k_gemm_tile(GemmArgs g) {
                 if (!BETWEEN) read_all(buffer, step, step % 2 ? half1 : half0);
                 multiply(step % 2 ? half0 : half1, [&](uint32_t k) { read_beside(buffer, step, k, step % 2 ? half1 : half0); });
             }
-            vm_wait_barrier<(T::NB - 2) * T::LOADS, STORES>(stores_behind);
-            stores_behind = stores_behind ? stores_behind - 1 : 0;
-            buffer = buffer + 1 == T::NB ? 0u : buffer + 1;
+            vm_wait_barrier<0, STORES>(stores_behind);
+            stores_behind = 0;
+            buffer ^= 1u;
             if (!BETWEEN) read_all(buffer, 0, half0);                         // (behind the last item reads and loads go on, of a buffer and of nothing)
             multiply(half1, [&](uint32_t k) {
                 read_beside(buffer, 0, k, half0);
@@ -573,13 +577,13 @@ __global__ __launch_bounds__(64 * T::WAVES, 2) void k_gemm_tile(GemmArgs g) {
 #pragma unroll
                     for (uint32_t e = 0; e < 4; ++e) to[(4 * (i * T::TJ + j) + e) * 64] = f32x4{x[4 * e], x[4 * e + 1], x[4 * e + 2], x[4 * e + 3]};
                 }
-            stores_behind = T::NB - 1;
+            stores_behind = 1;
         } else {
             uint32_t tm, tn;
             tile_at(it.tile, g.tiles_m, g.tiles_n, g.band, tm, tn);
-            float* mine = reinterpret_cast<float*>(s_mem + T::NB * T::STAGE + wave * T::OUT);
+            float* mine = reinterpret_cast<float*>(s_mem + 2 * T::STAGE + wave * T::OUT);
             const bool counted = gemm_end<TYPE, T, T::TI, END>(g, acc, mine, (uint64_t)tm * BM, (uint64_t)tn * BN, wm * (BM / WM), wn);
-            stores_behind = counted ? T::NB - 1 : 0u;
+            stores_behind = counted ? 1u : 0u;
         }
         read_all(buffer, 0, half0);                                           // (once more: kept through the end, it would cost 24 registers)
     }

@@ -23,11 +23,9 @@ constexpr uint64_t OUT_LD_MOST = 1ull << 24;             // results: 32 rows
 constexpr uint64_t ROWS_MOST = 65535ull * SUM_ROWS;      // 4194240: the column sums' grid
 constexpr uint64_t MATRIX_MOST = 1ull << 33;             // elements of a matrix are fewer: the grid of what lays two of them out
 
-typedef GemmTile<256, 256, 2, 4, 64, 2> Gemm256;
-typedef GemmTile<128, 128, 2, 2, 64, 2> Gemm128;
-typedef GemmTile<64, 64, 2, 2, 64, 2> Gemm64;
-constexpr uint64_t STAGE_K = 64;
-static_assert(Gemm256::SK == STAGE_K && Gemm128::SK == STAGE_K && Gemm64::SK == STAGE_K, "stages of the tiles");
+typedef GemmTile<256, 256, 2, 4> Gemm256;
+typedef GemmTile<128, 128, 2, 2> Gemm128;
+typedef GemmTile<64, 64, 2, 2> Gemm64;
 
 template <class F>
 int with_half_type(uint32_t type, F f) {
@@ -47,9 +45,18 @@ struct Room {
     }
 };
 
-// How a product is shared out: by the least of the times below, which are fits (us) to measurements of each tile alone: rounds of as many tiles as compute units, and a
-// last one that costs less the fewer units it fills.  The tiles of a last round may be shared out along the sum too (`splits` parts, which are of fp32 and are added by a
-// second launch).
+// How a product is shared out: by the least of the times below, which are fits (us) to measurements of each tile alone: rounds of as many tiles as compute units hold, and a
+// last one that costs less the fewer of them it has.  The tiles of a last round may be shared out along the sum too (`splits` parts, which are of fp32 and are added by a
+// second launch).  Measured into 16 bits (us; each tile without parts, and the best way of all that were tried; the choice comes within 7 % of it but at 2048 x 2048 x 2048, 14 %):
+//                   M      N      K        256     128     64      best                 M      N      K        256     128     64      best
+//   both along K    77     1000   520      21      12      8.1     7.4 few rows         1024   4096   4096     101     60      57      52  256, 4 parts
+//                   64     8192   8192     184     102     64      27  64, 4 parts      2048   5632   2048     56      67      80      56  256
+//                   256    768    768      25      13      8.7     8.7 64               4096   768    16384    369     208     156     105 256, 5 parts
+//                   2048   2048   2048     56      29      33      29  128              8192   5632   2048     174     200     295     174 256
+//   B across K      299    3683   9456     240     135     88      45  128, 5 parts     4096   768    50304    1431    859     604     342 256, 5 parts
+//                   300    1000   1000     30      17      10      10  64               8192   2048   5632     158     189     299     158 256
+//   both across K   1000   520    104      15      8.9     6.1     6.1 64               50257  768    4096     395     411     832     353 256, 3 parts of the last
+//                   768    768    8192     194     112     71      26  64, 5 parts      5632   2048   8192     196     230     347     196 256
 struct GemmPlan {
     enum { FEW, T64, T128, T256 } kind;
     uint64_t tiles_m, tiles_n, whole;
@@ -63,7 +70,7 @@ struct GemmPlan {
 GemmPlan gemm_plan(uint64_t M, uint64_t N, uint64_t K, bool wide, bool may_split, uint32_t few) {
     GemmPlan best{};
     best.splits = 1;
-    const uint64_t stages = (K + STAGE_K - 1) / STAGE_K;
+    const uint64_t stages = (K + GEMM_STAGE_K - 1) / GEMM_STAGE_K;
     best.share = (uint32_t)stages;
     // k_gemm_few, whose waves read all of A each; rows that begin off 16-byte addresses cost it nearly twice as much, and the tiles a copy.
     const double copy = few == 2 ? 4.0 + (double)((M + N) * K) * 4.0 / 4.5e6 : 0.0;
