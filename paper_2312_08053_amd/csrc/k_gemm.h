@@ -128,7 +128,7 @@ constexpr uint32_t GEMM_STAGE_K = 64;
 //   one element's four.  Of a row the 64-byte pieces stand turned by its k, so that the four rows of such a read lie in different banks.
 //
 // What bounds it, by copies with parts left out (8192 x 2048 x 5632 along K, one tile of 256 a unit, 88 stages; microseconds): products and reads of LDS alone 101, loads
-// alone 94 (64 KB a stage and unit, 16 TB/s in all), together on zeros 119 to 126, on random numbers 154 to 175 by machine: the matrix cores work in half of the cycles, and with numbers in
+// alone 94 (64 KB a stage and unit, 16 TB/s in all), together on zeros 119 to 126, on random numbers 154 to 175 by machine: the matrix cores work in 61 % of the cycles, and with numbers in
 // them the power limit, not the schedule, sets the pace; a library's product of these sizes takes 139.  Across K both (8192 x 8192 x 8192) 541, 661 and 870 on zeros as on random
 // numbers: loads and transposing reads, which share LDS.  8192 x 8192 x 8192 along K 811 to 880, 1250 to 1360 TFLOP/s.
 template <uint32_t BM_, uint32_t BN_, uint32_t WM_, uint32_t WN_>
