@@ -71,8 +71,8 @@ __device__ __forceinline__ float act_of(float z, uint32_t act) {
 // ---- tiles ---------------------------------------------------------------------------------------------------------------------
 
 // Exponentials e = exp(s - m), 0 to 1, in 16 bits, whose rounding is small beside the type's.  They are made, and summed, as 2^UP e.
-//   A product in bfloat16 takes them as fp16 numbers 2^15 e: exact to 2^-11 of e down to 2^-29, to 2^-40 below.
-//   One in fp16 as numbers without a sign, twelve bits of mantissa and four of exponent: exact to 2^-13 of e down to 2^-14, to 2^-28 below.  The float e 2^-112 has such
+//   A product in bfloat16 takes them as fp16 numbers 2^15 e: exact to 2^-11 of e down to 2^-29, to 2^-40 below (a smaller one may become 0).
+//   One in fp16 as numbers without a sign, twelve bits of mantissa and four of exponent: exact to 2^-13 of e down to 2^-14, to 2^-27 below.  The float e 2^-112 has such
 //   an exponent, and its bits, rounded, are the code.
 template <uint32_t TYPE>
 struct SmallFloat {
