@@ -287,10 +287,11 @@ __device__ __forceinline__ bool gemm_end(const GemmArgs& g, const f32x16 (&acc)[
             m = fmaxf(m, __uint_as_float(dpp_u32<DPP_XOR1>(__float_as_uint(m))));
             m = fmaxf(m, __uint_as_float(dpp_u32<DPP_XOR2>(__float_as_uint(m))));
             if (LANES == 8) m = fmaxf(m, __uint_as_float(dpp_u32<DPP_HALF_MIRROR>(__float_as_uint(m))));
-            const float from = SmallFloat<TYPE>::UP - (m == -INFINITY ? 0.f : m) * LOG2E;
+            const float from = m == -INFINITY ? 0.f : m;
 #pragma unroll
             for (uint32_t k = 0; k < EACH; ++k) {
-                v[k] = __builtin_amdgcn_exp2f(fmaf(v[k], LOG2E, from));
+                // (the difference first: that from the largest is then 0, whatever its size, where m LOG2E would be off by |m| 2^-24)
+                v[k] = __builtin_amdgcn_exp2f(fmaf(v[k] - from, LOG2E, SmallFloat<TYPE>::UP));
                 sum += v[k];
             }
             sum += __uint_as_float(dpp_u32<DPP_XOR1>(__float_as_uint(sum)));
