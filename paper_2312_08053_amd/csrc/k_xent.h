@@ -2,7 +2,7 @@
 //     loss_r = w_r (lse_r - z_{r, t_r}),   G = w (p - onehot(t)),   dx = G W,   dW = G^T x.
 // The product z goes by tiles (k_gemm.h) whose end is END_SOFTMAX: of a strip of a row's columns (32 or 64) only its largest sum m and s = sum exp(z - m)
 // are kept, and for a gradient e = exp(z - m) in 16 bits (SmallFloat, whose rounding is small beside the type's), of a piece of the rows at a time.  With lse known, e
-// becomes G in its place, e exp(m - lse) w, in the type of the products.  At the target, where p - 1 may be much smaller than p, it is taken from the fp32
+// becomes G in its place, e exp(m - lse) w, in the type of the products; lse stays in two parts, the largest logit and what is beside it, so that G is as near at any size of the logits.  At the target, where p - 1 may be much smaller than p, it is taken from the fp32
 // logit.  A second product for z in the place of e would cost 2 R V D operations more; e costs 4 bytes of traffic an element.
 #pragma once
 #include "k_linear.h"
@@ -15,7 +15,7 @@ struct XentArgs {
     const int32_t* target;
     const float* weight;         // or null: 1
     float *loss, *lse;           // or null
-    f32x2* rows_out;             // [rows]: lse, and the row's weight times `scale` (0: the row does not count)
+    f32x4* rows_out;             // [rows]: the largest logit, ln of the sum of exponentials of differences from it, the row's weight times `scale` (0: the row does not count)
     void* e;                     // [rows, pitch]: exp(z - m) as a SmallFloat, and then G
     const float* scale;          // two numbers on the device: what G is multiplied by, and its inverse (k_rows_copy)
     uint64_t rows, pitch;
@@ -39,10 +39,11 @@ __global__ __launch_bounds__(256) void k_xent_rows(XentArgs a) {
         live = q.s != 0.f;                                                    // (every logit -Inf: the row leaves nothing)
     }
     if (threadIdx.x) return;
-    const float lse = live ? q.m + logf(q.s) : 0.f;
-    if (a.loss) a.loss[row] = live ? w * ((q.m - a.picked[row]) + logf(q.s)) : 0.f;
-    if (a.lse) a.lse[row] = lse;
-    if (a.rows_out) a.rows_out[row] = f32x2{lse, live ? w * a.scale[0] : 0.f};
+    const float log_s = logf(q.s);
+    if (a.loss) a.loss[row] = live ? w * ((q.m - a.picked[row]) + log_s) : 0.f;
+    if (a.lse) a.lse[row] = live ? q.m + log_s : 0.f;
+    // (lse in its two parts: as one number it is off by |lse| 2^-24, and every probability by as much of itself)
+    if (a.rows_out) a.rows_out[row] = f32x4{q.m, log_s, live ? w * a.scale[0] : 0.f, 0.f};
 }
 
 // e becomes G.  A thread takes eight columns.  Bound by memory.
@@ -51,20 +52,20 @@ __global__ __launch_bounds__(256) void k_xent_gradient(XentArgs a, uint32_t chun
     const uint64_t row = blockIdx.x / chunks;
     const uint64_t col = ((uint64_t)(blockIdx.x % chunks) * 256 + threadIdx.x) * 8;
     if (col >= a.pitch) return;
-    const f32x2 of = a.rows_out[row];
+    const f32x4 of = a.rows_out[row];
     u32x4* at = reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.e) + row * a.pitch + col);
-    const bool live = of[1] != 0.f && col < a.vocab;
+    const bool live = of[2] != 0.f && col < a.vocab;
     u32x4 out = {0u, 0u, 0u, 0u};
     if (live) {
         const u32x4 w = *at;
-        const float m = a.strips[row * a.strips_row + col / a.strip][0], f = __builtin_amdgcn_exp2f((m - of[0]) * LOG2E) * of[1];
+        const float m = a.strips[row * a.strips_row + col / a.strip][0], f = __builtin_amdgcn_exp2f(((m - of[0]) - of[1]) * LOG2E) * of[2];
         const float fe = f * SmallFloat<TYPE>::TO_E;
         const uint32_t t = (uint32_t)a.target[row] - (uint32_t)col;
         float v[8];
 #pragma unroll
         for (uint32_t k = 0; k < 8; ++k) v[k] = col + k < a.vocab ? SmallFloat<TYPE>::at(w[k / 2], k % 2) * fe : 0.f;
         if (t < 8) {
-            const float p = expm1f(a.picked[row] - of[0]) * of[1];
+            const float p = expm1f((a.picked[row] - of[0]) - of[1]) * of[2];
 #pragma unroll
             for (uint32_t k = 0; k < 8; ++k)
                 if (t == k) v[k] = p;

@@ -268,7 +268,8 @@ constexpr uint64_t PIECE_BYTES = 1ull << 30;
 struct XentRoom {
     uint64_t piece, pieces, pitch;
     uint16_t *x, *w, *e;
-    f32x2 *strips, *rows_out;
+    f32x2* strips;
+    f32x4* rows_out;
     float *picked, *scale, *sum, *parts;
     struct { GemmPlan z, dx, dw; } plans[2];             // of a piece, and of the last one, which may have fewer rows
 };
@@ -298,7 +299,7 @@ XentRoom xent_room(Room& room, const void* x, uint64_t ld_x, const void* w, uint
     r.strips = room.take<f32x2>(strips);
     r.picked = room.take<float>(r.piece);
     if (!grad) return r;
-    r.rows_out = room.take<f32x2>(r.piece);
+    r.rows_out = room.take<f32x4>(r.piece);
     r.scale = room.take<float>(2);
     r.e = room.take<uint16_t>(r.piece * r.pitch);
     if (dw && r.pieces > 1 && dw_type != KIMAD_VALUES_F32) r.sum = room.take<float>(vocab * dim);

@@ -66,3 +66,24 @@ def test_loss(rows, vocab, base, dtype):
         assert (got["loss"] >= 0).all()
         assert (np.abs(got["loss"] - loss) <= weight * sum_error(vocab) + 2.0 ** -22 * np.abs(loss)).all(), np.abs(got["loss"] - loss).max()
         assert (np.abs(got["lse"] - lse) <= sum_error(vocab) + 2.0 ** -23 * np.abs(lse)).all()
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("base", BASES)
+@pytest.mark.parametrize("rows,vocab", SHAPES)
+def test_gradients(rows, vocab, base, dtype):
+    """G is off by the sum of exponentials, by its own argument a (4 |a| 2^-24), by two roundings to the type (e, and G); in fp16 an exponential below 2^-14 of its strip's
+    largest is off by 2^-27 of that, in bfloat16 one below 2^-29 by 2^-40, and fp16's G by half its smallest step, 2^-25, over 4096 of the largest weight.  At the
+    target it is expm1 of an argument that is off by the sum's error.  Nothing of this grows with the logits."""
+    x, w, target, weight = inputs(rows, vocab, base, dtype, rows + 1)
+    _, _, G, d, log_s = true(x, w, target, weight)
+    got = call(x, w, target, weight, ("dx", "dw"))
+    u, wt = HALF[dtype], weight[:, None].astype(np.float64)
+    off = np.abs(G) * (2 * u + u * u + sum_error(vocab) + 2.0 ** -20 + 2.0 ** -22 * np.abs(d - log_s[:, None]))
+    off += wt * 2.0 ** -27 + wt.max() * 2.0 ** -37 if dtype == F16 else wt * 2.0 ** -40
+    off[np.arange(rows), target] += weight * (sum_error(vocab) + 2.0 ** -22)
+    X, W = x.double().numpy(), w.double().numpy()
+    for name, want, bound, ulp in (("dx", G @ W, off @ np.abs(W) + vocab * 2.0 ** -23 * (np.abs(G) @ np.abs(W)), u),
+                                   ("dw", G.T @ X, off.T @ np.abs(X) + rows * 2.0 ** -23 * (np.abs(G).T @ np.abs(X)), HALF[F32])):
+        bound = bound + ulp * (np.abs(want) + bound) + 2.0 ** -24
+        assert (np.abs(got[name] - want) <= bound).all(), (name, np.abs(got[name] - want).max(), bound.max())
