@@ -8,6 +8,7 @@
 // v_mfma_f32_32x32x16: lane l holds elements k = 8 (l / 32) .. + 7 of row l % 32, of A and of B; element i of the result's lane l is
 // C[8 (i / 4) + 4 (l / 32) + i % 4][l % 32].
 #pragma once
+#include "gemm_stage.h"
 #include "k_mx4_matmul.h"
 
 namespace kimad {
@@ -176,11 +177,9 @@ struct GemmSide {
         k_left = k_left > SK ? k_left - SK : 0u;
         measure();
     }
-    // Bytes of the stage, beyond which are zeros.  (Across, whole words: half of the last one may be beyond the array, never of another page.)
     __device__ __forceinline__ void measure() {
-        const uint32_t k = k_left < SK ? k_left : SK, lines = ACROSS ? k : rows, line = ACROSS ? (2 * rows + 3) & ~3u : 2 * k;
-        bytes = ((lines - 1) * (uint32_t)ld_bytes + line) & (lines == 0 || line == 0 ? 0u : ~0u);
-        bytes = __builtin_amdgcn_readfirstlane(bytes);                        // (made once, not with every load)
+        const uint32_t k = k_left < SK ? k_left : SK;
+        bytes = __builtin_amdgcn_readfirstlane(stage_bytes(ACROSS, ACROSS ? k : rows, ACROSS ? rows : k, (uint32_t)ld_bytes));   // (made once, not with every load)
     }
     __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer() const { return buffer_of(base, bytes); }
     // The lane's offset in its first load; along K, a row's end would run into the next row: such lanes are beyond every buffer, in all of their loads.

@@ -175,7 +175,6 @@ int zeros(void* out, uint32_t type, uint64_t rows, uint64_t cols, uint64_t ld, h
 
 // Whether the tiles' loads reach an operand as it lies: rows at 16-byte addresses, and for one that is stored along K rows that end at one.
 bool lies_well(const void* p, uint64_t ld, uint64_t rows, uint64_t cols, bool along) { return aligned(p, 16) && (ld % 8 == 0 || rows <= 1) && (!along || cols % 8 == 0); }
-uint64_t pitch_of(uint64_t cols) { return (cols + 7) / 8 * 8; }
 // Two matrices (either may stay where it is: `to` null) laid out anew; the first one's rows that do not count become zeros.  scale: as k_rows_copy makes it.
 struct CopyOf {
     const void* from;
@@ -196,11 +195,12 @@ int copy_rows(const CopyOf& first, const CopyOf& second, const int32_t* target, 
     hipLaunchKernelGGL(k_rows_copy, dim3((uint32_t)(wgs[0] + wgs[1] + (scale ? 1 : 0))), dim3(256), 0, s, a);
     return launched();
 }
-// an operand: its address and leading dimension, in place or copied
+// an operand: its address and leading dimension, copied or in place
 struct Operand {
     const void* p;
     uint64_t ld;
 };
+Operand operand(const void* copy, const void* p, uint64_t ld, uint64_t rows, uint64_t cols) { return copy ? Operand{copy, pitch_of(cols)} : Operand{p, stage_ld(rows, cols, ld)}; }
 
 bool matrix_ok(const void* p, uint64_t rows, uint64_t cols, uint64_t ld, uint64_t bytes, uint64_t most) {
     return ld >= cols && ld <= most && (rows == 0 || cols == 0 || (p && aligned(p, bytes)));
@@ -335,7 +335,7 @@ int kimad_linear(const void* x, uint64_t ld_x, const void* w, uint64_t ld_w, uin
     const LinearRoom r = linear_room(room, x, ld_x, w, ld_w, M, N, K);
     if (room.used && (!workspace || workspace_bytes < room.used || !aligned(workspace, 16))) return KIMAD_ERR_WORKSPACE_TOO_SMALL;
     if (const int rc = copy_rows({x, ld_x, M, K, r.x}, {w, ld_w, N, K, r.w}, nullptr, 0, nullptr, nullptr, 0.f, s)) return rc;
-    const Operand ox = r.x ? Operand{r.x, pitch_of(K)} : Operand{x, ld_x}, ow = r.w ? Operand{r.w, pitch_of(K)} : Operand{w, ld_w};
+    const Operand ox = operand(r.x, x, ld_x, M, K), ow = operand(r.w, w, ld_w, N, K);
     g.a = static_cast<const uint8_t*>(ox.p); g.lda = ox.ld; g.b = static_cast<const uint8_t*>(ow.p); g.ldb = ow.ld;
     if (r.plan.kind != GemmPlan::FEW) g.K = pitch_of(K);
     return with_half_type(type, [&](auto t) { return launch_gemm<decltype(t)::value, false, false>(g, r.plan, out32, r.parts, s); });
@@ -367,8 +367,8 @@ int kimad_linear_grad(const void* dy, uint64_t ld_dy, const void* x, uint64_t ld
     const LinearGradRoom r = linear_grad_room(room, dy, ld_dy, x, ld_x, w, ld_w, M, N, K, act, wants);
     if (room.used && (!workspace || workspace_bytes < room.used || !aligned(workspace, 16))) return KIMAD_ERR_WORKSPACE_TOO_SMALL;
     if (const int rc = copy_rows({x, ld_x, M, K, r.x}, {w, ld_w, N, K, r.w}, nullptr, 0, nullptr, nullptr, 0.f, s)) return rc;
-    const Operand odz = r.dz_made ? Operand{r.dz, pitch_of(N)} : Operand{dy, ld_dy};
-    const Operand ox = r.x ? Operand{r.x, pitch_of(K)} : Operand{x, ld_x}, ow = r.w ? Operand{r.w, pitch_of(K)} : Operand{w, ld_w};
+    const Operand odz = operand(r.dz, dy, ld_dy, M, N);
+    const Operand ox = operand(r.x, x, ld_x, M, K), ow = operand(r.w, w, ld_w, N, K);
     if (r.dz_made || db) {
         ActGradArgs a{};
         a.dy = dy; a.z = act == KIMAD_ACT_NONE ? nullptr : z; a.dz = r.dz; a.M = M; a.N = N; a.ld_dy = ld_dy; a.ld_z = ld_z; a.pitch = pitch_of(N); a.act = act; a.rows = (uint32_t)r.sum_rows;
@@ -427,7 +427,7 @@ int kimad_linear_xent(const void* x, uint64_t ld_x, const void* w, uint64_t ld_w
     const XentRoom r = xent_room(room, x, ld_x, w, ld_w, type, rows, vocab, dim, wants, dw_type);
     if (!workspace || workspace_bytes < room.used || !aligned(workspace, 16)) return KIMAD_ERR_WORKSPACE_TOO_SMALL;
     if (const int rc = copy_rows({x, ld_x, rows, dim, r.x}, {w, ld_w, vocab, dim, r.w}, target, vocab, row_weight, r.scale, type == KIMAD_VALUES_F16 ? 4096.f : 1.f, s)) return rc;
-    const Operand ox = r.x ? Operand{r.x, pitch_of(dim)} : Operand{x, ld_x}, ow = r.w ? Operand{r.w, pitch_of(dim)} : Operand{w, ld_w};
+    const Operand ox = operand(r.x, x, ld_x, rows, dim), ow = operand(r.w, w, ld_w, vocab, dim);
     const bool dw32 = dw_type == KIMAD_VALUES_F32;
     return with_half_type(type, [&](auto t) {
         constexpr uint32_t TYPE = decltype(t)::value;
