@@ -524,8 +524,8 @@ int kimad_linear_grad(const void* dy, uint64_t ld_dy, const void* x, uint64_t ld
  * nothing to dw, and what it holds, Inf and NaN too, reaches nothing.  A row whose logits are all -Inf has loss, lse and G 0.  A NaN or +Inf among a row's logits makes its
  * loss and its G NaN, and with it dx's row and dw.  For a gradient the
  * exponentials of a piece of the rows are kept, 1 GiB at most or 256 rows, and turned into G, divided by the largest weight and rounded to
- * `type`, for the two products.  They are kept in 16 bits against the largest of 64 columns or fewer: a probability below 2^-29 of that one's (2^-14
- * in fp16) is off by up to 2^-40 of it (2^-27), so that a smaller one may be 0; the target's own entry is not taken from them. */
+ * `type`, for the two products.  They are kept in 16 bits against the largest of 64 columns or fewer: a probability is off by up to 2^-11 of itself
+ * (2^-12 in fp16), below 2^-62 of that largest one (2^-30) by up to 2^-73 of it (2^-42); the target's own entry is not taken from them. */
 uint64_t kimad_linear_xent_workspace_bytes(const void* x, uint64_t ld_x, const void* w, uint64_t ld_w, uint32_t type, uint64_t rows,
                                            uint64_t vocab, uint64_t dim, uint32_t wants, uint32_t dw_type);
 int kimad_linear_xent(const void* x, uint64_t ld_x, const void* w, uint64_t ld_w, uint32_t type, uint64_t rows, uint64_t vocab,

@@ -71,23 +71,18 @@ __device__ __forceinline__ float act_of(float z, uint32_t act) {
 
 // ---- tiles ---------------------------------------------------------------------------------------------------------------------
 
-// Exponentials e = exp(s - m), 0 to 1, in 16 bits, whose rounding is small beside the type's.  They are made, and summed, as 2^UP e.
-//   A product in bfloat16 takes them as fp16 numbers 2^15 e: exact to 2^-11 of e down to 2^-29, to 2^-40 below (a smaller one may become 0).
-//   One in fp16 as numbers without a sign, twelve bits of mantissa and four of exponent: exact to 2^-13 of e down to 2^-14, to 2^-27 below.  The float e 2^-112 has such
-//   an exponent, and its bits, rounded, are the code.
+// Exponentials e = exp(s - m), 0 to 1, in 16 bits without a sign, whose rounding is below the type's and whose range is beyond what G in the type reaches:
+//   of a product in bfloat16 six bits of exponent and ten of mantissa: exact to 2^-11 of e down to 2^-62, to 2^-73 below;
+//   of one in fp16 five and eleven: 2^-12 down to 2^-30, 2^-42 below.
+// The float e / 2^DOWN has such an exponent, and its bits, rounded, are the code.  (fp16 numbers 2^15 e, which the hardware rounds two at a time, lose what is below 2^-29 of the largest.)
 template <uint32_t TYPE>
 struct SmallFloat {
-    static constexpr float UP = TYPE == TYPE_BF16 ? 15.f : 0.f, DOWN = TYPE == TYPE_BF16 ? 0x1p-15f : 1.f;
-    static __device__ __forceinline__ uint32_t bits(float e) { return __float_as_uint(e * 0x1p-112f) + 0x400u; }
-    static __device__ __forceinline__ uint32_t pack(float a, float b) {       // of 2^UP e
-        if (TYPE == TYPE_BF16) return pack2<TYPE_F16>(a, b);
-        return bits(a) >> 11 | (bits(b) >> 11) << 16;
-    }
-    static __device__ __forceinline__ float at(uint32_t word, uint32_t half) {   // 2^UP e again, or e 2^-112
-        const uint32_t code = half ? word >> 16 : word & 0xFFFFu;
-        return TYPE == TYPE_BF16 ? half_to_float(code) : __uint_as_float(code << 11);
-    }
-    static constexpr float TO_E = TYPE == TYPE_BF16 ? 0x1p-15f : 0x1p112f;    // from what at() gives to e
+    static constexpr uint32_t EXPONENT = TYPE == TYPE_BF16 ? 6 : 5, DOWN = 128 - (1u << EXPONENT), LEFT = 9 - EXPONENT;   // LEFT: bits that are always 0 at the top
+    static constexpr float TO_E = TYPE == TYPE_BF16 ? 0x1p64f : 0x1p96f, FROM_E = 1.f / TO_E;
+    static_assert(DOWN == (TYPE == TYPE_BF16 ? 64 : 96), "the powers of two");
+    static __device__ __forceinline__ uint32_t bits(float e) { return (__float_as_uint(e * FROM_E) << LEFT) + 0x8000u; }   // the code in the upper half
+    static __device__ __forceinline__ uint32_t pack(float a, float b) { return __builtin_amdgcn_perm(bits(b), bits(a), 0x07060302u); }
+    static __device__ __forceinline__ float at(uint32_t word, uint32_t half) { return __uint_as_float((half ? word & 0xFFFF0000u : word << 16) >> LEFT); }   // e / 2^DOWN
 };
 
 // What becomes of a sum s:  z = scale s + bias, z kept, act(z) + residual.
@@ -290,7 +285,7 @@ __device__ __forceinline__ bool gemm_end(const GemmArgs& g, const f32x16 (&acc)[
 #pragma unroll
             for (uint32_t k = 0; k < EACH; ++k) {
                 // (the difference first: that from the largest is then 0, whatever its size, where m LOG2E would be off by |m| 2^-24)
-                v[k] = __builtin_amdgcn_exp2f(fmaf(v[k] - from, LOG2E, SmallFloat<TYPE>::UP));
+                v[k] = __builtin_amdgcn_exp2f((v[k] - from) * LOG2E);
                 sum += v[k];
             }
             sum += __uint_as_float(dpp_u32<DPP_XOR1>(__float_as_uint(sum)));
@@ -304,7 +299,7 @@ __device__ __forceinline__ bool gemm_end(const GemmArgs& g, const f32x16 (&acc)[
                 const __amdgpu_buffer_rsrc_t to = buffer_of(static_cast<uint8_t*>(o.e) + ((tile_m + first) * o.pitch + tile_n) * 2, 0xFFFFFF00u);
                 __builtin_amdgcn_raw_buffer_store_b128(out, to, in && tile_n + wcol < o.pitch ? ((8 * e + row) * (uint32_t)o.pitch + wcol) * 2 : BEYOND, 0, STREAM);
             }
-            if (in && l % LANES == 0 && wn * T::COLS < cols) o.strips[(tile_m + r) * o.strips_row + tile_n / T::STRIP + wn] = f32x2{m, sum * SmallFloat<TYPE>::DOWN};
+            if (in && l % LANES == 0 && wn * T::COLS < cols) o.strips[(tile_m + r) * o.strips_row + tile_n / T::STRIP + wn] = f32x2{m, sum};
         }
         return o.e != nullptr;
     } else {
