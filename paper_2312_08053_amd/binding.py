@@ -27,6 +27,7 @@ KIMAD_ACT_SILU = 3
 KIMAD_WANT_DX = 1
 KIMAD_WANT_DW = 2
 KIMAD_WANT_DB = 4
+FEW_ROWS = 96                                                    # products of so many rows may go by a kernel that needs no workspace
 
 EXPORTED_SYMBOLS = [
     "kimad_workspace_bytes", "kimad_plan_create", "kimad_plan_destroy", "kimad_plan_grid_sizes",
@@ -610,7 +611,7 @@ def kimad_linear(x, w, out, bias=None, residual=None, act: int = KIMAD_ACT_NONE,
     handle = _on_device(stream, x, w, out, bias, residual, z, workspace)
     L = lib()
     args = (x.data_ptr(), ld_x, w.data_ptr(), ld_w, kind, M, N, K, _ptr(bias), at_res, ld_res, act, at_z, ld_z, at_out, out_kind, ld_out)
-    if workspace is None and M <= 96:                            # (products of few rows seldom need one: asked for only then)
+    if workspace is None and M <= FEW_ROWS:                      # (these seldom need one: asked for only then)
         rc = L.kimad_linear(*args, 0, 0, handle)
     else:
         rc = KIMAD_ERR_WORKSPACE_TOO_SMALL

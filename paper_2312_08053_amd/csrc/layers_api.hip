@@ -17,7 +17,7 @@ using namespace kimad;
 
 static_assert(ACT_NONE == KIMAD_ACT_NONE && ACT_RELU == KIMAD_ACT_RELU && ACT_GELU == KIMAD_ACT_GELU && ACT_SILU == KIMAD_ACT_SILU, "header and kernel constants");
 
-constexpr uint64_t FEW_MOST = 96;                        // products of so many rows may go by k_gemm_few
+constexpr uint64_t FEW_MOST = 96;                        // products of so many rows may go by k_gemm_few (FEW_ROWS of the binding)
 constexpr uint64_t LD_MOST = 1ull << 22;                 // operands: 256 rows are reached by 32-bit offsets
 constexpr uint64_t OUT_LD_MOST = 1ull << 24;             // results: 32 rows
 constexpr uint64_t ROWS_MOST = 65535ull * SUM_ROWS;      // 4194240: the column sums' grid
