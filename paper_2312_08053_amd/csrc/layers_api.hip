@@ -273,7 +273,7 @@ struct XentRoom {
     float *picked, *scale, *sum, *parts;
     struct { GemmPlan z, dx, dw; } plans[2];             // of a piece, and of the last one, which may have fewer rows
 };
-XentRoom xent_room(Room& room, const void* x, uint64_t ld_x, const void* w, uint64_t ld_w, uint32_t type, uint64_t rows, uint64_t vocab, uint64_t dim, uint32_t wants, uint32_t dw_type) {
+XentRoom xent_room(Room& room, const void* x, uint64_t ld_x, const void* w, uint64_t ld_w, uint64_t rows, uint64_t vocab, uint64_t dim, uint32_t wants, uint32_t dw_type) {
     XentRoom r{};
     const bool dx = wants & KIMAD_WANT_DX, dw = wants & KIMAD_WANT_DW, grad = dx || dw;
     r.pitch = (vocab + 63) / 64 * 64;
@@ -404,11 +404,11 @@ int kimad_linear_grad(const void* dy, uint64_t ld_dy, const void* x, uint64_t ld
     return KIMAD_OK;
 }
 
-uint64_t kimad_linear_xent_workspace_bytes(const void* x, uint64_t ld_x, const void* w, uint64_t ld_w, uint32_t type, uint64_t rows, uint64_t vocab, uint64_t dim, uint32_t wants,
+uint64_t kimad_linear_xent_workspace_bytes(const void* x, uint64_t ld_x, const void* w, uint64_t ld_w, uint32_t /* both types take the same */, uint64_t rows, uint64_t vocab, uint64_t dim, uint32_t wants,
                                            uint32_t dw_type) {
     if (!xent_sizes_ok(rows, vocab, dim) || rows == 0) return 0;
     Room room{nullptr, 0};
-    xent_room(room, x, ld_x, w, ld_w, type, rows, vocab, dim, wants, dw_type);
+    xent_room(room, x, ld_x, w, ld_w, rows, vocab, dim, wants, dw_type);
     return room.used;
 }
 
@@ -424,7 +424,7 @@ int kimad_linear_xent(const void* x, uint64_t ld_x, const void* w, uint64_t ld_w
     const uint32_t wants = (dx ? KIMAD_WANT_DX : 0u) | (dw ? KIMAD_WANT_DW : 0u);
     if (rows == 0) return dw ? zeros(dw, dw_type, vocab, dim, ld_dw, s) : KIMAD_OK;
     Room room{static_cast<uint8_t*>(workspace), 0};
-    const XentRoom r = xent_room(room, x, ld_x, w, ld_w, type, rows, vocab, dim, wants, dw_type);
+    const XentRoom r = xent_room(room, x, ld_x, w, ld_w, rows, vocab, dim, wants, dw_type);
     if (!workspace || workspace_bytes < room.used || !aligned(workspace, 16)) return KIMAD_ERR_WORKSPACE_TOO_SMALL;
     if (const int rc = copy_rows({x, ld_x, rows, dim, r.x}, {w, ld_w, vocab, dim, r.w}, target, vocab, row_weight, r.scale, type == KIMAD_VALUES_F16 ? 4096.f : 1.f, s)) return rc;
     const Operand ox = operand(r.x, x, ld_x, rows, dim), ow = operand(r.w, w, ld_w, vocab, dim);
