@@ -125,7 +125,8 @@ constexpr uint32_t GEMM_STAGE_K = 64;
 //
 // What bounds it, by copies with parts left out (8192 x 2048 x 5632 along K, one tile of 256 a unit, 88 stages; microseconds): products and reads of LDS alone 101, loads
 // alone 94 (64 KB a stage and unit, 16 TB/s in all), together on zeros 119 to 126, on random numbers 154 to 175 by machine: the matrix cores work in 61 % of the cycles, and with numbers in
-// them the power limit, not the schedule, sets the pace; a library's product of these sizes takes 139.  Across K both (8192 x 8192 x 8192) 541, 661 and 870 on zeros as on random
+// them the clock falls to 1.9 GHz.  That is not the card's limit: a library's product of these sizes takes 90 on zeros and 121 on random numbers where this one, measured beside it, takes 117
+// and 153 (8192 x 5632 x 2048: 132 and 156, 140 and 173), so that a quarter of the time is this schedule's own.  Across K both (8192 x 8192 x 8192) 541, 661 and 870 on zeros as on random
 // numbers: loads and transposing reads, which share LDS.  8192 x 8192 x 8192 along K 811 to 880, 1250 to 1360 TFLOP/s.
 template <uint32_t BM_, uint32_t BN_, uint32_t WM_, uint32_t WN_>
 struct GemmTile {

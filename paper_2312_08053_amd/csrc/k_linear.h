@@ -181,6 +181,8 @@ __global__ __launch_bounds__(256) void k_rows_copy(CopyArgs a) {
 }
 
 // dz = dy act'(z), rounded to the type, and the sums of its columns in fp32 (of what was not rounded): of 64 rows a workgroup (128, if there are no more), 512 columns.  Bound by memory.
+// (Rounded for dw in fp32 too: the matrix cores take 16 bits, and a second product of what the rounding leaves would double both.  8192 x 5632 x 2048 in bfloat16 against 64 bits: 0.0023 of the
+// gradients' norm, 0.0017 with dz in fp32.)
 constexpr uint32_t SUM_ROWS = 64, SUM_COLS = 512;
 struct ActGradArgs {
     const void *dy, *z;          // z null: no activation
